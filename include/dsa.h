@@ -441,6 +441,160 @@ DSA_API int32_t dsa_debug_kept_indices(const dsa_problem *problem, const dsa_dia
 DSA_API int32_t dsa_decode_attention_static_scratch(const dsa_problem *problem, const dsa_diag_params *diag,
                                                     void *out, float *lse, void *stream);
 
+/* ==== Drafted tokens: several tokens of a request decoded in one pass ===============================
+ *
+ * A decode step with drafted tokens (speculative decoding; not in the paper) is, for every layer,
+ * dsa_tree_step; after the last layer dsa_verify_tree, which says which of the drafted tokens stand;
+ * and dsa_compact_kv, which moves their K/V rows up behind the cached ones and gives the new seq_len.
+ * The page calls below it keep the block table of a paged cache in step with that on the device:
+ * dsa_reserve_pages before a pass, dsa_release_pages after it, dsa_fork_pages to branch a request.
+ *
+ * All conventions above hold.  The calls in this part read nothing that the stream's earlier work may
+ * still be writing, and (unlike the attention calls) start none of their successors early before their
+ * own predecessors have finished; those that write seq_len, prompt_len or a block table (compact, fork,
+ * release, reserve) finish before anything behind them starts, so that a call behind them may make the
+ * promise DSA_PLAN_METADATA_STABLE.
+ */
+
+/* The drafted tokens ("nodes") of every request and what hangs on what. */
+typedef struct dsa_tree {
+    int32_t max_nodes;         /* N: nodes a request has room for in q, k_new, ..., 1 .. DSA_TREE_MAX_NODES */
+    const int32_t *parent;     /* device [B, N]: the node that node i follows, in [0, i); any other value    */
+                               /* (-1) makes node i a root that follows the cached tokens directly.          */
+                               /* NULL: a chain, parent[i] = i - 1                                           */
+    const int32_t *node_count; /* device [B]: nodes 0 .. node_count[b]-1 of the request exist (clamped to    */
+                               /* [0, N]); NULL: all N                                                       */
+} dsa_tree;
+#define DSA_TREE_MAX_NODES 64
+
+/* Bytes of workspace dsa_tree_step needs (diag as there). */
+DSA_API int32_t dsa_tree_workspace_size(const dsa_problem *problem, const dsa_diag_params *diag, const dsa_tree *tree,
+                                        size_t *bytes);
+
+/*
+ * dsa_decode_step for a tree of drafted tokens: appends the nodes' K/V rows to the cache and lets every
+ * node attend over the cached tokens and over its own line (its ancestors and itself):
+ *   x_j = sm_scale * q_i . k_j over the tokens j that node i sees,  lse_i = ln sum_j e^{x_j},
+ *   out_i = sum_j e^{x_j - lse_i} v_j.
+ * With S = seq_len[b] (tokens already cached; not modified) node i at depth d (roots: 0) has logical
+ * position S + d.  diag == NULL: it sees every cached token and its whole line.  diag->mode ==
+ * DSA_MASK_WINDOW: of both, the tokens fewer than `window` positions behind it, the prompt, and the
+ * first n_sink decode tokens.  Other modes are refused (DSA_ERR_UNSUPPORTED), and so is a bounded
+ * cache (ring_size > 0), whose slots the rejected rows would have overwritten.
+ *   problem->q [B, N, H_q, D], k_new / v_new [B, N, H_kv, D], out [B, N, H_q, D], lse [B, N, H_q]:
+ *   contiguous, the first four 16-byte aligned.  Of problem->plan_flags nothing is used; split_tokens
+ *   is honoured (cached tokens per thread block, rounded up to 64).
+ *   The rows of node i go to cache position S + i whatever the tree's shape (dsa_compact_kv puts the
+ *   accepted ones in order).  Nodes without room (S + i >= max_seq_len) are dropped like those at and
+ *   behind node_count[b]: nothing is appended, out = 0, lse = -inf; k_new, v_new and q of such nodes may
+ *   hold anything.  A negative seq_len drops all nodes.
+ *   Cached rows that no node of the request sees may hold anything (NaN included); a NaN or infinity in
+ *   the V row of a token that some node sees reaches the other nodes of the request as well.
+ */
+DSA_API int32_t dsa_tree_step(const dsa_problem *problem, const dsa_diag_params *diag, const dsa_tree *tree,
+                              const void *k_new, const void *v_new, void *out, float *lse,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* What dsa_verify_tree checks the drafted tokens against. */
+typedef struct dsa_verify {
+    int32_t batch;             /* B                                                                          */
+    int32_t vocab;             /* V >= 1                                                                     */
+    int32_t dtype;             /* dsa_dtype of target_probs and draft_probs                                  */
+    const int32_t *tokens;     /* device [B, N]: the token drafted at each node (node 0's is not read)       */
+    const void *target_probs;  /* device, row (b, i) at (b*N + i) * target_stride: the target's distribution */
+                               /* of the token that follows node i (greedy: any scores, logits for instance) */
+    int64_t target_stride;     /* elements, >= V                                                             */
+    const void *draft_probs;   /* device, likewise: the distribution that node i's children were drawn from, */
+                               /* each on its own; NULL: the children were chosen, not drawn                 */
+    int64_t draft_stride;
+    const float *uniforms;     /* device [B, N] in [0, 1): [b][i] decides about node i, [b][0] the last      */
+                               /* token.  NULL: greedy                                                       */
+} dsa_verify;
+
+/*
+ * Which drafted tokens stand.  Node 0 is the last token that is settled already; the walk starts there.
+ * At a node c with target row p (and draft row q) the children of c are tested in index order; the first
+ * that is accepted becomes c, and where none is the walk ends and the token behind c is chosen:
+ *   greedy         a child stands iff its token is the (lowest) argmax of p; the token behind c is that argmax.
+ *   sampled        v = p, W = 1.  Child i with token x stands iff u_i W q(x) < v(x); otherwise
+ *                  v <- max(v - W q, 0), W <- sum v.  (The rejection sampling that leaves the target's
+ *                  distribution unchanged.)
+ *   chosen (draft_probs NULL)  the same with q a point: child i stands iff u_i W < v(x); otherwise
+ *                  W <- W - v(x), v(x) <- 0.
+ * The token behind c is then the lowest k with v(0) + ... + v(k) > u_0 sum v (v = p again where nothing is
+ * left of v; -1 where p has no positive entry either).  All of this is computed in double precision, so that
+ * the order of the sums decides about nothing.  Tokens outside [0, V) never stand and change nothing.
+ *   path [B, N] int32: the nodes that stand, node 0 first, -1 behind them; accepted [B]: how many they
+ *   are; next_token [B].  A request without nodes gets accepted = 0, next_token = -1.
+ * path / accepted are what dsa_compact_kv takes as keep / keep_count.  No workspace.
+ */
+DSA_API int32_t dsa_verify_tree(const dsa_verify *verify, const dsa_tree *tree, int32_t *path, int32_t *accepted,
+                                int32_t *next_token, void *stream);
+
+/*
+ * Moves kept tokens together: for i < keep_count[b] the K and V rows at position base[b] + keep[b][i] go to
+ * position base[b] + i, in place.  keep [B, max_keep] device, ascending without repeats (so keep[b][i] >= i);
+ * keep_count [B] device, clamped to [0, max_keep]; base [B] device, or NULL for 0.  After a verified tree:
+ * base = seq_len, keep = path.  To drop tokens for good: base = NULL, keep = the positions that stay.
+ * len_out [B] device or NULL: base[b] + (the clamped) keep_count[b]; may be seq_len or base itself.
+ * The cache is that of `problem` (q and max_seq_len's sense as elsewhere: rows at positions outside
+ * [0, max_seq_len) are neither read nor written; refused for bounded caches); with num_layers > 1 the
+ * layers' caches lie stride_layer elements apart behind k_cache and v_cache and one call serves all of them.
+ * A list that is not ascending gives wrong rows, not faults.
+ */
+DSA_API int32_t dsa_compact_kv(const dsa_problem *problem, int32_t num_layers, int64_t stride_layer,
+                               const int32_t *base, const int32_t *keep, const int32_t *keep_count, int32_t max_keep,
+                               int32_t *len_out, void *stream);
+
+/* The pages of a paged cache: a page is free while its count is 0.  Pages are taken lowest index first, so
+ * that equal calls give equal tables.  All arrays on the device; the caller zeroes ref_count to begin with
+ * (and fills block tables with -1, the mark of an entry without a page).  Calls on one pool are ordered by
+ * the caller: one stream, or events. */
+typedef struct dsa_page_pool {
+    int32_t num_blocks;        /* pages of the pool                                                          */
+    int32_t block_size;        /* tokens per page                                                            */
+    int32_t *ref_count;        /* [num_blocks] block-table entries that name the page                        */
+} dsa_page_pool;
+
+/*
+ * Gives every row of block_table [batch, max_blocks] the pages that it lacks to hold seq_len[b] +
+ * extra_tokens tokens (rows with a negative seq_len: none).  Rows are served in order; status[b] is 0, or
+ * the number of pages the row lacks and did not get: a row whose demand goes beyond what is left, then,
+ * gets nothing, and neither does any row behind it that lacks pages; a row longer than max_blocks gets
+ * nothing by itself.  Entries that are not -1 (any negative value counts as -1) are left as they are.
+ * At most 4000 rows per call (DSA_ERR_UNSUPPORTED).
+ */
+DSA_API int32_t dsa_reserve_pages(const dsa_page_pool *pool, int32_t *block_table, int32_t batch, int32_t max_blocks,
+                                  const int32_t *seq_len, int32_t extra_tokens, int32_t *status, void *stream);
+
+/*
+ * Gives back the pages behind the first keep_tokens[b] tokens of every row (negative: none of them;
+ * keep_tokens NULL: all pages of all rows): the entries become -1 and the pages' counts fall by one.
+ */
+DSA_API int32_t dsa_release_pages(const dsa_page_pool *pool, int32_t *block_table, int32_t batch, int32_t max_blocks,
+                                  const int32_t *keep_tokens, void *stream);
+
+/*
+ * Branches requests: row dst[i] of problem's block table becomes a continuation of row src[i], i < n.  The
+ * pages that src[i] has filled are shared (their counts rise); its part-filled last page is copied, in all
+ * layers, to a fresh page; the entries behind it become -1; seq_len and prompt_len of dst[i] become those
+ * of src[i].  (These arrays of `problem` are therefore WRITTEN.)  What row dst[i] held is overwritten without
+ * being given back: release it first.  One source may have many branches.
+ * status[i]: 0; 1: no free page was left for it, nothing was changed; 2: refused, nothing was changed:
+ * src[i] or dst[i] is no row of the table, or dst[i] is also src or an earlier dst of the same call.
+ * workspace: 16 * n bytes, 256-byte aligned.  num_layers, stride_layer as for dsa_compact_kv.
+ */
+DSA_API int32_t dsa_fork_pages(const dsa_page_pool *pool, const dsa_problem *problem, int32_t num_layers,
+                               int64_t stride_layer, const int32_t *src, const int32_t *dst, int32_t n, int32_t *status,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Copies whole pages src[i] -> dst[i], i < n, of all layers (device arrays; pairs with an index outside the
+ * pool are skipped).  No page may be the destination of two pairs, or destination and source.
+ */
+DSA_API int32_t dsa_copy_pages(const dsa_problem *problem, int32_t num_layers, int64_t stride_layer,
+                               const int32_t *src, const int32_t *dst, int32_t n, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,7 +40,9 @@ EXPORTS = ["dsa_version", "dsa_status_string", "dsa_last_cuda_error", "dsa_works
            "dsa_combine_splits", "dsa_debug_kept_indices",
            "dsa_decode_attention_static_scratch", "dsa_append_kv", "dsa_decode_attention_host_io",
            "dsa_decode_attention_host_mapped", "dsa_decode_step", "dsa_advance_seq_len", "dsa_prepare",
-           "dsa_wait_timeouts", "dsa_debug_wait_giveup", "dsa_debug_copy_only", "dsa_build_skip_bitmap"]
+           "dsa_wait_timeouts", "dsa_debug_wait_giveup", "dsa_debug_copy_only", "dsa_build_skip_bitmap",
+           "dsa_tree_workspace_size", "dsa_tree_step", "dsa_verify_tree", "dsa_compact_kv", "dsa_reserve_pages",
+           "dsa_release_pages", "dsa_fork_pages", "dsa_copy_pages"]
 
 
 class dsa_problem(ctypes.Structure):
@@ -76,6 +78,23 @@ class dsa_plan_info(ctypes.Structure):
                 ("block_warps", ctypes.c_int32), ("per_head_lists", ctypes.c_int32),
                 ("cluster_blocks", ctypes.c_int32), ("tensor_map_copies", ctypes.c_int32),
                 ("producer_warps", ctypes.c_int32)]
+
+
+DSA_TREE_MAX_NODES = 64
+
+
+class dsa_tree(ctypes.Structure):
+    _fields_ = [("max_nodes", ctypes.c_int32), ("parent", ctypes.c_void_p), ("node_count", ctypes.c_void_p)]
+
+
+class dsa_verify(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("tokens", ctypes.c_void_p), ("target_probs", ctypes.c_void_p), ("target_stride", ctypes.c_int64),
+                ("draft_probs", ctypes.c_void_p), ("draft_stride", ctypes.c_int64), ("uniforms", ctypes.c_void_p)]
+
+
+class dsa_page_pool(ctypes.Structure):
+    _fields_ = [("num_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32), ("ref_count", ctypes.c_void_p)]
 
 
 def _load() -> ctypes.CDLL:
@@ -122,6 +141,23 @@ def _load() -> ctypes.CDLL:
     lib.dsa_append_kv.argtypes = [vp, vp, vp, i32, vp]
     lib.dsa_debug_kept_indices.restype = i32
     lib.dsa_debug_kept_indices.argtypes = [vp, vp, vp, vp, i32, vp]
+    i64, size = ctypes.c_int64, ctypes.c_size_t
+    lib.dsa_tree_workspace_size.restype = i32
+    lib.dsa_tree_workspace_size.argtypes = [vp, vp, vp, ctypes.POINTER(size)]
+    lib.dsa_tree_step.restype = i32
+    lib.dsa_tree_step.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+    lib.dsa_verify_tree.restype = i32
+    lib.dsa_verify_tree.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.dsa_compact_kv.restype = i32
+    lib.dsa_compact_kv.argtypes = [vp, i32, i64, vp, vp, vp, i32, vp, vp]
+    lib.dsa_reserve_pages.restype = i32
+    lib.dsa_reserve_pages.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp]
+    lib.dsa_release_pages.restype = i32
+    lib.dsa_release_pages.argtypes = [vp, vp, i32, i32, vp, vp]
+    lib.dsa_fork_pages.restype = i32
+    lib.dsa_fork_pages.argtypes = [vp, vp, i32, i64, vp, vp, i32, vp, vp, size, vp]
+    lib.dsa_copy_pages.restype = i32
+    lib.dsa_copy_pages.argtypes = [vp, i32, i64, vp, vp, i32, vp]
     return lib
 
 
@@ -163,7 +199,7 @@ def _dtype_code(t: torch.Tensor) -> int:
 @dataclass
 class Problem:
     """Device tensors and host-side sizes of one decode-attention call (see dsa_problem)."""
-    q: torch.Tensor                       # [B, H_q, D]
+    q: torch.Tensor                       # [B, H_q, D] (dsa_tree_step: [B, N, H_q, D])
     k_cache: torch.Tensor                 # any shape; addressed through `strides`
     v_cache: torch.Tensor
     strides: tuple                        # (stride_batch_or_block, stride_token, stride_head), elements
@@ -183,6 +219,9 @@ class Problem:
 
     def c_struct(self) -> dsa_problem:
         b, hq, d = self.q.shape
+        return self._fill(b, hq, d)
+
+    def _fill(self, b: int, hq: int, d: int) -> dsa_problem:
         assert self.q.is_contiguous() and self.q.is_cuda
         assert self.seq_len.dtype == torch.int32 and self.prompt_len.dtype == torch.int32
         p = dsa_problem()
@@ -473,3 +512,251 @@ def problem_from_host(inp: dict, device: str = "cuda", dtype: torch.dtype = torc
         block_table=None if bt is None else torch.from_numpy(bt).to(device),
         block_size=inp["block_size"], num_blocks=0 if bt is None else int(bt.size),
         split_tokens=split_tokens, plan_flags=plan_flags)
+
+
+# ---- drafted tokens: tree attention, verification, pages ---------------------------------------------------
+def _on(device: torch.device):
+    """The tensors' device as the current one (the library launches on the current device)."""
+    return torch.cuda.device(device)
+
+
+def _same_device(device: torch.device, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("all tensors of a call must be on one device: %s and %s" % (device, t.device))
+
+
+def _int32(t: torch.Tensor, shape: tuple, what: str) -> None:
+    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (what, shape))
+
+
+@dataclass
+class Tree:
+    """The drafted tokens of every request (see dsa_tree)."""
+    max_nodes: int
+    parent: Optional[torch.Tensor] = None        # int32 [B, max_nodes]; None: a chain
+    node_count: Optional[torch.Tensor] = None    # int32 [B]; None: all nodes exist
+
+    def c_struct(self, batch: int) -> dsa_tree:
+        if self.parent is not None:
+            _int32(self.parent, (batch, self.max_nodes), "parent")
+        if self.node_count is not None:
+            _int32(self.node_count, (batch,), "node_count")
+        return dsa_tree(int(self.max_nodes), _dptr(self.parent), _dptr(self.node_count))
+
+
+def _tree_problem(problem: Problem, tree: Tree) -> dsa_problem:
+    b, n, hq, d = problem.q.shape
+    if n != tree.max_nodes:
+        raise ValueError("q must be [batch, max_nodes, heads, head_dim]")
+    return problem._fill(b, hq, d)
+
+
+def dsa_tree_workspace_size(problem: Problem, diag: Optional[Diag], tree: Tree) -> int:
+    p = _tree_problem(problem, tree)
+    d = diag.c_struct() if diag is not None else None
+    t = tree.c_struct(p.batch)
+    n = ctypes.c_size_t(0)
+    _check("dsa_tree_workspace_size", _lib.dsa_tree_workspace_size(_ref(p), _ref(d), _ref(t), ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_tree_outputs(problem: Problem):
+    """out [B, N, H_q, D] like q, lse [B, N, H_q] float32."""
+    return torch.empty_like(problem.q), torch.empty(problem.q.shape[:3], dtype=torch.float32, device=problem.q.device)
+
+
+def alloc_tree_workspace(problem: Problem, diag: Optional[Diag], tree: Tree) -> Optional[torch.Tensor]:
+    with _on(problem.q.device):
+        n = dsa_tree_workspace_size(problem, diag, tree)
+    return None if n == 0 else torch.empty(n, dtype=torch.uint8, device=problem.q.device)
+
+
+def dsa_tree_step(problem: Problem, diag: Optional[Diag], tree: Tree, k_new: torch.Tensor, v_new: torch.Tensor,
+                  out: torch.Tensor, lse: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Append + attention of a tree of drafted tokens in one call: ``problem.q`` is [B, N, H_q, D], ``k_new`` /
+    ``v_new`` [B, N, H_kv, D] are the nodes' rows, ``problem.seq_len`` counts the tokens already cached (it is
+    not advanced).  ``diag``: None (dense) or a WINDOW mask."""
+    p = _tree_problem(problem, tree)
+    b, n, hq, d = problem.q.shape
+    for t in (k_new, v_new):
+        if t.dtype != problem.q.dtype or not t.is_contiguous() or tuple(t.shape) != (b, n, problem.num_kv_heads, d):
+            raise ValueError("k_new and v_new must be contiguous [batch, max_nodes, kv heads, head_dim] of q's type")
+    if out.dtype != problem.q.dtype or not out.is_contiguous() or out.shape != problem.q.shape:
+        raise ValueError("out must be contiguous, of q's shape and type")
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (b, n, hq):
+        raise ValueError("lse must be a contiguous float32 tensor of shape %s" % ((b, n, hq),))
+    dev = problem.q.device
+    _same_device(dev, problem.k_cache, problem.v_cache, problem.seq_len, problem.prompt_len, problem.block_table, k_new, v_new,
+                 out, lse, workspace, tree.parent, tree.node_count)
+    dg = diag.c_struct() if diag is not None else None
+    tr = tree.c_struct(b)
+    ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    with _on(dev):
+        _check("dsa_tree_step",
+               _lib.dsa_tree_step(_ref(p), _ref(dg), _ref(tr), _dptr(k_new), _dptr(v_new), _dptr(out), _dptr(lse),
+                                  _dptr(workspace), ws_n, _stream(stream)))
+
+
+@dataclass
+class Verify:
+    """What the drafted tokens are checked against (see dsa_verify); rows may be padded (last-dimension stride 1)."""
+    tokens: torch.Tensor                          # int32 [B, N]
+    target_probs: torch.Tensor                    # [B, N, V] bf16 or float32
+    draft_probs: Optional[torch.Tensor] = None    # like target_probs; None: the children were chosen, not drawn
+    uniforms: Optional[torch.Tensor] = None       # float32 [B, N] in [0, 1); None: greedy
+
+    def _row_stride(self, t: torch.Tensor, what: str) -> int:
+        b, n = self.tokens.shape
+        if t.dim() != 3 or tuple(t.shape[:2]) != (b, n) or (t.shape[2] > 1 and t.stride(2) != 1):
+            raise ValueError("%s must be [batch, nodes, vocab] with contiguous rows" % what)
+        row = t.stride(1) if n > 1 else (t.stride(0) if b > 1 else t.shape[2])
+        if (b > 1 and t.stride(0) != n * row) or row < t.shape[2]:
+            raise ValueError("%s: rows must lie one fixed stride apart" % what)
+        return row
+
+    def c_struct(self) -> dsa_verify:
+        b, n = self.tokens.shape
+        _int32(self.tokens, (b, n), "tokens")
+        tp, dp, u = self.target_probs, self.draft_probs, self.uniforms
+        stride = self._row_stride(tp, "target_probs")
+        if dp is not None and (dp.dtype != tp.dtype or dp.shape != tp.shape):
+            raise ValueError("draft_probs must have the shape and type of target_probs")
+        if u is not None and (u.dtype != torch.float32 or not u.is_contiguous() or tuple(u.shape) != (b, n)):
+            raise ValueError("uniforms must be a contiguous float32 tensor of shape %s" % ((b, n),))
+        return dsa_verify(b, tp.shape[2], _dtype_code(tp), _dptr(self.tokens), _dptr(tp), stride, _dptr(dp),
+                          0 if dp is None else self._row_stride(dp, "draft_probs"), _dptr(u))
+
+
+def alloc_verify_outputs(verify: Verify):
+    """path [B, N], accepted [B], next_token [B], all int32."""
+    b, n = verify.tokens.shape
+    dev = verify.tokens.device
+    return (torch.empty((b, n), dtype=torch.int32, device=dev), torch.empty((b,), dtype=torch.int32, device=dev),
+            torch.empty((b,), dtype=torch.int32, device=dev))
+
+
+def dsa_verify_tree(verify: Verify, tree: Tree, path: torch.Tensor, accepted: torch.Tensor, next_token: torch.Tensor,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Which drafted tokens stand, and the token behind them."""
+    v = verify.c_struct()
+    b, n = verify.tokens.shape
+    if n != tree.max_nodes:
+        raise ValueError("tokens must be [batch, max_nodes]")
+    tr = tree.c_struct(b)
+    _int32(path, (b, n), "path")
+    _int32(accepted, (b,), "accepted")
+    _int32(next_token, (b,), "next_token")
+    dev = verify.tokens.device
+    _same_device(dev, verify.target_probs, verify.draft_probs, verify.uniforms, tree.parent, tree.node_count, path, accepted,
+                 next_token)
+    with _on(dev):
+        _check("dsa_verify_tree",
+               _lib.dsa_verify_tree(_ref(v), _ref(tr), _dptr(path), _dptr(accepted), _dptr(next_token), _stream(stream)))
+
+
+def dsa_compact_kv(problem: Problem, keep: torch.Tensor, keep_count: torch.Tensor, base: Optional[torch.Tensor] = None,
+                   len_out: Optional[torch.Tensor] = None, num_layers: int = 1, stride_layer: int = 0,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Moves the K / V rows at positions base + keep[b, i] to base + i (``keep`` int32 [B, max_keep] ascending,
+    ``keep_count`` int32 [B]; base None: 0); len_out[b] = base[b] + keep_count[b]."""
+    p = problem.c_struct()
+    b = problem.q.shape[0]
+    if keep.dim() != 2:
+        raise ValueError("keep must be [batch, max_keep]")
+    _int32(keep, (b, keep.shape[1]), "keep")
+    for t, what in ((keep_count, "keep_count"), (base, "base"), (len_out, "len_out")):
+        if t is not None:
+            _int32(t, (b,), what)
+    dev = problem.q.device
+    _same_device(dev, problem.k_cache, problem.v_cache, problem.block_table, keep, keep_count, base, len_out)
+    with _on(dev):
+        _check("dsa_compact_kv",
+               _lib.dsa_compact_kv(_ref(p), int(num_layers), int(stride_layer), _dptr(base), _dptr(keep), _dptr(keep_count),
+                                   keep.shape[1], _dptr(len_out), _stream(stream)))
+
+
+@dataclass
+class PagePool:
+    """The pages of a paged cache (see dsa_page_pool); a page is free while its count is 0."""
+    ref_count: torch.Tensor                       # int32 [num_blocks]
+    block_size: int
+
+    def c_struct(self) -> dsa_page_pool:
+        _int32(self.ref_count, (self.ref_count.numel(),), "ref_count")
+        return dsa_page_pool(self.ref_count.numel(), int(self.block_size), self.ref_count.data_ptr())
+
+
+def _table(block_table: torch.Tensor, rows: Optional[int] = None) -> tuple:
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [rows, max_blocks]")
+    _int32(block_table, (block_table.shape[0] if rows is None else rows, block_table.shape[1]), "block_table")
+    return block_table.shape
+
+
+def dsa_reserve_pages(pool: PagePool, block_table: torch.Tensor, seq_len: torch.Tensor, extra_tokens: int,
+                      status: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Pages for seq_len[b] + extra_tokens tokens in every row; status[b]: 0, or how many are missing."""
+    b, m = _table(block_table)
+    _int32(seq_len, (b,), "seq_len")
+    _int32(status, (b,), "status")
+    _same_device(block_table.device, pool.ref_count, seq_len, status)
+    c = pool.c_struct()
+    with _on(block_table.device):
+        _check("dsa_reserve_pages",
+               _lib.dsa_reserve_pages(_ref(c), _dptr(block_table), b, m, _dptr(seq_len), int(extra_tokens), _dptr(status),
+                                      _stream(stream)))
+
+
+def dsa_release_pages(pool: PagePool, block_table: torch.Tensor, keep_tokens: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Gives back the pages behind the first keep_tokens[b] tokens of every row (negative: none; None: all rows' all)."""
+    b, m = _table(block_table)
+    if keep_tokens is not None:
+        _int32(keep_tokens, (b,), "keep_tokens")
+    _same_device(block_table.device, pool.ref_count, keep_tokens)
+    c = pool.c_struct()
+    with _on(block_table.device):
+        _check("dsa_release_pages",
+               _lib.dsa_release_pages(_ref(c), _dptr(block_table), b, m, _dptr(keep_tokens), _stream(stream)))
+
+
+def alloc_fork_workspace(src: torch.Tensor) -> torch.Tensor:
+    return torch.empty(max(16 * src.numel(), 16), dtype=torch.uint8, device=src.device)
+
+
+def dsa_fork_pages(pool: PagePool, problem: Problem, src: torch.Tensor, dst: torch.Tensor, status: torch.Tensor,
+                   workspace: torch.Tensor, num_layers: int = 1, stride_layer: int = 0,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Row dst[i] of the problem's block table becomes a branch of row src[i]; seq_len and prompt_len follow.
+    status[i]: 0, 1 (no page left) or 2 (refused)."""
+    if problem.block_table is None:
+        raise ValueError("fork needs a paged cache")
+    n = src.numel()
+    for t, what in ((src, "src"), (dst, "dst"), (status, "status")):
+        _int32(t, (n,), what)
+    dev = problem.q.device
+    _same_device(dev, problem.k_cache, problem.v_cache, problem.block_table, problem.seq_len, problem.prompt_len, pool.ref_count,
+                 src, dst, status, workspace)
+    p, c = problem.c_struct(), pool.c_struct()
+    with _on(dev):
+        _check("dsa_fork_pages",
+               _lib.dsa_fork_pages(_ref(c), _ref(p), int(num_layers), int(stride_layer), _dptr(src), _dptr(dst), n,
+                                   _dptr(status), _dptr(workspace), workspace.numel() * workspace.element_size(),
+                                   _stream(stream)))
+
+
+def dsa_copy_pages(problem: Problem, src: torch.Tensor, dst: torch.Tensor, num_layers: int = 1, stride_layer: int = 0,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Whole pages src[i] -> dst[i] of all layers."""
+    n = src.numel()
+    _int32(src, (n,), "src")
+    _int32(dst, (n,), "dst")
+    dev = problem.q.device
+    _same_device(dev, problem.k_cache, problem.v_cache, src, dst)
+    p = problem.c_struct()
+    with _on(dev):
+        _check("dsa_copy_pages",
+               _lib.dsa_copy_pages(_ref(p), int(num_layers), int(stride_layer), _dptr(src), _dptr(dst), n, _stream(stream)))

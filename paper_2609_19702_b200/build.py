@@ -1,8 +1,9 @@
 """Build the CUDA library in-tree: ``python -m paper_2609_19702_b200.build``.
 
 Compiles the translation units under ``csrc/`` for sm_100a with nvcc -- ``dsa_api.cu`` (entry
-points, planner, small kernels) and one unit per (element type, head_dim) with the attention
-kernels, in parallel -- and links them into ``libdsa.so`` beside this file.  nvcc cross-compiles,
+points, planner, small kernels), one unit per (element type, head_dim) with the attention kernels,
+and those of the drafted-token calls (``dsa_tree.cu``, ``dsa_verify.cu``, ``dsa_pages.cu``), in
+parallel -- and links them into ``libdsa.so`` beside this file.  nvcc cross-compiles,
 so no GPU is needed to build.
 """
 from __future__ import annotations
@@ -18,7 +19,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdsa.so")
 SOURCES = ["dsa_api.cu", "dsa_kernels_bf16_d128.cu", "dsa_kernels_bf16_d64.cu", "dsa_kernels_f32_d128.cu",
-           "dsa_kernels_f32_d64.cu"]
+           "dsa_kernels_f32_d64.cu", "dsa_tree.cu", "dsa_verify.cu", "dsa_pages.cu"]
 
 
 def _newest_source_mtime() -> float:

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "dsa_aux.cuh"
+#include "dsa_host.cuh"
 #include "dsa_launch.cuh"
 
 namespace {
@@ -47,10 +48,6 @@ constexpr uint32_t kKnownPlanFlags = DSA_PLAN_CUDA_CORES | DSA_PLAN_NO_ITEM_WARP
                                      DSA_PLAN_GROUP_W4 | DSA_PLAN_HEADS_PER_WARP_MASK | DSA_PLAN_NO_CLUSTER |
                                      DSA_PLAN_CLUSTER2 | DSA_PLAN_CLUSTER4 | DSA_PLAN_GATHER | DSA_PLAN_NO_GATHER | DSA_PLAN_PRODUCERS |
                                      DSA_PLAN_NO_PRODUCERS | DSA_PLAN_METADATA_STABLE;
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-constexpr int kMaxSplits = 8192;                 // split weights of the combine kernel: 32 KB of shared memory
 
 // The launch plan: how many kept rows one block takes, how many splits that makes.
 struct Plan {
@@ -634,11 +631,7 @@ cudaError_t wait_timeouts_address(int** out) {
     return cudaSuccess;
 }
 
-// cuTensorMapEncodeTiled, looked up through the runtime (the library does not link the driver).
-using TensorMapEncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                       const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                       CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
+// (looked up through the runtime: the library does not link the driver)
 TensorMapEncodeFn tensor_map_encoder() {
     static std::atomic<void*> cached{nullptr};
     void* fn = cached.load(std::memory_order_acquire);
@@ -774,6 +767,26 @@ int32_t launch_append(const dsa_problem* problem, const void* k_new, const void*
 
 }  // namespace
 
+// What the other translation units with entry points use of this one (dsa_host.cuh).
+namespace dsa {
+int32_t host_cuda_fail(cudaError_t e) { return cuda_fail(e); }
+int host_sm_count() { return sm_count(); }
+int32_t host_check_problem(const dsa_problem* p) { return check_problem(p); }
+int32_t host_check_diag(const dsa_problem* p, const dsa_diag_params* d) { return check_diag(p, d); }
+cudaError_t host_wait_timeouts_address(int** out) { return wait_timeouts_address(out); }
+TensorMapEncodeFn host_tensor_map_encoder() { return tensor_map_encoder(); }
+void host_cache_args(const dsa_problem* p, AttnArgs* a) {
+    Plan pl = {};
+    pl.mode = MODE_DENSE;
+    pl.n_split = 1;
+    fill_args(p, nullptr, pl, a);
+}
+int32_t host_launch_combine(const float* out_part, const float* lse_part, int64_t rows, int D, int n_split, void* out,
+                            float* lse, int dtype, cudaStream_t st) {
+    return launch_combine(out_part, lse_part, rows, D, n_split, out, lse, dtype, st, nullptr, nullptr, nullptr, nullptr, 0, true);
+}
+}  // namespace dsa
+
 extern "C" {
 
 int32_t dsa_version(void) { return DSA_VERSION; }
@@ -836,6 +849,7 @@ int32_t dsa_prepare(void) {
     if (e == cudaSuccess) e = kernel_prepare<__nv_bfloat16, 128>();
     if (e == cudaSuccess) e = kernel_prepare<float, 64>();
     if (e == cudaSuccess) e = kernel_prepare<float, 128>();
+    if (e == cudaSuccess) e = tree_prepare();
     void* scratch = nullptr;
     if (e == cudaSuccess) e = static_scratch_address(&scratch);   // (and remember it for this device)
     int* counter = nullptr;

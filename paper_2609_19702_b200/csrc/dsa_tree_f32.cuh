@@ -1,0 +1,220 @@
+// Attention of a tree of drafted tokens over a cache, fp32 (dsa_tree_step; formulas in dsa_tree.cuh).
+//
+// fp32 inputs are multiplied in fp32 on the CUDA cores: the tensor cores would round them to tf32.  A block
+// of 256 threads handles 32 query rows of one (request, kv head) and a range of its 64-token tiles: scores
+// as 2 rows x 4 keys per thread, the running maximum and sum kept by the 16 threads that share a row, O as
+// 2 rows x D / 16 dims per thread.  Per tile 32 x 64 x D x 2 fused multiply-adds against 64 x D x 8 bytes:
+// up to some 16 rows the copies are the bound, beyond them the multiply-adds (and the shared-memory reads
+// that feed them, about as many cycles).  Rows are padded by 16 bytes so that the eight rows a quarter-warp
+// reads lie in different banks.  K rows are multiplied as they are (masked scores are replaced), rows of V
+// that no node sees are staged as zeros: their weight is 0, but 0 x NaN is not.
+#pragma once
+#include "dsa_tree.cuh"
+
+namespace dsa {
+
+constexpr int kTreeF32Rows = 32;
+constexpr int kTreeF32Threads = 256;
+
+template <int D>
+struct TreeF32Cfg {
+    static constexpr int LD = D + 4;                       // padded row of Q, K, V, in floats
+    static constexpr int LP = kTreeTile + 4;               // padded row of the weights
+    static constexpr int SMEM = (kTreeF32Rows * LD + 2 * kTreeTile * LD + kTreeF32Rows * LP) * 4;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const TreeArgs g) {
+    using C = TreeF32Cfg<D>;
+    constexpr int DV = D / 4;                              // 16-byte pieces of a row
+    constexpr int OC = D / 64;                             // float4 columns of O per thread
+    extern __shared__ __align__(16) float sm[];
+    float* s_q = sm;
+    float* s_k = s_q + kTreeF32Rows * C::LD;
+    float* s_v = s_k + kTreeTile * C::LD;
+    float* s_p = s_v + kTreeTile * C::LD;
+    __shared__ unsigned long long line_of[kTreeMaxNodes];
+    __shared__ int s_min_depth;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int idx = blockIdx.x;
+    const int rt = idx % g.row_tiles; idx /= g.row_tiles;
+    const int kvh = idx % g.a.H_kv; idx /= g.a.H_kv;
+    const int split = idx % g.a.n_split;
+    const int b = idx / g.a.n_split;
+    const int G = g.G, per_tile = kTreeF32Rows / G, first_node = rt * per_tile;
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    int S, L_p, n;
+    tree_lengths(g, b, S, L_p, n);
+    const int rows_all = min(per_tile, g.N - first_node) * G;
+    const int rows = max(0, min(per_tile, n - first_node)) * G;
+    if (rows == 0) {
+        tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
+        return;
+    }
+    if (warp == 0) {
+        tree_lines(g, b, line_of, lane);
+        __syncwarp();
+        int d = kTreeMaxNodes;
+        for (int i = first_node + lane; i < first_node + rows / G; i += 32) d = min(d, __popcll(line_of[i]) - 1);
+        d = __reduce_min_sync(0xffffffffu, d);
+        if (lane == 0) s_min_depth = d;
+    }
+    __syncthreads();
+    const TreeSpan span = tree_span(g, S, L_p, s_min_depth);
+    const int per_split = (span.T + g.a.n_split - 1) / g.a.n_split;
+    const int t0 = min(span.T, split * per_split), t1 = min(span.T, t0 + per_split);
+    const int cached = t1 - t0, tiles = cached + (split == 0 ? 1 : 0);
+    if (tiles == 0) {
+        tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
+        return;
+    }
+    if (split == 0 && rt == 0) tree_append<float, D>(g, b, kvh, S, L_p, n, tid, kTreeF32Threads);
+
+    for (int i = tid; i < kTreeF32Rows * DV; i += kTreeF32Threads) {
+        const int row = i / DV, c = (i - row * DV) * 4;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row < rows)
+            x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(g.a.q) +
+                                                 (((int64_t)b * g.N + first_node + row / G) * g.a.H_q + kvh * G + row % G) * D + c);
+        *reinterpret_cast<float4*>(s_q + row * C::LD + c) = x;
+    }
+    const int tx = tid & 15, ty = tid >> 4;                // keys tx + 16 k; rows ty, ty + 16
+    const float sl = g.a.scale_log2;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float4 o[2][OC];
+    unsigned long long own[2];
+    int64_t win_lo[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        for (int c = 0; c < OC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int row = ty + 16 * r;
+        own[r] = 0ull;
+        win_lo[r] = 0;
+        if (row >= rows) continue;
+        const unsigned long long line = line_of[first_node + row / G];
+        const int depth = __popcll(line) - 1;
+        win_lo[r] = (int64_t)S + depth + 1 - g.a.mask.window;
+        own[r] = line;                                     // (ancestors of a node that exists exist)
+        if (g.windowed) {
+            unsigned long long todo = line;
+            while (todo) {
+                const int j = __ffsll(todo) - 1;
+                todo &= todo - 1;
+                const int dj = __popcll(line_of[j]) - 1;
+                if (depth - dj >= g.a.mask.window && (int64_t)S + dj >= (int64_t)L_p + g.a.mask.n_sink) own[r] &= ~(1ull << j);
+            }
+        }
+    }
+
+    for (int t = 0; t < tiles; ++t) {
+        int start = 0, from = 0, to = n;
+        if (t < cached) span.tile(t0 + t, start, from, to);
+        __syncthreads();                                   // the last tile has been read (and Q is in place)
+        for (int i = tid; i < kTreeTile * DV; i += kTreeF32Threads) {
+            const int row = i / DV, c = (i - row * DV) * 4;
+            const int pos = start + row;
+            const bool seen = pos >= from && pos < to;
+            int64_t off = 0;
+            if (seen)
+                off = t < cached ? token_offset(g.a, b, L_p, pos) + (int64_t)kvh * g.a.stride_head + c
+                                 : (((int64_t)b * g.N + pos) * g.a.H_kv + kvh) * D + c;
+            const float* kp = reinterpret_cast<const float*>(t < cached ? g.a.k : g.a.k_new) + off;
+            const float* vp = reinterpret_cast<const float*>(t < cached ? g.a.v : g.a.v_new) + off;
+            cp_async16(s_k + row * C::LD + c, kp, seen);
+            cp_async16(s_v + row * C::LD + c, vp, seen);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncthreads();
+        float x[2][4] = {};
+#pragma unroll 4
+        for (int c = 0; c < D; c += 4) {
+            float4 q[2], k[4];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) q[r] = *reinterpret_cast<const float4*>(s_q + (ty + 16 * r) * C::LD + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(s_k + (tx + 16 * j) * C::LD + c);
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    x[r][j] = fmaf(q[r].x, k[j].x, fmaf(q[r].y, k[j].y, fmaf(q[r].z, k[j].z, fmaf(q[r].w, k[j].w, x[r][j]))));
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = tx + 16 * j, pos = start + key;
+                bool seen = ty + 16 * r < rows;
+                if (t < cached) seen = seen && pos >= from && pos < to && (t0 + t < span.T1 || pos >= win_lo[r]);
+                else seen = seen && ((own[r] >> key) & 1ull) != 0;
+                if (!seen) x[r][j] = -INFINITY;
+                mx = fmaxf(mx, x[r][j]);
+            }
+#pragma unroll
+            for (int off = 8; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+            const float m_new = fmaxf(m[r], mx);
+            const float sub = m_new == -INFINITY ? 0.f : m_new * sl;
+            const float alpha = m_new == -INFINITY ? 1.f : exp2f((m[r] - m_new) * sl);
+            m[r] = m_new;
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = exp2f(fmaf(x[r][j], sl, -sub));
+                sum += p;
+                s_p[(ty + 16 * r) * C::LP + tx + 16 * j] = p;
+            }
+#pragma unroll
+            for (int off = 8; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            l[r] = l[r] * alpha + sum;
+#pragma unroll
+            for (int c = 0; c < OC; ++c) { o[r][c].x *= alpha; o[r][c].y *= alpha; o[r][c].z *= alpha; o[r][c].w *= alpha; }
+        }
+        __syncwarp();                                      // a row's 16 threads are in one warp
+#pragma unroll 2
+        for (int j = 0; j < kTreeTile; j += 4) {
+            float4 p[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) p[r] = *reinterpret_cast<const float4*>(s_p + (ty + 16 * r) * C::LP + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int c = 0; c < OC; ++c) {
+                    const float4 v = *reinterpret_cast<const float4*>(s_v + (j + e) * C::LD + 64 * c + 4 * tx);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float w = e == 0 ? p[r].x : e == 1 ? p[r].y : e == 2 ? p[r].z : p[r].w;
+                        o[r][c].x = fmaf(w, v.x, o[r][c].x);
+                        o[r][c].y = fmaf(w, v.y, o[r][c].y);
+                        o[r][c].z = fmaf(w, v.z, o[r][c].z);
+                        o[r][c].w = fmaf(w, v.w, o[r][c].w);
+                    }
+                }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = ty + 16 * r;
+        if (row >= rows_all) continue;
+        const int64_t orow = ((int64_t)b * g.N + first_node + row / G) * g.a.H_q + kvh * G + row % G;
+        const bool none = l[r] == 0.f;
+        const float inv = none ? 0.f : 1.f / l[r];
+        float* dst = g.a.n_split > 1 ? g.a.out_part + (orow * g.a.n_split + split) * D : reinterpret_cast<float*>(g.a.out) + orow * D;
+#pragma unroll
+        for (int c = 0; c < OC; ++c)
+            *reinterpret_cast<float4*>(dst + 64 * c + 4 * tx) =
+                none ? make_float4(0.f, 0.f, 0.f, 0.f)
+                     : make_float4(o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv);
+        if (tx == 0) {
+            const float lse = none ? -INFINITY : (m[r] * sl + log2f(l[r])) * LN2;
+            if (g.a.n_split > 1) g.a.lse_part[orow * g.a.n_split + split] = lse;
+            else g.a.lse[orow] = lse;
+        }
+    }
+}
+
+}  // namespace dsa
