@@ -224,25 +224,18 @@ class Problem:
     def _fill(self, b: int, hq: int, d: int) -> dsa_problem:
         assert self.q.is_contiguous() and self.q.is_cuda
         assert self.seq_len.dtype == torch.int32 and self.prompt_len.dtype == torch.int32
-        p = dsa_problem()
-        p.batch, p.num_q_heads, p.num_kv_heads, p.head_dim = b, hq, self.num_kv_heads, d
-        p.dtype = _dtype_code(self.q)
-        p.sm_scale = float(self.sm_scale)
-        p.q, p.k_cache, p.v_cache = self.q.data_ptr(), self.k_cache.data_ptr(), self.v_cache.data_ptr()
-        p.stride_batch, p.stride_token, p.stride_head = (int(s) for s in self.strides)
-        p.seq_len, p.prompt_len = self.seq_len.data_ptr(), self.prompt_len.data_ptr()
-        if self.block_table is not None:
-            assert self.block_table.dtype == torch.int32 and self.block_table.is_contiguous()
-            p.block_table = self.block_table.data_ptr()
-            p.max_blocks = self.block_table.shape[1]
-            p.block_size = self.block_size
-            p.num_blocks = self.num_blocks
-        p.max_seq_len = int(self.max_seq_len)
-        p.max_prompt_len = int(self.max_prompt_len)
-        p.split_tokens = int(self.split_tokens)
-        p.ring_size, p.ring_sinks = int(self.ring_size), int(self.ring_sinks)
-        p.plan_flags = int(self.plan_flags)
-        return p
+        bt = self.block_table
+        max_blocks = 0
+        if bt is not None:
+            assert bt.dtype == torch.int32 and bt.is_contiguous()
+            max_blocks = bt.shape[1]
+        s0, s1, s2 = self.strides
+        return dsa_problem(b, hq, self.num_kv_heads, d, _dtype_code(self.q), float(self.sm_scale), self.q.data_ptr(),
+                           self.k_cache.data_ptr(), self.v_cache.data_ptr(), int(s0), int(s1), int(s2),
+                           self.seq_len.data_ptr(), self.prompt_len.data_ptr(), None if bt is None else bt.data_ptr(), max_blocks,
+                           0 if bt is None else self.block_size, 0 if bt is None else self.num_blocks, int(self.max_seq_len),
+                           int(self.max_prompt_len), int(self.split_tokens), int(self.ring_size), int(self.ring_sinks),
+                           int(self.plan_flags))
 
 
 @dataclass
@@ -515,19 +508,35 @@ def problem_from_host(inp: dict, device: str = "cuda", dtype: torch.dtype = torc
 
 
 # ---- drafted tokens: tree attention, verification, pages ---------------------------------------------------
-def _on(device: torch.device):
-    """The tensors' device as the current one (the library launches on the current device)."""
-    return torch.cuda.device(device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _same_device(device: torch.device, *tensors: Optional[torch.Tensor]) -> None:
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError("all tensors of a call must be on one device: %s and %s" % (device, t.device))
+def _call(name: str, index: int, stream: Optional[torch.cuda.Stream], *args) -> None:
+    """The library's function `name` on CUDA device `index` (where all of the call's tensors are)."""
+    if index < 0:
+        raise ValueError("%s: the tensors must be on a CUDA device" % name)
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return _call(name, index, stream, *args)
+    if stream is not None:
+        st = stream.cuda_stream
+    else:
+        st = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
+    status = getattr(_lib, name)(*args, st)
+    if status != 0:
+        raise DsaError(name, status)
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    index = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError("all tensors of a call must be on one device: %s and %s" % (first.device, t.device))
+    return index
 
 
 def _int32(t: torch.Tensor, shape: tuple, what: str) -> None:
-    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (what, shape))
 
 
@@ -568,7 +577,7 @@ def alloc_tree_outputs(problem: Problem):
 
 
 def alloc_tree_workspace(problem: Problem, diag: Optional[Diag], tree: Tree) -> Optional[torch.Tensor]:
-    with _on(problem.q.device):
+    with torch.cuda.device(problem.q.device):
         n = dsa_tree_workspace_size(problem, diag, tree)
     return None if n == 0 else torch.empty(n, dtype=torch.uint8, device=problem.q.device)
 
@@ -582,22 +591,19 @@ def dsa_tree_step(problem: Problem, diag: Optional[Diag], tree: Tree, k_new: tor
     p = _tree_problem(problem, tree)
     b, n, hq, d = problem.q.shape
     for t in (k_new, v_new):
-        if t.dtype != problem.q.dtype or not t.is_contiguous() or tuple(t.shape) != (b, n, problem.num_kv_heads, d):
+        if t.dtype != problem.q.dtype or t.shape != (b, n, problem.num_kv_heads, d) or not t.is_contiguous():
             raise ValueError("k_new and v_new must be contiguous [batch, max_nodes, kv heads, head_dim] of q's type")
     if out.dtype != problem.q.dtype or not out.is_contiguous() or out.shape != problem.q.shape:
         raise ValueError("out must be contiguous, of q's shape and type")
-    if lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (b, n, hq):
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != (b, n, hq):
         raise ValueError("lse must be a contiguous float32 tensor of shape %s" % ((b, n, hq),))
-    dev = problem.q.device
-    _same_device(dev, problem.k_cache, problem.v_cache, problem.seq_len, problem.prompt_len, problem.block_table, k_new, v_new,
-                 out, lse, workspace, tree.parent, tree.node_count)
+    dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.seq_len, problem.prompt_len, problem.block_table, k_new,
+                       v_new, out, lse, workspace, tree.parent, tree.node_count)
     dg = diag.c_struct() if diag is not None else None
     tr = tree.c_struct(b)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    with _on(dev):
-        _check("dsa_tree_step",
-               _lib.dsa_tree_step(_ref(p), _ref(dg), _ref(tr), _dptr(k_new), _dptr(v_new), _dptr(out), _dptr(lse),
-                                  _dptr(workspace), ws_n, _stream(stream)))
+    _call("dsa_tree_step", dev, stream, _ref(p), _ref(dg), _ref(tr), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(),
+          lse.data_ptr(), _dptr(workspace), ws_n)
 
 
 @dataclass
@@ -610,7 +616,7 @@ class Verify:
 
     def _row_stride(self, t: torch.Tensor, what: str) -> int:
         b, n = self.tokens.shape
-        if t.dim() != 3 or tuple(t.shape[:2]) != (b, n) or (t.shape[2] > 1 and t.stride(2) != 1):
+        if t.dim() != 3 or t.shape[:2] != (b, n) or (t.shape[2] > 1 and t.stride(2) != 1):
             raise ValueError("%s must be [batch, nodes, vocab] with contiguous rows" % what)
         row = t.stride(1) if n > 1 else (t.stride(0) if b > 1 else t.shape[2])
         if (b > 1 and t.stride(0) != n * row) or row < t.shape[2]:
@@ -624,7 +630,7 @@ class Verify:
         stride = self._row_stride(tp, "target_probs")
         if dp is not None and (dp.dtype != tp.dtype or dp.shape != tp.shape):
             raise ValueError("draft_probs must have the shape and type of target_probs")
-        if u is not None and (u.dtype != torch.float32 or not u.is_contiguous() or tuple(u.shape) != (b, n)):
+        if u is not None and (u.dtype != torch.float32 or not u.is_contiguous() or u.shape != (b, n)):
             raise ValueError("uniforms must be a contiguous float32 tensor of shape %s" % ((b, n),))
         return dsa_verify(b, tp.shape[2], _dtype_code(tp), _dptr(self.tokens), _dptr(tp), stride, _dptr(dp),
                           0 if dp is None else self._row_stride(dp, "draft_probs"), _dptr(u))
@@ -649,12 +655,9 @@ def dsa_verify_tree(verify: Verify, tree: Tree, path: torch.Tensor, accepted: to
     _int32(path, (b, n), "path")
     _int32(accepted, (b,), "accepted")
     _int32(next_token, (b,), "next_token")
-    dev = verify.tokens.device
-    _same_device(dev, verify.target_probs, verify.draft_probs, verify.uniforms, tree.parent, tree.node_count, path, accepted,
-                 next_token)
-    with _on(dev):
-        _check("dsa_verify_tree",
-               _lib.dsa_verify_tree(_ref(v), _ref(tr), _dptr(path), _dptr(accepted), _dptr(next_token), _stream(stream)))
+    dev = _same_device(verify.tokens, verify.target_probs, verify.draft_probs, verify.uniforms, tree.parent, tree.node_count, path,
+                       accepted, next_token)
+    _call("dsa_verify_tree", dev, stream, _ref(v), _ref(tr), path.data_ptr(), accepted.data_ptr(), next_token.data_ptr())
 
 
 def dsa_compact_kv(problem: Problem, keep: torch.Tensor, keep_count: torch.Tensor, base: Optional[torch.Tensor] = None,
@@ -670,12 +673,9 @@ def dsa_compact_kv(problem: Problem, keep: torch.Tensor, keep_count: torch.Tenso
     for t, what in ((keep_count, "keep_count"), (base, "base"), (len_out, "len_out")):
         if t is not None:
             _int32(t, (b,), what)
-    dev = problem.q.device
-    _same_device(dev, problem.k_cache, problem.v_cache, problem.block_table, keep, keep_count, base, len_out)
-    with _on(dev):
-        _check("dsa_compact_kv",
-               _lib.dsa_compact_kv(_ref(p), int(num_layers), int(stride_layer), _dptr(base), _dptr(keep), _dptr(keep_count),
-                                   keep.shape[1], _dptr(len_out), _stream(stream)))
+    dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.block_table, keep, keep_count, base, len_out)
+    _call("dsa_compact_kv", dev, stream, _ref(p), int(num_layers), int(stride_layer), _dptr(base), keep.data_ptr(),
+          keep_count.data_ptr(), keep.shape[1], _dptr(len_out))
 
 
 @dataclass
@@ -702,12 +702,10 @@ def dsa_reserve_pages(pool: PagePool, block_table: torch.Tensor, seq_len: torch.
     b, m = _table(block_table)
     _int32(seq_len, (b,), "seq_len")
     _int32(status, (b,), "status")
-    _same_device(block_table.device, pool.ref_count, seq_len, status)
+    dev = _same_device(block_table, pool.ref_count, seq_len, status)
     c = pool.c_struct()
-    with _on(block_table.device):
-        _check("dsa_reserve_pages",
-               _lib.dsa_reserve_pages(_ref(c), _dptr(block_table), b, m, _dptr(seq_len), int(extra_tokens), _dptr(status),
-                                      _stream(stream)))
+    _call("dsa_reserve_pages", dev, stream, _ref(c), block_table.data_ptr(), b, m, seq_len.data_ptr(), int(extra_tokens),
+          status.data_ptr())
 
 
 def dsa_release_pages(pool: PagePool, block_table: torch.Tensor, keep_tokens: Optional[torch.Tensor] = None,
@@ -716,11 +714,9 @@ def dsa_release_pages(pool: PagePool, block_table: torch.Tensor, keep_tokens: Op
     b, m = _table(block_table)
     if keep_tokens is not None:
         _int32(keep_tokens, (b,), "keep_tokens")
-    _same_device(block_table.device, pool.ref_count, keep_tokens)
+    dev = _same_device(block_table, pool.ref_count, keep_tokens)
     c = pool.c_struct()
-    with _on(block_table.device):
-        _check("dsa_release_pages",
-               _lib.dsa_release_pages(_ref(c), _dptr(block_table), b, m, _dptr(keep_tokens), _stream(stream)))
+    _call("dsa_release_pages", dev, stream, _ref(c), block_table.data_ptr(), b, m, _dptr(keep_tokens))
 
 
 def alloc_fork_workspace(src: torch.Tensor) -> torch.Tensor:
@@ -737,15 +733,11 @@ def dsa_fork_pages(pool: PagePool, problem: Problem, src: torch.Tensor, dst: tor
     n = src.numel()
     for t, what in ((src, "src"), (dst, "dst"), (status, "status")):
         _int32(t, (n,), what)
-    dev = problem.q.device
-    _same_device(dev, problem.k_cache, problem.v_cache, problem.block_table, problem.seq_len, problem.prompt_len, pool.ref_count,
-                 src, dst, status, workspace)
+    dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.block_table, problem.seq_len, problem.prompt_len,
+                       pool.ref_count, src, dst, status, workspace)
     p, c = problem.c_struct(), pool.c_struct()
-    with _on(dev):
-        _check("dsa_fork_pages",
-               _lib.dsa_fork_pages(_ref(c), _ref(p), int(num_layers), int(stride_layer), _dptr(src), _dptr(dst), n,
-                                   _dptr(status), _dptr(workspace), workspace.numel() * workspace.element_size(),
-                                   _stream(stream)))
+    _call("dsa_fork_pages", dev, stream, _ref(c), _ref(p), int(num_layers), int(stride_layer), src.data_ptr(), dst.data_ptr(), n,
+          status.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
 def dsa_copy_pages(problem: Problem, src: torch.Tensor, dst: torch.Tensor, num_layers: int = 1, stride_layer: int = 0,
@@ -754,9 +746,6 @@ def dsa_copy_pages(problem: Problem, src: torch.Tensor, dst: torch.Tensor, num_l
     n = src.numel()
     _int32(src, (n,), "src")
     _int32(dst, (n,), "dst")
-    dev = problem.q.device
-    _same_device(dev, problem.k_cache, problem.v_cache, src, dst)
+    dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.block_table, src, dst)
     p = problem.c_struct()
-    with _on(dev):
-        _check("dsa_copy_pages",
-               _lib.dsa_copy_pages(_ref(p), int(num_layers), int(stride_layer), _dptr(src), _dptr(dst), n, _stream(stream)))
+    _call("dsa_copy_pages", dev, stream, _ref(p), int(num_layers), int(stride_layer), src.data_ptr(), dst.data_ptr(), n)

@@ -156,6 +156,19 @@ def test_binding_refuses_shapes(dsa):
         dsa.PagePool(torch.zeros(4, dtype=torch.int64), 16).c_struct()
 
 
+def test_binding_refuses_host_tensors(dsa):
+    """Nothing is handed to the library unless it lies on a CUDA device."""
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    v = dsa.Verify(i(2, 3), torch.zeros(2, 3, 8))
+    with pytest.raises(ValueError):
+        dsa.dsa_verify_tree(v, dsa.Tree(3), i(2, 3), i(2), i(2))
+    pool = dsa.PagePool(i(8), 4)
+    with pytest.raises(ValueError):
+        dsa.dsa_reserve_pages(pool, i(2, 3), i(2), 1, i(2))
+    with pytest.raises(ValueError):
+        dsa.dsa_release_pages(pool, i(2, 3))
+
+
 def test_references_by_hand():
     # a line of two over two cached tokens, one head: weights from logits (0, ln 3, ln 4)
     q = torch.zeros((2, 1, 2), dtype=torch.float64)
