@@ -12,11 +12,29 @@ namespace {
 using namespace dsa;
 
 struct TreePlan {
-    int G, row_tiles, n_split;
+    int G, row_tiles;
+    int n_split;                                   // pieces whose partial results go through the workspace (1: none)
+    int cluster;                                   // or blocks of a cluster that merge on chip (1: none)
     int64_t blocks;
     int box_tokens, align_tokens;
     size_t ws_out_bytes, ws_total;
 };
+
+// How many blocks of a cluster should share the tiles of one (request, kv head, 128 rows).  The estimate: waves of
+// blocks x the time of one, in units of a tile, where a block's set-up costs about four tiles and a merge two more; a
+// last wave that is only part full costs a full one.  The lengths on the device are not known here and may be
+// shorter than the bound: what counts is their ratio.
+int choose_cluster(int64_t items, int64_t tiles, int64_t places) {
+    int best = 1;
+    double best_cost = 0;
+    for (int c = 1; c <= 8; c *= 2) {
+        if (c > 1 && tiles < 2 * c) break;
+        const int64_t waves = (items * c + places - 1) / places;
+        const double cost = (double)waves * (4.0 + (double)((tiles + c - 1) / c) + (c > 1 ? 2.0 : 0.0));
+        if (c == 1 || cost < best_cost) { best = c; best_cost = cost; }
+    }
+    return best;
+}
 
 int32_t make_tree_plan(const dsa_problem* p, const dsa_diag_params* d, const dsa_tree* tree, TreePlan* pl) {
     int32_t rc = host_check_problem(p);
@@ -50,18 +68,23 @@ int32_t make_tree_plan(const dsa_problem* p, const dsa_diag_params* d, const dsa
     tiles = std::max<int64_t>(tiles, 1);
     const int64_t items = std::max<int64_t>(1, (int64_t)p->batch * p->num_kv_heads * pl->row_tiles);
     int64_t want = 1;
+    pl->cluster = 1;
+    const bool bf16 = p->dtype == DSA_BF16;
     if (p->split_tokens > 0) {
         const int64_t per = (p->split_tokens + (int64_t)kTreeTile - 1) / kTreeTile;
         want = (tiles + per - 1) / per;
     } else {
-        // two blocks share an SM: split until every place is taken, but not below four tiles per block
-        const int64_t places = 2 * (int64_t)host_sm_count();
-        want = std::min((places + items - 1) / items, std::max<int64_t>(1, tiles / 4));
-        if (items * 2 > places) want = 1;
+        const int64_t places = 2 * (int64_t)host_sm_count();         // two blocks share an SM
+        if (bf16) pl->cluster = choose_cluster(items, tiles, places);
+        // eight blocks are too few where even they leave most places empty and have many tiles each
+        if (!bf16 || (pl->cluster == 8 && items * 16 <= places && tiles >= 8 * 16)) {
+            want = std::min(std::max<int64_t>(places / items, 1), std::max<int64_t>(1, tiles / 4));
+            if (want > 1) pl->cluster = 1;
+        }
     }
     if (want > kMaxSplits) return DSA_ERR_UNSUPPORTED;
     pl->n_split = (int)want;
-    pl->blocks = items * want;
+    pl->blocks = items * want * pl->cluster;
     if (pl->blocks > 0x7fffffffLL) return DSA_ERR_UNSUPPORTED;
     pl->ws_out_bytes = pl->ws_total = 0;
     if (want > 1) {
@@ -121,17 +144,21 @@ int32_t build_tree_maps(const dsa_problem* p, const dsa_tree* tree, const TreePl
 }
 
 template <class Kern, class... Args>
-cudaError_t launch_tree(Kern kern, int64_t blocks, int threads, int smem, cudaStream_t st, const Args&... args) {
+cudaError_t launch_tree(Kern kern, int64_t blocks, int threads, int smem, int cluster, cudaStream_t st, const Args&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
@@ -148,12 +175,12 @@ cudaError_t configure_f32() {
 template <int D>
 cudaError_t run_bf16(const TreeArgs& g, const TreeMaps& m, int64_t blocks, cudaStream_t st) {
     const cudaError_t e = configure_bf16<D>();
-    return e != cudaSuccess ? e : launch_tree(dsa_tree_kernel<D>, blocks, kTreeThreads, TreeCfg<D>::SMEM, st, g, m);
+    return e != cudaSuccess ? e : launch_tree(dsa_tree_kernel<D>, blocks, kTreeThreads, TreeCfg<D>::SMEM, g.cluster, st, g, m);
 }
 template <int D>
 cudaError_t run_f32(const TreeArgs& g, int64_t blocks, cudaStream_t st) {
     const cudaError_t e = configure_f32<D>();
-    return e != cudaSuccess ? e : launch_tree(dsa_tree_f32_kernel<D>, blocks, kTreeF32Threads, TreeF32Cfg<D>::SMEM, st, g);
+    return e != cudaSuccess ? e : launch_tree(dsa_tree_f32_kernel<D>, blocks, kTreeF32Threads, TreeF32Cfg<D>::SMEM, 1, st, g);
 }
 
 }  // namespace
@@ -205,6 +232,8 @@ int32_t dsa_tree_step(const dsa_problem* problem, const dsa_diag_params* diag, c
     g.G = pl.G;
     g.row_tiles = pl.row_tiles;
     g.box_tokens = pl.box_tokens;
+    for (g.box_shift = 0; (1 << g.box_shift) < pl.box_tokens;) ++g.box_shift;
+    g.cluster = pl.cluster;
     g.align_tokens = pl.align_tokens;
     if (pl.n_split > 1) {
         g.a.out_part = reinterpret_cast<float*>(workspace);

@@ -17,8 +17,16 @@
 // warps 0-3 own the 128 rows, one thread per row (32 TMEM lanes per warp): they read S = Q K^T from TMEM,
 // keep the running maximum and sum, and write P = e^{x - m} back to TMEM as bf16, where it is the A
 // operand of O += P V.  S is double buffered: S(j + 1) is computed while tile j's softmax runs.  Warps
-// whose 32 rows do not exist sit out.  TMEM: 2 x 64 columns of S (P takes the place of the S it came from) +
-// D of O, 256 allocated; two blocks share an SM, so one's set-up and last tile hide behind the other's.
+// whose 32 rows do not exist sit out.  Warps 6 and 7 append the nodes' rows to the cache meanwhile (by the
+// softmax warps, before their first tile, that took 6 us of a 60 us block).  TMEM: 2 x 64 columns of S (P
+// takes the place of the S it came from) + D of O, 256 allocated; two blocks share an SM, so one's set-up
+// and last tile hide behind the other's.
+//
+// Work is cut along the cached tokens where there are fewer blocks than places, or where their number leaves
+// the last wave of blocks half empty: the 2, 4 or 8 blocks of a thread-block cluster share the tiles of one
+// (request, kv head) and merge their states through distributed shared memory, without partial results in
+// HBM or a second launch.  Only where eight are too few (a long sequence under one or two heads) partial
+// results go to the workspace and the combine kernel.
 //
 // The maximum that the exponentials are taken against trails the true one by at most 2^8 (it is replaced,
 // and O rescaled, only when a row's maximum has grown beyond that): e^{x - m} then reaches at most 256,
@@ -36,7 +44,7 @@ namespace dsa {
 constexpr int kTreeMaxNodes = 64;
 constexpr int kTreeTile = 64;                      // tokens per K / V tile
 constexpr int kTreeRows = 128;                     // query rows per block: the M of the products
-constexpr int kTreeThreads = 192;
+constexpr int kTreeThreads = 256;
 
 struct TreeArgs {
     AttnArgs a;                                    // lengths, block table, strides, scale, outputs
@@ -46,7 +54,9 @@ struct TreeArgs {
     int row_tiles;                                 // blocks of kTreeRows query rows per (request, kv head)
     int windowed;                                  // 0: dense
     int box_tokens;                                // tokens per tensor-map box of the caches
+    int box_shift;                                 // and its logarithm
     int align_tokens;                              // where a box may start: box_tokens (pages), 1 (contiguous)
+    int cluster;                                   // blocks that share the tiles and merge on chip (1: none; else n_split is 1)
     int blk_coord, head_coord;                     // 0: the map's outer / head dimension has one entry (stride 0)
 };
 
@@ -64,6 +74,7 @@ struct TreeCfg {
     static constexpr int SLOTS = D == 128 ? 5 : 10;                        // two blocks per SM with either
     static constexpr int TAIL = 1024;                                      // barriers and node tables
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT_BYTES + TAIL;
+    static constexpr int PART_LD = D + 4;                                  // row of a partial result, in floats
     static constexpr int TMEM_COLS = 256;
     static constexpr int COL_S = 0, COL_O = 2 * kTreeTile;
 };
@@ -130,7 +141,7 @@ __host__ __device__ constexpr unsigned instr_desc(int M, int N, bool b_mn) {
 }
 
 // ---- what a block works on, in 64-token tiles ---------------------------------------------------------
-// The cached tokens that some node of the block sees: [0, P0) (dense: everything; windowed: prompt and
+// The cached tokens that some node of the request sees: [0, P0) (dense: everything; windowed: prompt and
 // sinks) and [lo, S).  Tiles 0 .. T1-1 start at 64 t, tiles T1 .. T-1 at lo_al + 64 (t - T1) with lo_al = lo
 // rounded down to a whole box.
 struct TreeSpan {
@@ -150,14 +161,14 @@ __device__ __forceinline__ void tree_lengths(const TreeArgs& g, int b, int& S, i
     n = raw < 0 ? 0 : min(n, g.a.max_seq_len - S);
 }
 
-__device__ __forceinline__ TreeSpan tree_span(const TreeArgs& g, int S, int L_p, int min_depth) {
+__device__ __forceinline__ TreeSpan tree_span(const TreeArgs& g, int S, int L_p) {
     TreeSpan s;
     s.S = S;
     if (!g.windowed) {
         s.P0 = S; s.lo = s.lo_al = S;
     } else {
         s.P0 = L_p + min(g.a.mask.n_sink, S - L_p);
-        s.lo = min(S, max(s.P0, S + min_depth + 1 - g.a.mask.window));
+        s.lo = min(S, max(s.P0, S + 1 - g.a.mask.window));          // (a root's window)
         s.lo_al = s.lo / g.align_tokens * g.align_tokens;
     }
     s.T1 = (s.P0 + kTreeTile - 1) / kTreeTile;
@@ -197,14 +208,16 @@ __device__ __forceinline__ void tree_lines(const TreeArgs& g, int b, unsigned lo
     line_of[lane + 32] = m[1];
 }
 
-// The nodes' K / V rows of kv head kvh to the cache, by `count` threads.
+// K / V rows of the nodes first, first + step, ... below n, kv head kvh, to the cache, by `count` threads.
 template <typename T, int D>
-__device__ __forceinline__ void tree_append(const TreeArgs& g, int b, int kvh, int S, int L_p, int n, int tid, int count) {
+__device__ __forceinline__ void tree_append(const TreeArgs& g, int b, int kvh, int S, int L_p, int first, int step, int n, int tid,
+                                            int count) {
     constexpr int VEC = 16 / (int)sizeof(T), CPR = D / VEC;
     T* kc = reinterpret_cast<T*>(const_cast<void*>(g.a.k));
     T* vc = reinterpret_cast<T*>(const_cast<void*>(g.a.v));
-    for (int i = tid; i < n * CPR; i += count) {
-        const int node = i / CPR, c = (i - node * CPR) * VEC;
+#pragma unroll 4
+    for (int i = tid; i < (n - first + step - 1) / step * CPR; i += count) {
+        const int node = first + i / CPR * step, c = i % CPR * VEC;
         const int64_t src = (((int64_t)b * g.N + node) * g.a.H_kv + kvh) * D + c;
         const int64_t dst = token_offset(g.a, b, L_p, S + node) + (int64_t)kvh * g.a.stride_head + c;
         *reinterpret_cast<uint4*>(kc + dst) = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(g.a.k_new) + src);
@@ -246,6 +259,32 @@ __device__ __forceinline__ bool tree_wait(unsigned long long* bar, unsigned pari
     return __all_sync(0xffffffffu, ok);                       // (one answer for the warp)
 }
 
+// ---- thread-block clusters ---------------------------------------------------------------------------
+__device__ __forceinline__ void tree_cluster_barrier() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ unsigned tree_peer(const void* p, unsigned rank) {   // p in the shared memory of block `rank`
+    unsigned r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float2 tree_peer_f2(unsigned addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 tree_peer_f4(unsigned addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+    unsigned r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArgs g, const __grid_constant__ TreeMaps maps) {
     using C = TreeCfg<D>;
@@ -262,139 +301,154 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     unsigned long long* pv_done = q_full + 5;                 // [2] O holds the tile
     unsigned long long* drained = q_full + 7;
     unsigned long long* line_of = q_full + 8;                 // [64]
-    int* s_misc = reinterpret_cast<int*>(line_of + kTreeMaxNodes);   // [0] TMEM address, [1] abort, [2] lowest depth
-    static_assert((2 * C::SLOTS + 8 + kTreeMaxNodes) * 8 + 12 <= C::TAIL, "tail of the shared memory");
+    int* s_misc = reinterpret_cast<int*>(line_of + kTreeMaxNodes);   // [0] TMEM address, [1] abort
+    static_assert((2 * C::SLOTS + 8 + kTreeMaxNodes) * 8 + 8 <= C::TAIL, "tail of the shared memory");
     volatile int* abort = s_misc + 1;
+    // after the last product, for a merge within the cluster: O (rows padded against bank conflicts) and per row
+    // (maximum in base-2 units, sum)
+    float* s_part = reinterpret_cast<float*>(s_ring);
+    float2* s_ml = reinterpret_cast<float2*>(s_q);
+    static_assert(kTreeRows * C::PART_LD * 4 <= C::SLOTS * C::SLOT_BYTES, "the partial result takes the ring's place");
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int idx = blockIdx.x;
+    const int pieces = g.cluster * g.a.n_split;               // (one of the two is 1)
+    const int piece = idx % pieces; idx /= pieces;
     const int rt = idx % g.row_tiles; idx /= g.row_tiles;
-    const int kvh = idx % g.a.H_kv; idx /= g.a.H_kv;
-    const int split = idx % g.a.n_split;
-    const int b = idx / g.a.n_split;
+    const int kvh = idx % g.a.H_kv;
+    const int b = idx / g.a.H_kv;
     const int G = g.G, per_tile = kTreeRows / G, first_node = rt * per_tile;
 
+    // set-up that reads nothing: it may run while the launch in front finishes
+    if (warp == 4 && lane == 0) {
+        for (int s = 0; s < C::SLOTS; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 1); }
+        mbar_init(q_full, 1);
+        for (int s = 0; s < 2; ++s) { mbar_init(s_full + s, 1); mbar_init(pv_done + s, 1); }
+        mbar_init(drained, 1);
+        s_misc[1] = 0;
+    } else if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(s_misc)), "r"((unsigned)C::TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        tc_fence_before();
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     int S, L_p, n;
     tree_lengths(g, b, S, L_p, n);
     const int rows_all = min(per_tile, g.N - first_node) * G;              // rows that this block writes
     const int rows = max(0, min(per_tile, n - first_node)) * G;            // rows of nodes that exist
-    if (rows == 0) {
-        tree_write_empty<T, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeThreads);
-        return;
-    }
-    const int active_warps = (rows + 31) / 32;
-    if (warp == 0) {
-        tree_lines(g, b, line_of, lane);
-        __syncwarp();
-        int d = kTreeMaxNodes;
-        for (int i = first_node + lane; i < first_node + rows / G; i += 32) d = min(d, __popcll(line_of[i]) - 1);
-        d = __reduce_min_sync(0xffffffffu, d);
-        if (lane == 0) { s_misc[2] = d; s_misc[1] = 0; }
-    } else if (warp == 5 && lane == 0) {
-        for (int s = 0; s < C::SLOTS; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 1); }
-        mbar_init(q_full, 1);
-        for (int s = 0; s < 2; ++s) { mbar_init(s_full + s, 1); mbar_init(p_ready + s, active_warps); mbar_init(pv_done + s, 1); }
-        mbar_init(drained, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
-    const TreeSpan span = tree_span(g, S, L_p, s_misc[2]);
-    const int per_split = (span.T + g.a.n_split - 1) / g.a.n_split;
-    const int t0 = min(span.T, split * per_split), t1 = min(span.T, t0 + per_split);
-    const bool has_nodes = split == 0;                                      // the nodes' own rows: one tile more, the last
-    const int cached = t1 - t0, tiles = cached + (has_nodes ? 1 : 0);
-    if (tiles == 0) {
-        tree_write_empty<T, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeThreads);
-        return;
-    }
+    const int active_warps = (rows + 31) / 32;                              // warps with rows
+    const TreeSpan span = tree_span(g, S, L_p);
+    const int per_piece = (span.T + pieces - 1) / pieces;
+    const int t0 = min(span.T, piece * per_piece), t1 = min(span.T, t0 + per_piece);
+    const bool has_nodes = piece == 0;                                      // the nodes' own rows: one tile more, the last
+    const int cached = t1 - t0;
+    const int tiles = rows == 0 ? 0 : cached + (has_nodes ? 1 : 0);
 
+    float m_ref = -INFINITY, l = 0.f;                         // softmax threads: maximum (of the raw scores) and sum of their row
+    unsigned tmem = 0;
     if (warp == 4) {
         // ---- copies -------------------------------------------------------------------------------
-        const int r = g.box_tokens;
         if (lane == 0) {
-            const int box_nodes = min(per_tile, g.N);
-            mbar_expect_tx(q_full, (unsigned)(C::HALVES * box_nodes * G * 128));
-            for (int h = 0; h < C::HALVES; ++h) tma_box4(s_q + h * C::Q_HALF, &maps.q, 64 * h, kvh * G, first_node, b, q_full);
+            for (int s = 0; s < 2; ++s) mbar_init(p_ready + s, max(active_warps, 1));
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
-        int issued = 0;
-        // the page (or request) of this lane's boxes `lane` and `lane + 32` of tile t; loaded a tile ahead of its copies
-        auto ids_of = [&](int t, int (&blk)[2]) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                blk[h] = g.blk_coord ? b : 0;
-                const int j = lane + 32 * h;
-                if (t < cached && g.a.block_table && j * r < kTreeTile) {
-                    int start, from, to;
-                    span.tile(t0 + t, start, from, to);
-                    const int bi = min((start + j * r) / g.a.block_size, g.a.max_blocks - 1);
-                    blk[h] = max(0, min(g.a.block_table[(int64_t)b * g.a.max_blocks + bi], g.a.num_blocks - 1)) * g.blk_coord;
-                }
-            }
-        };
-        auto issue = [&](int t, bool is_v, const int (&blk)[2]) -> bool {
-            const int s = issued % C::SLOTS;
-            if (issued >= C::SLOTS && !tree_wait(empty + s, (issued / C::SLOTS - 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
-            unsigned char* dst = s_ring + s * C::SLOT_BYTES;
-            if (t < cached) {
-                int start, from, to;
-                span.tile(t0 + t, start, from, to);
-                const int j0 = (from - start) / r, j1 = (to - start + r - 1) / r;
-                if (lane == 0) mbar_expect_tx(full + s, (unsigned)((j1 - j0) * C::HALVES * r * 128));
-                __syncwarp();
-#pragma unroll
-                for (int h2 = 0; h2 < 2; ++h2) {
-                    const int j = lane + 32 * h2;
-                    if (j < j0 || j >= j1) continue;
-                    const int pos = start + j * r;
-                    const int tok = g.a.block_table ? pos % g.a.block_size : pos;
-                    for (int h = 0; h < C::HALVES; ++h)
-                        tma_box4(dst + h * C::KV_HALF + j * r * 128, is_v ? &maps.v : &maps.k, 64 * h, tok, kvh * g.head_coord,
-                                 blk[h2], full + s);
-                }
-            } else if (lane == 0) {
-                mbar_expect_tx(full + s, (unsigned)(C::HALVES * g.N * 128));
-                for (int h = 0; h < C::HALVES; ++h)
-                    tma_box4(dst + h * C::KV_HALF, is_v ? &maps.v_new : &maps.k_new, 64 * h, 0, kvh, b, full + s);
+        asm volatile("bar.arrive 1, 192;" ::: "memory");      // (the barriers are ready)
+        if (tiles > 0) {
+            if (lane == 0) {
+                const int box_nodes = min(per_tile, g.N);
+                mbar_expect_tx(q_full, (unsigned)(C::HALVES * box_nodes * G * 128));
+                for (int h = 0; h < C::HALVES; ++h) tma_box4(s_q + h * C::Q_HALF, &maps.q, 64 * h, kvh * G, first_node, b, q_full);
             }
             __syncwarp();
-            ++issued;
-            return true;
-        };
-        int id0[2], id1[2], id2[2];
-        ids_of(0, id0);
-        ids_of(1, id1);
-        bool ok = issue(0, false, id0) && (tiles < 2 || issue(1, false, id1));
-        for (int t = 0; ok && t < tiles; ++t) {
-            ids_of(t + 2, id2);
-            ok = issue(t, true, id0) && (t + 2 >= tiles || issue(t + 2, false, id2));
+            const int shift = g.box_shift;
+            // where this lane's boxes `lane` and `lane + 32` of a tile come from: (page or request, token in it);
+            // looked up two tiles ahead of their copies
+            struct Where { int blk[2], tok[2]; };
+            auto where = [&](int t) -> Where {
+                Where w;
+                int start = 0, from, to;
+                if (t < cached) span.tile(t0 + t, start, from, to);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) { id0[h] = id1[h]; id1[h] = id2[h]; }
+                for (int h = 0; h < 2; ++h) {
+                    const int pos = start + ((lane + 32 * h) << shift);
+                    w.blk[h] = g.blk_coord ? b : 0;
+                    w.tok[h] = pos;
+                    if (g.a.block_table) {
+                        const int bi = pos / g.a.block_size;
+                        w.tok[h] = pos - bi * g.a.block_size;
+                        if (t < cached && ((lane + 32 * h) << shift) < kTreeTile)
+                            w.blk[h] = max(0, min(__ldg(g.a.block_table + (int64_t)b * g.a.max_blocks + min(bi, g.a.max_blocks - 1)),
+                                                  g.a.num_blocks - 1)) * g.blk_coord;
+                    }
+                }
+                return w;
+            };
+            int issued = 0, slot = 0, round = 0;
+            auto issue = [&](int t, bool is_v, const Where& w) -> bool {
+                if (round > 0 && !tree_wait(empty + slot, (round - 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
+                unsigned char* dst = s_ring + slot * C::SLOT_BYTES;
+                unsigned long long* bar = full + slot;
+                if (t < cached) {
+                    int start, from, to;
+                    span.tile(t0 + t, start, from, to);
+                    const int j0 = (from - start) >> shift, j1 = (to - start + (1 << shift) - 1) >> shift;
+                    if (lane == 0) mbar_expect_tx(bar, (unsigned)(((j1 - j0) * C::HALVES) << shift) * 128u);
+                    __syncwarp();
+                    const CUtensorMap* map = is_v ? &maps.v : &maps.k;
+#pragma unroll
+                    for (int h2 = 0; h2 < 2; ++h2) {
+                        const int j = lane + 32 * h2;
+                        if (j >= j0 && j < j1) {
+#pragma unroll
+                            for (int h = 0; h < C::HALVES; ++h)
+                                tma_box4(dst + h * C::KV_HALF + ((j << shift) * 128), map, 64 * h, w.tok[h2], kvh * g.head_coord,
+                                         w.blk[h2], bar);
+                        }
+                        if (shift >= 1) break;
+                    }
+                } else if (lane == 0) {
+                    mbar_expect_tx(bar, (unsigned)(C::HALVES * g.N * 128));
+#pragma unroll
+                    for (int h = 0; h < C::HALVES; ++h)
+                        tma_box4(dst + h * C::KV_HALF, is_v ? &maps.v_new : &maps.k_new, 64 * h, 0, kvh, b, bar);
+                }
+                __syncwarp();
+                ++issued;
+                if (++slot == C::SLOTS) { slot = 0; ++round; }
+                return true;
+            };
+            Where w0 = where(0), w1 = where(1), w2 = where(2);
+            bool ok = issue(0, false, w0) && (tiles < 2 || issue(1, false, w1));
+            for (int t = 0; ok && t < tiles; ++t) {
+                const Where w3 = where(t + 3);
+                ok = issue(t, true, w0) && (t + 2 >= tiles || issue(t + 2, false, w2));
+                w0 = w1; w1 = w2; w2 = w3;
+            }
+            // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
+            volatile int no_abort = 0;
+            tree_wait(q_full, 0u, &no_abort, nullptr, lane);
+            for (int c = max(0, issued - C::SLOTS); c < issued; ++c)
+                if (!tree_wait(full + c % C::SLOTS, (c / C::SLOTS) & 1, &no_abort, nullptr, lane)) break;
         }
-        // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
-        volatile int no_abort = 0;
-        tree_wait(q_full, 0u, &no_abort, nullptr, lane);
-        for (int c = max(0, issued - C::SLOTS); c < issued; ++c)
-            if (!tree_wait(full + c % C::SLOTS, (c / C::SLOTS) & 1, &no_abort, nullptr, lane)) break;
+    } else if (warp >= 6) {
+        // ---- the nodes' rows to the cache: every block those of its own nodes, the pieces in turn ----------------
+        tree_append<T, D>(g, b, kvh, S, L_p, first_node + piece, pieces, min(n, first_node + per_tile), tid - 192, 64);
     } else {
-        if (warp == 5) {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                         ::"r"(smem_u32(s_misc)), "r"((unsigned)C::TMEM_COLS) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-            tc_fence_before();
-        }
-        asm volatile("bar.sync 1, 160;" ::: "memory");
+        if (warp == 0) tree_lines(g, b, line_of, lane);
+        asm volatile("bar.sync 1, 192;" ::: "memory");
         tc_fence_after();
-        const unsigned tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
+        tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
         if (warp == 5) {
             // ---- products ---------------------------------------------------------------------------
             constexpr unsigned kIdescS = instr_desc(kTreeRows, kTreeTile, false), kIdescO = instr_desc(kTreeRows, D, true);
-            int used = 0;
+            int slot = 0, round = 0;                         // of the ring
+            auto next_slot = [&]() { if (++slot == C::SLOTS) { slot = 0; ++round; } };
             auto scores = [&](int t) -> bool {
-                const int s = used % C::SLOTS;
-                if (!tree_wait(full + s, (used / C::SLOTS) & 1, abort, g.a.wait_timeouts, lane)) return false;
+                const int s = slot;
+                if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
                 tc_fence_after();
                 if (lane == 0) {
                     const unsigned qa = smem_u32(s_q), ka = smem_u32(s_ring + s * C::SLOT_BYTES);
@@ -407,13 +461,13 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                     tc_commit(s_full + (t & 1));
                 }
                 __syncwarp();
-                ++used;
+                next_slot();
                 return true;
             };
             auto values = [&](int t) -> bool {
                 if (!tree_wait(p_ready + (t & 1), (t >> 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
-                const int s = used % C::SLOTS;
-                if (!tree_wait(full + s, (used / C::SLOTS) & 1, abort, g.a.wait_timeouts, lane)) return false;
+                const int s = slot;
+                if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
                 unsigned char* v = s_ring + s * C::SLOT_BYTES;
                 // rows of V that nobody sees: zero, whatever the cache or the slot held there
                 int lo = 0, hi = n;
@@ -444,12 +498,12 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                     tc_commit(pv_done + (t & 1));
                 }
                 __syncwarp();
-                ++used;
+                next_slot();
                 return true;
             };
-            bool ok = tree_wait(q_full, 0u, abort, g.a.wait_timeouts, lane) && scores(0) && (tiles < 2 || scores(1));
+            bool ok = tiles > 0 && tree_wait(q_full, 0u, abort, g.a.wait_timeouts, lane) && scores(0) && (tiles < 2 || scores(1));
             for (int t = 0; ok && t < tiles; ++t) ok = values(t) && (t + 2 >= tiles || scores(t + 2));
-            if (!ok) {                                       // TMEM is given back only when no product uses it
+            if (!ok && tiles > 0) {                          // TMEM is given back only when no product uses it
                 if (lane == 0) tc_commit(drained);
                 __syncwarp();
                 volatile int no_abort = 0;
@@ -457,14 +511,12 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
             }
         } else {
             // ---- softmax: one thread per query row --------------------------------------------------
-            if (has_nodes && rt == 0) tree_append<T, D>(g, b, kvh, S, L_p, n, tid, 128);
             const int row = tid;                              // of the block's 128
             const int node = first_node + row / G;
             const bool alive = row < rows;
-            const bool work = warp < active_warps;
+            const bool work = tiles > 0 && warp < active_warps;
             const unsigned lane_base = (unsigned)(warp * 32) << 16;
             const float sl = g.a.scale_log2;
-            float m_ref = -INFINITY, l = 0.f;                 // (m_ref in units of the raw scores)
             bool ok = true;
             if (work) {
                 const unsigned long long line = alive ? line_of[node] : 0ull;
@@ -548,7 +600,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                         const float p0 = fast_exp2(fmaf(__uint_as_float(a0), sl, -sub));
                         const float p1 = fast_exp2(fmaf(__uint_as_float(a1), sl, -sub));
                         sum[i & 3] += p0 + p1;
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(pk[i]) : "f"(p1), "f"(p0));
+                        pk[i] = pack_bf16(p0, p1);
                     }
                     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     tc_st32(s_addr, pk);
@@ -561,7 +613,9 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 tc_fence_after();
             }
             // ---- results --------------------------------------------------------------------------
-            if (work && ok) {
+            if (g.cluster > 1) {
+                // (merged below)
+            } else if (work && ok) {
                 const bool mine = row < rows_all;
                 const bool none = l == 0.f;                    // nothing seen: zeros and -inf
                 const float inv = none ? 0.f : 1.f / l;
@@ -577,7 +631,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     #pragma unroll
                         for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : __uint_as_float(o[i]) * inv;
                         if (g.a.n_split > 1) {
-                            float* dst = g.a.out_part + (orow * g.a.n_split + split) * D + c;
+                            float* dst = g.a.out_part + (orow * g.a.n_split + piece) * D + c;
     #pragma unroll
                             for (int i = 0; i < 32; i += 4)
                                 *reinterpret_cast<float4*>(dst + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
@@ -588,7 +642,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                                 unsigned w[4];
     #pragma unroll
                                 for (int k = 0; k < 4; ++k)
-                                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(f[i + 2 * k + 1]), "f"(f[i + 2 * k]));
+                                    w[k] = pack_bf16(f[i + 2 * k], f[i + 2 * k + 1]);
                                 *reinterpret_cast<uint4*>(dst + i) = make_uint4(w[0], w[1], w[2], w[3]);
                             }
                         }
@@ -596,16 +650,61 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                     __syncwarp();
                 }
                 if (mine) {
-                    if (g.a.n_split > 1) g.a.lse_part[orow * g.a.n_split + split] = lse;
+                    if (g.a.n_split > 1) g.a.lse_part[orow * g.a.n_split + piece] = lse;
                     else g.a.lse[orow] = lse;
                 }
             } else if (!work) {
-                // rows of nodes that do not exist, beyond the last warp with rows
-                const int first = active_warps * 32;
-                tree_write_empty<T, D>(g, b, kvh, split, first_node, first, rows_all, tid - first, 128 - first);
+                // rows of nodes that do not exist, beyond the last warp with rows; all rows where there is nothing to see
+                const int first = tiles > 0 ? active_warps * 32 : 0;
+                tree_write_empty<T, D>(g, b, kvh, piece, first_node, first, rows_all, tid - first, 128 - first);
             }
         }
         tc_fence_before();
+    }
+    if (g.cluster > 1) {
+        // ---- merge: out = sum_i e^{m_i - M} O_i / sum_i e^{m_i - M} l_i over the cluster's blocks --------------
+        __syncthreads();                                      // the ring and Q have been read for the last time
+        if (warp < 4) {
+            s_ml[tid] = make_float2(l == 0.f ? -INFINITY : m_ref * g.a.scale_log2, l);
+            if (tiles > 0 && warp < active_warps) {
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    unsigned o[32];
+                    tc_ld32(o, tmem + ((unsigned)(warp * 32) << 16) + C::COL_O + c);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<uint4*>(s_part + tid * C::PART_LD + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                }
+                tc_fence_before();
+            }
+        }
+        tree_cluster_barrier();
+        constexpr int LPR = D / 4, RPW = 32 / LPR;            // lanes per row (four dims each), rows per warp
+        const int sub = lane / LPR, c4 = (lane % LPR) * 4;
+        for (int r = piece + (warp * RPW + sub) * g.cluster; r < rows_all; r += 8 * RPW * g.cluster) {
+            float m_max = -INFINITY;
+            for (int i = 0; i < g.cluster; ++i) m_max = fmaxf(m_max, tree_peer_f2(tree_peer(s_ml + r, i)).x);
+            float sum = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = 0; i < g.cluster; ++i) {
+                const float2 ml = tree_peer_f2(tree_peer(s_ml + r, i));
+                if (ml.y == 0.f) continue;                    // (a piece that saw nothing has no O either)
+                const float w = fast_exp2(ml.x - m_max);
+                const float4 o = tree_peer_f4(tree_peer(s_part + r * C::PART_LD + c4, i));
+                sum = fmaf(w, ml.y, sum);
+                acc.x = fmaf(w, o.x, acc.x); acc.y = fmaf(w, o.y, acc.y);
+                acc.z = fmaf(w, o.z, acc.z); acc.w = fmaf(w, o.w, acc.w);
+            }
+            const bool none = sum == 0.f;
+            const float inv = none ? 0.f : 1.f / sum;
+            const int64_t orow = ((int64_t)b * g.N + first_node + r / G) * g.a.H_q + kvh * G + r % G;
+            *reinterpret_cast<uint2*>(reinterpret_cast<T*>(g.a.out) + orow * D + c4) =
+                none ? make_uint2(0u, 0u) : make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+            if (c4 == 0) g.a.lse[orow] = none ? -INFINITY : (m_max + log2f(sum)) * LN2;
+        }
+        tree_cluster_barrier();                               // nobody leaves while its shared memory may be read
     }
     __syncthreads();
     if (warp == 5) {

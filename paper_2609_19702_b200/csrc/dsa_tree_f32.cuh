@@ -34,14 +34,13 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
     float* s_v = s_k + kTreeTile * C::LD;
     float* s_p = s_v + kTreeTile * C::LD;
     __shared__ unsigned long long line_of[kTreeMaxNodes];
-    __shared__ int s_min_depth;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int idx = blockIdx.x;
+    const int split = idx % g.a.n_split; idx /= g.a.n_split;
     const int rt = idx % g.row_tiles; idx /= g.row_tiles;
-    const int kvh = idx % g.a.H_kv; idx /= g.a.H_kv;
-    const int split = idx % g.a.n_split;
-    const int b = idx / g.a.n_split;
+    const int kvh = idx % g.a.H_kv;
+    const int b = idx / g.a.H_kv;
     const int G = g.G, per_tile = kTreeF32Rows / G, first_node = rt * per_tile;
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -54,24 +53,17 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
         tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
         return;
     }
-    if (warp == 0) {
-        tree_lines(g, b, line_of, lane);
-        __syncwarp();
-        int d = kTreeMaxNodes;
-        for (int i = first_node + lane; i < first_node + rows / G; i += 32) d = min(d, __popcll(line_of[i]) - 1);
-        d = __reduce_min_sync(0xffffffffu, d);
-        if (lane == 0) s_min_depth = d;
-    }
+    if (warp == 0) tree_lines(g, b, line_of, lane);
     __syncthreads();
-    const TreeSpan span = tree_span(g, S, L_p, s_min_depth);
+    const TreeSpan span = tree_span(g, S, L_p);
     const int per_split = (span.T + g.a.n_split - 1) / g.a.n_split;
     const int t0 = min(span.T, split * per_split), t1 = min(span.T, t0 + per_split);
     const int cached = t1 - t0, tiles = cached + (split == 0 ? 1 : 0);
+    tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
     if (tiles == 0) {
         tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
         return;
     }
-    if (split == 0 && rt == 0) tree_append<float, D>(g, b, kvh, S, L_p, n, tid, kTreeF32Threads);
 
     for (int i = tid; i < kTreeF32Rows * DV; i += kTreeF32Threads) {
         const int row = i / DV, c = (i - row * DV) * 4;
