@@ -850,6 +850,7 @@ int32_t dsa_prepare(void) {
     if (e == cudaSuccess) e = kernel_prepare<float, 64>();
     if (e == cudaSuccess) e = kernel_prepare<float, 128>();
     if (e == cudaSuccess) e = tree_prepare();
+    if (e == cudaSuccess) e = verify_prepare();
     void* scratch = nullptr;
     if (e == cudaSuccess) e = static_scratch_address(&scratch);   // (and remember it for this device)
     int* counter = nullptr;

@@ -29,6 +29,7 @@ int32_t host_launch_combine(const float* out_part, const float* lse_part, int64_
                             float* lse, int dtype, cudaStream_t st);
 
 cudaError_t tree_prepare();                                  // configure the drafted-token kernels for the current device
+cudaError_t verify_prepare();
 
 // Kernels that use more than 48 KB of dynamic shared memory must be told so once per device (idempotent).
 template <class Kern>

@@ -78,6 +78,14 @@ def test_vocabularies(dsa, dtype, mode, v):
 
 
 @pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("v", [2049, 65537, 100003, 131072, 150001, 230003])
+def test_large_vocabularies(dsa, mode, v):
+    rng = np.random.default_rng(v)
+    _check(dsa, _draw(rng, 3, 5, v, 1, mode, torch.bfloat16, sharp=0.2))
+    _check(dsa, _draw(rng, 2, 6, v, 0, mode, torch.float32, pad=1))
+
+
+@pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("n,branch,chain", [(1, 1, False), (2, 1, False), (33, 1, False), (64, 4, False), (64, 0, False), (17, 0, True)])
 def test_trees(dsa, mode, n, branch, chain):
     rng = np.random.default_rng(n + branch)
