@@ -10,14 +10,15 @@
 // What bounds it: one or two rows of p and q per request, some 100 KB to 1 MB, and then the latency of the
 // passes, one after the other.  So a request is worked on by a cluster of up to 8 blocks, each with a
 // contiguous piece of the vocabulary cut into one run per warp, and blocks exchange nothing but one sum per
-// warp through distributed shared memory.  The residual of the current node stays in the blocks' shared memory,
-// every thread its own entries, so that a second rejection reads q only and the draw reads nothing (in
-// registers it cost so many that one block filled an SM: 60 us against 26 for 64 requests x 65536 entries).
-// Pieces that shared memory cannot hold (vocabularies beyond some 220000 entries) are read again in every pass
-// and the residual is recomputed from the k weights W.
+// warp through distributed shared memory.  The residual of the current node stays in their shared memory, every
+// thread its own entries, so that a second rejection reads q only and the draw reads nothing; pieces too large for
+// that (vocabularies beyond some 220000 entries) are read again in every pass and the residual is recomputed from
+// the k weights W.
 //
-// Sums are in double precision: with 32 bits the token at the border of a cumulative sum would hang on the
-// order of the additions (at 65536 entries and 24 bits once in some hundred draws), with 53 it does not.
+// Precision: with 24-bit sums the token at the border of a cumulative sum would hang on the order of the additions
+// (at 65536 entries once in some hundred draws).  Entries and sums are pairs of floats (high + low, about 48 bits,
+// error-free sums and products after Knuth and Dekker) and not doubles, whose unit is narrow.  One warp of a block
+// walks the tree and tells the others what to do.
 #include "dsa_host.cuh"
 
 #include <algorithm>
@@ -73,35 +74,50 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// What is left of the target's row at the current node: v_0 = p, v_{k+1} = max(v_k - W_k q, 0), or p with
-// the turned-down tokens taken out.
-struct Residual {
-    int k;                         // rejections at this node
-    const double* weight;          // shared: W_0 .. W_{k-1}
-    const int* out;                // shared: the k turned-down tokens (draft given as points)
-    __device__ __forceinline__ double with_draft(double p, double q) const {
-        for (int r = 0; r < k; ++r) p = fmax(fma(-weight[r], q, p), 0.0);
-        return p;
-    }
-    __device__ __forceinline__ double with_points(double p, int x) const {
-        for (int r = 0; r < k; ++r)
-            if (out[r] == x) p = 0.0;
-        return p;
-    }
-};
-
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    return v;
+// ---- pairs of floats: the value is h + l, |l| at most half a unit of h ----------------------------------
+struct Pair { float h, l; };
+__device__ __forceinline__ Pair two_sum(float a, float b) {                 // a + b without an error
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
 }
-__device__ __forceinline__ double warp_prefix(double v, int lane) {          // inclusive
+__device__ __forceinline__ void add_to(Pair& acc, const Pair& x) {
+    const Pair s = two_sum(acc.h, x.h);
+    acc.h = s.h;
+    acc.l = __fadd_rn(acc.l, __fadd_rn(s.l, x.l));
+}
+__device__ __forceinline__ Pair times(const Pair& a, float b) {
+    const float h = __fmul_rn(a.h, b);
+    return {h, __fmaf_rn(a.l, b, __fmaf_rn(a.h, b, -h))};
+}
+__device__ __forceinline__ bool exceeds(const Pair& a, const Pair& b) {     // (near each other a.h - b.h is exact)
+    return __fadd_rn(__fsub_rn(a.h, b.h), __fsub_rn(a.l, b.l)) > 0.f;
+}
+// max(v - w q, 0)
+__device__ __forceinline__ Pair reject(const Pair& v, const Pair& w, float q) {
+    const float ph = __fmul_rn(w.h, q), pl = __fmaf_rn(w.l, q, __fmaf_rn(w.h, q, -ph));
+    const Pair d = two_sum(v.h, -ph);
+    const float e = __fadd_rn(d.l, __fsub_rn(v.l, pl));
+    const float h = __fadd_rn(d.h, e);
+    const bool some = h > 0.f;
+    return {some ? h : 0.f, some ? __fsub_rn(e, __fsub_rn(h, d.h)) : 0.f};
+}
+
+__device__ __forceinline__ Pair warp_sum(Pair v) {                          // lane 0's order of additions, for every lane
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) {
+        const Pair o = {__shfl_down_sync(0xffffffffu, v.h, off), __shfl_down_sync(0xffffffffu, v.l, off)};
+        add_to(v, o);
+    }
+    return {__shfl_sync(0xffffffffu, v.h, 0), __shfl_sync(0xffffffffu, v.l, 0)};
+}
+__device__ __forceinline__ Pair warp_prefix(Pair v, int lane) {             // of the lanes before this one
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const double o = __shfl_up_sync(0xffffffffu, v, off);
-        if (lane >= off) v += o;
+        const Pair o = {__shfl_up_sync(0xffffffffu, v.h, off), __shfl_up_sync(0xffffffffu, v.l, off)};
+        if (lane >= off) add_to(v, o);
     }
-    return v;
+    const Pair up = {__shfl_up_sync(0xffffffffu, v.h, 1), __shfl_up_sync(0xffffffffu, v.l, 1)};
+    return lane > 0 ? up : Pair{0.f, 0.f};
 }
 // (score, index): the larger score, of equal ones the lower index; kNone: no entry yet
 constexpr int kNone = 0x7fffffff;
@@ -109,30 +125,43 @@ __device__ __forceinline__ void take_better(float& best, int& arg, float o, int 
     if (oi != kNone && (arg == kNone || o > best || (o == best && oi < arg))) { best = o; arg = oi; }
 }
 
+// What the blocks' warps are told to do next: sum what is left at `node` after `k` rejections; draw from it (warp
+// `run` of the cluster, whose entries begin at the cumulative sum `before`, looks for `goal`); or nothing any more.
+enum : int { kSum, kDraw, kDone };
+struct Task {
+    int what, node, k, run;
+    Pair before, goal;
+};
+
 // W warps per block; KEEP: the residual is kept (dynamic shared memory, 8 bytes per entry of the block's piece)
 template <typename T, int W, bool GREEDY, bool KEEP>
-__global__ void __launch_bounds__(32 * W, 32 / W) dsa_verify_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_kernel(const VerifyArgs a) {
     constexpr int kRuns = kVerifyMaxCluster * W;
     // one sum (greedy: best score and its index) per warp of the cluster, two sets: the blocks may be one pass apart
-    __shared__ double s_sum[2][kRuns];
+    __shared__ Pair s_sum[2][kRuns];
     __shared__ float s_best[2][kRuns];
     __shared__ int s_arg[2][kRuns];
-    extern __shared__ __align__(16) double s_left[];
-    __shared__ double s_weight[kVerifyMaxNodes];
-    __shared__ int s_out[kVerifyMaxNodes];
+    __shared__ Task s_task;
+    __shared__ Pair s_weight[kVerifyMaxNodes];               // W of the rejections at the current node
+    __shared__ int s_out[kVerifyMaxNodes];                   // and the turned-down tokens (draft given as points)
     __shared__ int s_token[kVerifyMaxNodes], s_parent[kVerifyMaxNodes], s_path[kVerifyMaxNodes];
+    __shared__ unsigned s_children[2 * kVerifyMaxNodes];     // of every node, a bit each
     __shared__ float s_u[kVerifyMaxNodes], s_p[kVerifyMaxNodes], s_q[kVerifyMaxNodes];
+    extern __shared__ __align__(16) Pair s_left[];
 
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned rank, blocks;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
+    if (blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // (this block has started)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int b = blockIdx.x / blocks;
     const int n = a.node_count ? max(0, min(a.node_count[b], a.N)) : a.N;
     const T* p0 = reinterpret_cast<const T*>(a.p);
     const T* q0 = reinterpret_cast<const T*>(a.q);
     const bool points = a.q == nullptr;
+    if (tid < 2 * kVerifyMaxNodes) s_children[tid] = 0u;
+    __syncthreads();
     if (tid < a.N) {
         const int64_t i = (int64_t)b * a.N + tid;
         const int x = a.tokens[i];
@@ -140,22 +169,17 @@ __global__ void __launch_bounds__(32 * W, 32 / W) dsa_verify_kernel(const Verify
         if (up < 0 || up >= tid) up = -1;
         s_token[tid] = x;
         s_parent[tid] = up;
+        if (up >= 0 && tid < n) atomicOr(&s_children[2 * up + (tid >> 5)], 1u << (tid & 31));
         s_u[tid] = GREEDY ? 0.f : a.u[i];
         const bool valid = up >= 0 && x >= 0 && x < a.V;
         const int64_t row = (int64_t)b * a.N + max(up, 0);
         s_p[tid] = valid && !GREEDY ? (float)p0[row * a.p_stride + x] : 0.f;
         s_q[tid] = valid && !GREEDY && !points ? (float)q0[row * a.q_stride + x] : 0.f;
-        s_path[tid] = -1;
+        s_path[tid] = tid == 0 && n > 0 ? 0 : -1;
     }
     __syncthreads();
-    if (n == 0) {                                            // (the same for every block of the cluster)
-        if (rank == 0) {
-            if (tid < a.N) a.path[(int64_t)b * a.N + tid] = -1;
-            if (tid == 0) { a.accepted[b] = 0; a.next_token[b] = -1; }
-        }
-        return;
-    }
-    if (blocks > 1) cluster_barrier();                       // every block has started: its shared memory may be written
+    // every block has started: its shared memory may be written
+    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 
     const int slot = (int)rank * W + warp;                   // this warp's run of the vocabulary: [lo, hi)
     const int n_runs = (int)blocks * W, per_lane = (n_runs + 31) / 32;
@@ -171,227 +195,320 @@ __global__ void __launch_bounds__(32 * W, 32 / W) dsa_verify_kernel(const Verify
         constexpr uintptr_t mask = 4 * sizeof(T) - 1;
         vec = ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & mask) == 0;
     };
-    double* kept = s_left + warp * a.run;                    // what is left of the current node's row: this warp's run
-    int held = -1;                                           // the node that it belongs to
-    // the sum of what is left at `node` after res.k rejections; leaves the warps' sums in s_sum[(pass - 1) & 1]
-    auto sum_left = [&](int node, const Residual& res) -> double {
-        const T *p, *q;
-        bool vec;
-        rows_of(node, p, q, vec);
-        double acc[4] = {0.0, 0.0, 0.0, 0.0};
-        const bool need_q = !points && res.k > 0;
-        // a node's first pass follows its first rejection, and every one its own: `kept` lacks the last one only
-        const bool fresh = !KEEP || held != node || res.k == 0;
-        const double w = KEEP && need_q ? -res.weight[res.k - 1] : 0.0;
+    int length = n > 0 ? 1 : 0;                              // of the path
+
+    if constexpr (GREEDY) {
+        // the lowest index of the largest score at `node`; `next` (or -1): the node whose row is wanted next, likely
+        auto best_of = [&](int node, int next) -> int {
+            const T *p, *q;
+            bool vec;
+            rows_of(node, p, q, vec);
+            if (next >= 0) {                                 // one line of the next row per lane and step
+                const T* ahead = p0 + ((int64_t)b * a.N + next) * a.p_stride;
+                for (int i = lo + lane * (128 / (int)sizeof(T)); i < hi; i += 32 * (128 / (int)sizeof(T)))
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + i));
+            }
+            float best = -INFINITY;
+            int arg = kNone;
 #pragma unroll 4
-        for (int i = lo + 4 * lane; i < hi; i += 128) {
-            float fp[4], fq[4] = {0.f, 0.f, 0.f, 0.f};
-            double x[4];
-            if (fresh) load4(p, i, hi, vec, fp);
-            if (need_q) load4(q, i, hi, vec, fq);
-            if (fresh) {
+            for (int i = lo + 4 * lane; i < hi; i += 128) {
+                float f[4];
+                load4(p, i, hi, vec, f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = (double)fp[e];
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < hi && (f[e] > best || arg == kNone)) { best = f[e]; arg = i + e; }
+            }
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1)
+                take_better(best, arg, __shfl_xor_sync(0xffffffffu, best, off), __shfl_xor_sync(0xffffffffu, arg, off));
+            if (lane < (int)blocks) {
+                asm volatile("st.shared::cluster.f32 [%0], %1;"
+                             ::"r"(map_to_rank(smem_u32(&s_best[pass & 1][slot]), lane)), "f"(best) : "memory");
+                asm volatile("st.shared::cluster.u32 [%0], %1;"
+                             ::"r"(map_to_rank(smem_u32(&s_arg[pass & 1][slot]), lane)), "r"(arg) : "memory");
+            }
+            meet();
+            best = -INFINITY;
+            arg = kNone;
+            for (int w = lane * per_lane; w < min(n_runs, (lane + 1) * per_lane); ++w)
+                take_better(best, arg, s_best[pass & 1][w], s_arg[pass & 1][w]);
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1)
+                take_better(best, arg, __shfl_xor_sync(0xffffffffu, best, off), __shfl_xor_sync(0xffffffffu, arg, off));
+            ++pass;
+            return arg;
+        };
+        auto first_child = [&](int node) -> int {
+            const unsigned low = s_children[2 * node], high = s_children[2 * node + 1];
+            return low ? __ffs(low) - 1 : high ? 31 + __ffs(high) : -1;
+        };
+        int best = -1;
+        if (n > 0) best = best_of(0, first_child(0));
+        int cur = 0;
+        for (int i = 1; i < n; ++i) {                        // (every thread of every block takes the same decisions)
+            if (s_parent[i] != cur || s_token[i] != best) continue;
+            cur = i;
+            if (tid == 0) s_path[length] = i;
+            ++length;
+            best = best_of(cur, first_child(cur));
+        }
+        if (rank == 0 && tid == 0) a.next_token[b] = best;
+    } else {
+        Pair* kept = s_left + warp * a.run;                  // what is left of the current node's row: this warp's run
+        int held = -1;                                       // the node that it belongs to
+        // one entry after k rejections, from p and q
+        auto left_of = [&](float p, float q, int x, int k) -> Pair {
+            Pair v = {p, 0.f};
+            if (points) {
+                for (int r = 0; r < k; ++r)
+                    if (s_out[r] == x) v.h = 0.f;
             } else {
-                const double2 x0 = *reinterpret_cast<const double2*>(kept + (i - lo)), x1 = *reinterpret_cast<const double2*>(kept + (i - lo) + 2);
-                x[0] = x0.x; x[1] = x0.y; x[2] = x1.x; x[3] = x1.y;
+                for (int r = 0; r < k; ++r) v = reject(v, s_weight[r], q);
             }
+            return v;
+        };
+        Pair runs_before = {0.f, 0.f};                       // warp 0: the sum of the runs before this lane's
+        // the sum of what is left at `node` after k rejections; leaves the warps' sums in s_sum[(pass - 1) & 1]
+        auto sum_left = [&](int node, int k) -> Pair {
+            const T *p, *q;
+            bool vec;
+            rows_of(node, p, q, vec);
+            Pair acc[4] = {};
+            const bool need_q = !points && k > 0;
+            // a node's first pass follows its first rejection, and every one its own: `kept` lacks the last one only
+            const bool fresh = !KEEP || held != node || k == 0;
+            const Pair w = KEEP && need_q ? s_weight[k - 1] : Pair{0.f, 0.f};
+            for (int i0 = lo; i0 < hi; i0 += 512) {          // four stretches of 128 entries: all loads, then the arithmetic
+                float fp[16], fq[16];
+                if (fresh) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (KEEP && need_q) x[e] = fmax(fma(w, (double)fq[e], x[e]), 0.0);
-                else if (need_q) x[e] = res.with_draft(x[e], fq[e]);
-                else if (points) x[e] = res.with_points(x[e], i + e);
-                acc[e] += x[e];
-            }
-            if (KEEP) {
-                *reinterpret_cast<double2*>(kept + (i - lo)) = make_double2(x[0], x[1]);
-                *reinterpret_cast<double2*>(kept + (i - lo) + 2) = make_double2(x[2], x[3]);
-            }
-        }
-        held = node;
-        const double mine = warp_sum((acc[0] + acc[1]) + (acc[2] + acc[3]));
-        if (lane < (int)blocks)
-            asm volatile("st.shared::cluster.f64 [%0], %1;"
-                         ::"r"(map_to_rank(smem_u32(&s_sum[pass & 1][slot]), lane)), "d"(mine) : "memory");
-        meet();
-        double total = 0.0;                                  // (the same additions in every warp of every block)
-        for (int w = lane * per_lane; w < min(n_runs, (lane + 1) * per_lane); ++w) total += s_sum[pass & 1][w];
-        ++pass;
-        return warp_sum(total);
-    };
-    // the lowest index whose cumulative sum exceeds u * total; the warps' sums are in s_sum[(pass - 1) & 1]
-    auto draw = [&](int node, const Residual& res, float u, double total) {
-        const double* sums = s_sum[(pass - 1) & 1];
-        const double goal = (double)u * total;
-        const int w0 = lane * per_lane, w1 = min(n_runs, w0 + per_lane);
-        double mine = 0.0;
-        for (int w = w0; w < w1; ++w) mine += sums[w];
-        const double upto_run = warp_prefix(mine, lane);
-        int hit_run = kNone, last_run = -1;
-        double at_run = upto_run - mine, at_hit = 0.0, at_last = 0.0;
-        for (int w = w0; w < w1; ++w) {
-            const double s = sums[w];
-            if (s > 0.0) {
-                last_run = w; at_last = at_run;
-                if (hit_run == kNone && at_run + s > goal) { hit_run = w; at_hit = at_run; }
-            }
-            at_run += s;
-        }
-        int run = __reduce_min_sync(0xffffffffu, hit_run);
-        const bool hit = run != kNone;
-        if (!hit) run = __reduce_max_sync(0xffffffffu, last_run);    // (rounding: the last run with anything in it)
-        if (run != slot) return;                             // (every warp finds the same run; the one it belongs to goes on)
-        double before = __shfl_sync(0xffffffffu, hit ? at_hit : at_last, run / per_lane);
-        int found = -1, last = -1;
-        // 128 entries in order, four a lane: the first that takes the sum beyond the goal, and the last that is not 0
-        auto look = [&](int i, const double (&x)[4]) {
-            const double four = (x[0] + x[1]) + (x[2] + x[3]);
-            const double upto = warp_prefix(four, lane);
-            double at = before + (upto - four);
-            int first = kNone, some = -1;
+                    for (int s = 0; s < 4; ++s) {
+                        float f[4];
+                        load4(p, min(i0 + 128 * s + 4 * lane, hi), hi, vec, f);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                at += x[e];
-                if (x[e] > 0.0) {
-                    some = i + e;
-                    if (at > goal) first = min(first, i + e);
+                        for (int e = 0; e < 4; ++e) fp[4 * s + e] = f[e];
+                    }
+                }
+                if (need_q) {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        float f[4];
+                        load4(q, min(i0 + 128 * s + 4 * lane, hi), hi, vec, f);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) fq[4 * s + e] = f[e];
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int i = i0 + 128 * s + 4 * lane;
+                    if (i >= hi) break;
+                    Pair x[4];
+                    if (KEEP && !fresh) {
+                        const float4 x0 = *reinterpret_cast<const float4*>(kept + (i - lo)), x1 = *reinterpret_cast<const float4*>(kept + (i - lo) + 2);
+                        x[0] = {x0.x, x0.y}; x[1] = {x0.z, x0.w}; x[2] = {x1.x, x1.y}; x[3] = {x1.z, x1.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = reject(x[e], w, fq[4 * s + e]);
+                    } else if (KEEP && need_q) {             // the first rejection at a node: W is 1
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[e] = two_sum(fp[4 * s + e], -fq[4 * s + e]);
+                            if (!(x[e].h > 0.f)) x[e] = {0.f, 0.f};
+                        }
+                    } else if (KEEP && k == 0) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = {fp[4 * s + e], 0.f};
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = left_of(fp[4 * s + e], need_q ? fq[4 * s + e] : 0.f, i + e, k);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) add_to(acc[e], x[e]);
+                    if (KEEP) {
+                        *reinterpret_cast<float4*>(kept + (i - lo)) = make_float4(x[0].h, x[0].l, x[1].h, x[1].l);
+                        *reinterpret_cast<float4*>(kept + (i - lo) + 2) = make_float4(x[2].h, x[2].l, x[3].h, x[3].l);
+                    }
                 }
             }
-            first = __reduce_min_sync(0xffffffffu, first);
-            last = max(last, __reduce_max_sync(0xffffffffu, some));
-            if (found < 0 && first != kNone) found = first;
-            before += __shfl_sync(0xffffffffu, upto, 31);
+            held = node;
+            add_to(acc[0], acc[1]);
+            add_to(acc[2], acc[3]);
+            add_to(acc[0], acc[2]);
+            const Pair mine = warp_sum(acc[0]);
+            if (lane < (int)blocks)
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};"
+                             ::"r"(map_to_rank(smem_u32(&s_sum[pass & 1][slot]), lane)), "f"(mine.h), "f"(mine.l) : "memory");
+            meet();
+            Pair total = {0.f, 0.f};
+            if (warp == 0) {                                 // (the same additions in warp 0 of every block)
+                Pair own[4];                                 // per_lane is at most 4
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int at = lane * per_lane + w;
+                    own[w] = w < per_lane && at < n_runs ? s_sum[pass & 1][at] : Pair{0.f, 0.f};
+                }
+                Pair other = own[2];
+                total = own[0];
+                add_to(total, own[1]);
+                add_to(other, own[3]);
+                add_to(total, other);
+                runs_before = warp_prefix(total, lane);
+                add_to(total, runs_before);
+                total = {__shfl_sync(0xffffffffu, total.h, 31), __shfl_sync(0xffffffffu, total.l, 31)};
+            }
+            ++pass;
+            return total;
         };
-        const T *p, *q;
-        bool vec;
-        rows_of(node, p, q, vec);
-        const bool need_q = !points && res.k > 0;
-        for (int i0 = lo; i0 < hi && found < 0; i0 += 128) {
-            const int i = i0 + 4 * lane;
-            double x[4] = {0.0, 0.0, 0.0, 0.0};
-            if (i < hi) {
-                if (KEEP) {
+        // this warp's entries hold the lowest index whose cumulative sum exceeds the goal: which it is
+        auto draw = [&](const Task& task) {
+            const T *p, *q;
+            bool vec;
+            rows_of(task.node, p, q, vec);
+            auto entries = [&](int i, Pair (&x)[4]) {        // four entries from i on
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = {0.f, 0.f};
+                if (i >= hi) return;
+                if constexpr (KEEP) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[e] = kept[i - lo + e];
                 } else {
                     float fp[4], fq[4] = {0.f, 0.f, 0.f, 0.f};
                     load4(p, i, hi, vec, fp);
-                    if (need_q) load4(q, i, hi, vec, fq);
+                    if (!points && task.k > 0) load4(q, i, hi, vec, fq);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        x[e] = need_q ? res.with_draft(fp[e], fq[e]) : points ? res.with_points(fp[e], i + e) : (double)fp[e];
+                    for (int e = 0; e < 4; ++e) x[e] = left_of(fp[e], fq[e], i + e, task.k);
+                }
+            };
+            Pair before = task.before, before_last = task.before;
+            int at = lo, last = lo;                          // the stretch of 128 entries; the last one with anything in it
+            bool hit = false;
+            for (; at < hi; at += 128) {
+                Pair x[4];
+                entries(at + 4 * lane, x);
+                for (int e = 1; e < 4; ++e) add_to(x[0], x[e]);
+                const Pair sum = warp_sum(x[0]);
+                if (sum.h > 0.f) {
+                    last = at;
+                    before_last = before;
+                    add_to(before, sum);
+                    if (exceeds(before, task.goal)) { hit = true; break; }
                 }
             }
-            look(i, x);
-        }
-        if (found < 0) found = last;                         // (rounding: the last entry with anything in it)
-        if (lane == 0) a.next_token[b] = found;
-    };
-    // the lowest index of the largest score at `node`; `next` (or -1): the node whose row is wanted next, likely
-    auto best_of = [&](int node, int next) -> int {
-        const T *p, *q;
-        bool vec;
-        rows_of(node, p, q, vec);
-        if (next >= 0) {                                     // one line of the next row per lane and step
-            const T* ahead = p0 + ((int64_t)b * a.N + next) * a.p_stride;
-            for (int i = lo + lane * (128 / (int)sizeof(T)); i < hi; i += 32 * (128 / (int)sizeof(T)))
-                asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + i));
-        }
-        float best = -INFINITY;
-        int arg = kNone;
-#pragma unroll 4
-        for (int i = lo + 4 * lane; i < hi; i += 128) {
-            float f[4];
-            load4(p, i, hi, vec, f);
+            // (rounding may leave the goal unreached: the last entry with anything in it then)
+            Pair x[4];
+            const int i = last + 4 * lane;
+            entries(i, x);
+            Pair four = x[0];
+            for (int e = 1; e < 4; ++e) add_to(four, x[e]);
+            Pair upto = before_last;
+            add_to(upto, warp_prefix(four, lane));
+            int first = kNone, some = -1;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (i + e < hi && (f[e] > best || arg == kNone)) { best = f[e]; arg = i + e; }
-        }
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1)
-            take_better(best, arg, __shfl_xor_sync(0xffffffffu, best, off), __shfl_xor_sync(0xffffffffu, arg, off));
-        if (lane < (int)blocks) {
-            asm volatile("st.shared::cluster.f32 [%0], %1;"
-                         ::"r"(map_to_rank(smem_u32(&s_best[pass & 1][slot]), lane)), "f"(best) : "memory");
-            asm volatile("st.shared::cluster.u32 [%0], %1;"
-                         ::"r"(map_to_rank(smem_u32(&s_arg[pass & 1][slot]), lane)), "r"(arg) : "memory");
-        }
-        meet();
-        best = -INFINITY;
-        arg = kNone;
-        for (int w = lane * per_lane; w < min(n_runs, (lane + 1) * per_lane); ++w) take_better(best, arg, s_best[pass & 1][w], s_arg[pass & 1][w]);
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1)
-            take_better(best, arg, __shfl_xor_sync(0xffffffffu, best, off), __shfl_xor_sync(0xffffffffu, arg, off));
-        ++pass;
-        return arg;
-    };
-    auto first_child = [&](int node) -> int {
-        for (int i = node + 1; i < n; ++i)
-            if (s_parent[i] == node) return i;
-        return -1;
-    };
+            for (int e = 0; e < 4; ++e) {
+                add_to(upto, x[e]);
+                if (x[e].h > 0.f) {
+                    some = i + e;
+                    if (hit && exceeds(upto, task.goal)) first = min(first, i + e);
+                }
+            }
+            first = __reduce_min_sync(0xffffffffu, first);
+            some = __reduce_max_sync(0xffffffffu, some);
+            if (lane == 0) a.next_token[b] = first != kNone ? first : some;
+        };
 
-    // ---- the walk: every thread of every block takes the same decisions ----------------------------
-    int cur = 0, length = 1;
-    Residual res{0, s_weight, s_out};
-    double weight = 1.0;                                     // W of the next test
-    bool summed = false;                                     // s_sum holds the sums for (cur, res)
-    int best = 0;
-    if constexpr (GREEDY) best = best_of(0, first_child(0));
-    if (tid == 0) s_path[0] = 0;
-    for (int i = 1; i < n; ++i) {
-        if (s_parent[i] != cur) continue;
-        const int x = s_token[i];
-        bool stands;
-        if constexpr (GREEDY) {
-            stands = x == best;
-        } else {
-            if (x < 0 || x >= a.V) continue;
-            const double q = points ? 1.0 : (double)s_q[i];
-            const double left = points ? res.with_points(s_p[i], x) : res.with_draft(s_p[i], q);
-            stands = (double)s_u[i] * weight * q < left;
-            if (!stands) {
-                __syncthreads();                             // (the last reads of the lists are done)
-                if (tid == 0) { s_weight[res.k] = weight; s_out[res.k] = x; }
-                __syncthreads();
-                ++res.k;
+        // warp 0 walks the tree (of every block the same way, on the same sums)
+        int cur = 0, k = 0;
+        unsigned low = 0, high = 0;                          // the children of cur that are still to be tested
+        Pair weight = {1.f, 0.f};                            // W of the next test
+        bool summed = false;                                 // s_sum holds the sums for (cur, k), and weight their total
+        const Pair zero = {0.f, 0.f};
+        if (n > 0) { low = s_children[0]; high = s_children[1]; }
+        auto next_task = [&](Pair sum) -> Task {             // `sum`: of the task before, if it was a sum
+            if (n == 0) {
+                if (rank == 0 && lane == 0) a.next_token[b] = -1;
+                return Task{kDone, 0, 0, 0, zero, zero};
+            }
+            if (summed) weight = sum;
+            while (low | high) {
+                const int i = low ? __ffs(low) - 1 : 31 + __ffs(high);
+                if (low) low &= low - 1; else high &= high - 1;
+                const int x = s_token[i];
+                if (x < 0 || x >= a.V) continue;
+                const float q = points ? 1.f : s_q[i];
+                const Pair left = left_of(s_p[i], q, x, k);
+                if (exceeds(left, times(times(weight, s_u[i]), q))) {
+                    cur = i;
+                    if (lane == 0) s_path[length] = i;
+                    ++length;
+                    k = 0;
+                    weight = {1.f, 0.f};
+                    summed = false;
+                    low = s_children[2 * i];
+                    high = s_children[2 * i + 1];
+                    continue;
+                }
+                if (lane == 0) { s_weight[k] = weight; s_out[k] = x; }
+                __syncwarp();
+                ++k;
                 if (points) {
-                    weight -= left;
+                    add_to(weight, {-left.h, -left.l});
                 } else {
-                    weight = sum_left(cur, res);
                     summed = true;
+                    return Task{kSum, cur, k, 0, zero, zero};
                 }
             }
+            if (!summed) {                                   // the sum at the last node
+                summed = true;
+                return Task{kSum, cur, k, 0, zero, zero};
+            }
+            if (!(weight.h > 0.f)) {
+                if (k > 0) {                                 // nothing is left of v: the target's row itself
+                    k = 0;
+                    return Task{kSum, cur, 0, 0, zero, zero};
+                }
+                if (rank == 0 && lane == 0) a.next_token[b] = -1;
+                return Task{kDone, 0, 0, 0, zero, zero};
+            }
+            // the warp whose run takes the cumulative sum beyond the goal
+            const Pair* sums = s_sum[(pass - 1) & 1];
+            const Pair goal = times(weight, s_u[0]);
+            const int w0 = lane * per_lane, w1 = min(n_runs, w0 + per_lane);
+            Pair at_run = runs_before, before = zero;
+            int hit_run = kNone, last_run = -1;
+            for (int w = w0; w < w1 && hit_run == kNone; ++w) {
+                if (sums[w].h > 0.f) {
+                    last_run = w;
+                    before = at_run;
+                    add_to(at_run, sums[w]);
+                    if (exceeds(at_run, goal)) hit_run = w;
+                }
+            }
+            int run = __reduce_min_sync(0xffffffffu, hit_run);
+            if (run == kNone) run = __reduce_max_sync(0xffffffffu, last_run);    // (rounding: the last run with anything in it)
+            const int from = run / per_lane;
+            return Task{kDraw, cur, k, run, {__shfl_sync(0xffffffffu, before.h, from), __shfl_sync(0xffffffffu, before.l, from)}, goal};
+        };
+        Pair sum = {0.f, 0.f};
+        for (;;) {
+            if (warp == 0) {
+                const Task next = next_task(sum);
+                if (lane == 0) s_task = next;
+            }
+            __syncthreads();
+            const Task task = s_task;
+            if (task.what == kSum) {
+                sum = sum_left(task.node, task.k);           // (meets, so that the next task finds this one read)
+            } else {
+                if (task.what == kDraw && task.run == slot) draw(task);
+                break;
+            }
         }
-        if (stands) {
-            cur = i;
-            if (tid == 0) s_path[length] = i;
-            ++length;
-            if constexpr (GREEDY) best = best_of(cur, first_child(cur));
-            res.k = 0;
-            weight = 1.0;
-            summed = false;
-        }
-    }
-    if constexpr (GREEDY) {
-        if (rank == 0 && tid == 0) a.next_token[b] = best;
-    } else {
-        double total = weight;
-        if (!summed) total = sum_left(cur, res);
-        if (!(total > 0.0) && res.k > 0) {                   // nothing is left of v: the target's row itself
-            res.k = 0;
-            total = sum_left(cur, res);
-        }
-        if (total > 0.0) draw(cur, res, s_u[0], total);
-        else if (rank == 0 && tid == 0) a.next_token[b] = -1;
     }
     __syncthreads();
+    // (the last writes to another block's shared memory lie before the last meeting: a block may leave)
     if (rank == 0) {
         if (tid < a.N) a.path[(int64_t)b * a.N + tid] = s_path[tid];
         if (tid == 0) a.accepted[b] = length;
     }
-    if (blocks > 1) cluster_barrier();                       // nobody leaves while its shared memory may be written
 }
 
 template <typename T, int W, bool GREEDY, bool KEEP>
@@ -407,7 +524,7 @@ cudaError_t launch_verify(const VerifyArgs& a, int batch, int blocks, cudaStream
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)batch * blocks));
     cfg.blockDim = dim3(32 * W);
-    cfg.dynamicSmemBytes = KEEP ? (size_t)W * a.run * sizeof(double) : 0;
+    cfg.dynamicSmemBytes = KEEP ? (size_t)W * a.run * sizeof(Pair) : 0;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -423,19 +540,23 @@ cudaError_t launch_verify(const VerifyArgs& a, int batch, int blocks, cudaStream
 
 template <typename T>
 cudaError_t run_verify(VerifyArgs& a, int batch, cudaStream_t st) {
-    // Four warps and 512 entries each are enough for small vocabularies; else sixteen, and as many blocks (up to
-    // eight) as keep a warp's run at 512 entries, whatever the batch: a pass is all latency, so that more and
-    // shorter ones at a time are the faster way through many requests as well.
+    // Small vocabularies: four warps a request.  Else sixteen, and as many blocks (up to eight) as keep a warp's run at
+    // 512 entries, whatever the batch: a pass is all latency, and more blocks per request beat fewer at every batch.
     const bool greedy = a.u == nullptr;
-    const int warps = a.V <= 2048 ? 4 : 16;
-    int blocks = 1;
-    while (blocks < kVerifyMaxCluster && (int64_t)blocks * warps * 512 < a.V) blocks *= 2;
-    const int runs = blocks * warps;
-    a.run = ((a.V + runs - 1) / runs + 127) / 128 * 128;
-    const bool keep = (int64_t)warps * a.run * 8 <= kVerifyKeepBytes;
-    if (warps == 4) return greedy ? launch_verify<T, 4, true, false>(a, batch, blocks, st) : launch_verify<T, 4, false, true>(a, batch, blocks, st);
+    auto fit = [&](int warps, int run) {
+        int blocks = 1;
+        while (blocks < kVerifyMaxCluster && (int64_t)blocks * warps * run < a.V) blocks *= 2;
+        a.run = ((a.V + blocks * warps - 1) / (blocks * warps) + 127) / 128 * 128;
+        return blocks;
+    };
+    if (a.V <= 2048) {
+        const int blocks = fit(4, 512);
+        return greedy ? launch_verify<T, 4, true, false>(a, batch, blocks, st) : launch_verify<T, 4, false, true>(a, batch, blocks, st);
+    }
+    const int blocks = fit(16, 512);
     if (greedy) return launch_verify<T, 16, true, false>(a, batch, blocks, st);
-    return keep ? launch_verify<T, 16, false, true>(a, batch, blocks, st) : launch_verify<T, 16, false, false>(a, batch, blocks, st);
+    if (16 * (int64_t)a.run * (int)sizeof(Pair) <= kVerifyKeepBytes) return launch_verify<T, 16, false, true>(a, batch, blocks, st);
+    return launch_verify<T, 16, false, false>(a, batch, blocks, st);
 }
 
 }  // namespace
