@@ -13,6 +13,7 @@ using namespace dsa;
 
 struct TreePlan {
     int G, row_tiles;
+    int rows;                                      // query rows per block
     int n_split;                                   // pieces whose partial results go through the workspace (1: none)
     int cluster;                                   // or blocks of a cluster that merge on chip (1: none)
     int64_t blocks;
@@ -47,8 +48,8 @@ int32_t make_tree_plan(const dsa_problem* p, const dsa_diag_params* d, const dsa
     if (d && d->mode != DSA_MASK_WINDOW) return DSA_ERR_UNSUPPORTED;
     const int N = tree->max_nodes;
     pl->G = p->num_q_heads / p->num_kv_heads;
-    const int rows = p->dtype == DSA_BF16 ? kTreeRows : kTreeF32Rows;
-    pl->row_tiles = (N * pl->G + rows - 1) / rows;
+    pl->rows = p->dtype == DSA_BF16 ? kTreeRows : N * pl->G <= 8 ? 8 : N * pl->G <= 16 ? 16 : kTreeF32Rows;
+    pl->row_tiles = (N * pl->G + pl->rows - 1) / pl->rows;
 
     // a box of the caches' tensor maps must not cross the end of a page: the largest power of two that divides it
     pl->box_tokens = kTreeTile;
@@ -75,11 +76,16 @@ int32_t make_tree_plan(const dsa_problem* p, const dsa_diag_params* d, const dsa
         want = (tiles + per - 1) / per;
     } else {
         const int64_t places = 2 * (int64_t)host_sm_count();         // two blocks share an SM
-        if (bf16) pl->cluster = choose_cluster(items, tiles, places);
-        // eight blocks are too few where even they leave most places empty and have many tiles each
-        if (!bf16 || (pl->cluster == 8 && items * 16 <= places && tiles >= 8 * 16)) {
-            want = std::min(std::max<int64_t>(places / items, 1), std::max<int64_t>(1, tiles / 4));
-            if (want > 1) pl->cluster = 1;
+        if (bf16) {
+            pl->cluster = choose_cluster(items, tiles, places);
+            // eight blocks are too few where even they leave most places empty and have many tiles each
+            if (pl->cluster == 8 && items * 16 <= places && tiles >= 8 * 16) {
+                want = std::min(places / items, tiles / 4);
+                pl->cluster = 1;
+            }
+        } else {
+            // fp32: about two blocks for every place (requests differ in length), none below two tiles
+            want = std::min((2 * places + items - 1) / items, std::max<int64_t>(1, tiles / 2));
         }
     }
     if (want > kMaxSplits) return DSA_ERR_UNSUPPORTED;
@@ -169,8 +175,11 @@ cudaError_t configure_bf16() {
 }
 template <int D>
 cudaError_t configure_f32() {
-    static std::atomic<bool> done[kMaxDevices] = {};
-    return configure_smem(dsa_tree_f32_kernel<D>, TreeF32Cfg<D>::SMEM, done);
+    static std::atomic<bool> done[kMaxDevices] = {}, done8[kMaxDevices] = {}, done16[kMaxDevices] = {};
+    cudaError_t e = configure_smem(dsa_tree_f32_kernel<D>, TreeF32Cfg<D>::SMEM, done);
+    if (e == cudaSuccess) e = configure_smem(dsa_tree_few_kernel<D, 8>, TreeFewCfg<D, 8>::SMEM, done8);
+    if (e == cudaSuccess) e = configure_smem(dsa_tree_few_kernel<D, 16>, TreeFewCfg<D, 16>::SMEM, done16);
+    return e;
 }
 template <int D>
 cudaError_t run_bf16(const TreeArgs& g, const TreeMaps& m, int64_t blocks, cudaStream_t st) {
@@ -178,9 +187,12 @@ cudaError_t run_bf16(const TreeArgs& g, const TreeMaps& m, int64_t blocks, cudaS
     return e != cudaSuccess ? e : launch_tree(dsa_tree_kernel<D>, blocks, kTreeThreads, TreeCfg<D>::SMEM, g.cluster, st, g, m);
 }
 template <int D>
-cudaError_t run_f32(const TreeArgs& g, int64_t blocks, cudaStream_t st) {
+cudaError_t run_f32(const TreeArgs& g, int rows, int64_t blocks, cudaStream_t st) {
     const cudaError_t e = configure_f32<D>();
-    return e != cudaSuccess ? e : launch_tree(dsa_tree_f32_kernel<D>, blocks, kTreeF32Threads, TreeF32Cfg<D>::SMEM, 1, st, g);
+    if (e != cudaSuccess) return e;
+    if (rows == 8) return launch_tree(dsa_tree_few_kernel<D, 8>, blocks, kTreeF32Threads, TreeFewCfg<D, 8>::SMEM, 1, st, g);
+    if (rows == 16) return launch_tree(dsa_tree_few_kernel<D, 16>, blocks, kTreeF32Threads, TreeFewCfg<D, 16>::SMEM, 1, st, g);
+    return launch_tree(dsa_tree_f32_kernel<D>, blocks, kTreeF32Threads, TreeF32Cfg<D>::SMEM, 1, st, g);
 }
 
 }  // namespace
@@ -252,7 +264,7 @@ int32_t dsa_tree_step(const dsa_problem* problem, const dsa_diag_params* diag, c
         if (rc != DSA_OK) return rc;
         e = problem->head_dim == 64 ? run_bf16<64>(g, m, pl.blocks, st) : run_bf16<128>(g, m, pl.blocks, st);
     } else {
-        e = problem->head_dim == 64 ? run_f32<64>(g, pl.blocks, st) : run_f32<128>(g, pl.blocks, st);
+        e = problem->head_dim == 64 ? run_f32<64>(g, pl.rows, pl.blocks, st) : run_f32<128>(g, pl.rows, pl.blocks, st);
     }
     if (e != cudaSuccess) return host_cuda_fail(e);
     if (pl.n_split > 1)
