@@ -75,7 +75,7 @@ int32_t make_tree_plan(const dsa_problem* p, const dsa_diag_params* d, const dsa
         const int64_t per = (p->split_tokens + (int64_t)kTreeTile - 1) / kTreeTile;
         want = (tiles + per - 1) / per;
     } else {
-        const int64_t places = 2 * (int64_t)host_sm_count();         // two blocks share an SM
+        int64_t places = 2 * (int64_t)host_sm_count();               // two blocks share an SM
         if (bf16) {
             pl->cluster = choose_cluster(items, tiles, places);
             // eight blocks are too few where even they leave most places empty and have many tiles each
@@ -84,8 +84,10 @@ int32_t make_tree_plan(const dsa_problem* p, const dsa_diag_params* d, const dsa
                 pl->cluster = 1;
             }
         } else {
-            // fp32: about two blocks for every place (requests differ in length), none below two tiles
-            want = std::min((2 * places + items - 1) / items, std::max<int64_t>(1, tiles / 2));
+            // fp32: about as many blocks as there are places, none below two tiles
+            if (pl->rows == 8 && p->head_dim == 64) places *= 2;      // (four blocks share an SM)
+            want = std::min((places + items / 2) / items, std::max<int64_t>(1, tiles / 2));
+            want = std::max<int64_t>(want, 1);
         }
     }
     if (want > kMaxSplits) return DSA_ERR_UNSUPPORTED;

@@ -9,8 +9,10 @@
 // address in all lanes), and exchange halves until each holds one or two rows' totals; O is cut into four dims
 // per thread and 256 / (D / 4) groups of tokens, whose parts are added once at the end.
 //
-// More rows: 32 query rows a block and tiles of 64 tokens, scores as 2 rows x 4 keys per thread, the running
-// maximum and sum kept by the 16 threads that share a row, O as 2 rows x D / 16 dims per thread.
+// More rows: 32 query rows a block and tiles of 64 tokens.  A warp's scores are 16 rows x 16 tokens, its lanes
+// 4 x 8 of 4 rows x 2 tokens each, so that one read of q serves four rows' lanes and one of K eight in a single
+// cycle of shared memory (6 of them for 8 cycles of multiply-adds; lanes 2 x 16 need 10); O likewise as 16 rows x
+// D / 4 dims.  Groups of tokens and rows that do not exist are skipped.
 //
 // Rows in shared memory are padded by 16 bytes so that the eight rows a quarter-warp reads lie in different
 // banks.  K rows are multiplied as they are (masked scores are replaced), rows of V that no node sees are
@@ -21,25 +23,26 @@
 namespace dsa {
 
 constexpr int kTreeF32Rows = 32;
-constexpr int kTreeF32Threads = 256;
+constexpr int kTreeF32Threads = 256;                       // few rows
 
 template <int D>
 struct TreeF32Cfg {
     static constexpr int LD = D + 4;                       // padded row of Q, K, V, in floats
     static constexpr int LP = kTreeTile + 4;               // padded row of the weights
-    static constexpr int SMEM = (kTreeF32Rows * LD + 2 * kTreeTile * LD + kTreeF32Rows * LP) * 4;
+    static constexpr int SMEM = (kTreeF32Rows * LD + 2 * kTreeTile * LD + kTreeF32Rows * LP + 4 * kTreeF32Rows) * 4;
 };
 
 template <int D>
 __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const TreeArgs g) {
     using C = TreeF32Cfg<D>;
     constexpr int DV = D / 4;                              // 16-byte pieces of a row
-    constexpr int OC = D / 64;                             // float4 columns of O per thread
+    constexpr int OD = D / 32;                             // dims of O per thread: 4, or 2
     extern __shared__ __align__(16) float sm[];
     float* s_q = sm;
     float* s_k = s_q + kTreeF32Rows * C::LD;
     float* s_v = s_k + kTreeTile * C::LD;
     float* s_p = s_v + kTreeTile * C::LD;
+    float* s_max = s_p + kTreeF32Rows * C::LP;             // [token group][row]
     __shared__ unsigned long long line_of[kTreeMaxNodes];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -56,22 +59,41 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
     tree_lengths(g, b, S, L_p, n);
     const int rows_all = min(per_tile, g.N - first_node) * G;
     const int rows = max(0, min(per_tile, n - first_node)) * G;
-    if (rows == 0) {
-        tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
-        return;
-    }
-    if (warp == 0) tree_lines(g, b, line_of, lane);
-    __syncthreads();
     const TreeSpan span = tree_span(g, S, L_p);
     const int per_split = (span.T + g.a.n_split - 1) / g.a.n_split;
     const int t0 = min(span.T, split * per_split), t1 = min(span.T, t0 + per_split);
-    const int cached = t1 - t0, tiles = cached + (split == 0 ? 1 : 0);
-    tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
+    const int cached = t1 - t0, tiles = rows == 0 ? 0 : cached + (split == 0 ? 1 : 0);
     if (tiles == 0) {
+        if (rows > 0) tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
         tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
         return;
     }
-
+    auto bounds = [&](int t, int& start, int& from, int& to) {
+        start = 0; from = 0; to = n;
+        if (t < cached) span.tile(t0 + t, start, from, to);
+    };
+    // K (and then V) rows of tile t; rows that nobody sees: zeros
+    auto stage = [&](int t, bool is_v) {
+        int start, from, to;
+        bounds(t, start, from, to);
+        const float* src = reinterpret_cast<const float*>(t < cached ? (is_v ? g.a.v : g.a.k) : (is_v ? g.a.v_new : g.a.k_new));
+        // four threads a row, every fourth piece each: one address per thread
+        const int row = tid >> 2, pos = start + row;
+        const bool seen = pos >= from && pos < to;
+        if (seen)
+            src += t < cached ? token_offset(g.a, b, L_p, pos) + (int64_t)kvh * g.a.stride_head
+                              : (((int64_t)b * g.N + pos) * g.a.H_kv + kvh) * D;
+        float* dst = (is_v ? s_v : s_k) + row * C::LD;
+#pragma unroll
+        for (int j = 0; j < DV / 4; ++j) {
+            const int c = ((tid & 3) + 4 * j) * 4;
+            cp_async16(dst + c, src + c, seen);
+        }
+        cp_async_commit();
+    };
+    stage(0, false);
+    stage(0, true);
+    if (warp == 0) tree_lines(g, b, line_of, lane);
     for (int i = tid; i < kTreeF32Rows * DV; i += kTreeF32Threads) {
         const int row = i / DV, c = (i - row * DV) * 4;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -80,16 +102,23 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
                                                  (((int64_t)b * g.N + first_node + row / G) * g.a.H_q + kvh * G + row % G) * D + c);
         *reinterpret_cast<float4*>(s_q + row * C::LD + c) = x;
     }
-    const int tx = tid & 15, ty = tid >> 4;                // keys tx + 16 k; rows ty, ty + 16
+    __syncthreads();
+
+    const int kg = lane & 7, rg = lane >> 3;               // lane: tokens kg, kg + 8 of the warp's group; rows rg + 4 r of its half
+    const int row0 = (warp & 1) * 16 + rg, group = warp >> 1;
+    const int key0 = group * 16 + kg, dim0 = group * (D / 4) + kg * OD;
+    const bool rows_here = (warp & 1) * 16 < rows;
     const float sl = g.a.scale_log2;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    float4 o[2][OC];
-    unsigned long long own[2];
-    int64_t win_lo[2];
+    float m[4], l[4], o[4][OD];
+    unsigned long long own[4];
+    int64_t win_lo[4];
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        for (int c = 0; c < OC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int row = ty + 16 * r;
+    for (int r = 0; r < 4; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < OD; ++c) o[r][c] = 0.f;
+        const int row = row0 + 4 * r;
         own[r] = 0ull;
         win_lo[r] = 0;
         if (row >= rows) continue;
@@ -109,107 +138,121 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
     }
 
     for (int t = 0; t < tiles; ++t) {
-        int start = 0, from = 0, to = n;
-        if (t < cached) span.tile(t0 + t, start, from, to);
-        __syncthreads();                                   // the last tile has been read (and Q is in place)
-        for (int i = tid; i < kTreeTile * DV; i += kTreeF32Threads) {
-            const int row = i / DV, c = (i - row * DV) * 4;
-            const int pos = start + row;
-            const bool seen = pos >= from && pos < to;
-            int64_t off = 0;
-            if (seen)
-                off = t < cached ? token_offset(g.a, b, L_p, pos) + (int64_t)kvh * g.a.stride_head + c
-                                 : (((int64_t)b * g.N + pos) * g.a.H_kv + kvh) * D + c;
-            const float* kp = reinterpret_cast<const float*>(t < cached ? g.a.k : g.a.k_new) + off;
-            const float* vp = reinterpret_cast<const float*>(t < cached ? g.a.v : g.a.v_new) + off;
-            cp_async16(s_k + row * C::LD + c, kp, seen);
-            cp_async16(s_v + row * C::LD + c, vp, seen);
-        }
-        cp_async_commit();
-        cp_async_wait<0>();
+        int start, from, to;
+        bounds(t, start, from, to);
+        const int count = to - start;                      // tokens of the tile that may be seen: [0, count)
+        cp_async_wait<1>();                                // K is there (V may be on its way)
         __syncthreads();
-        float x[2][4] = {};
+        float x[4][2] = {};
+        if (rows_here && group * 16 < count) {
 #pragma unroll 4
-        for (int c = 0; c < D; c += 4) {
-            float4 q[2], k[4];
+            for (int c = 0; c < D; c += 4) {
+                float4 q[4], k[2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) q[r] = *reinterpret_cast<const float4*>(s_q + (ty + 16 * r) * C::LD + c);
+                for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const float4*>(s_q + (row0 + 4 * r) * C::LD + c);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(s_k + (tx + 16 * j) * C::LD + c);
+                for (int j = 0; j < 2; ++j) k[j] = *reinterpret_cast<const float4*>(s_k + (key0 + 8 * j) * C::LD + c);
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    x[r][j] = fmaf(q[r].x, k[j].x, fmaf(q[r].y, k[j].y, fmaf(q[r].z, k[j].z, fmaf(q[r].w, k[j].w, x[r][j]))));
+                    for (int j = 0; j < 2; ++j)
+                        x[r][j] = fmaf(q[r].x, k[j].x, fmaf(q[r].y, k[j].y, fmaf(q[r].z, k[j].z, fmaf(q[r].w, k[j].w, x[r][j]))));
+            }
         }
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < 4; ++r) {
             float mx = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int key = tx + 16 * j, pos = start + key;
-                bool seen = ty + 16 * r < rows;
-                if (t < cached) seen = seen && pos >= from && pos < to && (t0 + t < span.T1 || pos >= win_lo[r]);
+            for (int j = 0; j < 2; ++j) {
+                const int key = key0 + 8 * j, pos = start + key;
+                bool seen = row0 + 4 * r < rows && pos >= from && pos < to;
+                if (t < cached) seen = seen && (t0 + t < span.T1 || pos >= win_lo[r]);
                 else seen = seen && ((own[r] >> key) & 1ull) != 0;
                 if (!seen) x[r][j] = -INFINITY;
                 mx = fmaxf(mx, x[r][j]);
             }
 #pragma unroll
-            for (int off = 8; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-            const float m_new = fmaxf(m[r], mx);
+            for (int off = 4; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+            if (kg == 0) s_max[group * kTreeF32Rows + row0 + 4 * r] = mx;
+        }
+        __syncthreads();                                   // (K has been read for the last time)
+        if (t + 1 < tiles) stage(t + 1, false); else cp_async_commit();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = row0 + 4 * r;
+            float m_new = m[r];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m_new = fmaxf(m_new, s_max[w * kTreeF32Rows + row]);
             const float sub = m_new == -INFINITY ? 0.f : m_new * sl;
             const float alpha = m_new == -INFINITY ? 1.f : exp2f((m[r] - m_new) * sl);
             m[r] = m_new;
-            float sum = 0.f;
+            l[r] *= alpha;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 2; ++j) {
                 const float p = exp2f(fmaf(x[r][j], sl, -sub));
-                sum += p;
-                s_p[(ty + 16 * r) * C::LP + tx + 16 * j] = p;
+                l[r] += p;
+                s_p[row * C::LP + key0 + 8 * j] = p;
             }
 #pragma unroll
-            for (int off = 8; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            l[r] = l[r] * alpha + sum;
-#pragma unroll
-            for (int c = 0; c < OC; ++c) { o[r][c].x *= alpha; o[r][c].y *= alpha; o[r][c].z *= alpha; o[r][c].w *= alpha; }
+            for (int c = 0; c < OD; ++c) o[r][c] *= alpha;
         }
-        __syncwarp();                                      // a row's 16 threads are in one warp
+        cp_async_wait<1>();                                // V is there
+        __syncthreads();
+        if (rows_here)
 #pragma unroll 2
-        for (int j = 0; j < kTreeTile; j += 4) {
-            float4 p[2];
+            for (int j = 0; j < count; j += 4) {
+                float4 p[4];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) p[r] = *reinterpret_cast<const float4*>(s_p + (ty + 16 * r) * C::LP + j);
+                for (int r = 0; r < 4; ++r) p[r] = *reinterpret_cast<const float4*>(s_p + (row0 + 4 * r) * C::LP + j);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) {
+                    float v[OD];
+                    const float* src = s_v + (j + e) * C::LD + dim0;
+                    if constexpr (OD == 4) {
+                        const float4 y = *reinterpret_cast<const float4*>(src);
+                        v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w;
+                    } else {
+                        const float2 y = *reinterpret_cast<const float2*>(src);
+                        v[0] = y.x; v[1] = y.y;
+                    }
 #pragma unroll
-                for (int c = 0; c < OC; ++c) {
-                    const float4 v = *reinterpret_cast<const float4*>(s_v + (j + e) * C::LD + 64 * c + 4 * tx);
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
+                    for (int r = 0; r < 4; ++r) {
                         const float w = e == 0 ? p[r].x : e == 1 ? p[r].y : e == 2 ? p[r].z : p[r].w;
-                        o[r][c].x = fmaf(w, v.x, o[r][c].x);
-                        o[r][c].y = fmaf(w, v.y, o[r][c].y);
-                        o[r][c].z = fmaf(w, v.z, o[r][c].z);
-                        o[r][c].w = fmaf(w, v.w, o[r][c].w);
+#pragma unroll
+                        for (int c = 0; c < OD; ++c) o[r][c] = fmaf(w, v[c], o[r][c]);
                     }
                 }
-        }
+            }
+        __syncthreads();                                   // V and the weights have been read
+        if (t + 1 < tiles) stage(t + 1, true); else cp_async_commit();
     }
+    cp_async_wait<0>();
+    tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
+    // the rows' sums: over the lanes of a group, then over the groups
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int row = ty + 16 * r;
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int off = 4; off >= 1; off >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], off);
+        if (kg == 0) s_max[group * kTreeF32Rows + row0 + 4 * r] = l[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = row0 + 4 * r;
         if (row >= rows_all) continue;
-        const int64_t orow = ((int64_t)b * g.N + first_node + row / G) * g.a.H_q + kvh * G + row % G;
-        const bool none = l[r] == 0.f;
-        const float inv = none ? 0.f : 1.f / l[r];
-        float* dst = g.a.n_split > 1 ? g.a.out_part + (orow * g.a.n_split + split) * D : reinterpret_cast<float*>(g.a.out) + orow * D;
+        float sum = 0.f;
 #pragma unroll
-        for (int c = 0; c < OC; ++c)
-            *reinterpret_cast<float4*>(dst + 64 * c + 4 * tx) =
-                none ? make_float4(0.f, 0.f, 0.f, 0.f)
-                     : make_float4(o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv);
-        if (tx == 0) {
-            const float lse = none ? -INFINITY : (m[r] * sl + log2f(l[r])) * LN2;
+        for (int w = 0; w < 4; ++w) sum += s_max[w * kTreeF32Rows + row];
+        const int64_t orow = ((int64_t)b * g.N + first_node + row / G) * g.a.H_q + kvh * G + row % G;
+        const bool none = sum == 0.f;
+        const float inv = none ? 0.f : 1.f / sum;
+        float* dst = (g.a.n_split > 1 ? g.a.out_part + (orow * g.a.n_split + split) * D : reinterpret_cast<float*>(g.a.out) + orow * D) + dim0;
+#pragma unroll
+        for (int c = 0; c < OD; ++c) o[r][c] = none ? 0.f : o[r][c] * inv;
+        if constexpr (OD == 4) *reinterpret_cast<float4*>(dst) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+        else *reinterpret_cast<float2*>(dst) = make_float2(o[r][0], o[r][1]);
+        if (dim0 == 0) {
+            const float lse = none ? -INFINITY : (m[r] * sl + log2f(sum)) * LN2;
             if (g.a.n_split > 1) g.a.lse_part[orow * g.a.n_split + split] = lse;
             else g.a.lse[orow] = lse;
         }
@@ -232,7 +275,7 @@ struct TreeFewCfg {
 };
 
 template <int D, int ROWS>
-__global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_few_kernel(const TreeArgs g) {
+__global__ void __launch_bounds__(kTreeF32Threads, D == 64 && ROWS == 8 ? 4 : 2) dsa_tree_few_kernel(const TreeArgs g) {
     using C = TreeFewCfg<D, ROWS>;
     constexpr int DV = D / 4, PART = D / 8;                // float4 pieces of a row; dims per thread of the scores
     constexpr int RPL = ROWS / 8;                          // rows whose totals a thread ends up with
@@ -284,24 +327,25 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_few_kernel(const 
     };
     auto stage = [&](int t) {
         if (t < tiles) {
-            float* k = s_ring + (t % kTreeFewStages) * C::SLOT;
-            float* v = k + kTreeFewTile * C::LD;
             int start, from, to;
             bounds(t, start, from, to);
-            const float* kb = reinterpret_cast<const float*>(t < cached ? g.a.k : g.a.k_new);
-            const float* vb = reinterpret_cast<const float*>(t < cached ? g.a.v : g.a.v_new);
+            const float* k = reinterpret_cast<const float*>(t < cached ? g.a.k : g.a.k_new);
+            const float* v = reinterpret_cast<const float*>(t < cached ? g.a.v : g.a.v_new);
+            // eight threads a row, every eighth piece each: one address per thread
+            const int row = tid >> 3, pos = start + row;
+            const bool seen = pos >= from && pos < to;
+            if (seen) {
+                const int64_t off = t < cached ? token_offset(g.a, b, L_p, pos) + (int64_t)kvh * g.a.stride_head
+                                               : (((int64_t)b * g.N + pos) * g.a.H_kv + kvh) * D;
+                k += off;
+                v += off;
+            }
+            float* dst = s_ring + (t % kTreeFewStages) * C::SLOT + row * C::LD;
 #pragma unroll
-            for (int j = 0; j < kTreeFewTile * DV / kTreeF32Threads; ++j) {
-                const int i = tid + j * kTreeF32Threads;
-                const int row = i / DV, c = (i % DV) * 4;
-                const int pos = start + row;
-                const bool seen = pos >= from && pos < to;
-                int64_t off = 0;
-                if (seen)
-                    off = t < cached ? token_offset(g.a, b, L_p, pos) + (int64_t)kvh * g.a.stride_head + c
-                                     : (((int64_t)b * g.N + pos) * g.a.H_kv + kvh) * D + c;
-                cp_async16(k + row * C::LD + c, kb + off, seen);
-                cp_async16(v + row * C::LD + c, vb + off, seen);
+            for (int j = 0; j < DV / 8; ++j) {
+                const int c = ((tid & 7) + 8 * j) * 4;
+                cp_async16(dst + c, k + c, seen);
+                cp_async16(dst + kTreeFewTile * C::LD + c, v + c, seen);
             }
         }
         cp_async_commit();
