@@ -244,6 +244,7 @@ int32_t dsa_tree_step(const dsa_problem* problem, const dsa_diag_params* diag, c
     g.node_count = tree->node_count;
     g.N = tree->max_nodes;
     g.G = pl.G;
+    for (g.g_shift = 0; (1 << g.g_shift) < pl.G;) ++g.g_shift;
     g.row_tiles = pl.row_tiles;
     g.box_tokens = pl.box_tokens;
     for (g.box_shift = 0; (1 << g.box_shift) < pl.box_tokens;) ++g.box_shift;

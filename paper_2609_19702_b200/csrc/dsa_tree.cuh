@@ -22,10 +22,14 @@
 // takes the place of the S it came from) + D of O, 256 allocated; two blocks share an SM, so one's set-up
 // and last tile hide behind the other's.
 //
-// Work is cut along the cached tokens where there are fewer blocks than places, or where their number leaves
-// the last wave of blocks half empty: the 2, 4 or 8 blocks of a thread-block cluster share the tiles of one
-// (request, kv head) and merge their states through distributed shared memory, without partial results in
-// HBM or a second launch.  Only where eight are too few (a long sequence under one or two heads) partial
+// A block's set-up, its first copies and its results take some 10 us that nobody else uses on a short sequence.  So
+// blocks are persistent: a running one takes over the next block that has not been launched yet (cluster launch
+// control), its copying warp runs ahead into the next item, and the ring never drains.  Sequences differ in length,
+// and a taken-over block goes to whoever is done first.
+//
+// Where there are fewer blocks than places, the cached tokens are cut: the 2, 4 or 8 blocks of a thread-block cluster
+// share the tiles of one (request, kv head) and merge their states through distributed shared memory, without partial
+// results in HBM or a second launch.  Only where eight are too few (a long sequence under one or two heads) partial
 // results go to the workspace and the combine kernel.
 //
 // The maximum that the exponentials are taken against trails the true one by at most 2^8 (it is replaced,
@@ -50,7 +54,7 @@ struct TreeArgs {
     AttnArgs a;                                    // lengths, block table, strides, scale, outputs
     const int* parent;                             // [B, N] or NULL (a chain)
     const int* node_count;                         // [B] or NULL (N)
-    int N, G;
+    int N, G, g_shift;                             // G: a power of two
     int row_tiles;                                 // blocks of kTreeRows query rows per (request, kv head)
     int windowed;                                  // 0: dense
     int box_tokens;                                // tokens per tensor-map box of the caches
@@ -92,17 +96,33 @@ __device__ __forceinline__ void tc_commit(unsigned long long* bar) {
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Shared-memory operand descriptors, 128-byte swizzle: atoms of 8 rows x 128 bytes, 1024 bytes from one to the next
+// along the rows; `lead`: bytes from one 64-element column block to the next, where the 64 contiguous elements run
+// along N and the operand is wider than they are.  The upper half is the same for all of them.
+constexpr unsigned kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ unsigned desc_low(unsigned addr, unsigned lead) { return ((addr >> 4) & 0x3fffu) | ((lead >> 4) << 16); }
+// Instruction descriptor: bf16 x bf16 -> fp32, M x N; b_mn: B's contiguous dimension is N, not K.
+__host__ __device__ constexpr unsigned instr_desc(int M, int N, bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((unsigned)(N >> 3) << 17) |
+           ((unsigned)(M >> 4) << 24);
+}
 // D[tmem] (+)= A[smem] B[smem]^T
-__device__ __forceinline__ void tc_mma_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool acc) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+__device__ __forceinline__ void tc_mma_ss(unsigned d, unsigned a_low, unsigned b_low, unsigned idesc, bool acc) {
+    asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}"
+                 ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"((unsigned)acc), "r"(kDescHigh) : "memory");
 }
 // D[tmem] (+)= A[tmem] B[smem]^T
-__device__ __forceinline__ void tc_mma_ts(unsigned d, unsigned a, unsigned long long b, unsigned idesc, bool acc) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+__device__ __forceinline__ void tc_mma_ts(unsigned d, unsigned a, unsigned b_low, unsigned idesc, bool acc) {
+    asm volatile("{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 b, {%2, %5};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}"
+                 ::"r"(d), "r"(a), "r"(b_low), "r"(idesc), "r"((unsigned)acc), "r"(kDescHigh) : "memory");
+}
+// one lane of the warp, the same every time (products and their commits come from one thread)
+__device__ __forceinline__ bool elect_one() {
+    unsigned yes;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes != 0;
 }
 __device__ __forceinline__ void tc_ld32(unsigned (&r)[32], unsigned addr) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -126,19 +146,6 @@ __device__ __forceinline__ void tc_st32(unsigned addr, const unsigned (&r)[32]) 
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// Shared-memory operand descriptor, 128-byte swizzle: atoms of 8 rows x 128 bytes.  `stride`: bytes from one
-// 8-row atom to the next along the rows; `lead`: from one 64-element column block to the next (used where the
-// 64 contiguous elements run along M / N and the operand is wider than they are).
-__device__ __forceinline__ unsigned long long smem_desc(unsigned addr, unsigned lead, unsigned stride) {
-    return (unsigned long long)((addr >> 4) & 0x3fffu) | ((unsigned long long)((lead >> 4) & 0x3fffu) << 16) |
-           ((unsigned long long)((stride >> 4) & 0x3fffu) << 32) | (1ull << 46) | (2ull << 61);
-}
-// Instruction descriptor: bf16 x bf16 -> fp32, M x N; b_mn: B's contiguous dimension is N, not K.
-__host__ __device__ constexpr unsigned instr_desc(int M, int N, bool b_mn) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((unsigned)(N >> 3) << 17) |
-           ((unsigned)(M >> 4) << 24);
-}
 
 // ---- what a block works on, in 64-token tiles ---------------------------------------------------------
 // The cached tokens that some node of the request sees: [0, P0) (dense: everything; windowed: prompt and
@@ -169,43 +176,12 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& g, int S, int L_p)
     } else {
         s.P0 = L_p + min(g.a.mask.n_sink, S - L_p);
         s.lo = min(S, max(s.P0, S + 1 - g.a.mask.window));          // (a root's window)
-        s.lo_al = s.lo / g.align_tokens * g.align_tokens;
+        s.lo_al = s.lo & -g.align_tokens;                                   // (a power of two)
     }
     s.T1 = (s.P0 + kTreeTile - 1) / kTreeTile;
     s.T = s.T1 + (S - s.lo_al + kTreeTile - 1) / kTreeTile;
     if (s.lo >= S) s.T = s.T1;
     return s;
-}
-
-// Ancestor sets of the nodes as 64-bit words (bit j: node j is node i or an ancestor of it), by one warp: every
-// round doubles the length of the line that a word covers.
-__device__ __forceinline__ void tree_lines(const TreeArgs& g, int b, unsigned long long* line_of, int lane) {
-    unsigned long long m[2];
-    int up[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int i = lane + 32 * h;
-        m[h] = 1ull << i;
-        int p = i < g.N ? (g.parent ? g.parent[(int64_t)b * g.N + i] : i - 1) : -1;
-        up[h] = (p >= 0 && p < i) ? p : -1;
-    }
-#pragma unroll
-    for (int round = 0; round < 6; ++round) {
-        unsigned long long am[2];
-        int au[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int src = up[h] & 31;
-            const unsigned long long m0 = __shfl_sync(0xffffffffu, m[0], src), m1 = __shfl_sync(0xffffffffu, m[1], src);
-            const int u0 = __shfl_sync(0xffffffffu, up[0], src), u1 = __shfl_sync(0xffffffffu, up[1], src);
-            am[h] = up[h] < 0 ? 0ull : (up[h] < 32 ? m0 : m1);
-            au[h] = up[h] < 0 ? -1 : (up[h] < 32 ? u0 : u1);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) { m[h] |= am[h]; up[h] = au[h]; }
-    }
-    line_of[lane] = m[0];
-    line_of[lane + 32] = m[1];
 }
 
 // K / V rows of the nodes first, first + step, ... below n, kv head kvh, to the cache, by `count` threads.
@@ -231,7 +207,7 @@ template <typename T, int D>
 __device__ __forceinline__ void tree_write_empty(const TreeArgs& g, int b, int kvh, int split, int first_node, int r0, int r1,
                                                  int tid, int count) {
     for (int r = r0 + tid; r < r1; r += count) {
-        const int64_t row = ((int64_t)b * g.N + first_node + r / g.G) * g.a.H_q + kvh * g.G + r % g.G;
+        const int64_t row = ((int64_t)b * g.N + first_node + (r >> g.g_shift)) * g.a.H_q + kvh * g.G + (r & (g.G - 1));
         if (g.a.n_split > 1) { g.a.lse_part[row * g.a.n_split + split] = -INFINITY; continue; }
         g.a.lse[row] = -INFINITY;
         T* out = reinterpret_cast<T*>(g.a.out) + row * D;
@@ -285,6 +261,42 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
     return r;
 }
 
+// ---- dynamic scheduling: a running block takes over blocks that have not been launched yet --------------------
+__device__ __forceinline__ void steal_block(void* response, unsigned long long* bar) {      // one thread
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // (the last response has been read)
+    mbar_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(smem_u32(response)), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ int stolen_block(const void* response) {         // its index, or -1: there is none any more
+    unsigned ok;
+    int x;
+    asm volatile("{\n.reg .b128 r;\n.reg .pred p;\n"
+                 "ld.shared.b128 r, [%2];\n"
+                 "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
+                 "selp.u32 %0, 1, 0, p;\n"
+                 "mov.b32 %1, 0;\n"
+                 "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
+                 : "=r"(ok), "=r"(x) : "r"(smem_u32(response)) : "memory");
+    return ok ? x : -1;
+}
+
+// What a block works on: the piece `piece` of the tiles that the nodes of row tile `rt` of (b, kvh) see.
+struct TreeItem {
+    int index, b, kvh, rt, piece, S, L_p, n;                  // index < 0: nothing any more
+};
+// Its tiles: [t0, t0 + cached) of the request's, then (has_nodes) the nodes' own rows.
+struct TreeWork {
+    TreeSpan span;
+    int t0, cached, tiles, first_node;
+    int rows_all, rows;                                       // rows that the block writes; rows of nodes that exist
+};
+struct TreeInfo {
+    TreeItem item;
+    TreeWork work;
+    signed char up[kTreeMaxNodes];                            // parents of the nodes, -1: a root
+};
+
 template <int D>
 __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArgs g, const __grid_constant__ TreeMaps maps) {
     using C = TreeCfg<D>;
@@ -295,14 +307,21 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + C::Q_BYTES + C::SLOTS * C::SLOT_BYTES);
     unsigned long long* full = bars;                          // a ring slot has landed
     unsigned long long* empty = bars + C::SLOTS;              // the products that read it are done
-    unsigned long long* q_full = bars + 2 * C::SLOTS;
-    unsigned long long* s_full = q_full + 1;                  // [2] scores are in TMEM
-    unsigned long long* p_ready = q_full + 3;                 // [2] weights are in TMEM
-    unsigned long long* pv_done = q_full + 5;                 // [2] O holds the tile
-    unsigned long long* drained = q_full + 7;
-    unsigned long long* line_of = q_full + 8;                 // [64]
-    int* s_misc = reinterpret_cast<int*>(line_of + kTreeMaxNodes);   // [0] TMEM address, [1] abort
-    static_assert((2 * C::SLOTS + 8 + kTreeMaxNodes) * 8 + 8 <= C::TAIL, "tail of the shared memory");
+    unsigned long long* s_full = bars + 2 * C::SLOTS;         // [2] scores are in TMEM
+    unsigned long long* p_ready = s_full + 2;                 // [2] weights are in TMEM
+    unsigned long long* pv_done = s_full + 4;                 // [2] O holds the tile
+    unsigned long long* info_full = s_full + 6;               // [2] the next item is known
+    unsigned long long* info_empty = s_full + 8;              // [2] every warp has read it
+    unsigned long long* q_full = s_full + 10;                 // q has landed
+    unsigned long long* q_empty = s_full + 11;                // the scores of an item's last tile are done
+    unsigned long long* o_free = s_full + 12;                 // O has been read
+    unsigned long long* stolen = s_full + 13;
+    uint4* s_response = reinterpret_cast<uint4*>(s_full + 14);
+    unsigned long long* drained = s_full + 16;
+    TreeInfo* s_info = reinterpret_cast<TreeInfo*>(s_full + 17);                 // [2]
+    int* s_misc = reinterpret_cast<int*>(s_info + 2);         // [0] TMEM address, [1] abort
+    static_assert((2 * C::SLOTS + 17) * 8 + 2 * sizeof(TreeInfo) + 8 <= C::TAIL, "tail of the shared memory");
+    static_assert((2 * C::SLOTS) % 2 == 0, "the response lies on 16 bytes");
     volatile int* abort = s_misc + 1;
     // after the last product, for a merge within the cluster: O (rows padded against bank conflicts) and per row
     // (maximum in base-2 units, sum)
@@ -311,315 +330,396 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     static_assert(kTreeRows * C::PART_LD * 4 <= C::SLOTS * C::SLOT_BYTES, "the partial result takes the ring's place");
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int idx = blockIdx.x;
     const int pieces = g.cluster * g.a.n_split;               // (one of the two is 1)
-    const int piece = idx % pieces; idx /= pieces;
-    const int rt = idx % g.row_tiles; idx /= g.row_tiles;
-    const int kvh = idx % g.a.H_kv;
-    const int b = idx / g.a.H_kv;
-    const int G = g.G, per_tile = kTreeRows / G, first_node = rt * per_tile;
+    const int G = g.G, per_tile = kTreeRows >> g.g_shift;
 
     // set-up that reads nothing: it may run while the launch in front finishes
     if (warp == 4 && lane == 0) {
         for (int s = 0; s < C::SLOTS; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 1); }
-        mbar_init(q_full, 1);
-        for (int s = 0; s < 2; ++s) { mbar_init(s_full + s, 1); mbar_init(pv_done + s, 1); }
-        mbar_init(drained, 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
+            mbar_init(info_full + s, 1); mbar_init(info_empty + s, 7);
+        }
+        mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_free, 4);
+        mbar_init(stolen, 1); mbar_init(drained, 1);
         s_misc[1] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     } else if (warp == 5) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(smem_u32(s_misc)), "r"((unsigned)C::TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         tc_fence_before();
     }
+    __syncthreads();
+    tc_fence_after();
+    const unsigned tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    int S, L_p, n;
-    tree_lengths(g, b, S, L_p, n);
-    const int rows_all = min(per_tile, g.N - first_node) * G;              // rows that this block writes
-    const int rows = max(0, min(per_tile, n - first_node)) * G;            // rows of nodes that exist
-    const int active_warps = (rows + 31) / 32;                              // warps with rows
-    const TreeSpan span = tree_span(g, S, L_p);
-    const int per_piece = (span.T + pieces - 1) / pieces;
-    const int t0 = min(span.T, piece * per_piece), t1 = min(span.T, t0 + per_piece);
-    const bool has_nodes = piece == 0;                                      // the nodes' own rows: one tile more, the last
-    const int cached = t1 - t0;
-    const int tiles = rows == 0 ? 0 : cached + (has_nodes ? 1 : 0);
+
+    // the item number `i` of this block, once the copying warp has found it; false: there is none, or give up
+    TreeItem it = {};
+    TreeWork w = {};
+    auto next_item = [&](int i) -> bool {
+        if (!tree_wait(info_full + (i & 1), (i >> 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
+        it = s_info[i & 1].item;
+        w = s_info[i & 1].work;
+        return it.index >= 0;
+    };
+    auto item_read = [&](int i) {                             // this warp needs item i's description no longer
+        __syncwarp();
+        if (lane == 0) mbar_arrive(info_empty + (i & 1));
+    };
 
     float m_ref = -INFINITY, l = 0.f;                         // softmax threads: maximum (of the raw scores) and sum of their row
-    unsigned tmem = 0;
     if (warp == 4) {
         // ---- copies -------------------------------------------------------------------------------
-        if (lane == 0) {
-            for (int s = 0; s < 2; ++s) mbar_init(p_ready + s, max(active_warps, 1));
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        __syncwarp();
-        asm volatile("bar.arrive 1, 192;" ::: "memory");      // (the barriers are ready)
-        if (tiles > 0) {
-            if (lane == 0) {
-                const int box_nodes = min(per_tile, g.N);
-                mbar_expect_tx(q_full, (unsigned)(C::HALVES * box_nodes * G * 128));
-                for (int h = 0; h < C::HALVES; ++h) tma_box4(s_q + h * C::Q_HALF, &maps.q, 64 * h, kvh * G, first_node, b, q_full);
+        const int shift = g.box_shift;
+        // where this lane's boxes `lane` and `lane + 32` of a tile come from: (page or request, token in it);
+        // looked up two tiles ahead of their copies
+        struct Where { int blk[2], tok[2]; };
+        auto where = [&](int t) -> Where {
+            Where r;
+            int start = 0, from, to;
+            if (t < w.cached) w.span.tile(w.t0 + t, start, from, to);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int pos = start + ((lane + 32 * h) << shift);
+                r.blk[h] = g.blk_coord ? it.b : 0;
+                r.tok[h] = pos;
+                if (g.a.block_table) {
+                    const int bi = pos / g.a.block_size;
+                    r.tok[h] = pos - bi * g.a.block_size;
+                    // (as the table has it: put into range when the copy is made, so that nobody waits for it here)
+                    if (t < w.cached && ((lane + 32 * h) << shift) < kTreeTile)
+                        r.blk[h] = g.a.block_table[(int64_t)it.b * g.a.max_blocks + min(bi, g.a.max_blocks - 1)];
+                }
             }
-            __syncwarp();
-            const int shift = g.box_shift;
-            // where this lane's boxes `lane` and `lane + 32` of a tile come from: (page or request, token in it);
-            // looked up two tiles ahead of their copies
-            struct Where { int blk[2], tok[2]; };
-            auto where = [&](int t) -> Where {
-                Where w;
-                int start = 0, from, to;
-                if (t < cached) span.tile(t0 + t, start, from, to);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int pos = start + ((lane + 32 * h) << shift);
-                    w.blk[h] = g.blk_coord ? b : 0;
-                    w.tok[h] = pos;
-                    if (g.a.block_table) {
-                        const int bi = pos / g.a.block_size;
-                        w.tok[h] = pos - bi * g.a.block_size;
-                        if (t < cached && ((lane + 32 * h) << shift) < kTreeTile)
-                            w.blk[h] = max(0, min(__ldg(g.a.block_table + (int64_t)b * g.a.max_blocks + min(bi, g.a.max_blocks - 1)),
-                                                  g.a.num_blocks - 1)) * g.blk_coord;
-                    }
-                }
-                return w;
-            };
-            int issued = 0, slot = 0, round = 0;
-            auto issue = [&](int t, bool is_v, const Where& w) -> bool {
-                if (round > 0 && !tree_wait(empty + slot, (round - 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
-                unsigned char* dst = s_ring + slot * C::SLOT_BYTES;
-                unsigned long long* bar = full + slot;
-                if (t < cached) {
-                    int start, from, to;
-                    span.tile(t0 + t, start, from, to);
-                    const int j0 = (from - start) >> shift, j1 = (to - start + (1 << shift) - 1) >> shift;
-                    if (lane == 0) mbar_expect_tx(bar, (unsigned)(((j1 - j0) * C::HALVES) << shift) * 128u);
-                    __syncwarp();
-                    const CUtensorMap* map = is_v ? &maps.v : &maps.k;
-#pragma unroll
-                    for (int h2 = 0; h2 < 2; ++h2) {
-                        const int j = lane + 32 * h2;
-                        if (j >= j0 && j < j1) {
-#pragma unroll
-                            for (int h = 0; h < C::HALVES; ++h)
-                                tma_box4(dst + h * C::KV_HALF + ((j << shift) * 128), map, 64 * h, w.tok[h2], kvh * g.head_coord,
-                                         w.blk[h2], bar);
-                        }
-                        if (shift >= 1) break;
-                    }
-                } else if (lane == 0) {
-                    mbar_expect_tx(bar, (unsigned)(C::HALVES * g.N * 128));
-#pragma unroll
-                    for (int h = 0; h < C::HALVES; ++h)
-                        tma_box4(dst + h * C::KV_HALF, is_v ? &maps.v_new : &maps.k_new, 64 * h, 0, kvh, b, bar);
-                }
+            return r;
+        };
+        int issued = 0, slot = 0, round = 0;
+        auto issue = [&](int t, bool is_v, const Where& r) -> bool {
+            if (round > 0 && !tree_wait(empty + slot, (round - 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
+            unsigned char* dst = s_ring + slot * C::SLOT_BYTES;
+            unsigned long long* bar = full + slot;
+            if (t < w.cached) {
+                int start, from, to;
+                w.span.tile(w.t0 + t, start, from, to);
+                const int j0 = (from - start) >> shift, j1 = (to - start + (1 << shift) - 1) >> shift;
+                if (lane == 0) mbar_expect_tx(bar, (unsigned)(((j1 - j0) * C::HALVES) << shift) * 128u);
                 __syncwarp();
-                ++issued;
-                if (++slot == C::SLOTS) { slot = 0; ++round; }
-                return true;
-            };
-            Where w0 = where(0), w1 = where(1), w2 = where(2);
-            bool ok = issue(0, false, w0) && (tiles < 2 || issue(1, false, w1));
-            for (int t = 0; ok && t < tiles; ++t) {
-                const Where w3 = where(t + 3);
-                ok = issue(t, true, w0) && (t + 2 >= tiles || issue(t + 2, false, w2));
-                w0 = w1; w1 = w2; w2 = w3;
-            }
-            // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
-            volatile int no_abort = 0;
-            tree_wait(q_full, 0u, &no_abort, nullptr, lane);
-            for (int c = max(0, issued - C::SLOTS); c < issued; ++c)
-                if (!tree_wait(full + c % C::SLOTS, (c / C::SLOTS) & 1, &no_abort, nullptr, lane)) break;
-        }
-    } else if (warp >= 6) {
-        // ---- the nodes' rows to the cache: every block those of its own nodes, the pieces in turn ----------------
-        tree_append<T, D>(g, b, kvh, S, L_p, first_node + piece, pieces, min(n, first_node + per_tile), tid - 192, 64);
-    } else {
-        if (warp == 0) tree_lines(g, b, line_of, lane);
-        asm volatile("bar.sync 1, 192;" ::: "memory");
-        tc_fence_after();
-        tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
-        if (warp == 5) {
-            // ---- products ---------------------------------------------------------------------------
-            constexpr unsigned kIdescS = instr_desc(kTreeRows, kTreeTile, false), kIdescO = instr_desc(kTreeRows, D, true);
-            int slot = 0, round = 0;                         // of the ring
-            auto next_slot = [&]() { if (++slot == C::SLOTS) { slot = 0; ++round; } };
-            auto scores = [&](int t) -> bool {
-                const int s = slot;
-                if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
-                tc_fence_after();
-                if (lane == 0) {
-                    const unsigned qa = smem_u32(s_q), ka = smem_u32(s_ring + s * C::SLOT_BYTES);
+                const CUtensorMap* map = is_v ? &maps.v : &maps.k;
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                        tc_mma_ss(tmem + C::COL_S + (t & 1) * kTreeTile,
-                                  smem_desc(qa + (kk / 4) * C::Q_HALF + (kk % 4) * 32, 16, 1024),
-                                  smem_desc(ka + (kk / 4) * C::KV_HALF + (kk % 4) * 32, 16, 1024), kIdescS, kk > 0);
-                    tc_commit(empty + s);
-                    tc_commit(s_full + (t & 1));
-                }
-                __syncwarp();
-                next_slot();
-                return true;
-            };
-            auto values = [&](int t) -> bool {
-                if (!tree_wait(p_ready + (t & 1), (t >> 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
-                const int s = slot;
-                if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
-                unsigned char* v = s_ring + s * C::SLOT_BYTES;
-                // rows of V that nobody sees: zero, whatever the cache or the slot held there
-                int lo = 0, hi = n;
-                if (t < cached) {
-                    int start;
-                    span.tile(t0 + t, start, lo, hi);
-                    lo -= start; hi -= start;
-                }
-                if (lo > 0 || hi < kTreeTile) {
-                    for (int i = lane; i < kTreeTile * 8; i += 32) {
-                        const int row = i >> 3;
-                        if (row >= lo && row < hi) continue;
+                for (int h2 = 0; h2 < 2; ++h2) {
+                    const int j = lane + 32 * h2;
+                    if (j >= j0 && j < j1) {
+                        const int blk = g.a.block_table ? max(0, min(r.blk[h2], g.a.num_blocks - 1)) * g.blk_coord : r.blk[h2];
 #pragma unroll
                         for (int h = 0; h < C::HALVES; ++h)
-                            *reinterpret_cast<uint4*>(v + h * C::KV_HALF + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            tma_box4(dst + h * C::KV_HALF + ((j << shift) * 128), map, 64 * h, r.tok[h2], it.kvh * g.head_coord,
+                                     blk, bar);
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
+                    if (shift >= 1) break;
                 }
-                tc_fence_after();
-                if (lane == 0) {
-                    const unsigned va = smem_u32(v);
+            } else if (lane == 0) {
+                mbar_expect_tx(bar, (unsigned)(C::HALVES * g.N * 128));
 #pragma unroll
-                    for (int kk = 0; kk < kTreeTile / 16; ++kk)
-                        tc_mma_ts(tmem + C::COL_O, tmem + C::COL_S + (t & 1) * kTreeTile + kk * 8,
-                                  smem_desc(va + kk * 2048, C::KV_HALF, 1024), kIdescO, t > 0 || kk > 0);
-                    tc_commit(empty + s);
-                    tc_commit(pv_done + (t & 1));
+                for (int h = 0; h < C::HALVES; ++h)
+                    tma_box4(dst + h * C::KV_HALF, is_v ? &maps.v_new : &maps.k_new, 64 * h, 0, it.kvh, it.b, bar);
+            }
+            __syncwarp();
+            ++issued;
+            if (++slot == C::SLOTS) { slot = 0; ++round; }
+            return true;
+        };
+        bool ok = true;
+        int live = 0;                                         // items with tiles so far
+        it.index = (int)blockIdx.x;
+        for (int i = 0; ok; ++i) {
+            int up[2] = {-1, -1};                             // parents of the nodes lane and lane + 32
+            if (it.index >= 0) {
+                int idx = it.index;
+                it.piece = idx % pieces; idx /= pieces;
+                it.rt = idx % g.row_tiles; idx /= g.row_tiles;
+                it.kvh = idx % g.a.H_kv;
+                it.b = idx / g.a.H_kv;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int node = lane + 32 * h;
+                    if (node < g.N) up[h] = g.parent ? g.parent[(int64_t)it.b * g.N + node] : node - 1;
+                    if (up[h] >= node) up[h] = -1;
                 }
-                __syncwarp();
-                next_slot();
-                return true;
+                tree_lengths(g, it.b, it.S, it.L_p, it.n);
+            }
+            if (i >= 2) ok = tree_wait(info_empty + (i & 1), ((i >> 1) - 1) & 1, abort, g.a.wait_timeouts, lane);
+            if (!ok) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) s_info[i & 1].up[lane + 32 * h] = (signed char)max(up[h], -1);
+            if (it.index >= 0) {
+                w.first_node = it.rt * per_tile;
+                w.rows_all = min(per_tile, g.N - w.first_node) << g.g_shift;
+                w.rows = max(0, min(per_tile, it.n - w.first_node)) << g.g_shift;
+                w.span = tree_span(g, it.S, it.L_p);
+                const int per_piece = pieces > 1 ? (w.span.T + pieces - 1) / pieces : w.span.T;
+                w.t0 = min(w.span.T, it.piece * per_piece);
+                w.cached = min(w.span.T, w.t0 + per_piece) - w.t0;
+                w.tiles = w.rows == 0 ? 0 : w.cached + (it.piece == 0 ? 1 : 0);
+            }
+            if (lane == 0) { s_info[i & 1].item = it; s_info[i & 1].work = w; }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(info_full + (i & 1));
+            if (it.index < 0) break;
+            // the next item is taken over when this one's copies are nearly all on their way: late, so that it goes to
+            // whoever has room for it, but early enough to know its lengths and pages in time
+            bool asked = g.cluster > 1;
+            auto ask = [&]() {
+                if (!asked && lane == 0) steal_block(s_response, stolen);
+                asked = true;
             };
-            bool ok = tiles > 0 && tree_wait(q_full, 0u, abort, g.a.wait_timeouts, lane) && scores(0) && (tiles < 2 || scores(1));
-            for (int t = 0; ok && t < tiles; ++t) ok = values(t) && (t + 2 >= tiles || scores(t + 2));
-            if (!ok && tiles > 0) {                          // TMEM is given back only when no product uses it
-                if (lane == 0) tc_commit(drained);
+            if (w.tiles > 0) {
+                Where w0 = where(0), w1 = where(1), w2 = where(2);
+                if (live > 0) ok = tree_wait(q_empty, (live - 1) & 1, abort, g.a.wait_timeouts, lane);
+                if (ok && lane == 0) {
+                    const int box_nodes = min(per_tile, g.N);
+                    mbar_expect_tx(q_full, (unsigned)(C::HALVES * box_nodes * G * 128));
+                    for (int h = 0; h < C::HALVES; ++h) tma_box4(s_q + h * C::Q_HALF, &maps.q, 64 * h, it.kvh * G, w.first_node, it.b, q_full);
+                }
                 __syncwarp();
-                volatile int no_abort = 0;
-                tree_wait(drained, 0u, &no_abort, nullptr, lane);
-            }
-        } else {
-            // ---- softmax: one thread per query row --------------------------------------------------
-            const int row = tid;                              // of the block's 128
-            const int node = first_node + row / G;
-            const bool alive = row < rows;
-            const bool work = tiles > 0 && warp < active_warps;
-            const unsigned lane_base = (unsigned)(warp * 32) << 16;
-            const float sl = g.a.scale_log2;
-            bool ok = true;
-            if (work) {
-                const unsigned long long line = alive ? line_of[node] : 0ull;
-                const int depth = __popcll(line) - 1;
-                // the first cached position of the window (dense: everything is in [0, P0))
-                const int64_t win_lo = (int64_t)S + depth + 1 - g.a.mask.window;
-                unsigned long long own = line & (n < 64 ? (1ull << n) - 1ull : ~0ull);
-                if (g.windowed && alive) {
-                    // drafted tokens of the own line that the window has left behind (sinks stay)
-                    unsigned long long keep = own, todo = own;
-                    while (todo) {
-                        const int j = __ffsll(todo) - 1;
-                        todo &= todo - 1;
-                        const int dj = __popcll(line_of[j]) - 1;
-                        if (depth - dj >= g.a.mask.window && (int64_t)S + dj >= (int64_t)L_p + g.a.mask.n_sink) keep &= ~(1ull << j);
-                    }
-                    own = keep;
+                if (ok) ++live;
+                ok = ok && issue(0, false, w0) && (w.tiles < 2 || issue(1, false, w1));
+                for (int t = 0; ok && t < w.tiles; ++t) {
+                    if (t + 4 >= w.tiles) ask();
+                    const Where w3 = where(t + 3);
+                    ok = issue(t, true, w0) && (t + 2 >= w.tiles || issue(t + 2, false, w2));
+                    w0 = w1; w1 = w2; w2 = w3;
                 }
-                for (int t = 0; t < tiles; ++t) {
-                    const int buf = t & 1;
-                    if (!tree_wait(s_full + buf, (t >> 1) & 1, abort, g.a.wait_timeouts, lane)) { ok = false; break; }
-                    tc_fence_after();
-                    const unsigned s_addr = tmem + lane_base + C::COL_S + buf * kTreeTile;
-                    unsigned x0[32], x1[32];
-                    tc_ld32(x0, s_addr);
-                    tc_ld32(x1, s_addr + 32);
-                    unsigned long long see;
-                    if (t < cached) {
-                        int start, from, to;
-                        span.tile(t0 + t, start, from, to);
-                        int c0 = 0, c1 = to - start;
-                        if (t0 + t >= span.T1) c0 = (int)max((int64_t)from, min((int64_t)to, win_lo)) - start;
-                        if (!alive) c1 = 0;
-                        see = c1 >= 64 ? ~0ull : (1ull << c1) - 1ull;
-                        see = c0 >= 64 ? 0ull : (c0 > 0 ? (see >> c0) << c0 : see);
-                    } else {
-                        see = own;
-                    }
-                    tc_wait_ld();
-                    if (__any_sync(0xffffffffu, see != ~0ull)) {
-                        const unsigned lo = (unsigned)see, hi = (unsigned)(see >> 32);
+            }
+            ask();
+            it.index = -1;
+            if (g.cluster == 1) {
+                volatile int no_abort = 0;                    // (the response is waited for whatever else has happened)
+                if (tree_wait(stolen, i & 1, &no_abort, g.a.wait_timeouts, lane)) it.index = stolen_block(s_response);
+                else { *abort = 1; ok = false; }
+            }
+        }
+        // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
+        volatile int no_abort = 0;
+        if (live > 0) tree_wait(q_full, (live - 1) & 1, &no_abort, nullptr, lane);
+        for (int c = max(0, issued - C::SLOTS); c < issued; ++c)
+            if (!tree_wait(full + c % C::SLOTS, (c / C::SLOTS) & 1, &no_abort, nullptr, lane)) break;
+    } else if (warp >= 6) {
+        // ---- the nodes' rows to the cache: every block those of its own nodes, the pieces in turn ----------------
+        for (int i = 0; next_item(i); ++i) {
+            item_read(i);
+            const int first = it.rt * per_tile;
+            tree_append<T, D>(g, it.b, it.kvh, it.S, it.L_p, first + it.piece, pieces, min(it.n, first + per_tile), tid - 192, 64);
+        }
+    } else if (warp == 5) {
+        // ---- products ---------------------------------------------------------------------------
+        constexpr unsigned kIdescS = instr_desc(kTreeRows, kTreeTile, false), kIdescO = instr_desc(kTreeRows, D, true);
+        const unsigned q_desc = desc_low(smem_u32(s_q), 16), k_desc = desc_low(smem_u32(s_ring), 16);
+        const unsigned v_desc = desc_low(smem_u32(s_ring), C::KV_HALF);
+        int slot = 0, round = 0;                              // of the ring
+        int done = 0;                                         // tiles of the items before this one
+        auto next_slot = [&]() { if (++slot == C::SLOTS) { slot = 0; ++round; } };
+        auto scores = [&](int t) -> bool {
+            const int s = slot, buf = (done + t) & 1;
+            if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
+            tc_fence_after();
+            if (elect_one()) {
+                const unsigned qa = q_desc, ka = k_desc + s * (C::SLOT_BYTES / 16), d = tmem + C::COL_S + buf * kTreeTile;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (!((lo >> i) & 1u)) x0[i] = 0xff800000u;
-                            if (!((hi >> i) & 1u)) x1[i] = 0xff800000u;
-                        }
-                    }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                for (int kk = 0; kk < D / 16; ++kk)
+                    tc_mma_ss(d, qa + ((kk / 4) * C::Q_HALF + (kk % 4) * 32) / 16, ka + ((kk / 4) * C::KV_HALF + (kk % 4) * 32) / 16,
+                              kIdescS, kk > 0);
+                tc_commit(empty + s);
+                tc_commit(s_full + buf);
+                if (t == w.tiles - 1) tc_commit(q_empty);
+            }
+            __syncwarp();
+            next_slot();
+            return true;
+        };
+        auto values = [&](int t) -> bool {
+            const int gt = done + t, buf = gt & 1;
+            if (!tree_wait(p_ready + buf, (gt >> 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
+            const int s = slot;
+            if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
+            unsigned char* v = s_ring + s * C::SLOT_BYTES;
+            // rows of V that nobody sees: zero, whatever the cache or the slot held there
+            int lo = 0, hi = it.n;
+            if (t < w.cached) {
+                int start;
+                w.span.tile(w.t0 + t, start, lo, hi);
+                lo -= start; hi -= start;
+            }
+            if (lo > 0 || hi < kTreeTile) {
+                for (int i = lane; i < kTreeTile * 8; i += 32) {
+                    const int row = i >> 3;
+                    if (row >= lo && row < hi) continue;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        mx[i & 1] = fmaxf(mx[i & 1], __uint_as_float(x0[i]));
-                        mx[2 + (i & 1)] = fmaxf(mx[2 + (i & 1)], __uint_as_float(x1[i]));
-                    }
-                    const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                    // (-inf - -inf is NaN: compares false, nothing to rescale)
-                    if (__any_sync(0xffffffffu, (m_tile - m_ref) * sl > 8.f)) {
-                        const float m_new = fmaxf(m_ref, m_tile);
-                        const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m_ref - m_new) * sl);
-                        m_ref = m_new;
-                        l *= alpha;
-                        if (t > 0) {
-                            if (!tree_wait(pv_done + ((t - 1) & 1), ((t - 1) >> 1) & 1, abort, g.a.wait_timeouts, lane)) { ok = false; break; }
-                            tc_fence_after();
-#pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                unsigned o[32];
-                                tc_ld32(o, tmem + lane_base + C::COL_O + c);
-                                tc_wait_ld();
+                    for (int h = 0; h < C::HALVES; ++h)
+                        *reinterpret_cast<uint4*>(v + h * C::KV_HALF + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            tc_fence_after();
+            if (elect_one()) {
+                const unsigned va = v_desc + s * (C::SLOT_BYTES / 16), pa = tmem + C::COL_S + buf * kTreeTile;
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tc_st32(tmem + lane_base + C::COL_O + c, o);
-                            }
-                        }
-                    }
-                    const float sub = m_ref == -INFINITY ? 0.f : m_ref * sl;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                    unsigned pk[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const unsigned a0 = i < 16 ? x0[2 * i] : x1[2 * i - 32], a1 = i < 16 ? x0[2 * i + 1] : x1[2 * i - 31];
-                        const float p0 = fast_exp2(fmaf(__uint_as_float(a0), sl, -sub));
-                        const float p1 = fast_exp2(fmaf(__uint_as_float(a1), sl, -sub));
-                        sum[i & 3] += p0 + p1;
-                        pk[i] = pack_bf16(p0, p1);
-                    }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tc_st32(s_addr, pk);
-                    tc_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
+                for (int kk = 0; kk < kTreeTile / 16; ++kk)
+                    tc_mma_ts(tmem + C::COL_O, pa + kk * 8, va + kk * (2048 / 16), kIdescO, t > 0 || kk > 0);
+                tc_commit(empty + s);
+                tc_commit(pv_done + buf);
+            }
+            __syncwarp();
+            next_slot();
+            return true;
+        };
+        int live = 0;
+        bool ok = true;
+        for (int i = 0; next_item(i); ++i) {
+            item_read(i);
+            if (w.tiles == 0) continue;
+            ok = tree_wait(q_full, live & 1, abort, g.a.wait_timeouts, lane) && scores(0) && (w.tiles < 2 || scores(1));
+            // (the first product of P and V replaces the last item's O)
+            if (ok && live > 0) ok = tree_wait(o_free, (live - 1) & 1, abort, g.a.wait_timeouts, lane);
+            for (int t = 0; ok && t < w.tiles; ++t) ok = values(t) && (t + 2 >= w.tiles || scores(t + 2));
+            if (!ok) break;
+            done += w.tiles;
+            ++live;
+        }
+        if (__any_sync(0xffffffffu, !ok || *abort)) {         // TMEM is given back only when no product uses it
+            if (elect_one()) tc_commit(drained);
+            __syncwarp();
+            volatile int no_abort = 0;
+            tree_wait(drained, 0u, &no_abort, nullptr, lane);
+        }
+    } else {
+        // ---- softmax: one thread per query row --------------------------------------------------
+        const int row = tid;                                  // of the block's 128
+        const unsigned lane_base = (unsigned)(warp * 32) << 16;
+        const float sl = g.a.scale_log2;
+        int done = 0;                                         // tiles of the items before this one
+        bool ok = true;
+        for (int i = 0; ok && next_item(i); ++i) {
+            m_ref = -INFINITY;
+            l = 0.f;
+            const bool work = w.tiles > 0 && warp * 32 < w.rows;     // a warp without rows only keeps step
+            const int node = w.first_node + (row >> g.g_shift);
+            const bool alive = row < w.rows;
+            unsigned long long own = 0ull;                    // drafted tokens that the row's node sees
+            int64_t win_lo = 0;                               // and where the window begins (dense: everything is in [0, P0))
+            if (work && alive) {
+                const signed char* up = s_info[i & 1].up;
+                int depth = 0;                                // (ancestors of a node that exists exist)
+                for (int j = node; j >= 0; j = up[j], ++depth) own |= 1ull << j;
+                --depth;
+                win_lo = (int64_t)it.S + depth + 1 - g.a.mask.window;
+                if (g.windowed) {
+                    // tokens of the own line that the window has left behind (sinks stay): `back` positions behind
+                    const int64_t sinks = (int64_t)it.L_p + g.a.mask.n_sink - it.S;       // depths below this are sinks
+                    int back = 0;
+                    for (int j = node; j >= 0; j = up[j], ++back)
+                        if (back >= g.a.mask.window && depth - back >= sinks) own &= ~(1ull << j);
+                }
+            }
+            item_read(i);
+            if (w.tiles == 0) {
+                if (g.cluster == 1) tree_write_empty<T, D>(g, it.b, it.kvh, it.piece, w.first_node, 0, w.rows_all, tid, 128);
+                continue;
+            }
+            for (int t = 0; ok && t < w.tiles; ++t) {
+                const int gt = done + t, buf = gt & 1;
+                ok = tree_wait(s_full + buf, (gt >> 1) & 1, abort, g.a.wait_timeouts, lane);
+                if (!ok) break;
+                if (!work) {
                     if (lane == 0) mbar_arrive(p_ready + buf);
+                    continue;
                 }
-                if (ok) ok = tree_wait(pv_done + ((tiles - 1) & 1), ((tiles - 1) >> 1) & 1, abort, g.a.wait_timeouts, lane);
                 tc_fence_after();
+                const unsigned s_addr = tmem + lane_base + C::COL_S + buf * kTreeTile;
+                unsigned x0[32], x1[32];
+                tc_ld32(x0, s_addr);
+                tc_ld32(x1, s_addr + 32);
+                unsigned long long see;
+                if (t < w.cached) {
+                    int start, from, to;
+                    w.span.tile(w.t0 + t, start, from, to);
+                    int c0 = 0, c1 = to - start;
+                    if (w.t0 + t >= w.span.T1) c0 = (int)max((int64_t)from, min((int64_t)to, win_lo)) - start;
+                    if (!alive) c1 = 0;
+                    see = c1 >= 64 ? ~0ull : (1ull << c1) - 1ull;
+                    see = c0 >= 64 ? 0ull : (c0 > 0 ? (see >> c0) << c0 : see);
+                } else {
+                    see = own;
+                }
+                tc_wait_ld();
+                if (__any_sync(0xffffffffu, see != ~0ull)) {
+                    const unsigned lo = (unsigned)see, hi = (unsigned)(see >> 32);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        if (!((lo >> k) & 1u)) x0[k] = 0xff800000u;
+                        if (!((hi >> k) & 1u)) x1[k] = 0xff800000u;
+                    }
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    mx[k & 1] = fmaxf(mx[k & 1], __uint_as_float(x0[k]));
+                    mx[2 + (k & 1)] = fmaxf(mx[2 + (k & 1)], __uint_as_float(x1[k]));
+                }
+                const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                // (-inf - -inf is NaN: compares false, nothing to rescale)
+                if (__any_sync(0xffffffffu, (m_tile - m_ref) * sl > 8.f)) {
+                    const float m_new = fmaxf(m_ref, m_tile);
+                    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m_ref - m_new) * sl);
+                    m_ref = m_new;
+                    l *= alpha;
+                    if (t > 0) {
+                        ok = tree_wait(pv_done + ((gt - 1) & 1), ((gt - 1) >> 1) & 1, abort, g.a.wait_timeouts, lane);
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            unsigned o[32];
+                            tc_ld32(o, tmem + lane_base + C::COL_O + c);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                            tc_st32(tmem + lane_base + C::COL_O + c, o);
+                        }
+                    }
+                }
+                const float sub = m_ref == -INFINITY ? 0.f : m_ref * sl;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                unsigned pk[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    const unsigned a0 = k < 16 ? x0[2 * k] : x1[2 * k - 32], a1 = k < 16 ? x0[2 * k + 1] : x1[2 * k - 31];
+                    const float p0 = fast_exp2(fmaf(__uint_as_float(a0), sl, -sub));
+                    const float p1 = fast_exp2(fmaf(__uint_as_float(a1), sl, -sub));
+                    sum[k & 3] += p0 + p1;
+                    pk[k] = pack_bf16(p0, p1);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tc_st32(s_addr, pk);
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_ready + buf);
             }
-            // ---- results --------------------------------------------------------------------------
-            if (g.cluster > 1) {
-                // (merged below)
-            } else if (work && ok) {
-                const bool mine = row < rows_all;
+            if (!ok) break;
+            done += w.tiles;
+            ok = tree_wait(pv_done + ((done - 1) & 1), ((done - 1) >> 1) & 1, abort, g.a.wait_timeouts, lane);
+            tc_fence_after();
+            if (g.cluster > 1) break;                         // (one item, merged below)
+            // ---- results ------------------------------------------------------------------------
+            if (work) {
+                const bool mine = ok && row < w.rows_all;
                 const bool none = l == 0.f;                    // nothing seen: zeros and -inf
                 const float inv = none ? 0.f : 1.f / l;
-                const int64_t orow = ((int64_t)b * g.N + node) * g.a.H_q + kvh * G + row % G;
+                const int64_t orow = ((int64_t)it.b * g.N + node) * g.a.H_q + it.kvh * G + (row & (G - 1));
                 const float lse = none ? -INFINITY : (m_ref * sl + log2f(l)) * LN2;
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
@@ -628,45 +728,45 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                     tc_wait_ld();
                     if (mine) {
                         float f[32];
-    #pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : __uint_as_float(o[i]) * inv;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) f[k] = none ? 0.f : __uint_as_float(o[k]) * inv;
                         if (g.a.n_split > 1) {
-                            float* dst = g.a.out_part + (orow * g.a.n_split + piece) * D + c;
-    #pragma unroll
-                            for (int i = 0; i < 32; i += 4)
-                                *reinterpret_cast<float4*>(dst + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+                            float* dst = g.a.out_part + (orow * g.a.n_split + it.piece) * D + c;
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4)
+                                *reinterpret_cast<float4*>(dst + k) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
                         } else {
                             T* dst = reinterpret_cast<T*>(g.a.out) + orow * D + c;
-    #pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                unsigned w[4];
-    #pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    w[k] = pack_bf16(f[i + 2 * k], f[i + 2 * k + 1]);
-                                *reinterpret_cast<uint4*>(dst + i) = make_uint4(w[0], w[1], w[2], w[3]);
-                            }
+#pragma unroll
+                            for (int k = 0; k < 32; k += 8)
+                                *reinterpret_cast<uint4*>(dst + k) = make_uint4(pack_bf16(f[k], f[k + 1]), pack_bf16(f[k + 2], f[k + 3]),
+                                                                                pack_bf16(f[k + 4], f[k + 5]), pack_bf16(f[k + 6], f[k + 7]));
                         }
                     }
                     __syncwarp();
                 }
+                tc_fence_before();
                 if (mine) {
-                    if (g.a.n_split > 1) g.a.lse_part[orow * g.a.n_split + piece] = lse;
+                    if (g.a.n_split > 1) g.a.lse_part[orow * g.a.n_split + it.piece] = lse;
                     else g.a.lse[orow] = lse;
                 }
-            } else if (!work) {
-                // rows of nodes that do not exist, beyond the last warp with rows; all rows where there is nothing to see
-                const int first = tiles > 0 ? active_warps * 32 : 0;
-                tree_write_empty<T, D>(g, b, kvh, piece, first_node, first, rows_all, tid - first, 128 - first);
+            } else {
+                // rows of nodes that do not exist, beyond the last warp with rows
+                const int first = (w.rows + 31) / 32 * 32;
+                tree_write_empty<T, D>(g, it.b, it.kvh, it.piece, w.first_node, first, w.rows_all, tid - first, 128 - first);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(o_free);
         }
-        tc_fence_before();
     }
+    __syncthreads();                                          // (every role has come to its end)
     if (g.cluster > 1) {
         // ---- merge: out = sum_i e^{m_i - M} O_i / sum_i e^{m_i - M} l_i over the cluster's blocks --------------
-        __syncthreads();                                      // the ring and Q have been read for the last time
+        it = s_info[0].item;
+        w = s_info[0].work;
         if (warp < 4) {
             s_ml[tid] = make_float2(l == 0.f ? -INFINITY : m_ref * g.a.scale_log2, l);
-            if (tiles > 0 && warp < active_warps) {
+            if (w.tiles > 0 && warp * 32 < w.rows) {
                 tc_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
@@ -674,8 +774,8 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                     tc_ld32(o, tmem + ((unsigned)(warp * 32) << 16) + C::COL_O + c);
                     tc_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<uint4*>(s_part + tid * C::PART_LD + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<uint4*>(s_part + tid * C::PART_LD + c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                 }
                 tc_fence_before();
             }
@@ -683,7 +783,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
         tree_cluster_barrier();
         constexpr int LPR = D / 4, RPW = 32 / LPR;            // lanes per row (four dims each), rows per warp
         const int sub = lane / LPR, c4 = (lane % LPR) * 4;
-        for (int r = piece + (warp * RPW + sub) * g.cluster; r < rows_all; r += 8 * RPW * g.cluster) {
+        for (int r = it.piece + (warp * RPW + sub) * g.cluster; r < w.rows_all; r += 8 * RPW * g.cluster) {
             float m_max = -INFINITY;
             for (int i = 0; i < g.cluster; ++i) m_max = fmaxf(m_max, tree_peer_f2(tree_peer(s_ml + r, i)).x);
             float sum = 0.f;
@@ -691,15 +791,15 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
             for (int i = 0; i < g.cluster; ++i) {
                 const float2 ml = tree_peer_f2(tree_peer(s_ml + r, i));
                 if (ml.y == 0.f) continue;                    // (a piece that saw nothing has no O either)
-                const float w = fast_exp2(ml.x - m_max);
+                const float wt = fast_exp2(ml.x - m_max);
                 const float4 o = tree_peer_f4(tree_peer(s_part + r * C::PART_LD + c4, i));
-                sum = fmaf(w, ml.y, sum);
-                acc.x = fmaf(w, o.x, acc.x); acc.y = fmaf(w, o.y, acc.y);
-                acc.z = fmaf(w, o.z, acc.z); acc.w = fmaf(w, o.w, acc.w);
+                sum = fmaf(wt, ml.y, sum);
+                acc.x = fmaf(wt, o.x, acc.x); acc.y = fmaf(wt, o.y, acc.y);
+                acc.z = fmaf(wt, o.z, acc.z); acc.w = fmaf(wt, o.w, acc.w);
             }
             const bool none = sum == 0.f;
             const float inv = none ? 0.f : 1.f / sum;
-            const int64_t orow = ((int64_t)b * g.N + first_node + r / G) * g.a.H_q + kvh * G + r % G;
+            const int64_t orow = ((int64_t)it.b * g.N + w.first_node + (r >> g.g_shift)) * g.a.H_q + it.kvh * G + (r & (G - 1));
             *reinterpret_cast<uint2*>(reinterpret_cast<T*>(g.a.out) + orow * D + c4) =
                 none ? make_uint2(0u, 0u) : make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
             if (c4 == 0) g.a.lse[orow] = none ? -INFINITY : (m_max + log2f(sum)) * LN2;
@@ -709,8 +809,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     __syncthreads();
     if (warp == 5) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;"
-                     ::"r"((unsigned)*reinterpret_cast<volatile int*>(s_misc)), "r"((unsigned)C::TMEM_COLS));
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((unsigned)C::TMEM_COLS));
     }
 }
 

@@ -22,6 +22,42 @@
 
 namespace dsa {
 
+// Parents of the nodes lane and lane + 32 (-1: a root).
+struct TreeParents { int up[2]; };
+__device__ __forceinline__ TreeParents tree_parents(const TreeArgs& g, int b, int lane) {
+    TreeParents t;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = lane + 32 * h;
+        const int p = i < g.N ? (g.parent ? g.parent[(int64_t)b * g.N + i] : i - 1) : -1;
+        t.up[h] = (p >= 0 && p < i) ? p : -1;
+    }
+    return t;
+}
+// Ancestor sets of the nodes as 64-bit words (bit j: node j is node i or an ancestor of it), by one warp: every
+// round doubles the length of the line that a word covers.
+__device__ __forceinline__ void tree_lines(TreeParents t, unsigned long long* line_of, int lane) {
+    unsigned long long m[2] = {1ull << lane, 1ull << (lane + 32)};
+    int (&up)[2] = t.up;
+#pragma unroll
+    for (int round = 0; round < 6; ++round) {
+        unsigned long long am[2];
+        int au[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int src = up[h] & 31;
+            const unsigned long long m0 = __shfl_sync(0xffffffffu, m[0], src), m1 = __shfl_sync(0xffffffffu, m[1], src);
+            const int u0 = __shfl_sync(0xffffffffu, up[0], src), u1 = __shfl_sync(0xffffffffu, up[1], src);
+            am[h] = up[h] < 0 ? 0ull : (up[h] < 32 ? m0 : m1);
+            au[h] = up[h] < 0 ? -1 : (up[h] < 32 ? u0 : u1);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) { m[h] |= am[h]; up[h] = au[h]; }
+    }
+    line_of[lane] = m[0];
+    line_of[lane + 32] = m[1];
+}
+
 constexpr int kTreeF32Rows = 32;
 constexpr int kTreeF32Threads = 256;                       // few rows
 
@@ -93,7 +129,7 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
     };
     stage(0, false);
     stage(0, true);
-    if (warp == 0) tree_lines(g, b, line_of, lane);
+    if (warp == 0) tree_lines(tree_parents(g, b, lane), line_of, lane);
     for (int i = tid; i < kTreeF32Rows * DV; i += kTreeF32Threads) {
         const int row = i / DV, c = (i - row * DV) * 4;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -352,7 +388,7 @@ __global__ void __launch_bounds__(kTreeF32Threads, D == 64 && ROWS == 8 ? 4 : 2)
     };
     stage(0);
     stage(1);
-    if (warp == 0) tree_lines(g, b, line_of, lane);
+    if (warp == 0) tree_lines(tree_parents(g, b, lane), line_of, lane);
     for (int i = tid; i < ROWS * DV; i += kTreeF32Threads) {
         const int row = i / DV, c = (i - row * DV) * 4;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);

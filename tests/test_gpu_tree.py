@@ -231,6 +231,19 @@ def test_scale_and_large_logits(dsa, dtype):
     s.check(*s.run())
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,page", [(0, 16), (40, 16), (0, 0)])
+def test_more_blocks_than_places(dsa, d, window, page):
+    """Blocks that take over others' work: several hundred (request, kv head) pairs of very different lengths, among them
+    requests without nodes, without cached tokens and without either."""
+    rng = np.random.default_rng(d + window + page)
+    lens = [int(x) for x in rng.integers(0, 200, size=130)]
+    counts = [int(x) for x in rng.integers(0, 6, size=130)]
+    lens[3] = lens[7] = counts[7] = 0
+    s = Setup(dsa, d=d, hq=8, hkv=8, n=5, lens=lens, counts=counts, window=window, sinks=3, page=page, prompt=9)
+    s.check(*s.run())
+
+
 def test_requests_share_a_cache(dsa):
     # a batch stride of 0: every request reads the same rows; nodes without room append nothing
     s = Setup(dsa, lens=(48, 48, 48), page=0, shared=True, cap=48, counts=(8, 8, 8))
