@@ -249,6 +249,10 @@ int32_t dsa_tree_step(const dsa_problem* problem, const dsa_diag_params* diag, c
     g.box_tokens = pl.box_tokens;
     for (g.box_shift = 0; (1 << g.box_shift) < pl.box_tokens;) ++g.box_shift;
     g.cluster = pl.cluster;
+    // division of positions (below 2^31) by the page size: with 2^s >= d the product by ceil(2^(31 + s) / d) is exact
+    const unsigned d = problem->block_table ? (unsigned)problem->block_size : 1u;
+    for (g.page_shift = 31; (1ull << (g.page_shift - 31)) < d;) ++g.page_shift;
+    g.page_mul = (unsigned)(((1ull << g.page_shift) + d - 1) / d);
     g.align_tokens = pl.align_tokens;
     if (pl.n_split > 1) {
         g.a.out_part = reinterpret_cast<float*>(workspace);

@@ -12,13 +12,14 @@
 // pipe, and their 32 KB take the SM 1300 cycles to fetch.
 //
 // A block handles 128 query rows (128 / G nodes) of one (request, kv head) and a range of its 64-token
-// tiles.  Warp 4 copies K and V tiles into a ring of shared-memory slots with tensor-map copies (boxes of
-// 64 elements x as many tokens as a page holds in one piece, 128-byte swizzle), warp 5 issues the products,
+// tiles.  Warps 4 and 6 copy K and V tiles into a ring of shared-memory slots each with tensor-map copies (boxes of
+// 64 elements x as many tokens as a page holds in one piece, 128-byte swizzle; issuing a tile's copies from
+// 16-token pages takes a warp some 700 cycles, and one warp for both fell behind), warp 5 issues the products,
 // warps 0-3 own the 128 rows, one thread per row (32 TMEM lanes per warp): they read S = Q K^T from TMEM,
 // keep the running maximum and sum, and write P = e^{x - m} back to TMEM as bf16, where it is the A
 // operand of O += P V.  S is double buffered: S(j + 1) is computed while tile j's softmax runs.  Warps
-// whose 32 rows do not exist sit out.  Warps 6 and 7 append the nodes' rows to the cache meanwhile (by the
-// softmax warps, before their first tile, that took 6 us of a 60 us block).  TMEM: 2 x 64 columns of S (P
+// whose 32 rows do not exist sit out.  Warp 7 appends the nodes' rows to the cache meanwhile (by the softmax
+// warps, before their first tile, that took 6 us of a 60 us block).  TMEM: 2 x 64 columns of S (P
 // takes the place of the S it came from) + D of O, 256 allocated; two blocks share an SM, so one's set-up
 // and last tile hide behind the other's.
 //
@@ -59,6 +60,8 @@ struct TreeArgs {
     int windowed;                                  // 0: dense
     int box_tokens;                                // tokens per tensor-map box of the caches
     int box_shift;                                 // and its logarithm
+    unsigned page_mul;                             // position / block_size = (position * page_mul) >> page_shift
+    int page_shift;
     int align_tokens;                              // where a box may start: box_tokens (pages), 1 (contiguous)
     int cluster;                                   // blocks that share the tiles and merge on chip (1: none; else n_split is 1)
     int blk_coord, head_coord;                     // 0: the map's outer / head dimension has one entry (stride 0)
@@ -75,7 +78,8 @@ struct TreeCfg {
     static constexpr int Q_BYTES = HALVES * Q_HALF;
     static constexpr int KV_HALF = kTreeTile * 128;
     static constexpr int SLOT_BYTES = HALVES * KV_HALF;                    // one K or one V tile
-    static constexpr int SLOTS = D == 128 ? 5 : 10;                        // two blocks per SM with either
+    static constexpr int K_SLOTS = D == 128 ? 2 : 5, V_SLOTS = D == 128 ? 3 : 5;   // two blocks per SM with either
+    static constexpr int SLOTS = K_SLOTS + V_SLOTS;
     static constexpr int TAIL = 1024;                                      // barriers and node tables
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT_BYTES + TAIL;
     static constexpr int PART_LD = D + 4;                                  // row of a partial result, in floats
@@ -305,8 +309,11 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     unsigned char* s_q = smem;
     unsigned char* s_ring = smem + C::Q_BYTES;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + C::Q_BYTES + C::SLOTS * C::SLOT_BYTES);
-    unsigned long long* full = bars;                          // a ring slot has landed
-    unsigned long long* empty = bars + C::SLOTS;              // the products that read it are done
+    unsigned char* s_vring = s_ring + C::K_SLOTS * C::SLOT_BYTES;
+    unsigned long long* k_full = bars;                        // a ring slot has landed
+    unsigned long long* v_full = bars + C::K_SLOTS;
+    unsigned long long* k_empty = bars + C::SLOTS;            // the products that read it are done
+    unsigned long long* v_empty = k_empty + C::K_SLOTS;
     unsigned long long* s_full = bars + 2 * C::SLOTS;         // [2] scores are in TMEM
     unsigned long long* p_ready = s_full + 2;                 // [2] weights are in TMEM
     unsigned long long* pv_done = s_full + 4;                 // [2] O holds the tile
@@ -335,7 +342,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
 
     // set-up that reads nothing: it may run while the launch in front finishes
     if (warp == 4 && lane == 0) {
-        for (int s = 0; s < C::SLOTS; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 1); }
+        for (int s = 0; s < 2 * C::SLOTS; ++s) mbar_init(bars + s, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
             mbar_init(info_full + s, 1); mbar_init(info_empty + s, 7);
@@ -370,67 +377,74 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
         if (lane == 0) mbar_arrive(info_empty + (i & 1));
     };
 
+    // ---- copies of K and V tiles -------------------------------------------------------------------------
+    // A tile is 64 >> box_shift boxes of HALVES pieces; piece p = box * HALVES + half is copied by lane p % 32.
+    // Where this lane's pieces of a tile come from: (page or request, token in it), looked up tiles ahead of the copies.
+    constexpr int PIECES = kTreeTile * C::HALVES / 32;        // per lane, with boxes of one token
+    struct Where { int blk[PIECES], tok[PIECES]; };
+    const int n_pieces = (kTreeTile >> g.box_shift) * C::HALVES;
+    auto where = [&](int t, Where& r) {
+        int start = 0, from, to;
+        if (t < w.cached) w.span.tile(w.t0 + t, start, from, to);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            if (k > 0 && 32 * k >= n_pieces) break;
+            const int box = (lane + 32 * k) / C::HALVES;
+            const int pos = start + (box << g.box_shift);
+            r.blk[k] = g.blk_coord ? it.b : 0;
+            r.tok[k] = pos;
+            if (g.a.block_table) {
+                const int bi = (int)(((unsigned long long)(unsigned)pos * g.page_mul) >> g.page_shift);
+                r.tok[k] = pos - bi * g.a.block_size;
+                // (as the table has it: put into range when the copy is made, so that nobody waits for it here)
+                if (t < w.cached && (box << g.box_shift) < kTreeTile)
+                    r.blk[k] = g.a.block_table[(int64_t)it.b * g.a.max_blocks + min(bi, g.a.max_blocks - 1)];
+            }
+        }
+    };
+    auto copy_tile = [&](int t, const Where& r, const CUtensorMap* cached_map, const CUtensorMap* new_map, unsigned char* dst,
+                         unsigned long long* bar) {
+        if (t < w.cached) {
+            int start, from, to;
+            w.span.tile(w.t0 + t, start, from, to);
+            const int j0 = (from - start) >> g.box_shift, j1 = (to - start + (1 << g.box_shift) - 1) >> g.box_shift;
+            if (lane == 0) mbar_expect_tx(bar, (unsigned)(((j1 - j0) * C::HALVES) << g.box_shift) * 128u);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                if (k > 0 && 32 * k >= n_pieces) break;
+                const int box = (lane + 32 * k) / C::HALVES, h = lane % C::HALVES;
+                if (box < j0 || box >= j1) continue;
+                const int blk = g.a.block_table ? max(0, min(r.blk[k], g.a.num_blocks - 1)) * g.blk_coord : r.blk[k];
+                tma_box4(dst + h * C::KV_HALF + ((box << g.box_shift) * 128), cached_map, 64 * h, r.tok[k], it.kvh * g.head_coord, blk, bar);
+            }
+        } else {
+            if (lane == 0) mbar_expect_tx(bar, (unsigned)(C::HALVES * g.N * 128));
+            __syncwarp();
+            if (lane < C::HALVES) tma_box4(dst + lane * C::KV_HALF, new_map, 64 * lane, 0, it.kvh, it.b, bar);
+        }
+        __syncwarp();
+    };
+    // a ring of `slots` slots: the next one, free again
+    struct Ring { int slot, round, issued; };
+    auto next_free = [&](Ring& ring, unsigned long long* empty) -> bool {
+        return ring.round == 0 || tree_wait(empty + ring.slot, (ring.round - 1) & 1, abort, g.a.wait_timeouts, lane);
+    };
+    auto advance = [&](Ring& ring, int slots) {
+        ++ring.issued;
+        if (++ring.slot == slots) { ring.slot = 0; ++ring.round; }
+    };
+    // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
+    auto drain = [&](const Ring& ring, unsigned long long* full, int slots) {
+        volatile int no_abort = 0;
+        for (int c = max(0, ring.issued - slots); c < ring.issued; ++c)
+            if (!tree_wait(full + c % slots, (c / slots) & 1, &no_abort, nullptr, lane)) break;
+    };
+
     float m_ref = -INFINITY, l = 0.f;                         // softmax threads: maximum (of the raw scores) and sum of their row
     if (warp == 4) {
-        // ---- copies -------------------------------------------------------------------------------
-        const int shift = g.box_shift;
-        // where this lane's boxes `lane` and `lane + 32` of a tile come from: (page or request, token in it);
-        // looked up two tiles ahead of their copies
-        struct Where { int blk[2], tok[2]; };
-        auto where = [&](int t) -> Where {
-            Where r;
-            int start = 0, from, to;
-            if (t < w.cached) w.span.tile(w.t0 + t, start, from, to);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int pos = start + ((lane + 32 * h) << shift);
-                r.blk[h] = g.blk_coord ? it.b : 0;
-                r.tok[h] = pos;
-                if (g.a.block_table) {
-                    const int bi = pos / g.a.block_size;
-                    r.tok[h] = pos - bi * g.a.block_size;
-                    // (as the table has it: put into range when the copy is made, so that nobody waits for it here)
-                    if (t < w.cached && ((lane + 32 * h) << shift) < kTreeTile)
-                        r.blk[h] = g.a.block_table[(int64_t)it.b * g.a.max_blocks + min(bi, g.a.max_blocks - 1)];
-                }
-            }
-            return r;
-        };
-        int issued = 0, slot = 0, round = 0;
-        auto issue = [&](int t, bool is_v, const Where& r) -> bool {
-            if (round > 0 && !tree_wait(empty + slot, (round - 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
-            unsigned char* dst = s_ring + slot * C::SLOT_BYTES;
-            unsigned long long* bar = full + slot;
-            if (t < w.cached) {
-                int start, from, to;
-                w.span.tile(w.t0 + t, start, from, to);
-                const int j0 = (from - start) >> shift, j1 = (to - start + (1 << shift) - 1) >> shift;
-                if (lane == 0) mbar_expect_tx(bar, (unsigned)(((j1 - j0) * C::HALVES) << shift) * 128u);
-                __syncwarp();
-                const CUtensorMap* map = is_v ? &maps.v : &maps.k;
-#pragma unroll
-                for (int h2 = 0; h2 < 2; ++h2) {
-                    const int j = lane + 32 * h2;
-                    if (j >= j0 && j < j1) {
-                        const int blk = g.a.block_table ? max(0, min(r.blk[h2], g.a.num_blocks - 1)) * g.blk_coord : r.blk[h2];
-#pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h)
-                            tma_box4(dst + h * C::KV_HALF + ((j << shift) * 128), map, 64 * h, r.tok[h2], it.kvh * g.head_coord,
-                                     blk, bar);
-                    }
-                    if (shift >= 1) break;
-                }
-            } else if (lane == 0) {
-                mbar_expect_tx(bar, (unsigned)(C::HALVES * g.N * 128));
-#pragma unroll
-                for (int h = 0; h < C::HALVES; ++h)
-                    tma_box4(dst + h * C::KV_HALF, is_v ? &maps.v_new : &maps.k_new, 64 * h, 0, it.kvh, it.b, bar);
-            }
-            __syncwarp();
-            ++issued;
-            if (++slot == C::SLOTS) { slot = 0; ++round; }
-            return true;
-        };
+        // ---- what to work on; copies of q and K -----------------------------------------------------
+        Ring ring = {0, 0, 0};
         bool ok = true;
         int live = 0;                                         // items with tiles so far
         it.index = (int)blockIdx.x;
@@ -476,7 +490,9 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 asked = true;
             };
             if (w.tiles > 0) {
-                Where w0 = where(0), w1 = where(1), w2 = where(2);
+                Where r0, r1, r2;
+                where(0, r0);
+                where(1, r1);
                 if (live > 0) ok = tree_wait(q_empty, (live - 1) & 1, abort, g.a.wait_timeouts, lane);
                 if (ok && lane == 0) {
                     const int box_nodes = min(per_tile, g.N);
@@ -485,12 +501,15 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 }
                 __syncwarp();
                 if (ok) ++live;
-                ok = ok && issue(0, false, w0) && (w.tiles < 2 || issue(1, false, w1));
                 for (int t = 0; ok && t < w.tiles; ++t) {
-                    if (t + 4 >= w.tiles) ask();
-                    const Where w3 = where(t + 3);
-                    ok = issue(t, true, w0) && (t + 2 >= w.tiles || issue(t + 2, false, w2));
-                    w0 = w1; w1 = w2; w2 = w3;
+                    if (t + 3 >= w.tiles) ask();
+                    where(t + 2, r2);
+                    ok = next_free(ring, k_empty);
+                    if (!ok) break;
+                    copy_tile(t, r0, &maps.k, &maps.k_new, s_ring + ring.slot * C::SLOT_BYTES, k_full + ring.slot);
+                    advance(ring, C::K_SLOTS);
+                    r0 = r1;
+                    r1 = r2;
                 }
             }
             ask();
@@ -501,29 +520,47 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 else { *abort = 1; ok = false; }
             }
         }
-        // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
         volatile int no_abort = 0;
         if (live > 0) tree_wait(q_full, (live - 1) & 1, &no_abort, nullptr, lane);
-        for (int c = max(0, issued - C::SLOTS); c < issued; ++c)
-            if (!tree_wait(full + c % C::SLOTS, (c / C::SLOTS) & 1, &no_abort, nullptr, lane)) break;
-    } else if (warp >= 6) {
+        drain(ring, k_full, C::K_SLOTS);
+    } else if (warp == 6) {
+        // ---- copies of V ----------------------------------------------------------------------------
+        Ring ring = {0, 0, 0};
+        bool ok = true;
+        for (int i = 0; ok && next_item(i); ++i) {
+            item_read(i);
+            if (w.tiles == 0) continue;
+            Where r0, r1, r2;
+            where(0, r0);
+            where(1, r1);
+            for (int t = 0; t < w.tiles; ++t) {
+                where(t + 2, r2);
+                ok = next_free(ring, v_empty);
+                if (!ok) break;
+                copy_tile(t, r0, &maps.v, &maps.v_new, s_vring + ring.slot * C::SLOT_BYTES, v_full + ring.slot);
+                advance(ring, C::V_SLOTS);
+                r0 = r1;
+                r1 = r2;
+            }
+        }
+        drain(ring, v_full, C::V_SLOTS);
+    } else if (warp == 7) {
         // ---- the nodes' rows to the cache: every block those of its own nodes, the pieces in turn ----------------
         for (int i = 0; next_item(i); ++i) {
             item_read(i);
             const int first = it.rt * per_tile;
-            tree_append<T, D>(g, it.b, it.kvh, it.S, it.L_p, first + it.piece, pieces, min(it.n, first + per_tile), tid - 192, 64);
+            tree_append<T, D>(g, it.b, it.kvh, it.S, it.L_p, first + it.piece, pieces, min(it.n, first + per_tile), lane, 32);
         }
     } else if (warp == 5) {
         // ---- products ---------------------------------------------------------------------------
         constexpr unsigned kIdescS = instr_desc(kTreeRows, kTreeTile, false), kIdescO = instr_desc(kTreeRows, D, true);
         const unsigned q_desc = desc_low(smem_u32(s_q), 16), k_desc = desc_low(smem_u32(s_ring), 16);
-        const unsigned v_desc = desc_low(smem_u32(s_ring), C::KV_HALF);
-        int slot = 0, round = 0;                              // of the ring
+        const unsigned v_desc = desc_low(smem_u32(s_vring), C::KV_HALF);
+        int k_slot = 0, k_round = 0, v_slot = 0, v_round = 0;  // of the rings
         int done = 0;                                         // tiles of the items before this one
-        auto next_slot = [&]() { if (++slot == C::SLOTS) { slot = 0; ++round; } };
         auto scores = [&](int t) -> bool {
-            const int s = slot, buf = (done + t) & 1;
-            if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
+            const int s = k_slot, buf = (done + t) & 1;
+            if (!tree_wait(k_full + s, k_round & 1, abort, g.a.wait_timeouts, lane)) return false;
             tc_fence_after();
             if (elect_one()) {
                 const unsigned qa = q_desc, ka = k_desc + s * (C::SLOT_BYTES / 16), d = tmem + C::COL_S + buf * kTreeTile;
@@ -531,20 +568,20 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 for (int kk = 0; kk < D / 16; ++kk)
                     tc_mma_ss(d, qa + ((kk / 4) * C::Q_HALF + (kk % 4) * 32) / 16, ka + ((kk / 4) * C::KV_HALF + (kk % 4) * 32) / 16,
                               kIdescS, kk > 0);
-                tc_commit(empty + s);
+                tc_commit(k_empty + s);
                 tc_commit(s_full + buf);
                 if (t == w.tiles - 1) tc_commit(q_empty);
             }
             __syncwarp();
-            next_slot();
+            if (++k_slot == C::K_SLOTS) { k_slot = 0; ++k_round; }
             return true;
         };
         auto values = [&](int t) -> bool {
             const int gt = done + t, buf = gt & 1;
             if (!tree_wait(p_ready + buf, (gt >> 1) & 1, abort, g.a.wait_timeouts, lane)) return false;
-            const int s = slot;
-            if (!tree_wait(full + s, round & 1, abort, g.a.wait_timeouts, lane)) return false;
-            unsigned char* v = s_ring + s * C::SLOT_BYTES;
+            const int s = v_slot;
+            if (!tree_wait(v_full + s, v_round & 1, abort, g.a.wait_timeouts, lane)) return false;
+            unsigned char* v = s_vring + s * C::SLOT_BYTES;
             // rows of V that nobody sees: zero, whatever the cache or the slot held there
             int lo = 0, hi = it.n;
             if (t < w.cached) {
@@ -569,11 +606,11 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
 #pragma unroll
                 for (int kk = 0; kk < kTreeTile / 16; ++kk)
                     tc_mma_ts(tmem + C::COL_O, pa + kk * 8, va + kk * (2048 / 16), kIdescO, t > 0 || kk > 0);
-                tc_commit(empty + s);
+                tc_commit(v_empty + s);
                 tc_commit(pv_done + buf);
             }
             __syncwarp();
-            next_slot();
+            if (++v_slot == C::V_SLOTS) { v_slot = 0; ++v_round; }
             return true;
         };
         int live = 0;
