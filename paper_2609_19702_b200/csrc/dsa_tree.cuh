@@ -188,20 +188,33 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& g, int S, int L_p)
     return s;
 }
 
-// K / V rows of the nodes first, first + step, ... below n, kv head kvh, to the cache, by `count` threads.
+// K / V rows of the nodes first, first + step, ... below n, kv head kvh, to the cache, by one warp: every lane looks up
+// one node's place, then the rows are copied eight 512-byte steps at a time.
 template <typename T, int D>
-__device__ __forceinline__ void tree_append(const TreeArgs& g, int b, int kvh, int S, int L_p, int first, int step, int n, int tid,
-                                            int count) {
-    constexpr int VEC = 16 / (int)sizeof(T), CPR = D / VEC;
-    T* kc = reinterpret_cast<T*>(const_cast<void*>(g.a.k));
-    T* vc = reinterpret_cast<T*>(const_cast<void*>(g.a.v));
-#pragma unroll 4
-    for (int i = tid; i < (n - first + step - 1) / step * CPR; i += count) {
-        const int node = first + i / CPR * step, c = i % CPR * VEC;
-        const int64_t src = (((int64_t)b * g.N + node) * g.a.H_kv + kvh) * D + c;
-        const int64_t dst = token_offset(g.a, b, L_p, S + node) + (int64_t)kvh * g.a.stride_head + c;
-        *reinterpret_cast<uint4*>(kc + dst) = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(g.a.k_new) + src);
-        *reinterpret_cast<uint4*>(vc + dst) = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(g.a.v_new) + src);
+__device__ __forceinline__ void tree_append(const TreeArgs& g, int b, int kvh, int S, int L_p, int first, int step, int n, int lane) {
+    constexpr int VEC = 16 / (int)sizeof(T), CPR = D / VEC, PAIR = 2 * CPR;        // 16-byte pieces of a K and a V row
+    for (int base = first; base < n; base += 32 * step) {
+        const int64_t node0 = (int64_t)b * g.N + base;
+        const int count = min(32, (n - base + step - 1) / step);
+        const int64_t place = lane < count ? token_offset(g.a, b, L_p, S + base + lane * step) + (int64_t)kvh * g.a.stride_head : 0;
+        for (int i0 = 0; i0 < count * PAIR; i0 += 8 * 32) {
+            uint4 x[8];
+            int64_t dst[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 32 * j + lane, r = i / PAIR, c = i % CPR * VEC;
+                dst[j] = __shfl_sync(0xffffffffu, place, min(r, 31)) + c;
+                if (r < count)
+                    x[j] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(i % PAIR < CPR ? g.a.k_new : g.a.v_new) +
+                                                           ((node0 + r * step) * g.a.H_kv + kvh) * D + c);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 32 * j + lane;
+                if (i / PAIR < count)
+                    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(const_cast<void*>(i % PAIR < CPR ? g.a.k : g.a.v)) + dst[j]) = x[j];
+            }
+        }
     }
 }
 
@@ -549,7 +562,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
         for (int i = 0; next_item(i); ++i) {
             item_read(i);
             const int first = it.rt * per_tile;
-            tree_append<T, D>(g, it.b, it.kvh, it.S, it.L_p, first + it.piece, pieces, min(it.n, first + per_tile), lane, 32);
+            tree_append<T, D>(g, it.b, it.kvh, it.S, it.L_p, first + it.piece, pieces, min(it.n, first + per_tile), lane);
         }
     } else if (warp == 5) {
         // ---- products ---------------------------------------------------------------------------

@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
     const int t0 = min(span.T, split * per_split), t1 = min(span.T, t0 + per_split);
     const int cached = t1 - t0, tiles = rows == 0 ? 0 : cached + (split == 0 ? 1 : 0);
     if (tiles == 0) {
-        if (rows > 0) tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
+        if (rows > 0) tree_append<float, D>(g, b, kvh, S, L_p, first_node + split + warp * g.a.n_split, 8 * g.a.n_split, min(n, first_node + per_tile), lane);
         tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
         return;
     }
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
         if (t + 1 < tiles) stage(t + 1, true); else cp_async_commit();
     }
     cp_async_wait<0>();
-    tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
+    tree_append<float, D>(g, b, kvh, S, L_p, first_node + split + warp * g.a.n_split, 8 * g.a.n_split, min(n, first_node + per_tile), lane);
     // the rows' sums: over the lanes of a group, then over the groups
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kTreeF32Threads, D == 64 && ROWS == 8 ? 4 : 2)
     const int cached = t1 - t0;
     const int tiles = rows == 0 ? 0 : cached + (split == 0 ? (n + kTreeFewTile - 1) / kTreeFewTile : 0);
     if (tiles == 0) {
-        if (rows > 0) tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
+        if (rows > 0) tree_append<float, D>(g, b, kvh, S, L_p, first_node + split + warp * g.a.n_split, 8 * g.a.n_split, min(n, first_node + per_tile), lane);
         tree_write_empty<float, D>(g, b, kvh, split, first_node, 0, rows_all, tid, kTreeF32Threads);
         return;
     }
@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(kTreeF32Threads, D == 64 && ROWS == 8 ? 4 : 2)
     if (lane < 8)
 #pragma unroll
         for (int r = 0; r < RPL; ++r) s_max[warp * ROWS + part * RPL + r] = l[r];
-    tree_append<float, D>(g, b, kvh, S, L_p, first_node + split, g.a.n_split, min(n, first_node + per_tile), tid, kTreeF32Threads);
+    tree_append<float, D>(g, b, kvh, S, L_p, first_node + split + warp * g.a.n_split, 8 * g.a.n_split, min(n, first_node + per_tile), lane);
     __syncthreads();
     for (int i = tid; i < rows_all * DV; i += kTreeF32Threads) {
         const int row = i / DV, c = (i - row * DV) * 4;
