@@ -657,9 +657,9 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
             l = 0.f;
             const bool work = w.tiles > 0 && warp * 32 < w.rows;     // a warp without rows only keeps step
             const int node = w.first_node + (row >> g.g_shift);
-            const bool alive = row < w.rows;
-            unsigned long long own = 0ull;                    // drafted tokens that the row's node sees
-            int64_t win_lo = 0;                               // and where the window begins (dense: everything is in [0, P0))
+            const bool alive = row < w.rows;                  // (a row that does not exist computes along, unmasked, and decides nothing)
+            unsigned long long own = alive ? 0ull : ~0ull;    // drafted tokens that the row's node sees
+            int64_t win_lo = INT64_MIN;                       // and where the window begins (dense: everything is in [0, P0))
             if (work && alive) {
                 const signed char* up = s_info[i & 1].up;
                 int depth = 0;                                // (ancestors of a node that exists exist)
@@ -698,7 +698,6 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                     w.span.tile(w.t0 + t, start, from, to);
                     int c0 = 0, c1 = to - start;
                     if (w.t0 + t >= w.span.T1) c0 = (int)max((int64_t)from, min((int64_t)to, win_lo)) - start;
-                    if (!alive) c1 = 0;
                     see = c1 >= 64 ? ~0ull : (1ull << c1) - 1ull;
                     see = c0 >= 64 ? 0ull : (c0 > 0 ? (see >> c0) << c0 : see);
                 } else {
@@ -721,7 +720,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 }
                 const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 // (-inf - -inf is NaN: compares false, nothing to rescale)
-                if (__any_sync(0xffffffffu, (m_tile - m_ref) * sl > 8.f)) {
+                if (__any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f)) {
                     const float m_new = fmaxf(m_ref, m_tile);
                     const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m_ref - m_new) * sl);
                     m_ref = m_new;
@@ -767,7 +766,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
             // ---- results ------------------------------------------------------------------------
             if (work) {
                 const bool mine = ok && row < w.rows_all;
-                const bool none = l == 0.f;                    // nothing seen: zeros and -inf
+                const bool none = !alive || l == 0.f;          // nothing seen: zeros and -inf
                 const float inv = none ? 0.f : 1.f / l;
                 const int64_t orow = ((int64_t)it.b * g.N + node) * g.a.H_q + it.kvh * G + (row & (G - 1));
                 const float lse = none ? -INFINITY : (m_ref * sl + log2f(l)) * LN2;
@@ -815,7 +814,8 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
         it = s_info[0].item;
         w = s_info[0].work;
         if (warp < 4) {
-            s_ml[tid] = make_float2(l == 0.f ? -INFINITY : m_ref * g.a.scale_log2, l);
+            const bool none = tid >= w.rows || l == 0.f;
+            s_ml[tid] = none ? make_float2(-INFINITY, 0.f) : make_float2(m_ref * g.a.scale_log2, l);
             if (w.tiles > 0 && warp * 32 < w.rows) {
                 tc_fence_after();
 #pragma unroll 1
