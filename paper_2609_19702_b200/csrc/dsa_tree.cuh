@@ -78,7 +78,7 @@ struct TreeCfg {
     static constexpr int Q_BYTES = HALVES * Q_HALF;
     static constexpr int KV_HALF = kTreeTile * 128;
     static constexpr int SLOT_BYTES = HALVES * KV_HALF;                    // one K or one V tile
-    static constexpr int K_SLOTS = D == 128 ? 2 : 5, V_SLOTS = D == 128 ? 3 : 5;   // two blocks per SM with either
+    static constexpr int K_SLOTS = D == 128 ? 3 : 5, V_SLOTS = D == 128 ? 2 : 5;   // two blocks per SM with either
     static constexpr int SLOTS = K_SLOTS + V_SLOTS;
     static constexpr int TAIL = 1024;                                      // barriers and node tables
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT_BYTES + TAIL;
