@@ -15,7 +15,7 @@ using namespace dsa;
 
 constexpr int kCopyThreads = 128;
 constexpr int kCopyBatch = 8;                      // rows a thread has in flight
-constexpr int kListRows = 256;                     // rows whose offsets a block works out at a time
+constexpr int kListRows = 64;                      // rows whose places a block works out at a time
 constexpr int kPoolThreads = 1024;
 
 struct CacheArgs {
@@ -33,40 +33,59 @@ __device__ __forceinline__ int64_t piece_offset(const CacheArgs& c, int col) {
 }
 
 // ---- rows of a request move up ----------------------------------------------------------------------
-// One block: 128 of the 16-byte columns of one request's rows, in one layer's K or V.  A thread takes its
-// column through all rows in order, so what it overwrites it has read itself; since keep[i] >= i and the list
-// ascends, a batch of loads never needs what the batch before it has yet to store, and runs ahead of it.
-// The rows' offsets (page lookups) are worked out once per block and shared.
-__global__ void __launch_bounds__(kCopyThreads) dsa_compact_kernel(const CacheArgs c, const int* base, const int* keep,
-                                                                   const int* keep_count, int max_keep, int col_blocks,
-                                                                   int layers) {
+// One block: 128 of the 16-byte columns of one request's rows, in `planes` of the layers' K and V caches, and one
+// stretch of kListRows rows of the list; the rows' places (page lookups) are worked out once and shared by the planes.
+//
+// Kept positions ascend, so what stays in place is a prefix of the list, and where the first row that moves comes from
+// beyond all places that are written, no row is read from a place that another one is written to: the rows may move in
+// any order, and blocks take a stretch each.  Else (a list that overlaps its own destination) one block takes all
+// stretches in order: a thread takes its column through all rows, so what it overwrites it has read itself, and since
+// keep[i] >= i a batch of loads never needs what the batch before it has yet to store.
+__global__ void __launch_bounds__(kCopyThreads, 8) dsa_compact_kernel(const CacheArgs c, const int* base, const int* keep,
+                                                                      const int* keep_count, int max_keep, int col_blocks,
+                                                                      int planes, int plane_groups, int stretches, int layers,
+                                                                      int* len_out) {
     __shared__ int64_t s_src[kListRows], s_dst[kListRows];
-    __shared__ int s_n;
+    __shared__ int s_n, s_first;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31;
     int idx = blockIdx.x;
     const int col = (idx % col_blocks) * kCopyThreads + tid; idx /= col_blocks;
-    const bool is_v = idx & 1; idx >>= 1;
-    const int layer = idx % layers;
-    const int b = idx / layers;
+    const int group = idx % plane_groups; idx /= plane_groups;
+    const int stretch = idx % stretches;
+    const int b = idx / stretches;
+    const int* list = keep + (int64_t)b * max_keep;
     const int count = max(0, min(keep_count[b], max_keep));
     const int64_t first = base ? base[b] : 0;
+    if (len_out && idx == b * stretches && blockIdx.x % (col_blocks * plane_groups) == 0 && tid == 0) len_out[b] = (int)first + count;
+    if (stretch * kListRows >= count) return;
+    // the prefix that stays (keep[i] - i never falls)
+    if (tid == 0) s_first = count;
+    __syncthreads();
+    for (int i = tid; i < count; i += kCopyThreads)
+        if (list[i] != i) { atomicMin(&s_first, i); break; }
+    __syncthreads();
+    const int stays = s_first;
+    if (stays >= count) return;
+    const bool any_order = list[stays] >= count;
+    if (!any_order && stretch > 0) return;
     const bool mine = col < c.row_vecs;
-    unsigned char* cache = reinterpret_cast<unsigned char*>(const_cast<void*>(is_v ? c.a.v : c.a.k)) +
-                           (int64_t)layer * c.stride_layer * c.esize + (mine ? piece_offset(c, col) : 0);
-    for (int i0 = 0; i0 < count; i0 += kListRows) {
+    const int64_t column = mine ? piece_offset(c, col) : 0;
+    const int p0 = group * planes, p1 = min(2 * layers, p0 + planes);
+    const int from = any_order ? stretch * kListRows : 0, to = any_order ? min(count, from + kListRows) : count;
+    for (int i0 = max(from, stays / kListRows * kListRows); i0 < to; i0 += kListRows) {
         __syncthreads();
         if (tid < 32) {                            // the rows of this stretch that move, in order
             int n = 0;
-            for (int i = i0 + lane; i - lane < min(count, i0 + kListRows); i += 32) {
+            for (int i = i0 + lane; i - lane < min(to, i0 + kListRows); i += 32) {
                 bool moves = false;
                 int64_t src = 0, dst = 0;
-                if (i < count) {
-                    const int64_t from = first + keep[(int64_t)b * max_keep + i], to = first + i;
-                    moves = from != to && from >= 0 && from < c.a.max_seq_len && to >= 0 && to < c.a.max_seq_len;
+                if (i < to) {
+                    const int64_t at = first + list[i], goal = first + i;
+                    moves = at != goal && at >= 0 && at < c.a.max_seq_len && goal >= 0 && goal < c.a.max_seq_len;
                     if (moves) {
-                        src = token_offset(c.a, b, 0, (int)from) * c.esize;
-                        dst = token_offset(c.a, b, 0, (int)to) * c.esize;
+                        src = token_offset(c.a, b, 0, (int)at) * c.esize;
+                        dst = token_offset(c.a, b, 0, (int)goal) * c.esize;
                     }
                 }
                 const unsigned ballot = __ballot_sync(0xffffffffu, moves);
@@ -81,24 +100,30 @@ __global__ void __launch_bounds__(kCopyThreads) dsa_compact_kernel(const CacheAr
         }
         __syncthreads();
         const int n = s_n;
-        if (!mine) continue;
-        uint4 x[kCopyBatch], y[kCopyBatch];
-        auto load = [&](int i, uint4 (&r)[kCopyBatch]) {
+        if (!mine || n == 0) continue;
+        auto plane = [&](int p) -> unsigned char* {
+            return reinterpret_cast<unsigned char*>(const_cast<void*>((p & 1) ? c.a.v : c.a.k)) +
+                   (int64_t)(p >> 1) * c.stride_layer * c.esize + column;
+        };
+        // (plane, row) pairs, a plane's rows one behind the other
+        const int total = n * (p1 - p0);
+        int p_load = p0, i_load = 0, p_store = p0, i_store = 0;
+        unsigned char *at_load = plane(p0), *at_store = plane(p0);
+        for (int done = 0; done < total; done += kCopyBatch) {
+            uint4 x[kCopyBatch];
+            const int m = min(kCopyBatch, total - done);
 #pragma unroll
             for (int k = 0; k < kCopyBatch; ++k)
-                if (i + k < n) r[k] = *reinterpret_cast<const uint4*>(cache + s_src[i + k]);
-        };
-        auto store = [&](int i, const uint4 (&r)[kCopyBatch]) {
+                if (k < m) {
+                    x[k] = *reinterpret_cast<const uint4*>(at_load + s_src[i_load]);
+                    if (++i_load == n) { i_load = 0; if (++p_load < p1) at_load = plane(p_load); }
+                }
 #pragma unroll
             for (int k = 0; k < kCopyBatch; ++k)
-                if (i + k < n) *reinterpret_cast<uint4*>(cache + s_dst[i + k]) = r[k];
-        };
-        load(0, x);
-        for (int i = 0; i < n; i += 2 * kCopyBatch) {
-            load(i + kCopyBatch, y);
-            store(i, x);
-            load(i + 2 * kCopyBatch, x);
-            store(i + kCopyBatch, y);
+                if (k < m) {
+                    *reinterpret_cast<uint4*>(at_store + s_dst[i_store]) = x[k];
+                    if (++i_store == n) { i_store = 0; if (++p_store < p1) at_store = plane(p_store); }
+                }
         }
     }
 }
@@ -128,22 +153,38 @@ struct ForkArgs {
     ForkItem* items;
 };
 
-// Ranks of 0 / 1 flags over a block of kPoolThreads threads: exclusive prefix, and the total.
-__device__ __forceinline__ int block_rank(bool flag, int* s_warp, int& total) {
+// Exclusive prefix sums over a block of kPoolThreads threads, and the total.
+__device__ __forceinline__ int block_prefix(int mine, int* s_warp, int& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const unsigned ballot = __ballot_sync(0xffffffffu, flag);
-    __syncthreads();                               // s_warp free again
-    if (lane == 0) s_warp[warp] = __popc(ballot);
-    __syncthreads();
-    const int mine = s_warp[lane];                 // (32 warps)
     int upto = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
         const int o = __shfl_up_sync(0xffffffffu, upto, off);
         if (lane >= off) upto += o;
     }
-    total = __shfl_sync(0xffffffffu, upto, 31);
-    return __shfl_sync(0xffffffffu, upto - mine, warp) + __popc(ballot & ((1u << lane) - 1u));
+    __syncthreads();                               // s_warp free again
+    if (lane == 31) s_warp[warp] = upto;
+    __syncthreads();
+    const int of_warp = s_warp[lane];              // (32 warps)
+    int warps = of_warp;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, warps, off);
+        if (lane >= off) warps += o;
+    }
+    total = __shfl_sync(0xffffffffu, warps, 31);
+    return __shfl_sync(0xffffffffu, warps - of_warp, warp) + upto - mine;
+}
+
+// The counts of eight neighbouring pages from p on (a multiple of eight); beyond the pool: not free.
+__device__ __forceinline__ void eight_counts(const int* ref_count, int p, int num_blocks, int (&r)[8]) {
+    if (num_blocks - p >= 8 && (reinterpret_cast<uintptr_t>(ref_count) & 15) == 0) {
+        const int4 a = *reinterpret_cast<const int4*>(ref_count + p), b = *reinterpret_cast<const int4*>(ref_count + p + 4);
+        r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w; r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r[k] = p + k < num_blocks ? ref_count[p + k] : 1;
+    }
 }
 
 // Free pages in ascending order: take(rank, page) for the first `want` of them; returns how many there were
@@ -151,12 +192,23 @@ __device__ __forceinline__ int block_rank(bool flag, int* s_warp, int& total) {
 template <class F>
 __device__ __forceinline__ int free_pages(const int* ref_count, int num_blocks, int want, int* s_warp, F&& take) {
     int found = 0;
-    for (int p0 = 0; p0 < num_blocks && found < want; p0 += kPoolThreads) {
-        const int page = p0 + (int)threadIdx.x;
-        const bool free_page = page < num_blocks && ref_count[page] == 0;
+    for (int64_t p0 = 0; p0 < num_blocks && found < want; p0 += 8 * kPoolThreads) {
+        const int64_t p = p0 + 8 * (int64_t)threadIdx.x;
+        int r[8], mine = 0;
+        if (p < num_blocks) {
+            eight_counts(ref_count, (int)p, num_blocks, r);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) mine += r[k] == 0;
+        }
         int total;
-        const int rank = found + block_rank(free_page, s_warp, total);
-        if (free_page && rank < want) take(rank, page);
+        int rank = found + block_prefix(mine, s_warp, total);
+        if (p < num_blocks)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (r[k] == 0) {
+                    if (rank < want) take(rank, (int)p + k);
+                    ++rank;
+                }
         found += total;
     }
     return min(found, want);
@@ -165,6 +217,7 @@ __device__ __forceinline__ int free_pages(const int* ref_count, int num_blocks, 
 // Which branches can be made and which fresh page each gets: one block.
 __global__ void __launch_bounds__(kPoolThreads) dsa_fork_plan_kernel(const ForkArgs f) {
     __shared__ int s_warp[32];
+    __shared__ int s_src[kPoolThreads], s_dst[kPoolThreads];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x;
     // fresh pages wanted, in order; an item's rank among them is kept in to_page until the pages are known
@@ -172,19 +225,24 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_fork_plan_kernel(const ForkA
     for (int i0 = 0; i0 < f.n; i0 += kPoolThreads) {
         const int i = i0 + tid;
         ForkItem it = {0, -1, 0, 0};
-        if (i < f.n) {
-            const int s = f.src[i], d = f.dst[i];
-            bool ok = s >= 0 && s < f.batch && d >= 0 && d < f.batch;
-            for (int j = 0; ok && j < f.n; ++j) ok = f.src[j] != d && (j >= i || f.dst[j] != d);
-            if (ok) {
-                const int len = max(0, min(f.seq_len[s], f.max_seq_len));
-                it.tokens = len % f.block_size;
-                it.from_page = it.tokens ? f.table[(int64_t)s * f.max_blocks + len / f.block_size] : 0;
-                it.ok = 1;
-            }
+        const int s = i < f.n ? f.src[i] : -1, d = i < f.n ? f.dst[i] : -1;
+        bool ok = s >= 0 && s < f.batch && d >= 0 && d < f.batch;
+        int len = 0;
+        if (ok) len = max(0, min(f.seq_len[s], f.max_seq_len));
+        for (int j0 = 0; j0 < f.n; j0 += kPoolThreads) {    // (against all branches, a thousand at a time)
+            __syncthreads();
+            if (j0 + tid < f.n) { s_src[tid] = f.src[j0 + tid]; s_dst[tid] = f.dst[j0 + tid]; }
+            __syncthreads();
+            if (ok)
+                for (int j = 0; j < min(kPoolThreads, f.n - j0); ++j) ok = ok && s_src[j] != d && (j0 + j >= i || s_dst[j] != d);
+        }
+        if (ok) {
+            it.tokens = len % f.block_size;
+            it.from_page = it.tokens ? f.table[(int64_t)s * f.max_blocks + len / f.block_size] : 0;
+            it.ok = 1;
         }
         int total;
-        const int rank = want + block_rank(it.ok && it.tokens, s_warp, total);
+        const int rank = want + block_prefix(it.ok && it.tokens, s_warp, total);
         if (it.ok && it.tokens) it.to_page = rank;
         want += total;
         if (i < f.n) f.items[i] = it;
@@ -349,12 +407,7 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_reserve_kernel(int* table, i
     __syncthreads();
     const int total = s_total;
     // how many free pages there are (no further than what is wanted), then how many rows that serves
-    int found = 0;
-    for (int p0 = 0; p0 < num_blocks && found < total; p0 += kPoolThreads) {
-        const int page = p0 + tid;
-        found += __syncthreads_count(page < num_blocks && ref_count[page] == 0);
-    }
-    found = min(found, total);
+    const int found = free_pages(ref_count, num_blocks, total, s_warp, [](int, int) {});
     for (int b = tid; b < batch; b += kPoolThreads) {
         const int upto = b + 1 < batch ? s_lacks[b + 1] : total;
         if (upto <= found) {
@@ -366,12 +419,16 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_reserve_kernel(int* table, i
     }
     __syncthreads();
     const int granted = s_granted;
-    free_pages(ref_count, num_blocks, granted, s_warp, [&](int rank, int page) {
-        int lo = 0, hi = batch - 1;                // the last row with s_lacks[row] <= rank
+    auto row_of = [&](int rank) {                  // the last row with s_lacks[row] <= rank
+        int lo = 0, hi = batch - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (s_lacks[mid] <= rank) lo = mid; else hi = mid - 1;
         }
+        return lo;
+    };
+    free_pages(ref_count, num_blocks, granted, s_warp, [&](int rank, int page) {
+        const int lo = row_of(rank);
         int k = rank - s_lacks[lo];
         const int next = lo + 1 < batch ? s_lacks[lo + 1] : total;
         int* row = table + (int64_t)lo * max_blocks;
@@ -386,21 +443,27 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_reserve_kernel(int* table, i
         ref_count[page] = -1 - e;                  // (marked; the tables are written when all ranks have counted)
     });
     __syncthreads();
+    // the marked pages are the first `granted` free ones, in order: rank and row again
     int at = 0;
-    for (int p0 = 0; p0 < num_blocks && at < granted; p0 += kPoolThreads) {
-        const int page = p0 + tid;
-        const int mark = page < num_blocks ? ref_count[page] : 0;
-        int n;
-        const int rank = at + block_rank(mark < 0, s_warp, n);
-        if (mark < 0) {
-            int lo = 0, hi = batch - 1;
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (s_lacks[mid] <= rank) lo = mid; else hi = mid - 1;
-            }
-            table[(int64_t)lo * max_blocks + (-1 - mark)] = page;
-            ref_count[page] = 1;
+    for (int64_t p0 = 0; p0 < num_blocks && at < granted; p0 += 8 * kPoolThreads) {
+        const int64_t p = p0 + 8 * (int64_t)tid;
+        int r[8], mine = 0;
+        if (p < num_blocks) {
+            eight_counts(ref_count, (int)p, num_blocks, r);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) mine += r[k] < 0;
         }
+        int n;
+        int rank = at + block_prefix(mine, s_warp, n);
+        if (p < num_blocks)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (r[k] < 0) {
+                    const int e = -1 - r[k];       // (a count that was negative to begin with is no mark)
+                    if (rank < granted && e < max_blocks) table[(int64_t)row_of(rank) * max_blocks + e] = (int)p + k;
+                    ref_count[p + k] = 1;
+                    ++rank;
+                }
         at += n;
     }
 }
@@ -459,14 +522,22 @@ int32_t dsa_compact_kv(const dsa_problem* problem, int32_t num_layers, int64_t s
     if (problem->batch == 0) return DSA_OK;
     if (!keep_count || (max_keep > 0 && !keep)) return DSA_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const bool own_launch = len_out && (max_keep == 0 || base == len_out);
     if (max_keep > 0) {
         const int col_blocks = (c.row_vecs + kCopyThreads - 1) / kCopyThreads;
-        rc = launch(dsa_compact_kernel, (int64_t)problem->batch * num_layers * 2 * col_blocks, kCopyThreads, 0, st, true, c, base,
-                    keep, keep_count, (int)max_keep, col_blocks, (int)num_layers);
+        const int stretches = (max_keep + kListRows - 1) / kListRows;
+        // planes per block: enough of them for some eight loads in flight, as long as there are blocks for every SM
+        int planes = std::max(1, std::min(2 * (int)num_layers, 8 / std::min(max_keep, 8)));
+        while (planes > 1 && (int64_t)problem->batch * col_blocks * stretches * ((2 * num_layers + planes - 1) / planes) < 4 * host_sm_count())
+            planes /= 2;
+        const int groups = (2 * (int)num_layers + planes - 1) / planes;
+        rc = launch(dsa_compact_kernel, (int64_t)problem->batch * stretches * groups * col_blocks, kCopyThreads, 0, st, true, c, base,
+                    keep, keep_count, (int)max_keep, col_blocks, planes, groups, stretches, (int)num_layers,
+                    own_launch ? (int32_t*)nullptr : len_out);
         if (rc != DSA_OK) return rc;
     }
-    // (a launch of its own: base may be len_out, which every block of the other one reads)
-    if (len_out)
+    // (a launch of its own where base is len_out, which every block of the other one reads)
+    if (own_launch)
         rc = launch(dsa_compact_len_kernel, (problem->batch + 255) / 256, 256, 0, st, false, base, keep_count, (int)max_keep,
                     (int)problem->batch, len_out);
     return rc;
