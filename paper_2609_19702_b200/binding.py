@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -59,6 +60,11 @@ class dsa_problem(ctypes.Structure):
                 ("max_prompt_len", ctypes.c_int32), ("split_tokens", ctypes.c_int32),
                 ("ring_size", ctypes.c_int32), ("ring_sinks", ctypes.c_int32),
                 ("plan_flags", ctypes.c_uint32)]
+
+
+# the same layouts for struct.pack, which fills a structure in a third of the time that setting its fields takes
+_PROBLEM = struct.Struct("@5if3P3q3P8iI0q")
+assert _PROBLEM.size == ctypes.sizeof(dsa_problem)
 
 
 class dsa_diag_params(ctypes.Structure):
@@ -162,6 +168,9 @@ def _load() -> ctypes.CDLL:
 
 
 _lib = _load()
+_TREE, _POOL = struct.Struct("@iPP0q"), struct.Struct("@iiP0q")
+_VERIFY = struct.Struct("@iiiPPqPqP0q")
+assert (_TREE.size, _POOL.size, _VERIFY.size) == tuple(ctypes.sizeof(s) for s in (dsa_tree, dsa_page_pool, dsa_verify))
 
 
 class DsaError(RuntimeError):
@@ -219,9 +228,10 @@ class Problem:
 
     def c_struct(self) -> dsa_problem:
         b, hq, d = self.q.shape
-        return self._fill(b, hq, d)
+        return dsa_problem.from_buffer_copy(self._packed(b, hq, d))
 
-    def _fill(self, b: int, hq: int, d: int) -> dsa_problem:
+    def _packed(self, b: int, hq: int, d: int) -> bytes:
+        """The dsa_problem as bytes (which ctypes passes by address)."""
         assert self.q.is_contiguous() and self.q.is_cuda
         assert self.seq_len.dtype == torch.int32 and self.prompt_len.dtype == torch.int32
         bt = self.block_table
@@ -230,12 +240,12 @@ class Problem:
             assert bt.dtype == torch.int32 and bt.is_contiguous()
             max_blocks = bt.shape[1]
         s0, s1, s2 = self.strides
-        return dsa_problem(b, hq, self.num_kv_heads, d, _dtype_code(self.q), float(self.sm_scale), self.q.data_ptr(),
-                           self.k_cache.data_ptr(), self.v_cache.data_ptr(), int(s0), int(s1), int(s2),
-                           self.seq_len.data_ptr(), self.prompt_len.data_ptr(), None if bt is None else bt.data_ptr(), max_blocks,
-                           0 if bt is None else self.block_size, 0 if bt is None else self.num_blocks, int(self.max_seq_len),
-                           int(self.max_prompt_len), int(self.split_tokens), int(self.ring_size), int(self.ring_sinks),
-                           int(self.plan_flags))
+        return _PROBLEM.pack(b, hq, self.num_kv_heads, d, _dtype_code(self.q), self.sm_scale, self.q.data_ptr(),
+                             self.k_cache.data_ptr(), self.v_cache.data_ptr(), int(s0), int(s1), int(s2), self.seq_len.data_ptr(),
+                             self.prompt_len.data_ptr(), 0 if bt is None else bt.data_ptr(), max_blocks,
+                             0 if bt is None else self.block_size, 0 if bt is None else self.num_blocks, int(self.max_seq_len),
+                             int(self.max_prompt_len), int(self.split_tokens), int(self.ring_size), int(self.ring_sinks),
+                             int(self.plan_flags))
 
 
 @dataclass
@@ -511,20 +521,20 @@ def problem_from_host(inp: dict, device: str = "cuda", dtype: torch.dtype = torc
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _call(name: str, index: int, stream: Optional[torch.cuda.Stream], *args) -> None:
-    """The library's function `name` on CUDA device `index` (where all of the call's tensors are)."""
+def _call(fn, index: int, stream: Optional[torch.cuda.Stream], *args) -> None:
+    """A function of the library on CUDA device `index` (where all of the call's tensors are)."""
     if index < 0:
-        raise ValueError("%s: the tensors must be on a CUDA device" % name)
+        raise ValueError("%s: the tensors must be on a CUDA device" % fn.__name__)
     if torch.cuda.current_device() != index:
         with torch.cuda.device(index):
-            return _call(name, index, stream, *args)
+            return _call(fn, index, stream, *args)
     if stream is not None:
         st = stream.cuda_stream
     else:
         st = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
-    status = getattr(_lib, name)(*args, st)
+    status = fn(*args, st)
     if status != 0:
-        raise DsaError(name, status)
+        raise DsaError(fn.__name__, status)
 
 
 def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
@@ -548,26 +558,43 @@ class Tree:
     node_count: Optional[torch.Tensor] = None    # int32 [B]; None: all nodes exist
 
     def c_struct(self, batch: int) -> dsa_tree:
+        return dsa_tree.from_buffer_copy(self._packed(batch))
+
+    def _packed(self, batch: int) -> bytes:
         if self.parent is not None:
             _int32(self.parent, (batch, self.max_nodes), "parent")
         if self.node_count is not None:
             _int32(self.node_count, (batch,), "node_count")
-        return dsa_tree(int(self.max_nodes), _dptr(self.parent), _dptr(self.node_count))
+        return _TREE.pack(self.max_nodes, 0 if self.parent is None else self.parent.data_ptr(),
+                          0 if self.node_count is None else self.node_count.data_ptr())
 
 
-def _tree_problem(problem: Problem, tree: Tree) -> dsa_problem:
+def _rows(problem: Problem, b: int) -> None:
+    bt = problem.block_table
+    if problem.seq_len.shape != (b,) or problem.prompt_len.shape != (b,) or (bt is not None and bt.shape[0] != b):
+        raise ValueError("seq_len, prompt_len and block_table must have one row per request")
+
+
+def _tree_problem(problem: Problem, tree: Tree) -> bytes:
     b, n, hq, d = problem.q.shape
     if n != tree.max_nodes:
         raise ValueError("q must be [batch, max_nodes, heads, head_dim]")
-    return problem._fill(b, hq, d)
+    _rows(problem, b)
+    return problem._packed(b, hq, d)
+
+
+def _cache_problem(problem: Problem) -> bytes:
+    b, hq, d = problem.q.shape
+    _rows(problem, b)
+    return problem._packed(b, hq, d)
 
 
 def dsa_tree_workspace_size(problem: Problem, diag: Optional[Diag], tree: Tree) -> int:
     p = _tree_problem(problem, tree)
     d = diag.c_struct() if diag is not None else None
-    t = tree.c_struct(p.batch)
     n = ctypes.c_size_t(0)
-    _check("dsa_tree_workspace_size", _lib.dsa_tree_workspace_size(_ref(p), _ref(d), _ref(t), ctypes.byref(n)))
+    _check("dsa_tree_workspace_size",
+           _lib.dsa_tree_workspace_size(p, _ref(d), tree._packed(problem.q.shape[0]), ctypes.byref(n)))
     return int(n.value)
 
 
@@ -600,9 +627,9 @@ def dsa_tree_step(problem: Problem, diag: Optional[Diag], tree: Tree, k_new: tor
     dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.seq_len, problem.prompt_len, problem.block_table, k_new,
                        v_new, out, lse, workspace, tree.parent, tree.node_count)
     dg = diag.c_struct() if diag is not None else None
-    tr = tree.c_struct(b)
+    tr = tree._packed(b)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _call("dsa_tree_step", dev, stream, _ref(p), _ref(dg), _ref(tr), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(),
+    _call(_lib.dsa_tree_step, dev, stream, p, _ref(dg), tr, k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(),
           lse.data_ptr(), _dptr(workspace), ws_n)
 
 
@@ -624,6 +651,9 @@ class Verify:
         return row
 
     def c_struct(self) -> dsa_verify:
+        return dsa_verify.from_buffer_copy(self._packed())
+
+    def _packed(self) -> bytes:
         b, n = self.tokens.shape
         _int32(self.tokens, (b, n), "tokens")
         tp, dp, u = self.target_probs, self.draft_probs, self.uniforms
@@ -632,8 +662,9 @@ class Verify:
             raise ValueError("draft_probs must have the shape and type of target_probs")
         if u is not None and (u.dtype != torch.float32 or not u.is_contiguous() or u.shape != (b, n)):
             raise ValueError("uniforms must be a contiguous float32 tensor of shape %s" % ((b, n),))
-        return dsa_verify(b, tp.shape[2], _dtype_code(tp), _dptr(self.tokens), _dptr(tp), stride, _dptr(dp),
-                          0 if dp is None else self._row_stride(dp, "draft_probs"), _dptr(u))
+        return _VERIFY.pack(b, tp.shape[2], _dtype_code(tp), self.tokens.data_ptr(), tp.data_ptr(), stride,
+                            0 if dp is None else dp.data_ptr(), 0 if dp is None else self._row_stride(dp, "draft_probs"),
+                            0 if u is None else u.data_ptr())
 
 
 def alloc_verify_outputs(verify: Verify):
@@ -647,17 +678,17 @@ def alloc_verify_outputs(verify: Verify):
 def dsa_verify_tree(verify: Verify, tree: Tree, path: torch.Tensor, accepted: torch.Tensor, next_token: torch.Tensor,
                     stream: Optional[torch.cuda.Stream] = None) -> None:
     """Which drafted tokens stand, and the token behind them."""
-    v = verify.c_struct()
+    v = verify._packed()
     b, n = verify.tokens.shape
     if n != tree.max_nodes:
         raise ValueError("tokens must be [batch, max_nodes]")
-    tr = tree.c_struct(b)
+    tr = tree._packed(b)
     _int32(path, (b, n), "path")
     _int32(accepted, (b,), "accepted")
     _int32(next_token, (b,), "next_token")
     dev = _same_device(verify.tokens, verify.target_probs, verify.draft_probs, verify.uniforms, tree.parent, tree.node_count, path,
                        accepted, next_token)
-    _call("dsa_verify_tree", dev, stream, _ref(v), _ref(tr), path.data_ptr(), accepted.data_ptr(), next_token.data_ptr())
+    _call(_lib.dsa_verify_tree, dev, stream, v, tr, path.data_ptr(), accepted.data_ptr(), next_token.data_ptr())
 
 
 def dsa_compact_kv(problem: Problem, keep: torch.Tensor, keep_count: torch.Tensor, base: Optional[torch.Tensor] = None,
@@ -665,7 +696,7 @@ def dsa_compact_kv(problem: Problem, keep: torch.Tensor, keep_count: torch.Tenso
                    stream: Optional[torch.cuda.Stream] = None) -> None:
     """Moves the K / V rows at positions base + keep[b, i] to base + i (``keep`` int32 [B, max_keep] ascending,
     ``keep_count`` int32 [B]; base None: 0); len_out[b] = base[b] + keep_count[b]."""
-    p = problem.c_struct()
+    p = _cache_problem(problem)
     b = problem.q.shape[0]
     if keep.dim() != 2:
         raise ValueError("keep must be [batch, max_keep]")
@@ -674,7 +705,7 @@ def dsa_compact_kv(problem: Problem, keep: torch.Tensor, keep_count: torch.Tenso
         if t is not None:
             _int32(t, (b,), what)
     dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.block_table, keep, keep_count, base, len_out)
-    _call("dsa_compact_kv", dev, stream, _ref(p), int(num_layers), int(stride_layer), _dptr(base), keep.data_ptr(),
+    _call(_lib.dsa_compact_kv, dev, stream, p, int(num_layers), int(stride_layer), _dptr(base), keep.data_ptr(),
           keep_count.data_ptr(), keep.shape[1], _dptr(len_out))
 
 
@@ -685,8 +716,12 @@ class PagePool:
     block_size: int
 
     def c_struct(self) -> dsa_page_pool:
-        _int32(self.ref_count, (self.ref_count.numel(),), "ref_count")
-        return dsa_page_pool(self.ref_count.numel(), int(self.block_size), self.ref_count.data_ptr())
+        return dsa_page_pool.from_buffer_copy(self._packed())
+
+    def _packed(self) -> bytes:
+        n = self.ref_count.numel()
+        _int32(self.ref_count, (n,), "ref_count")
+        return _POOL.pack(n, self.block_size, self.ref_count.data_ptr())
 
 
 def _table(block_table: torch.Tensor, rows: Optional[int] = None) -> tuple:
@@ -703,8 +738,8 @@ def dsa_reserve_pages(pool: PagePool, block_table: torch.Tensor, seq_len: torch.
     _int32(seq_len, (b,), "seq_len")
     _int32(status, (b,), "status")
     dev = _same_device(block_table, pool.ref_count, seq_len, status)
-    c = pool.c_struct()
-    _call("dsa_reserve_pages", dev, stream, _ref(c), block_table.data_ptr(), b, m, seq_len.data_ptr(), int(extra_tokens),
+    c = pool._packed()
+    _call(_lib.dsa_reserve_pages, dev, stream, c, block_table.data_ptr(), b, m, seq_len.data_ptr(), int(extra_tokens),
           status.data_ptr())
 
 
@@ -715,8 +750,8 @@ def dsa_release_pages(pool: PagePool, block_table: torch.Tensor, keep_tokens: Op
     if keep_tokens is not None:
         _int32(keep_tokens, (b,), "keep_tokens")
     dev = _same_device(block_table, pool.ref_count, keep_tokens)
-    c = pool.c_struct()
-    _call("dsa_release_pages", dev, stream, _ref(c), block_table.data_ptr(), b, m, _dptr(keep_tokens))
+    c = pool._packed()
+    _call(_lib.dsa_release_pages, dev, stream, c, block_table.data_ptr(), b, m, _dptr(keep_tokens))
 
 
 def alloc_fork_workspace(src: torch.Tensor) -> torch.Tensor:
@@ -735,8 +770,8 @@ def dsa_fork_pages(pool: PagePool, problem: Problem, src: torch.Tensor, dst: tor
         _int32(t, (n,), what)
     dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.block_table, problem.seq_len, problem.prompt_len,
                        pool.ref_count, src, dst, status, workspace)
-    p, c = problem.c_struct(), pool.c_struct()
-    _call("dsa_fork_pages", dev, stream, _ref(c), _ref(p), int(num_layers), int(stride_layer), src.data_ptr(), dst.data_ptr(), n,
+    p, c = _cache_problem(problem), pool._packed()
+    _call(_lib.dsa_fork_pages, dev, stream, c, p, int(num_layers), int(stride_layer), src.data_ptr(), dst.data_ptr(), n,
           status.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
@@ -747,5 +782,5 @@ def dsa_copy_pages(problem: Problem, src: torch.Tensor, dst: torch.Tensor, num_l
     _int32(src, (n,), "src")
     _int32(dst, (n,), "dst")
     dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.block_table, src, dst)
-    p = problem.c_struct()
-    _call("dsa_copy_pages", dev, stream, _ref(p), int(num_layers), int(stride_layer), src.data_ptr(), dst.data_ptr(), n)
+    p = _cache_problem(problem)
+    _call(_lib.dsa_copy_pages, dev, stream, p, int(num_layers), int(stride_layer), src.data_ptr(), dst.data_ptr(), n)

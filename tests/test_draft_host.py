@@ -58,8 +58,10 @@ def test_tree_refusals(dsa):
     assert _size(dsa, _problem(dsa, stride_token=100), None, t)[0] == INVALID
     for bad in (dict(k=None), dict(v=None), dict(out=None), dict(lse=None), dict(k=FAKE + 4), dict(v=FAKE + 8), dict(out=FAKE + 2)):
         assert _step(dsa, p, None, t, **bad) == INVALID
+    assert _size(dsa, p, None, t)[1] == 0                                          # pieces of a request merge on chip
+    p = _problem(dsa, split_tokens=256)
     rc, need = _size(dsa, p, None, t)
-    assert need > 0                                                                # four requests are split
+    assert need > 0
     assert _step(dsa, p, None, t) == INVALID                                       # no workspace
     assert _step(dsa, p, None, t, ws=FAKE + 16, n=need) == INVALID                 # misaligned
     assert _step(dsa, p, None, t, ws=0x60000, n=need - 1) == SMALL
