@@ -488,6 +488,8 @@ DSA_API int32_t dsa_tree_workspace_size(const dsa_problem *problem, const dsa_di
  *   accepted ones in order).  Nodes without room (S + i >= max_seq_len) are dropped like those at and
  *   behind node_count[b]: nothing is appended, out = 0, lse = -inf; k_new, v_new and q of such nodes may
  *   hold anything.  A negative seq_len drops all nodes.
+ *   A node whose page is missing (its entry in the block table is outside [0, num_blocks), after
+ *   dsa_reserve_pages found none for instance) is computed, but its rows are stored nowhere.
  *   Cached rows that no node of the request sees may hold anything (NaN included); a NaN or infinity in
  *   the V row of a token that some node sees reaches the other nodes of the request as well.
  */
@@ -522,8 +524,10 @@ typedef struct dsa_verify {
  *   chosen (draft_probs NULL)  the same with q a point: child i stands iff u_i W < v(x); otherwise
  *                  W <- W - v(x), v(x) <- 0.
  * The token behind c is then the lowest k with v(0) + ... + v(k) > u_0 sum v (v = p again where nothing is
- * left of v; -1 where p has no positive entry either).  All of this is computed in double precision, so that
- * the order of the sums decides about nothing.  Tokens outside [0, V) never stand and change nothing.
+ * left of v; -1 where p has no positive entry either).  Sums and products carry some 48 bits, so that the
+ * order of the additions decides about nothing.  Tokens outside [0, V) never stand and change nothing.
+ * Greedy: a NaN counts as -inf.  Probabilities are finite and not negative; a row with others gives some
+ * token or -1, and no fault.
  *   path [B, N] int32: the nodes that stand, node 0 first, -1 behind them; accepted [B]: how many they
  *   are; next_token [B].  A request without nodes gets accepted = 0, next_token = -1.
  * path / accepted are what dsa_compact_kv takes as keep / keep_count.  No workspace.
@@ -536,11 +540,12 @@ DSA_API int32_t dsa_verify_tree(const dsa_verify *verify, const dsa_tree *tree, 
  * position base[b] + i, in place.  keep [B, max_keep] device, ascending without repeats (so keep[b][i] >= i);
  * keep_count [B] device, clamped to [0, max_keep]; base [B] device, or NULL for 0.  After a verified tree:
  * base = seq_len, keep = path.  To drop tokens for good: base = NULL, keep = the positions that stay.
- * len_out [B] device or NULL: base[b] + (the clamped) keep_count[b]; may be seq_len or base itself.
+ * len_out [B] device or NULL: base[b] + (the clamped) keep_count[b]; may be seq_len, base or keep_count itself.
  * The cache is that of `problem` (q and max_seq_len's sense as elsewhere: rows at positions outside
- * [0, max_seq_len) are neither read nor written; refused for bounded caches); with num_layers > 1 the
+ * [0, max_seq_len), or whose page is missing, are neither read nor written; refused for bounded caches); with num_layers > 1 the
  * layers' caches lie stride_layer elements apart behind k_cache and v_cache and one call serves all of them.
- * A list that is not ascending gives wrong rows, not faults.
+ * A list that is not ascending gives wrong rows, not faults.  Rows move in place, for every request that reads
+ * them: a page that several block-table entries name must not lie behind the first row that moves.
  */
 DSA_API int32_t dsa_compact_kv(const dsa_problem *problem, int32_t num_layers, int64_t stride_layer,
                                const int32_t *base, const int32_t *keep, const int32_t *keep_count, int32_t max_keep,
@@ -562,7 +567,7 @@ typedef struct dsa_page_pool {
  * the number of pages the row lacks and did not get: a row whose demand goes beyond what is left, then,
  * gets nothing, and neither does any row behind it that lacks pages; a row longer than max_blocks gets
  * nothing by itself.  Entries that are not -1 (any negative value counts as -1) are left as they are.
- * At most 4000 rows per call (DSA_ERR_UNSUPPORTED).
+ * At most 4000 rows per call (more: DSA_ERR_UNSUPPORTED).
  */
 DSA_API int32_t dsa_reserve_pages(const dsa_page_pool *pool, int32_t *block_table, int32_t batch, int32_t max_blocks,
                                   const int32_t *seq_len, int32_t extra_tokens, int32_t *status, void *stream);
@@ -579,7 +584,9 @@ DSA_API int32_t dsa_release_pages(const dsa_page_pool *pool, int32_t *block_tabl
  * pages that src[i] has filled are shared (their counts rise); its part-filled last page is copied, in all
  * layers, to a fresh page; the entries behind it become -1; seq_len and prompt_len of dst[i] become those
  * of src[i].  (These arrays of `problem` are therefore WRITTEN.)  What row dst[i] held is overwritten without
- * being given back: release it first.  One source may have many branches.
+ * being given back: release it first.  One source may have many branches.  New tokens of either go to pages of its
+ * own; rows within the shared length are not to be written again (moved, or taken back and appended anew) while the
+ * other lives.
  * status[i]: 0; 1: no free page was left for it, nothing was changed; 2: refused, nothing was changed:
  * src[i] or dst[i] is no row of the table, or dst[i] is also src or an earlier dst of the same call.
  * workspace: 16 * n bytes, 256-byte aligned.  num_layers, stride_layer as for dsa_compact_kv.

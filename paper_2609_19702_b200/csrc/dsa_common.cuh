@@ -96,6 +96,14 @@ __device__ __forceinline__ int64_t token_offset(const AttnArgs& a, int b, int L_
     return (int64_t)b * a.stride_b + (int64_t)pos * a.stride_tok;
 }
 
+// Whether position `pos` has a place of its own: with a block table, a page of the pool (an entry outside it is read as
+// the nearest page, but what is written there would be another request's).
+__device__ __forceinline__ bool token_has_page(const AttnArgs& a, int b, int pos) {
+    if (!a.block_table) return true;
+    const int blk = a.block_table[(int64_t)b * a.max_blocks + min(pos / a.block_size, a.max_blocks - 1)];
+    return blk >= 0 && blk < a.num_blocks;
+}
+
 template <typename T> struct Elem;
 template <> struct Elem<__nv_bfloat16> {
     static constexpr int VEC = 8;

@@ -82,7 +82,8 @@ __global__ void __launch_bounds__(kCopyThreads, 8) dsa_compact_kernel(const Cach
                 int64_t src = 0, dst = 0;
                 if (i < to) {
                     const int64_t at = first + list[i], goal = first + i;
-                    moves = at != goal && at >= 0 && at < c.a.max_seq_len && goal >= 0 && goal < c.a.max_seq_len;
+                    moves = at != goal && at >= 0 && at < c.a.max_seq_len && goal >= 0 && goal < c.a.max_seq_len &&
+                            token_has_page(c.a, b, (int)at) && token_has_page(c.a, b, (int)goal);
                     if (moves) {
                         src = token_offset(c.a, b, 0, (int)at) * c.esize;
                         dst = token_offset(c.a, b, 0, (int)goal) * c.esize;
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_reserve_kernel(int* table, i
             e += k;                                // no hole: the row's pages end before its first lacking entry
         } else {
             // a row with holes: its k-th lacking entry, counted before any of them is filled (see below)
-            for (;; ++e)
+            for (; e < max_blocks - 1; ++e)
                 if (row[e] < 0 && k-- == 0) break;
         }
         ref_count[page] = -1 - e;                  // (marked; the tables are written when all ranks have counted)
@@ -474,6 +475,7 @@ int32_t cache_args(const dsa_problem* p, int32_t num_layers, int64_t stride_laye
     if (rc != DSA_OK) return rc;
     if (num_layers < 1) return DSA_ERR_INVALID_ARG;
     if (p->ring_size > 0) return DSA_ERR_UNSUPPORTED;
+    if (num_layers > (1 << 16) || p->num_kv_heads > (1 << 16)) return DSA_ERR_UNSUPPORTED;
     const int esize = p->dtype == DSA_BF16 ? 2 : 4;
     if (num_layers > 1 && (stride_layer < 1 || stride_layer * esize % 16)) return DSA_ERR_INVALID_ARG;
     *c = CacheArgs{};
@@ -519,10 +521,11 @@ int32_t dsa_compact_kv(const dsa_problem* problem, int32_t num_layers, int64_t s
     int32_t rc = cache_args(problem, num_layers, stride_layer, &c);
     if (rc != DSA_OK) return rc;
     if (max_keep < 0) return DSA_ERR_INVALID_ARG;
+    if ((int64_t)problem->batch * max_keep > (1LL << 32)) return DSA_ERR_UNSUPPORTED;
     if (problem->batch == 0) return DSA_OK;
     if (!keep_count || (max_keep > 0 && !keep)) return DSA_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const bool own_launch = len_out && (max_keep == 0 || base == len_out);
+    const bool own_launch = len_out && (max_keep == 0 || base == len_out || keep_count == len_out);
     if (max_keep > 0) {
         const int col_blocks = (c.row_vecs + kCopyThreads - 1) / kCopyThreads;
         const int stretches = (max_keep + kListRows - 1) / kListRows;
@@ -536,7 +539,7 @@ int32_t dsa_compact_kv(const dsa_problem* problem, int32_t num_layers, int64_t s
                     own_launch ? (int32_t*)nullptr : len_out);
         if (rc != DSA_OK) return rc;
     }
-    // (a launch of its own where base is len_out, which every block of the other one reads)
+    // (a launch of its own where len_out is base or keep_count, which every block of the other one reads)
     if (own_launch)
         rc = launch(dsa_compact_len_kernel, (problem->batch + 255) / 256, 256, 0, st, false, base, keep_count, (int)max_keep,
                     (int)problem->batch, len_out);

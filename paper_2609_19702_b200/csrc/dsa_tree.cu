@@ -46,6 +46,7 @@ int32_t make_tree_plan(const dsa_problem* p, const dsa_diag_params* d, const dsa
     if (!tree || tree->max_nodes < 1) return DSA_ERR_INVALID_ARG;
     if (tree->max_nodes > DSA_TREE_MAX_NODES) return DSA_ERR_UNSUPPORTED;
     if (p->ring_size > 0) return DSA_ERR_UNSUPPORTED;
+    if (p->max_seq_len > 0x7fff0000) return DSA_ERR_UNSUPPORTED;     // (positions a tile or a tree further stay below 2^31)
     if (d && d->mode != DSA_MASK_WINDOW) return DSA_ERR_UNSUPPORTED;
     const int N = tree->max_nodes;
     pl->G = p->num_q_heads / p->num_kv_heads;

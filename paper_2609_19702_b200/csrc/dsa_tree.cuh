@@ -189,21 +189,23 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& g, int S, int L_p)
 }
 
 // K / V rows of the nodes first, first + step, ... below n, kv head kvh, to the cache, by one warp: every lane looks up
-// one node's place, then the rows are copied eight 512-byte steps at a time.
+// one node's place (-1: it has no page, and its rows are dropped), then the rows are copied eight 512-byte steps at a time.
 template <typename T, int D>
 __device__ __forceinline__ void tree_append(const TreeArgs& g, int b, int kvh, int S, int L_p, int first, int step, int n, int lane) {
     constexpr int VEC = 16 / (int)sizeof(T), CPR = D / VEC, PAIR = 2 * CPR;        // 16-byte pieces of a K and a V row
     for (int base = first; base < n; base += 32 * step) {
         const int64_t node0 = (int64_t)b * g.N + base;
         const int count = min(32, (n - base + step - 1) / step);
-        const int64_t place = lane < count ? token_offset(g.a, b, L_p, S + base + lane * step) + (int64_t)kvh * g.a.stride_head : 0;
+        const int pos = S + base + lane * step;
+        const int64_t place = lane < count && token_has_page(g.a, b, pos) ? token_offset(g.a, b, L_p, pos) + (int64_t)kvh * g.a.stride_head : -1;
         for (int i0 = 0; i0 < count * PAIR; i0 += 8 * 32) {
             uint4 x[8];
             int64_t dst[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int i = i0 + 32 * j + lane, r = i / PAIR, c = i % CPR * VEC;
-                dst[j] = __shfl_sync(0xffffffffu, place, min(r, 31)) + c;
+                const int64_t at = __shfl_sync(0xffffffffu, place, min(r, 31));
+                dst[j] = at < 0 ? -1 : at + c;
                 if (r < count)
                     x[j] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(i % PAIR < CPR ? g.a.k_new : g.a.v_new) +
                                                            ((node0 + r * step) * g.a.H_kv + kvh) * D + c);
@@ -211,7 +213,7 @@ __device__ __forceinline__ void tree_append(const TreeArgs& g, int b, int kvh, i
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int i = i0 + 32 * j + lane;
-                if (i / PAIR < count)
+                if (i / PAIR < count && dst[j] >= 0)
                     *reinterpret_cast<uint4*>(reinterpret_cast<T*>(const_cast<void*>(i % PAIR < CPR ? g.a.k : g.a.v)) + dst[j]) = x[j];
             }
         }

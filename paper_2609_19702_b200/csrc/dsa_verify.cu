@@ -215,8 +215,10 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
                 float f[4];
                 load4(p, i, hi, vec, f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (i + e < hi && (f[e] > best || arg == kNone)) { best = f[e]; arg = i + e; }
+                for (int e = 0; e < 4; ++e) {
+                    const float score = fmaxf(f[e], -INFINITY);               // (a NaN counts as -inf)
+                    if (i + e < hi && (score > best || arg == kNone)) { best = score; arg = i + e; }
+                }
             }
 #pragma unroll
             for (int off = 16; off >= 1; off >>= 1)

@@ -55,6 +55,7 @@ def test_tree_refusals(dsa):
     ring = _problem(dsa, ring_size=2048, ring_sinks=4)
     assert _size(dsa, ring, _window(dsa), t)[0] == UNSUPPORTED
     assert _size(dsa, _problem(dsa, head_dim=96), None, t)[0] == UNSUPPORTED
+    assert _size(dsa, _problem(dsa, max_seq_len=2 ** 31 - 1), None, t)[0] == UNSUPPORTED
     assert _size(dsa, _problem(dsa, stride_token=100), None, t)[0] == INVALID
     for bad in (dict(k=None), dict(v=None), dict(out=None), dict(lse=None), dict(k=FAKE + 4), dict(v=FAKE + 8), dict(out=FAKE + 2)):
         assert _step(dsa, p, None, t, **bad) == INVALID
@@ -111,6 +112,8 @@ def test_page_refusals(dsa):
     assert L.dsa_compact_kv(a(p), 1, 0, None, None, FAKE, 4, None, None) == INVALID
     assert L.dsa_compact_kv(a(p), 1, 0, None, FAKE, None, 4, None, None) == INVALID
     assert L.dsa_compact_kv(a(p), 1, 0, None, FAKE, FAKE, -1, None, None) == INVALID
+    assert L.dsa_compact_kv(a(p), 1 << 17, 4096, None, FAKE, FAKE, 4, None, None) == UNSUPPORTED
+    assert L.dsa_compact_kv(a(_problem(dsa, batch=64)), 1, 0, None, FAKE, FAKE, 2 ** 31 - 1, None, None) == UNSUPPORTED
     ring = _problem(dsa, ring_size=2048, **paged)
     assert L.dsa_compact_kv(a(ring), 1, 0, None, FAKE, FAKE, 4, None, None) == UNSUPPORTED
     # reserve, release

@@ -104,6 +104,33 @@ def test_compact_limits(dsa):
     assert c.seq.tolist() == [1, 10, 32, 7] and c.same()
 
 
+def test_compact_lengths_over_the_counts(dsa):
+    c = Cache(dsa, 3, 40, 8, lens=[0, 4, 2])
+    keep = [[1, 2, 5, 200], [0, 1, 2, 3], [2, 3, 250, 290]]
+    counts, want = _int([4, 2, 3]), [4, 6, 5]
+    for r, row in enumerate(keep):
+        for i in range([4, 2, 3][r]):
+            (so, si), (do, di) = c.place(r, [0, 4, 2][r] + row[i]), c.place(r, [0, 4, 2][r] + i)
+            for t in c.host:
+                t[:, do, di] = t[:, so, si].clone()
+    dsa.dsa_compact_kv(c.problem, _int(keep), counts, base=c.seq, len_out=counts)
+    assert c.same() and counts.tolist() == want and c.seq.tolist() == [0, 4, 2]
+
+
+def test_compact_leaves_missing_pages_alone(dsa):
+    c = Cache(dsa, 2, 4, 8)
+    c.table[0, 1], c.table[1, 3] = -1, 10 ** 6
+    host = [t.clone() for t in c.host]
+    for r, moves in ((0, [(2, 1), (20, 5)]), (1, [(3, 0), (9, 1)])):     # (row 0's fourth goes to, and row 1's third comes from, nowhere)
+        for a, b in moves:
+            (so, si), (do, di) = c.place(r, a), c.place(r, b)
+            for t, h in zip(host, c.host):
+                t[:, do, di] = h[:, so, si]
+    c.host = host
+    dsa.dsa_compact_kv(c.problem, _int([[0, 2, 10, 11, 12, 20, 21, 22, 23], [3, 9, 25, 26, 27, 28, 29, 30, 31]]), _int([6, 5]))
+    assert c.same()
+
+
 def _pool(dsa, c, refs):
     return dsa.PagePool(_int(refs), c.page)
 

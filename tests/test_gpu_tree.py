@@ -292,6 +292,26 @@ def test_same_bits_again_on_another_stream_and_replayed(dsa, dtype):
         assert torch.equal(out, o2) and torch.equal(lse, l2)
 
 
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("hq,n", [(2, 6), (8, 20)])
+def test_nodes_without_a_page_are_stored_nowhere(dsa, dtype, hq, n):
+    s = Setup(dsa, dtype=dtype, hq=hq, hkv=2, n=n, lens=(32, 40, 7), page=8, chain=True)
+    table = s.problem.block_table
+    spare = [x for x in range(s.problem.num_blocks) if x not in set(table.flatten().tolist())]
+    table[0, 4:], table[1, 6:] = -1, s.problem.num_blocks                # the pages behind the cached tokens (and, of one, some new ones)
+    s.table[0, 4:], s.table[1, 6:] = spare[0], spare[1]
+    rows = [n, n, n]
+    s.run()
+    out, lse = s.run()
+    # what the kernel may have written: rows 0 lacks all its pages, row 1 those from token 48 on
+    live = s.live
+    s.live = [0, min(n, 8), n]
+    s.check_cache()
+    s.live, s.check_cache = live, lambda: None
+    assert live == rows
+    s.check(out, lse)
+
+
 def test_two_calls_at_once(dsa):
     a = Setup(dsa, lens=(2000, 900, 1500, 60), split=256, n=30, poison=False)
     b = Setup(dsa, lens=(1700, 1900), split=192, n=64, hq=16, poison=False, seed=3)

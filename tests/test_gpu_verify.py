@@ -169,6 +169,33 @@ def test_greedy_ties_and_equal_scores(dsa):
         assert word.tolist() == [0, v // 2, 0] and accepted.tolist() == [2, 2, 2]
 
 
+def test_greedy_counts_a_nan_as_the_lowest(dsa):
+    for v in (7, 300, 20000):
+        p = torch.full((3, 2, v), float("nan"))
+        p[0, :, v // 2], p[1, :, v - 1] = -3.0, -float("inf")
+        c = dict(p=p, q=p, dp=p.cuda(), dq=p.cuda(), parent=np.array([[-1, 0]] * 3, np.int32),
+                 tokens=np.array([[0, v // 2], [0, 0], [0, 0]], np.int32), u=np.zeros((3, 2), np.float32), counts=[2] * 3,
+                 mode="greedy", chain=True)
+        path, accepted, word = _run(dsa, c)
+        assert word.tolist() == [v // 2, 0, 0] and accepted.tolist() == [2, 2, 2]
+
+
+@pytest.mark.parametrize("mode", ["sample", "point"])
+def test_probabilities_that_are_none(dsa, mode):
+    """NaN, infinite or negative entries, and numbers of 1 or NaN: a token or -1, and the other requests' tokens as they are."""
+    rng = np.random.default_rng(3)
+    c = _draw(rng, 6, 9, 5000, 2, mode, torch.float32)
+    want = [t.clone() for t in _run(dsa, c)]
+    for r, x in enumerate((float("nan"), float("inf"), -1.0)):
+        c["dp"][r, :, ::7] = x
+        c["dq"][r, :, ::5] = x
+    c["u"][3] = 1.0
+    c["u"][4] = float("nan")
+    path, accepted, word = _run(dsa, c)
+    assert torch.equal(path[5], want[0][5]) and accepted[5] == want[1][5] and word[5] == want[2][5]
+    assert ((word >= -1) & (word < 5000)).all() and ((accepted >= 1) & (accepted <= 9)).all()
+
+
 def test_accepted_tokens_follow_the_target(dsa):
     """One drafted token and the last one: over many numbers the first of the two that stands is distributed as p says,
     whatever q is.  64 cells of 200000 draws: every cell within five standard deviations, for fixed numbers."""
