@@ -74,50 +74,29 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// ---- pairs of floats: the value is h + l, |l| at most half a unit of h ----------------------------------
-struct Pair { float h, l; };
-__device__ __forceinline__ Pair two_sum(float a, float b) {                 // a + b without an error
-    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
-    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+// ---- fp64 -------------------------------------------------------------------------------------------------
+// A float as a double, by its bits (the unit that converts is a fourth as wide as the one that adds; a subnormal
+// float counts as 0).
+__device__ __forceinline__ double widen(float f) {
+    const int x = __float_as_int(f);
+    const bool some = (x & 0x7f800000) != 0;
+    return __hiloint2double(some ? ((x >> 3) & 0x8fffffff) + 0x38000000 : 0, some ? x << 29 : 0);
 }
-__device__ __forceinline__ void add_to(Pair& acc, const Pair& x) {
-    const Pair s = two_sum(acc.h, x.h);
-    acc.h = s.h;
-    acc.l = __fadd_rn(acc.l, __fadd_rn(s.l, x.l));
-}
-__device__ __forceinline__ Pair times(const Pair& a, float b) {
-    const float h = __fmul_rn(a.h, b);
-    return {h, __fmaf_rn(a.l, b, __fmaf_rn(a.h, b, -h))};
-}
-__device__ __forceinline__ bool exceeds(const Pair& a, const Pair& b) {     // (near each other a.h - b.h is exact)
-    return __fadd_rn(__fsub_rn(a.h, b.h), __fsub_rn(a.l, b.l)) > 0.f;
-}
-// max(v - w q, 0)
-__device__ __forceinline__ Pair reject(const Pair& v, const Pair& w, float q) {
-    const float ph = __fmul_rn(w.h, q), pl = __fmaf_rn(w.l, q, __fmaf_rn(w.h, q, -ph));
-    const Pair d = two_sum(v.h, -ph);
-    const float e = __fadd_rn(d.l, __fsub_rn(v.l, pl));
-    const float h = __fadd_rn(d.h, e);
-    const bool some = h > 0.f;
-    return {some ? h : 0.f, some ? __fsub_rn(e, __fsub_rn(h, d.h)) : 0.f};
-}
+__device__ __forceinline__ double reject(double v, double w, double q) { return fmax(__fma_rn(-w, q, v), 0.); }
 
-__device__ __forceinline__ Pair warp_sum(Pair v) {                          // lane 0's order of additions, for every lane
+__device__ __forceinline__ double warp_sum(double v) {                      // lane 0's order of additions, for every lane
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) {
-        const Pair o = {__shfl_down_sync(0xffffffffu, v.h, off), __shfl_down_sync(0xffffffffu, v.l, off)};
-        add_to(v, o);
-    }
-    return {__shfl_sync(0xffffffffu, v.h, 0), __shfl_sync(0xffffffffu, v.l, 0)};
+    for (int off = 16; off >= 1; off >>= 1) v += __shfl_down_sync(0xffffffffu, v, off);
+    return __shfl_sync(0xffffffffu, v, 0);
 }
-__device__ __forceinline__ Pair warp_prefix(Pair v, int lane) {             // of the lanes before this one
+__device__ __forceinline__ double warp_prefix(double v, int lane) {         // of the lanes before this one
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const Pair o = {__shfl_up_sync(0xffffffffu, v.h, off), __shfl_up_sync(0xffffffffu, v.l, off)};
-        if (lane >= off) add_to(v, o);
+        const double o = __shfl_up_sync(0xffffffffu, v, off);
+        if (lane >= off) v += o;
     }
-    const Pair up = {__shfl_up_sync(0xffffffffu, v.h, 1), __shfl_up_sync(0xffffffffu, v.l, 1)};
-    return lane > 0 ? up : Pair{0.f, 0.f};
+    const double up = __shfl_up_sync(0xffffffffu, v, 1);
+    return lane > 0 ? up : 0.;
 }
 // (score, index): the larger score, of equal ones the lower index; kNone: no entry yet
 constexpr int kNone = 0x7fffffff;
@@ -130,7 +109,7 @@ __device__ __forceinline__ void take_better(float& best, int& arg, float o, int 
 enum : int { kSum, kDraw, kDone };
 struct Task {
     int what, node, k, run;
-    Pair before, goal;
+    double before, goal;
 };
 
 // W warps per block; KEEP: the residual is kept (dynamic shared memory, 8 bytes per entry of the block's piece)
@@ -138,16 +117,16 @@ template <typename T, int W, bool GREEDY, bool KEEP>
 __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_kernel(const VerifyArgs a) {
     constexpr int kRuns = kVerifyMaxCluster * W;
     // one sum (greedy: best score and its index) per warp of the cluster, two sets: the blocks may be one pass apart
-    __shared__ Pair s_sum[2][kRuns];
+    __shared__ double s_sum[2][kRuns];
     __shared__ float s_best[2][kRuns];
     __shared__ int s_arg[2][kRuns];
     __shared__ Task s_task;
-    __shared__ Pair s_weight[kVerifyMaxNodes];               // W of the rejections at the current node
+    __shared__ double s_weight[kVerifyMaxNodes];               // W of the rejections at the current node
     __shared__ int s_out[kVerifyMaxNodes];                   // and the turned-down tokens (draft given as points)
     __shared__ int s_token[kVerifyMaxNodes], s_parent[kVerifyMaxNodes], s_path[kVerifyMaxNodes];
     __shared__ unsigned s_children[2 * kVerifyMaxNodes];     // of every node, a bit each
     __shared__ float s_u[kVerifyMaxNodes], s_p[kVerifyMaxNodes], s_q[kVerifyMaxNodes];
-    extern __shared__ __align__(16) Pair s_left[];
+    extern __shared__ __align__(16) double s_left[];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned rank, blocks;
@@ -256,30 +235,30 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
         }
         if (rank == 0 && tid == 0) a.next_token[b] = best;
     } else {
-        Pair* kept = s_left + warp * a.run;                  // what is left of the current node's row: this warp's run
+        double* kept = s_left + warp * a.run;                  // what is left of the current node's row: this warp's run
         int held = -1;                                       // the node that it belongs to
         // one entry after k rejections, from p and q
-        auto left_of = [&](float p, float q, int x, int k) -> Pair {
-            Pair v = {p, 0.f};
+        auto left_of = [&](float p, float q, int x, int k) -> double {
+            double v = widen(p);
             if (points) {
                 for (int r = 0; r < k; ++r)
-                    if (s_out[r] == x) v.h = 0.f;
+                    if (s_out[r] == x) v = 0.;
             } else {
-                for (int r = 0; r < k; ++r) v = reject(v, s_weight[r], q);
+                for (int r = 0; r < k; ++r) v = reject(v, s_weight[r], widen(q));
             }
             return v;
         };
-        Pair runs_before = {0.f, 0.f};                       // warp 0: the sum of the runs before this lane's
+        double runs_before = 0.;                       // warp 0: the sum of the runs before this lane's
         // the sum of what is left at `node` after k rejections; leaves the warps' sums in s_sum[(pass - 1) & 1]
-        auto sum_left = [&](int node, int k) -> Pair {
+        auto sum_left = [&](int node, int k) -> double {
             const T *p, *q;
             bool vec;
             rows_of(node, p, q, vec);
-            Pair acc[4] = {};
+            double acc[4] = {};
             const bool need_q = !points && k > 0;
             // a node's first pass follows its first rejection, and every one its own: `kept` lacks the last one only
             const bool fresh = !KEEP || held != node || k == 0;
-            const Pair w = KEEP && need_q ? s_weight[k - 1] : Pair{0.f, 0.f};
+            const double w = KEEP && need_q ? s_weight[k - 1] : 0.;
             for (int i0 = lo; i0 < hi; i0 += 512) {          // four stretches of 128 entries: all loads, then the arithmetic
                 float fp[16], fq[16];
                 if (fresh) {
@@ -304,58 +283,55 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
                 for (int s = 0; s < 4; ++s) {
                     const int i = i0 + 128 * s + 4 * lane;
                     if (i >= hi) break;
-                    Pair x[4];
+                    double x[4];
                     if (KEEP && !fresh) {
-                        const float4 x0 = *reinterpret_cast<const float4*>(kept + (i - lo)), x1 = *reinterpret_cast<const float4*>(kept + (i - lo) + 2);
-                        x[0] = {x0.x, x0.y}; x[1] = {x0.z, x0.w}; x[2] = {x1.x, x1.y}; x[3] = {x1.z, x1.w};
+                        const double2 x0 = *reinterpret_cast<const double2*>(kept + (i - lo)), x1 = *reinterpret_cast<const double2*>(kept + (i - lo) + 2);
+                        x[0] = x0.x; x[1] = x0.y; x[2] = x1.x; x[3] = x1.y;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = reject(x[e], w, fq[4 * s + e]);
+                        for (int e = 0; e < 4; ++e) x[e] = reject(x[e], w, widen(fq[4 * s + e]));
                     } else if (KEEP && need_q) {             // the first rejection at a node: W is 1
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            x[e] = two_sum(fp[4 * s + e], -fq[4 * s + e]);
-                            if (!(x[e].h > 0.f)) x[e] = {0.f, 0.f};
-                        }
+                        for (int e = 0; e < 4; ++e) x[e] = fmax(widen(fp[4 * s + e]) - widen(fq[4 * s + e]), 0.);
                     } else if (KEEP && k == 0) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = {fp[4 * s + e], 0.f};
+                        for (int e = 0; e < 4; ++e) x[e] = widen(fp[4 * s + e]);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = left_of(fp[4 * s + e], need_q ? fq[4 * s + e] : 0.f, i + e, k);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) add_to(acc[e], x[e]);
+                    for (int e = 0; e < 4; ++e) acc[e] += x[e];
                     if (KEEP) {
-                        *reinterpret_cast<float4*>(kept + (i - lo)) = make_float4(x[0].h, x[0].l, x[1].h, x[1].l);
-                        *reinterpret_cast<float4*>(kept + (i - lo) + 2) = make_float4(x[2].h, x[2].l, x[3].h, x[3].l);
+                        *reinterpret_cast<double2*>(kept + (i - lo)) = make_double2(x[0], x[1]);
+                        *reinterpret_cast<double2*>(kept + (i - lo) + 2) = make_double2(x[2], x[3]);
                     }
                 }
             }
             held = node;
-            add_to(acc[0], acc[1]);
-            add_to(acc[2], acc[3]);
-            add_to(acc[0], acc[2]);
-            const Pair mine = warp_sum(acc[0]);
+            acc[0] += acc[1];
+            acc[2] += acc[3];
+            acc[0] += acc[2];
+            const double mine = warp_sum(acc[0]);
             if (lane < (int)blocks)
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};"
-                             ::"r"(map_to_rank(smem_u32(&s_sum[pass & 1][slot]), lane)), "f"(mine.h), "f"(mine.l) : "memory");
+                asm volatile("st.shared::cluster.f64 [%0], %1;"
+                             ::"r"(map_to_rank(smem_u32(&s_sum[pass & 1][slot]), lane)), "d"(mine) : "memory");
             meet();
-            Pair total = {0.f, 0.f};
+            double total = 0.;
             if (warp == 0) {                                 // (the same additions in warp 0 of every block)
-                Pair own[4];                                 // per_lane is at most 4
+                double own[4];                                 // per_lane is at most 4
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int at = lane * per_lane + w;
-                    own[w] = w < per_lane && at < n_runs ? s_sum[pass & 1][at] : Pair{0.f, 0.f};
+                    own[w] = w < per_lane && at < n_runs ? s_sum[pass & 1][at] : 0.;
                 }
-                Pair other = own[2];
+                double other = own[2];
                 total = own[0];
-                add_to(total, own[1]);
-                add_to(other, own[3]);
-                add_to(total, other);
+                total += own[1];
+                other += own[3];
+                total += other;
                 runs_before = warp_prefix(total, lane);
-                add_to(total, runs_before);
-                total = {__shfl_sync(0xffffffffu, total.h, 31), __shfl_sync(0xffffffffu, total.l, 31)};
+                total += runs_before;
+                total = __shfl_sync(0xffffffffu, total, 31);
             }
             ++pass;
             return total;
@@ -365,9 +341,9 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
             const T *p, *q;
             bool vec;
             rows_of(task.node, p, q, vec);
-            auto entries = [&](int i, Pair (&x)[4]) {        // four entries from i on
+            auto entries = [&](int i, double (&x)[4]) {        // four entries from i on
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = {0.f, 0.f};
+                for (int e = 0; e < 4; ++e) x[e] = 0.;
                 if (i >= hi) return;
                 if constexpr (KEEP) {
 #pragma unroll
@@ -380,36 +356,36 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
                     for (int e = 0; e < 4; ++e) x[e] = left_of(fp[e], fq[e], i + e, task.k);
                 }
             };
-            Pair before = task.before, before_last = task.before;
+            double before = task.before, before_last = task.before;
             int at = lo, last = lo;                          // the stretch of 128 entries; the last one with anything in it
             bool hit = false;
             for (; at < hi; at += 128) {
-                Pair x[4];
+                double x[4];
                 entries(at + 4 * lane, x);
-                for (int e = 1; e < 4; ++e) add_to(x[0], x[e]);
-                const Pair sum = warp_sum(x[0]);
-                if (sum.h > 0.f) {
+                for (int e = 1; e < 4; ++e) x[0] += x[e];
+                const double sum = warp_sum(x[0]);
+                if (sum > 0.) {
                     last = at;
                     before_last = before;
-                    add_to(before, sum);
-                    if (exceeds(before, task.goal)) { hit = true; break; }
+                    before += sum;
+                    if (before > task.goal) { hit = true; break; }
                 }
             }
             // (rounding may leave the goal unreached: the last entry with anything in it then)
-            Pair x[4];
+            double x[4];
             const int i = last + 4 * lane;
             entries(i, x);
-            Pair four = x[0];
-            for (int e = 1; e < 4; ++e) add_to(four, x[e]);
-            Pair upto = before_last;
-            add_to(upto, warp_prefix(four, lane));
+            double four = x[0];
+            for (int e = 1; e < 4; ++e) four += x[e];
+            double upto = before_last;
+            upto += warp_prefix(four, lane);
             int first = kNone, some = -1;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                add_to(upto, x[e]);
-                if (x[e].h > 0.f) {
+                upto += x[e];
+                if (x[e] > 0.) {
                     some = i + e;
-                    if (hit && exceeds(upto, task.goal)) first = min(first, i + e);
+                    if (hit && upto > task.goal) first = min(first, i + e);
                 }
             }
             first = __reduce_min_sync(0xffffffffu, first);
@@ -420,11 +396,11 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
         // warp 0 walks the tree (of every block the same way, on the same sums)
         int cur = 0, k = 0;
         unsigned low = 0, high = 0;                          // the children of cur that are still to be tested
-        Pair weight = {1.f, 0.f};                            // W of the next test
+        double weight = 1.;                            // W of the next test
         bool summed = false;                                 // s_sum holds the sums for (cur, k), and weight their total
-        const Pair zero = {0.f, 0.f};
+        const double zero = 0.;
         if (n > 0) { low = s_children[0]; high = s_children[1]; }
-        auto next_task = [&](Pair sum) -> Task {             // `sum`: of the task before, if it was a sum
+        auto next_task = [&](double sum) -> Task {             // `sum`: of the task before, if it was a sum
             if (n == 0) {
                 if (rank == 0 && lane == 0) a.next_token[b] = -1;
                 return Task{kDone, 0, 0, 0, zero, zero};
@@ -436,13 +412,13 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
                 const int x = s_token[i];
                 if (x < 0 || x >= a.V) continue;
                 const float q = points ? 1.f : s_q[i];
-                const Pair left = left_of(s_p[i], q, x, k);
-                if (exceeds(left, times(times(weight, s_u[i]), q))) {
+                const double left = left_of(s_p[i], q, x, k);
+                if (left > weight * s_u[i] * q) {
                     cur = i;
                     if (lane == 0) s_path[length] = i;
                     ++length;
                     k = 0;
-                    weight = {1.f, 0.f};
+                    weight = 1.;
                     summed = false;
                     low = s_children[2 * i];
                     high = s_children[2 * i + 1];
@@ -452,7 +428,7 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
                 __syncwarp();
                 ++k;
                 if (points) {
-                    add_to(weight, {-left.h, -left.l});
+                    weight -= left;
                 } else {
                     summed = true;
                     return Task{kSum, cur, k, 0, zero, zero};
@@ -462,7 +438,7 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
                 summed = true;
                 return Task{kSum, cur, k, 0, zero, zero};
             }
-            if (!(weight.h > 0.f)) {
+            if (!(weight > 0.)) {
                 if (k > 0) {                                 // nothing is left of v: the target's row itself
                     k = 0;
                     return Task{kSum, cur, 0, 0, zero, zero};
@@ -471,25 +447,25 @@ __global__ void __launch_bounds__(32 * W, (GREEDY ? 48 : 32) / W) dsa_verify_ker
                 return Task{kDone, 0, 0, 0, zero, zero};
             }
             // the warp whose run takes the cumulative sum beyond the goal
-            const Pair* sums = s_sum[(pass - 1) & 1];
-            const Pair goal = times(weight, s_u[0]);
+            const double* sums = s_sum[(pass - 1) & 1];
+            const double goal = weight * s_u[0];
             const int w0 = lane * per_lane, w1 = min(n_runs, w0 + per_lane);
-            Pair at_run = runs_before, before = zero;
+            double at_run = runs_before, before = zero;
             int hit_run = kNone, last_run = -1;
             for (int w = w0; w < w1 && hit_run == kNone; ++w) {
-                if (sums[w].h > 0.f) {
+                if (sums[w] > 0.) {
                     last_run = w;
                     before = at_run;
-                    add_to(at_run, sums[w]);
-                    if (exceeds(at_run, goal)) hit_run = w;
+                    at_run += sums[w];
+                    if (at_run > goal) hit_run = w;
                 }
             }
             int run = __reduce_min_sync(0xffffffffu, hit_run);
             if (run == kNone) run = __reduce_max_sync(0xffffffffu, last_run);    // (rounding: the last run with anything in it)
             const int from = run / per_lane;
-            return Task{kDraw, cur, k, run, {__shfl_sync(0xffffffffu, before.h, from), __shfl_sync(0xffffffffu, before.l, from)}, goal};
+            return Task{kDraw, cur, k, run, __shfl_sync(0xffffffffu, before, from), goal};
         };
-        Pair sum = {0.f, 0.f};
+        double sum = 0.;
         for (;;) {
             if (warp == 0) {
                 const Task next = next_task(sum);
@@ -526,7 +502,7 @@ cudaError_t launch_verify(const VerifyArgs& a, int batch, int blocks, cudaStream
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)batch * blocks));
     cfg.blockDim = dim3(32 * W);
-    cfg.dynamicSmemBytes = KEEP ? (size_t)W * a.run * sizeof(Pair) : 0;
+    cfg.dynamicSmemBytes = KEEP ? (size_t)W * a.run * sizeof(double) : 0;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -557,7 +533,7 @@ cudaError_t run_verify(VerifyArgs& a, int batch, cudaStream_t st) {
     }
     const int blocks = fit(16, 512);
     if (greedy) return launch_verify<T, 16, true, false>(a, batch, blocks, st);
-    if (16 * (int64_t)a.run * (int)sizeof(Pair) <= kVerifyKeepBytes) return launch_verify<T, 16, false, true>(a, batch, blocks, st);
+    if (16 * (int64_t)a.run * (int)sizeof(double) <= kVerifyKeepBytes) return launch_verify<T, 16, false, true>(a, batch, blocks, st);
     return launch_verify<T, 16, false, false>(a, batch, blocks, st);
 }
 
