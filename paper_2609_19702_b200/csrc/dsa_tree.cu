@@ -250,7 +250,10 @@ int32_t dsa_tree_step(const dsa_problem* problem, const dsa_diag_params* diag, c
     g.row_tiles = pl.row_tiles;
     g.box_tokens = pl.box_tokens;
     for (g.box_shift = 0; (1 << g.box_shift) < pl.box_tokens;) ++g.box_shift;
+    g.batch = problem->batch;
     g.cluster = pl.cluster;
+    // where blocks take over work, the longest sequences go first: a long one that is begun last is waited for alone
+    g.sorted = pl.cluster == 1 && pl.blocks > 2 * (int64_t)host_sm_count() && problem->batch > 1 && problem->batch <= kTreeSorted;
     // division of positions (below 2^31) by the page size: with 2^s >= d the product by ceil(2^(31 + s) / d) is exact
     const unsigned d = problem->block_table ? (unsigned)problem->block_size : 1u;
     for (g.page_shift = 31; (1ull << (g.page_shift - 31)) < d;) ++g.page_shift;

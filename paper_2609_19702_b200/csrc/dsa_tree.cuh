@@ -50,12 +50,13 @@ constexpr int kTreeMaxNodes = 64;
 constexpr int kTreeTile = 64;                      // tokens per K / V tile
 constexpr int kTreeRows = 128;                     // query rows per block: the M of the products
 constexpr int kTreeThreads = 256;
+constexpr int kTreeSorted = 256;                   // requests, at most, that a block puts in order (one per thread)
 
 struct TreeArgs {
     AttnArgs a;                                    // lengths, block table, strides, scale, outputs
     const int* parent;                             // [B, N] or NULL (a chain)
     const int* node_count;                         // [B] or NULL (N)
-    int N, G, g_shift;                             // G: a power of two
+    int batch, N, G, g_shift;                      // G: a power of two
     int row_tiles;                                 // blocks of kTreeRows query rows per (request, kv head)
     int windowed;                                  // 0: dense
     int box_tokens;                                // tokens per tensor-map box of the caches
@@ -64,6 +65,7 @@ struct TreeArgs {
     int page_shift;
     int align_tokens;                              // where a box may start: box_tokens (pages), 1 (contiguous)
     int cluster;                                   // blocks that share the tiles and merge on chip (1: none; else n_split is 1)
+    int sorted;                                    // requests are taken in the order of their tiles, most first
     int blk_coord, head_coord;                     // 0: the map's outer / head dimension has one entry (stride 0)
 };
 
@@ -342,7 +344,8 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     unsigned long long* drained = s_full + 16;
     TreeInfo* s_info = reinterpret_cast<TreeInfo*>(s_full + 17);                 // [2]
     int* s_misc = reinterpret_cast<int*>(s_info + 2);         // [0] TMEM address, [1] abort
-    static_assert((2 * C::SLOTS + 17) * 8 + 2 * sizeof(TreeInfo) + 8 <= C::TAIL, "tail of the shared memory");
+    unsigned char* s_order = reinterpret_cast<unsigned char*>(s_misc + 2);       // [kTreeSorted] requests, most tiles first
+    static_assert((2 * C::SLOTS + 17) * 8 + 2 * sizeof(TreeInfo) + 8 + kTreeSorted <= C::TAIL, "tail of the shared memory");
     static_assert((2 * C::SLOTS) % 2 == 0, "the response lies on 16 bytes");
     volatile int* abort = s_misc + 1;
     // after the last product, for a merge within the cluster: O (rows padded against bank conflicts) and per row
@@ -377,6 +380,27 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     const unsigned tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
+
+    if (g.sorted) {
+        // the place of request `tid` among all of them (a request's tiles and its index make a key; q has not come yet)
+        unsigned* s_key = reinterpret_cast<unsigned*>(s_q);
+        unsigned key = 0;
+        if (tid < g.batch) {
+            int S, L_p, n;
+            tree_lengths(g, tid, S, L_p, n);
+            key = ((n > 0 ? (unsigned)min(tree_span(g, S, L_p).T, 0x3fffff) + 1u : 0u) << 8) | (255u - (unsigned)tid);
+        }
+        s_key[tid] = key;
+        __syncthreads();
+        int before = 0;
+        for (int j = 0; j < g.batch; j += 4) {
+            const uint4 other = *reinterpret_cast<const uint4*>(s_key + j);      // (behind the last request: 0)
+            before += (other.x > key) + (other.y > key) + (other.z > key) + (other.w > key);
+        }
+        if (tid < g.batch) s_order[before] = (unsigned char)tid;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // (q is copied to where the keys were)
+        __syncthreads();
+    }
 
     // the item number `i` of this block, once the copying warp has found it; false: there is none, or give up
     TreeItem it = {};
@@ -470,7 +494,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 it.piece = idx % pieces; idx /= pieces;
                 it.rt = idx % g.row_tiles; idx /= g.row_tiles;
                 it.kvh = idx % g.a.H_kv;
-                it.b = idx / g.a.H_kv;
+                it.b = g.sorted ? s_order[idx / g.a.H_kv] : idx / g.a.H_kv;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int node = lane + 32 * h;
