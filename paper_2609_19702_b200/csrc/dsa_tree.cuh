@@ -282,6 +282,28 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
     return r;
 }
 
+// two floats in one instruction (each rounded on its own)
+__device__ __forceinline__ unsigned long long pack_f32x2(float lo, float hi) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpack_f32x2(unsigned long long v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // ---- dynamic scheduling: a running block takes over blocks that have not been launched yet --------------------
 __device__ __forceinline__ void steal_block(void* response, unsigned long long* bar) {      // one thread
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // (the last response has been read)
@@ -740,10 +762,12 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    mx[k & 1] = fmaxf(mx[k & 1], __uint_as_float(x0[k]));
-                    mx[2 + (k & 1)] = fmaxf(mx[2 + (k & 1)], __uint_as_float(x1[k]));
-                }
+                for (int k = 0; k < 32; k += 4)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {             // (maxima of three)
+                        mx[h] = fmaxf(fmaxf(mx[h], __uint_as_float(x0[k + 2 * h])), __uint_as_float(x0[k + 2 * h + 1]));
+                        mx[2 + h] = fmaxf(fmaxf(mx[2 + h], __uint_as_float(x1[k + 2 * h])), __uint_as_float(x1[k + 2 * h + 1]));
+                    }
                 const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 // (-inf - -inf is NaN: compares false, nothing to rescale)
                 if (__any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f)) {
@@ -767,17 +791,19 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
                     }
                 }
                 const float sub = m_ref == -INFINITY ? 0.f : m_ref * sl;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                const unsigned long long sl2 = pack_f32x2(sl, sl), sub2 = pack_f32x2(-sub, -sub);
+                unsigned long long sum[2] = {0ull, 0ull};
                 unsigned pk[32];
 #pragma unroll
                 for (int k = 0; k < 32; ++k) {
                     const unsigned a0 = k < 16 ? x0[2 * k] : x1[2 * k - 32], a1 = k < 16 ? x0[2 * k + 1] : x1[2 * k - 31];
-                    const float p0 = fast_exp2(fmaf(__uint_as_float(a0), sl, -sub));
-                    const float p1 = fast_exp2(fmaf(__uint_as_float(a1), sl, -sub));
-                    sum[k & 3] += p0 + p1;
+                    const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(a0), __uint_as_float(a1)), sl2, sub2));
+                    const float p0 = fast_exp2(y.x), p1 = fast_exp2(y.y);
+                    sum[k & 1] = add_f32x2(sum[k & 1], pack_f32x2(p0, p1));
                     pk[k] = pack_bf16(p0, p1);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                const float2 both = unpack_f32x2(add_f32x2(sum[0], sum[1]));
+                l += both.x + both.y;
                 tc_st32(s_addr, pk);
                 tc_wait_st();
                 tc_fence_before();
