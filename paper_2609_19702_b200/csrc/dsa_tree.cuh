@@ -397,6 +397,15 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         tc_fence_before();
     }
+    // Rows of q that no copy fills: zeros.  Nobody reads their results, but what the products multiply there costs power
+    // and so clock (64 x 16 nodes with a window, over and over: 164 us with leftovers, 156 with zeros).
+    {
+        const int filled = min(per_tile, g.N) * G * 8;        // 16-byte pieces of a half
+        for (int i = filled + tid; i < kTreeRows * 8; i += kTreeThreads)
+#pragma unroll
+            for (int h = 0; h < C::HALVES; ++h) *reinterpret_cast<uint4*>(s_q + h * C::Q_HALF + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
@@ -404,8 +413,8 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
     asm volatile("griddepcontrol.launch_dependents;");
 
     if (g.sorted) {
-        // the place of request `tid` among all of them (a request's tiles and its index make a key; q has not come yet)
-        unsigned* s_key = reinterpret_cast<unsigned*>(s_q);
+        // the place of request `tid` among all of them (a request's tiles and its index make a key; nothing has come yet)
+        unsigned* s_key = reinterpret_cast<unsigned*>(s_ring);
         unsigned key = 0;
         if (tid < g.batch) {
             int S, L_p, n;
@@ -420,7 +429,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) dsa_tree_kernel(const TreeArg
             before += (other.x > key) + (other.y > key) + (other.z > key) + (other.w > key);
         }
         if (tid < g.batch) s_order[before] = (unsigned char)tid;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // (q is copied to where the keys were)
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // (tiles are copied to where the keys were)
         __syncthreads();
     }
 
