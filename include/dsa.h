@@ -524,10 +524,10 @@ typedef struct dsa_verify {
  *   chosen (draft_probs NULL)  the same with q a point: child i stands iff u_i W < v(x); otherwise
  *                  W <- W - v(x), v(x) <- 0.
  * The token behind c is then the lowest k with v(0) + ... + v(k) > u_0 sum v (v = p again where nothing is
- * left of v; -1 where p has no positive entry either).  Sums and products carry some 48 bits, so that the
- * order of the additions decides about nothing.  Tokens outside [0, V) never stand and change nothing.
- * Greedy: a NaN counts as -inf.  Probabilities are finite and not negative; a row with others gives some
- * token or -1, and no fault.
+ * left of v; -1 where p has no positive entry either).  Sums and products are fp64, so that the order of
+ * the additions decides about nothing.  Tokens outside [0, V) never stand and change nothing.
+ * Greedy: a NaN counts as -inf.  Probabilities are finite and not negative (subnormal floats count as 0); a
+ * row with others gives some token or -1, and no fault.
  *   path [B, N] int32: the nodes that stand, node 0 first, -1 behind them; accepted [B]: how many they
  *   are; next_token [B].  A request without nodes gets accepted = 0, next_token = -1.
  * path / accepted are what dsa_compact_kv takes as keep / keep_count.  No workspace.

@@ -16,9 +16,15 @@
 // the k weights W.
 //
 // Precision: with 24-bit sums the token at the border of a cumulative sum would hang on the order of the additions
-// (at 65536 entries once in some hundred draws).  Entries and sums are pairs of floats (high + low, about 48 bits,
-// error-free sums and products after Knuth and Dekker) and not doubles, whose unit is narrow.  One warp of a block
-// walks the tree and tells the others what to do.
+// (at 65536 entries once in some hundred draws).  Entries and sums are fp64; floats are widened by their bits, since the
+// unit that converts is much narrower than the one that adds (pairs of floats, high and low, took 38 us where this takes
+// 35).  One warp of a block walks the tree and tells the others what to do.
+//
+// Measured: 64 requests of 32 nodes, 65536 entries, sampled: 35-40 us, one to five passes a request (33 MB; a pass is
+// 3.3 us: 1 us of loads, 1 us of arithmetic and shared memory, the rest the meeting of the blocks and the next decision,
+// and the 512 blocks need two rounds of SMs).  One request, 16384 entries: 7 us.  Greedy, 32 requests of 16 nodes: 22 us,
+// 2.5 us a node on the path; taking a node and its first child in one pass was slower (24-26 us: the rows that are then
+// read in vain cost more than the passes saved), and so were 8 warps a block (one round: 34 us instead of 28).
 #include "dsa_host.cuh"
 
 #include <algorithm>
@@ -518,8 +524,10 @@ cudaError_t launch_verify(const VerifyArgs& a, int batch, int blocks, cudaStream
 
 template <typename T>
 cudaError_t run_verify(VerifyArgs& a, int batch, cudaStream_t st) {
-    // Small vocabularies: four warps a request.  Else sixteen, and as many blocks (up to eight) as keep a warp's run at
-    // 512 entries, whatever the batch: a pass is all latency, and more blocks per request beat fewer at every batch.
+    // Small vocabularies: four warps a request (beyond 2048 entries they would have longer runs than the 512 below).
+    // Else sixteen, and as many blocks (up to eight) as keep a warp's run at 512 entries, whatever the batch: a pass is all
+    // latency, and more blocks per request beat fewer at every batch (64 requests, 65536 entries: 38 us as 8 x 16 warps; as
+    // 8 x 8 warps 38 too, and 34 instead of 28 for half the requests).
     const bool greedy = a.u == nullptr;
     auto fit = [&](int warps, int run) {
         int blocks = 1;
