@@ -578,7 +578,7 @@ int32_t dsa_fork_pages(const dsa_page_pool* pool, const dsa_problem* problem, in
     CacheArgs c;
     int32_t rc = cache_args(problem, num_layers, stride_layer, &c);
     if (rc != DSA_OK) return rc;
-    if (!problem->block_table || n < 0) return DSA_ERR_INVALID_ARG;
+    if ((!problem->block_table && problem->batch > 0) || n < 0) return DSA_ERR_INVALID_ARG;
     rc = check_pool(pool, problem->block_table, problem->batch, problem->max_blocks);
     if (rc != DSA_OK) return rc;
     if (pool->num_blocks != problem->num_blocks || pool->block_size != problem->block_size) return DSA_ERR_INVALID_ARG;
@@ -614,7 +614,7 @@ int32_t dsa_copy_pages(const dsa_problem* problem, int32_t num_layers, int64_t s
     CacheArgs c;
     const int32_t rc = cache_args(problem, num_layers, stride_layer, &c);
     if (rc != DSA_OK) return rc;
-    if (!problem->block_table || n < 0) return DSA_ERR_INVALID_ARG;
+    if ((!problem->block_table && problem->batch > 0) || n < 0) return DSA_ERR_INVALID_ARG;
     if (problem->batch == 0 || n == 0) return DSA_OK;
     if (!src || !dst) return DSA_ERR_INVALID_ARG;
     const int col_blocks = (c.row_vecs + kCopyThreads - 1) / kCopyThreads;

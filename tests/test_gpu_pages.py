@@ -170,6 +170,61 @@ def test_reserve_fills_holes_and_leaves_long_rows(dsa):
     assert pool.ref_count.tolist() == model.refs
 
 
+@pytest.mark.parametrize("rows", [129, 1025, 4000])
+def test_reserve_many_rows(dsa, rows):
+    rng = np.random.default_rng(rows)
+    m, page, blocks = 9, 4, 5 * rows
+    refs = (rng.random(blocks) < 0.3).astype(np.int32).tolist()
+    table = np.full((rows, m), -1, np.int32)
+    table[::5, 1] = 7                                              # rows with a page behind a hole
+    lens = rng.integers(-1, 30, size=rows).tolist()
+    want, status, free, stopped = table.copy(), [], iter([i for i, r in enumerate(refs) if r == 0]), False
+    left = refs.count(0)
+    for row, length in zip(want, lens):
+        lacks = [e for e in range(0 if length < 0 else -(-(length + 3) // page)) if row[e] < 0]
+        stopped = stopped or len(lacks) > left
+        status.append(len(lacks) if stopped else 0)
+        if not stopped:
+            for e in lacks:
+                row[e] = next(free)
+            left -= len(lacks)
+    assert stopped and left > 0 or rows < 1000                      # (the pool runs out on the way)
+    pool, dt, st = dsa.PagePool(_int(refs), page), torch.from_numpy(table).cuda(), _int([0] * rows)
+    dsa.dsa_reserve_pages(pool, dt, _int(lens), 3, st)
+    assert st.tolist() == status and np.array_equal(dt.cpu().numpy(), want)
+    taken = np.array(refs)
+    taken[want[(want >= 0) & (table < 0)]] = 1
+    assert pool.ref_count.tolist() == taken.tolist()
+
+
+def test_offsets_beyond_32_bits(dsa):
+    """Pages more than 2^31 elements behind the start of the pool: moved, copied and branched."""
+    page, hkv, d = 16, 2, 128
+    blocks = 2 ** 31 // (page * hkv * d) + 1000
+    k, v = (torch.empty((blocks, page, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ids = [blocks - 1, 1, blocks - 800, blocks - 2, 0]
+    for t in (k, v):
+        for i in ids:
+            t[i].normal_()
+    table = _int([[blocks - 1, 1, blocks - 800], [-1, -1, -1]])
+    seq = _int([40, 0])
+    problem = dsa.Problem(q=torch.zeros((2, hkv, d), dtype=torch.bfloat16, device="cuda"), k_cache=k, v_cache=v,
+                          strides=(k.stride(0), k.stride(1), d), seq_len=seq, prompt_len=_int([0, 0]), num_kv_heads=hkv, max_seq_len=48,
+                          block_table=table, block_size=page, num_blocks=blocks)
+    was = [torch.cat([t[blocks - 1], t[1], t[blocks - 800]]).clone() for t in (k, v)]
+    dsa.dsa_compact_kv(problem, _int([[0, 3, 20, 35, 38]] * 2), _int([5, 0]), len_out=seq)
+    for t, w in zip((k, v), was):
+        assert torch.equal(t[blocks - 1, :5], w[[0, 3, 20, 35, 38]]) and torch.equal(t[blocks - 800], w[32:])
+    refs = torch.ones((blocks,), dtype=torch.int32, device="cuda")
+    refs[blocks - 2] = 0
+    pool, status, one = dsa.PagePool(refs, page), _int([9]), _int([1])
+    dsa.dsa_fork_pages(pool, problem, _int([0]), one, status, dsa.alloc_fork_workspace(one))
+    assert status.tolist() == [0] and seq.tolist() == [5, 5] and table[1].tolist() == [blocks - 2, -1, -1] and int(refs[blocks - 2]) == 1
+    dsa.dsa_copy_pages(problem, _int([blocks - 1]), _int([0]))
+    for t in (k, v):
+        assert torch.equal(t[blocks - 2, :5], t[blocks - 1, :5]) and torch.equal(t[0], t[blocks - 1])
+
+
 def test_release_extremes(dsa):
     pool, dt = dsa.PagePool(_int([1, 1, 0, 2]), 1), _int([[0, 1], [3, 99], [3, 2]])
     dsa.dsa_release_pages(pool, dt, _int([2 ** 31 - 1, -2 ** 31, 0]))

@@ -244,6 +244,16 @@ def test_more_blocks_than_places(dsa, d, window, page):
     s.check(*s.run())
 
 
+@pytest.mark.parametrize("b", [2, 100, 128, 129, 200, 256, 257])
+def test_requests_of_unequal_length_and_number(dsa, b):
+    """More blocks than places, so that requests are taken in the order of their tiles (up to 256 of them)."""
+    rng = np.random.default_rng(b)
+    hkv = max(2, -(-320 // b))
+    lens = [int(x) for x in rng.choice([0, 1, 5, 64, 65, 130, 300, 301, -1], size=b)]
+    s = Setup(dsa, d=64, hq=hkv, hkv=hkv, n=3, page=16, lens=lens, counts=[int(x) for x in rng.integers(0, 5, size=b)])
+    s.check(*s.run())
+
+
 def test_requests_share_a_cache(dsa):
     # a batch stride of 0: every request reads the same rows; nodes without room append nothing
     s = Setup(dsa, lens=(48, 48, 48), page=0, shared=True, cap=48, counts=(8, 8, 8))
@@ -310,6 +320,67 @@ def test_nodes_without_a_page_are_stored_nowhere(dsa, dtype, hq, n):
     s.live, s.check_cache = live, lambda: None
     assert live == rows
     s.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("layout", ["pages", "requests", "tokens"])
+def test_offsets_beyond_32_bits(dsa, dtype, layout):
+    """Rows more than 2^31 elements behind the start of the cache: pages, a request's start, or a request's own tokens."""
+    b, n, hq, hkv, d, length = 2, 6, 4, 2, 128, 40
+    blocks = 2 ** 31 // (16 * hkv * d) + 1000
+    size, strides = {"pages": (blocks * 16 * hkv * d, (16 * hkv * d, hkv * d, d)),
+                     "requests": (2 ** 31 + 64 * hkv * d, (2 ** 31, hkv * d, d)),
+                     "tokens": (2 ** 26 * 46, (hkv * d, 2 ** 26, d))}[layout]
+    g = torch.Generator().manual_seed(3)
+    rand = lambda *s: torch.randn(s, generator=g).to(dtype)  # noqa: E731
+    flat = [torch.empty(size, dtype=dtype, device="cuda") for _ in range(2)]
+    pages = [[blocks - 1, 2, blocks - 700], [0, blocks - 3, 1]]
+    at = lambda r, s: (pages[r][s // 16] * strides[0] + s % 16 * strides[1] if layout == "pages" else  # noqa: E731
+                       r * strides[0] + s * strides[1])
+    rows = [rand(b, length, hkv, d) for _ in range(2)]
+    for f, x in zip(flat, rows):
+        for r in range(b):
+            for s in range(length):
+                f[at(r, s):at(r, s) + hkv * d] = x[r, s].reshape(-1).cuda()
+    q, kn, vn = rand(b, n, hq, d), rand(b, n, hkv, d), rand(b, n, hkv, d)
+    problem = dsa.Problem(q=q.cuda(), k_cache=flat[0], v_cache=flat[1], strides=strides, seq_len=torch.tensor([length] * b, dtype=torch.int32).cuda(),
+                          prompt_len=torch.zeros((b,), dtype=torch.int32).cuda(), num_kv_heads=hkv, max_seq_len=length + n,
+                          block_table=torch.tensor(pages, dtype=torch.int32).cuda() if layout == "pages" else None, block_size=16,
+                          num_blocks=blocks)
+    tree = dsa.Tree(n)
+    out, lse = dsa.alloc_tree_outputs(problem)
+    dsa.dsa_tree_step(problem, None, tree, kn.cuda(), vn.cuda(), out, lse, dsa.alloc_tree_workspace(problem, None, tree))
+    torch.cuda.synchronize()
+    assert dsa.dsa_wait_timeouts() == 0
+    for r in range(b):
+        ro, rl, weight, big, count = draft_ref.tree_reference(q[r].double(), rows[0][r].double(), rows[1][r].double(), kn[r].double(),
+                                                              vn[r].double(), list(range(-1, n - 1)), length, 0, n, 1 / math.sqrt(d))
+        tol, ltol = draft_ref.tree_tolerances(ro, rl, weight, big, count, d, dtype == torch.bfloat16)
+        assert ((out[r].cpu().double() - ro).abs() <= tol).all() and ((lse[r].cpu().double() - rl).abs() <= ltol).all()
+        for f, new in zip(flat, (kn, vn)):
+            for i in range(n):
+                assert torch.equal(f[at(r, length + i):at(r, length + i) + hkv * d].cpu(), new[r, i].reshape(-1))
+
+
+def test_no_requests(dsa):
+    q = torch.zeros((0, 4, 4, 64), device="cuda")
+    none = torch.zeros((0,), dtype=torch.int32, device="cuda")
+    cache = torch.zeros((4, 16, 2, 64), device="cuda")
+    problem = dsa.Problem(q=q, k_cache=cache, v_cache=cache, strides=(2048, 128, 64), seq_len=none, prompt_len=none, num_kv_heads=2,
+                          max_seq_len=64, block_table=none.view(0, 4), block_size=16, num_blocks=4)
+    tree = dsa.Tree(4, parent=none.view(0, 4))
+    out, lse = dsa.alloc_tree_outputs(problem)
+    dsa.dsa_tree_step(problem, None, tree, q[:, :, :2].contiguous(), q[:, :, :2].contiguous(), out, lse)
+    ver = dsa.Verify(none.view(0, 4), torch.zeros((0, 4, 100), device="cuda"))
+    dsa.dsa_verify_tree(ver, tree, *dsa.alloc_verify_outputs(ver))
+    problem.q = q[:, 0].contiguous()
+    dsa.dsa_compact_kv(problem, none.view(0, 4), none, base=none, len_out=none)
+    pool = dsa.PagePool(torch.zeros((4,), dtype=torch.int32, device="cuda"), 16)
+    dsa.dsa_reserve_pages(pool, none.view(0, 4), none, 3, none)
+    dsa.dsa_release_pages(pool, none.view(0, 4), none)
+    dsa.dsa_fork_pages(pool, problem, none, none, none, dsa.alloc_fork_workspace(none))
+    dsa.dsa_copy_pages(problem, none, none)
+    torch.cuda.synchronize()
 
 
 def test_two_calls_at_once(dsa):

@@ -169,6 +169,26 @@ def test_greedy_ties_and_equal_scores(dsa):
         assert word.tolist() == [0, v // 2, 0] and accepted.tolist() == [2, 2, 2]
 
 
+def test_rows_beyond_32_bits(dsa):
+    b, n, v = 520, 64, 65536
+    p = torch.empty((b, n, v), dtype=torch.bfloat16, device="cuda")
+    last = torch.zeros((2, n, v), dtype=torch.bfloat16)
+    word = np.random.default_rng(0).integers(0, v, size=(2, n))
+    for r in range(2):
+        last[r, np.arange(n), word[r]] = 1.0
+    p[-2:] = last.cuda()
+    tokens = np.zeros((b, n), np.int32)
+    tokens[-2:, 1:] = word[:, :-1]
+    tokens[-1, 40] = (word[1, 39] + 1) % v
+    ver = dsa.Verify(torch.from_numpy(tokens).cuda(), p)
+    path, accepted, nxt = dsa.alloc_verify_outputs(ver)
+    dsa.dsa_verify_tree(ver, dsa.Tree(n), path, accepted, nxt)
+    assert accepted[-2:].tolist() == [64, 40] and nxt[-2:].tolist() == [int(word[0, 63]), int(word[1, 39])]
+    ver = dsa.Verify(ver.tokens, p, None, torch.zeros((b, n), device="cuda"))
+    dsa.dsa_verify_tree(ver, dsa.Tree(n), path, accepted, nxt)
+    assert accepted[-2:].tolist() == [64, 40] and nxt[-2:].tolist() == [int(word[0, 63]), int(word[1, 39])]
+
+
 def test_greedy_counts_a_nan_as_the_lowest(dsa):
     for v in (7, 300, 20000):
         p = torch.full((3, 2, v), float("nan"))
