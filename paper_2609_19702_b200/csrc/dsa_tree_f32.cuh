@@ -6,7 +6,7 @@
 // requests of 8 nodes, 20 heads of 64, up to 1144 tokens: 40 us, 7 of them the combine (49 MB; the few-row form is bound
 // by issue slots -- some 370 instructions a warp and tile, 128 of them multiply-adds, and as much again for a block's
 // set-up and results -- and by unequal lengths; the 32-row form took 122); 138 requests of 68 rows, 1000 tokens, D 128:
-// 109 us for 4.8 GFLOP.
+// 343 us for 4.8 GFLOP, bound by the reads of shared memory (352 with single multiply-adds).
 //
 // Few rows (up to 16): tiles of 32 tokens in a ring of three slots.  Eight threads share a token's scores, each
 // an eighth of the dims for all rows (one read of K per multiply-add's row count, q from registers of the same
@@ -14,9 +14,9 @@
 // per thread and 256 / (D / 4) groups of tokens, whose parts are added once at the end.
 //
 // More rows: 32 query rows a block and tiles of 64 tokens.  A warp's scores are 16 rows x 16 tokens, its lanes
-// 4 x 8 of 4 rows x 2 tokens each, so that one read of q serves four rows' lanes and one of K eight in a single
-// cycle of shared memory (6 of them for 8 cycles of multiply-adds; lanes 2 x 16 need 10); O likewise as 16 rows x
-// D / 4 dims.  Groups of tokens and rows that do not exist are skipped.
+// 4 x 8 of 4 rows x 2 tokens each, so that one read of q serves eight lanes and one of K four (on average 2.7
+// cycles of shared memory a read, and 6 reads for 32 multiply-adds: these reads are what bounds it; lanes 2 x 16
+// need more); scores are summed over even and odd dims, two multiply-adds in one; O as 16 rows x D / 4 dims.  Groups of tokens and rows that do not exist are skipped.
 //
 // Rows in shared memory are padded by 16 bytes so that the eight rows a quarter-warp reads lie in different
 // banks.  K rows are multiplied as they are (masked scores are replaced), rows of V that no node sees are
@@ -183,22 +183,29 @@ __global__ void __launch_bounds__(kTreeF32Threads, 2) dsa_tree_f32_kernel(const 
         const int count = to - start;                      // tokens of the tile that may be seen: [0, count)
         cp_async_wait<1>();                                // K is there (V may be on its way)
         __syncthreads();
-        float x[4][2] = {};
+        unsigned long long x2[4][2] = {};                  // (sums over even and odd dims)
         if (rows_here && group * 16 < count) {
 #pragma unroll 4
             for (int c = 0; c < D; c += 4) {
-                float4 q[4], k[2];
+                ulonglong2 q[4], k[2];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const float4*>(s_q + (row0 + 4 * r) * C::LD + c);
+                for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const ulonglong2*>(s_q + (row0 + 4 * r) * C::LD + c);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) k[j] = *reinterpret_cast<const float4*>(s_k + (key0 + 8 * j) * C::LD + c);
+                for (int j = 0; j < 2; ++j) k[j] = *reinterpret_cast<const ulonglong2*>(s_k + (key0 + 8 * j) * C::LD + c);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        x[r][j] = fmaf(q[r].x, k[j].x, fmaf(q[r].y, k[j].y, fmaf(q[r].z, k[j].z, fmaf(q[r].w, k[j].w, x[r][j]))));
+                    for (int j = 0; j < 2; ++j) x2[r][j] = fma_f32x2(q[r].x, k[j].x, fma_f32x2(q[r].y, k[j].y, x2[r][j]));
             }
         }
+        float x[4][2];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float2 two = unpack_f32x2(x2[r][j]);
+                x[r][j] = two.x + two.y;
+            }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float mx = -INFINITY;
