@@ -16,7 +16,8 @@
 // More rows: 32 query rows a block and tiles of 64 tokens.  A warp's scores are 16 rows x 16 tokens, its lanes
 // 4 x 8 of 4 rows x 2 tokens each, so that one read of q serves eight lanes and one of K four (on average 2.7
 // cycles of shared memory a read, and 6 reads for 32 multiply-adds: these reads are what bounds it; lanes 2 x 16
-// need more); scores are summed over even and odd dims, two multiply-adds in one; O as 16 rows x D / 4 dims.  Groups of tokens and rows that do not exist are skipped.
+// need more); scores are summed over even and odd dims, two multiply-adds in one; O as 16 rows x D / 4 dims.
+// Groups of tokens and rows that do not exist are skipped.
 //
 // Rows in shared memory are padded by 16 bytes so that the eight rows a quarter-warp reads lie in different
 // banks.  K rows are multiplied as they are (masked scores are replaced), rows of V that no node sees are

@@ -2,6 +2,10 @@
 attention, verification, accepted rows moved up in all layers, pages given back.  A small model whose greedy tokens the
 loop has to reproduce whatever the drafts are, in fp32 so that both ways of computing agree far better than two logits
 lie apart."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -255,3 +259,73 @@ def test_sampled_loop(dsa):
             assert path[r, :len(want)].tolist() == want and int(word[r]) == w
             assert int(m.seq[r]) == before[r] + len(want)
         last = word.tolist()
+
+
+CHILD = r"""
+import torch
+from paper_2609_19702_b200 import binding as dsa
+
+torch.manual_seed(0)
+i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+refs, table, seq, prompt = i32([1, 1, 1, 1] + [0] * 12), i32([[0, 1, -1, -1], [2, 3, -1, -1], [-1] * 4]), i32([30, 20, 0]), i32([4, 4, 0])
+pool, status = dsa.PagePool(refs, 16), i32([9, 9, 9])
+calls, state = [], [refs, table, seq, prompt, status]
+for dtype, d, hq, n, split in ((torch.bfloat16, 128, 8, 6, 0), (torch.bfloat16, 64, 2, 6, 64), (torch.float32, 64, 2, 4, 0),
+                               (torch.float32, 128, 8, 12, 0), (torch.float32, 128, 8, 4, 64)):
+    k, v = torch.randn((2, 16, 16, 2, d), device="cuda").to(dtype), torch.randn((2, 16, 16, 2, d), device="cuda").to(dtype)
+    prob = dsa.Problem(q=torch.randn((3, n, hq, d), device="cuda").to(dtype), k_cache=k, v_cache=v, strides=(32 * d, 2 * d, d), seq_len=seq,
+                       prompt_len=prompt, num_kv_heads=2, max_seq_len=64, block_table=table, block_size=16, num_blocks=16,
+                       split_tokens=split and 16)
+    tree = dsa.Tree(n)
+    out, lse = dsa.alloc_tree_outputs(prob)
+    args = (prob, None, tree, torch.randn((3, n, 2, d), device="cuda").to(dtype), torch.randn((3, n, 2, d), device="cuda").to(dtype), out, lse,
+            dsa.alloc_tree_workspace(prob, None, tree))
+    calls.append(lambda a=args: dsa.dsa_tree_step(*a))
+    state += [k, v, out, lse]
+flat = dsa.Problem(q=torch.zeros((3, 2, d), dtype=dtype, device="cuda"), k_cache=k, v_cache=v, strides=prob.strides, seq_len=seq, prompt_len=prompt,
+                   num_kv_heads=2, max_seq_len=64, block_table=table, block_size=16, num_blocks=16)
+for dtype in (torch.float32, torch.bfloat16):
+    for vocab in (1000, 30000, 230000):
+        for u in (None, torch.rand((3, 3)).cuda()):
+            probs = torch.softmax(torch.randn((3, 3, vocab), device="cuda") * 3, -1).to(dtype)
+            ver = dsa.Verify(probs.argmax(-1).roll(1, 1).int(), probs, None if u is None else probs.roll(1, 0), u)
+            outs = dsa.alloc_verify_outputs(ver)
+            calls.append(lambda a=(ver, dsa.Tree(3), *outs): dsa.dsa_verify_tree(*a))
+            state += list(outs)
+ws, one, two = dsa.alloc_fork_workspace(i32([0])), i32([0]), i32([2])
+keep, count, pages = i32([[0, 2, 3]] * 3), i32([3, 2, 0]), [i32([0]), i32([15])]
+calls = [lambda: dsa.dsa_reserve_pages(pool, table, seq, 16, status)] + calls + [
+    lambda: dsa.dsa_compact_kv(flat, keep, count, base=seq, len_out=seq, num_layers=2, stride_layer=k.stride(0)),
+    lambda: dsa.dsa_release_pages(pool, table, seq),
+    lambda: dsa.dsa_fork_pages(pool, flat, one, two, status[:1], ws, 2, k.stride(0)),
+    lambda: dsa.dsa_copy_pages(flat, *pages, 2, k.stride(0))]
+start = [t.clone() for t in state]
+torch.cuda.synchronize()
+
+dsa.dsa_prepare()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):          # the very first of these calls in this process
+    for call in calls:
+        call()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in state]
+for t, s in zip(state, start):
+    t.copy_(s)
+for call in calls:
+    call()
+torch.cuda.synchronize()
+bits = lambda t: t.contiguous().view(torch.uint8)
+for i, (a, b) in enumerate(zip(got, state)):
+    assert torch.equal(bits(a), bits(b)), i
+assert seq.tolist() == [33, 22, 33] and status[0] == 0 and dsa.dsa_wait_timeouts() == 0
+print("CAPTURED-FIRST-CALLS-OK")
+"""
+
+
+def test_first_calls_of_a_process_can_be_captured_after_prepare():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = dict(os.environ, PYTHONPATH=root + os.pathsep + os.environ.get("PYTHONPATH", ""))
+    res = subprocess.run([sys.executable, "-c", CHILD], cwd=root, env=env, capture_output=True, text=True, timeout=600)
+    assert res.returncode == 0, res.stdout[-2000:] + res.stderr[-4000:]
+    assert "CAPTURED-FIRST-CALLS-OK" in res.stdout
