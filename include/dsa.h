@@ -490,6 +490,10 @@ DSA_API int32_t dsa_tree_workspace_size(const dsa_problem *problem, const dsa_di
  *   hold anything.  A negative seq_len drops all nodes.
  *   A node whose page is missing (its entry in the block table is outside [0, num_blocks), after
  *   dsa_reserve_pages found none for instance) is computed, but its rows are stored nowhere.
+ *   dsa_verify_tree does not know which nodes have room and pages: a caller whose requests can run out of them
+ *   leaves such nodes out of node_count, on the device, between dsa_reserve_pages and this call (none where status[b] is not 0 or
+ *   seq_len[b] negative; else at most max_seq_len - seq_len[b]), and gives both calls the same.  dsa_compact_kv counts no
+ *   row that is missing.
  *   Cached rows that no node of the request sees may hold anything (NaN included); a NaN or infinity in
  *   the V row of a token that some node sees reaches the other nodes of the request as well.
  */
@@ -540,7 +544,9 @@ DSA_API int32_t dsa_verify_tree(const dsa_verify *verify, const dsa_tree *tree, 
  * position base[b] + i, in place.  keep [B, max_keep] device, ascending without repeats (so keep[b][i] >= i);
  * keep_count [B] device, clamped to [0, max_keep]; base [B] device, or NULL for 0.  After a verified tree:
  * base = seq_len, keep = path.  To drop tokens for good: base = NULL, keep = the positions that stay.
- * len_out [B] device or NULL: base[b] + (the clamped) keep_count[b]; may be seq_len, base or keep_count itself.
+ * len_out [B] device or NULL: base[b] + (the clamped) keep_count[b], but no further than the first kept row that the
+ * cache does not have or has no place for (a position outside [0, max_seq_len) or without a page): a length never counts
+ * rows that were stored nowhere.  It may be seq_len, base or keep_count itself.
  * The cache is that of `problem` (q and max_seq_len's sense as elsewhere: rows at positions outside
  * [0, max_seq_len), or whose page is missing, are neither read nor written; refused for bounded caches); with num_layers > 1 the
  * layers' caches lie stride_layer elements apart behind k_cache and v_cache and one call serves all of them.

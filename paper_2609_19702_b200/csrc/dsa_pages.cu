@@ -35,6 +35,22 @@ __device__ __forceinline__ int64_t piece_offset(const CacheArgs& c, int col) {
     return ((int64_t)head * c.a.stride_head) * c.esize + (int64_t)(col - head * c.head_vecs) * 16;
 }
 
+// Whether the cache has the token at position `pos` of request b.
+__device__ __forceinline__ bool row_in_cache(const CacheArgs& c, int b, int64_t pos) {
+    return pos >= 0 && pos < c.a.max_seq_len && token_has_page(c.a, b, (int)pos);
+}
+
+// How many kept rows of a request, from the first one on, the cache has and has a place for: what its length may
+// count.  By a whole block; s_stored is shared.
+__device__ __forceinline__ int rows_stored(const CacheArgs& c, int b, int64_t first, const int* list, int count, int* s_stored) {
+    if (threadIdx.x == 0) *s_stored = count;
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += blockDim.x)
+        if (!row_in_cache(c, b, first + list[i]) || !row_in_cache(c, b, first + i)) { atomicMin(s_stored, i); break; }
+    __syncthreads();
+    return *s_stored;
+}
+
 // ---- rows of a request move up ----------------------------------------------------------------------
 // One block: 128 of the 16-byte columns of one request's rows, in `planes` of the layers' K and V caches, and one
 // stretch of kListRows rows of the list; the rows' places (page lookups) are worked out once and shared by the planes.
@@ -49,7 +65,7 @@ __global__ void __launch_bounds__(kCopyThreads, 8) dsa_compact_kernel(const Cach
                                                                       int planes, int plane_groups, int stretches, int layers,
                                                                       int* len_out) {
     __shared__ int64_t s_src[kListRows], s_dst[kListRows];
-    __shared__ int s_n, s_first;
+    __shared__ int s_n, s_first, s_stored;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31;
     int idx = blockIdx.x;
@@ -60,7 +76,10 @@ __global__ void __launch_bounds__(kCopyThreads, 8) dsa_compact_kernel(const Cach
     const int* list = keep + (int64_t)b * max_keep;
     const int count = max(0, min(keep_count[b], max_keep));
     const int64_t first = base ? base[b] : 0;
-    if (len_out && idx == b * stretches && blockIdx.x % (col_blocks * plane_groups) == 0 && tid == 0) len_out[b] = (int)first + count;
+    if (len_out && idx == b * stretches && blockIdx.x % (col_blocks * plane_groups) == 0) {
+        const int stored = rows_stored(c, b, first, list, count, &s_stored);
+        if (tid == 0) len_out[b] = (int)first + stored;
+    }
     if (stretch * kListRows >= count) return;
     // the prefix that stays (keep[i] - i never falls)
     if (tid == 0) s_first = count;
@@ -85,8 +104,7 @@ __global__ void __launch_bounds__(kCopyThreads, 8) dsa_compact_kernel(const Cach
                 int64_t src = 0, dst = 0;
                 if (i < to) {
                     const int64_t at = first + list[i], goal = first + i;
-                    moves = at != goal && at >= 0 && at < c.a.max_seq_len && goal >= 0 && goal < c.a.max_seq_len &&
-                            token_has_page(c.a, b, (int)at) && token_has_page(c.a, b, (int)goal);
+                    moves = at != goal && row_in_cache(c, b, at) && row_in_cache(c, b, goal);
                     if (moves) {
                         src = token_offset(c.a, b, 0, (int)at) * c.esize;
                         dst = token_offset(c.a, b, 0, (int)goal) * c.esize;
@@ -132,9 +150,12 @@ __global__ void __launch_bounds__(kCopyThreads, 8) dsa_compact_kernel(const Cach
     }
 }
 
-__global__ void dsa_compact_len_kernel(const int* base, const int* keep_count, int max_keep, int batch, int* len_out) {
-    const int b = blockIdx.x * blockDim.x + threadIdx.x;
-    if (b < batch) len_out[b] = (base ? base[b] : 0) + max(0, min(keep_count[b], max_keep));
+__global__ void __launch_bounds__(kCopyThreads) dsa_compact_len_kernel(const CacheArgs c, const int* base, const int* keep,
+                                                                       const int* keep_count, int max_keep, int* len_out) {
+    __shared__ int s_stored;
+    const int b = blockIdx.x, first = base ? base[b] : 0;
+    const int stored = rows_stored(c, b, first, keep + (int64_t)b * max_keep, max(0, min(keep_count[b], max_keep)), &s_stored);
+    if (threadIdx.x == 0) len_out[b] = first + stored;     // (every thread has read base and keep_count, which it may be)
 }
 
 // ---- whole or part-filled pages --------------------------------------------------------------------------
@@ -544,8 +565,8 @@ int32_t dsa_compact_kv(const dsa_problem* problem, int32_t num_layers, int64_t s
     }
     // (a launch of its own where len_out is base or keep_count, which every block of the other one reads)
     if (own_launch)
-        rc = launch(dsa_compact_len_kernel, (problem->batch + 255) / 256, 256, 0, st, false, base, keep_count, (int)max_keep,
-                    (int)problem->batch, len_out);
+        rc = launch(dsa_compact_len_kernel, problem->batch, kCopyThreads, 0, st, false, c, base, keep, keep_count, (int)max_keep,
+                    len_out);
     return rc;
 }
 

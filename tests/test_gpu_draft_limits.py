@@ -1,0 +1,166 @@
+"""Decoding with drafted tokens where pages or room run out: lengths count nothing that was stored nowhere, and a loop that
+leaves nodes without room out of node_count gives the model's tokens all the same."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_draft_loop import CAP, LAYERS, PAGE, V, Model, _drafts, _rows, _sequential
+from tests.test_gpu_pages import Cache, _int
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dsa():
+    from paper_2609_19702_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("where", ["apart", "base", "counts"])
+def test_lengths_stop_at_rows_that_are_nowhere(dsa, where):
+    """Rows whose own place or the one they go to lies outside the cache or has no page end the kept ones."""
+    page, m = 8, 12
+    c = Cache(dsa, 9, m, page)
+    for r, e in ((1, 4), (2, 2), (3, 0), (5, 11), (8, 3)):
+        c.table[r, e] = -1
+    c.table[4, 5] = 10 ** 6
+    lists = [list(range(0, 80, 2)) for _ in range(9)]
+    lists[6] = list(range(40))                                     # nothing moves
+    lists[7] = list(range(10)) + list(range(60, 90))
+    lists[8] = list(range(40))                                     # nothing moves, but a page is missing
+    base = [3, 0, 6, 0, 1, 7, 50, 12, 5]
+    counts = [40, 40, 40, 40, 40, 40, 40, 99, 30]
+    want = []
+    for r in range(9):
+        kept = min(counts[r], 40)
+        gone = [i for i in range(kept) for at in (base[r] + lists[r][i], base[r] + i)
+                if not (at < m * page and 0 <= int(c.table[r, at // page]) < c.problem.num_blocks)]
+        want.append(base[r] + min(gone + [kept]))
+    assert want == [43, 16, 11, 0, 21, 47, 90, 46, 24]
+    first, keep, n = _int(base), _int(lists), _int(counts)
+    out = {"apart": _int([0] * 9), "base": first, "counts": n}[where]
+    dsa.dsa_compact_kv(c.problem, keep, n, base=first, len_out=out)
+    assert out.tolist() == want
+
+
+def test_lengths_of_long_lists(dsa):
+    # the missing page lies behind several stretches of the list; and positions outside the cache
+    c = Cache(dsa, 4, 200, 4)
+    c.table[0, 160] = c.table[1, 199] = c.table[2, 0] = -1
+    keep = [list(range(100, 700)), list(range(200, 800)), list(range(600)), list(range(201, 801))]
+    out = _int([7] * 4)
+    dsa.dsa_compact_kv(c.problem, _int(keep), _int([600] * 4), len_out=out)
+    assert out.tolist() == [540, 596, 0, 599]
+    dsa.dsa_compact_kv(c.problem, _int([[0, 1]] * 4), _int([2] * 4), base=_int([798, 799, -1, 2 ** 31 - 1]), len_out=out)
+    assert out.tolist() == [800, 799, -1, 2 ** 31 - 1]
+
+
+def _loop(dsa, m, rng, last, out, truth, gate, passes, between=None):
+    """Passes of the loop; `gate`: nodes without room or pages are left out of node_count."""
+    b, n = m.b, m.n
+    parent, tokens, depth = (torch.zeros((b, n), dtype=torch.int32, device="cuda") for _ in range(3))
+    count = torch.full((b,), n, dtype=torch.int32, device="cuda")
+    tree = dsa.Tree(n, parent=parent, node_count=count)
+    logits = torch.zeros((b, n, V), device="cuda")
+    ver = dsa.Verify(tokens, logits)
+    path, accepted, word = dsa.alloc_verify_outputs(ver)
+    for step in range(passes):
+        p, t, d = _drafts(rng, last, truth, [len(o) for o in out], n)
+        for x, y in zip((parent, tokens, depth), (p, t, d)):
+            x.copy_(torch.from_numpy(y))
+        m.reserve(n)
+        if gate:
+            count.copy_(torch.where((m.status == 0) & (m.seq >= 0), (CAP - m.seq).clamp(0, n), 0))
+        logits.copy_(m.tree_logits(tokens.long(), depth.long().clamp(max=15), tree))
+        dsa.dsa_verify_tree(ver, tree, path, accepted, word)
+        m.settle(path, accepted)
+        for r in range(b):
+            k = int(accepted[r])
+            if k:
+                out[r] += [int(t[r, i]) for i in path[r, 1:k].tolist()] + [int(word[r])]
+                last[r] = out[r][-1]
+        if between is not None:
+            between(step)
+
+
+@pytest.mark.parametrize("nodes", [3, 7])
+def test_a_pool_that_runs_out(dsa, nodes):
+    """Two requests share too few pages.  The one that gets none waits with no nodes, and goes on when the other's are given
+    back; what it says in the end is what it says alone."""
+    first, steps = [3, 17], 45
+    truth, ref = _sequential(dsa, first, steps + nodes + 1)
+    m = Model(dsa, 2, nodes)
+    free = (m.refs == 0).nonzero()[:, 0]
+    m.refs[free[9:]] = 1                                           # nine pages are left: not enough for both
+    rng, out, last = np.random.default_rng(nodes), [[], []], list(first)
+    lengths, waited = [], []
+
+    def between(step):
+        lengths.append(m.seq.tolist())
+        waited.append(m.status.tolist())
+
+    _loop(dsa, m, rng, last, out, truth, True, 12, between)
+    assert any(s != [0, 0] for s in waited)
+    for r in range(2):
+        assert out[r] == truth[r][:len(out[r])].tolist() and int(m.seq[r]) == len(out[r])
+    far = max(range(2), key=lambda r: len(out[r]))                 # the request that is further gives all of its pages back
+    other = 1 - far
+    keep = torch.full((2,), -1, dtype=torch.int32, device="cuda")
+    keep[far] = 0
+    dsa.dsa_release_pages(m.pool, m.table, keep)
+    m.seq[far] = -1                                                # (and is no longer served)
+    had = len(out[other])
+    _loop(dsa, m, rng, last, out, truth, True, 4)
+    assert len(out[other]) > had and int(m.seq[far]) == -1
+    assert out[other] == truth[other][:len(out[other])].tolist()
+    for a, b in zip(_rows(m, other, int(m.seq[other])), _rows(ref, other, int(m.seq[other]))):
+        assert torch.allclose(a, b, rtol=1e-4, atol=1e-4)
+    assert dsa.dsa_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("nodes", [2, 7])
+def test_lengths_without_the_gate(dsa, nodes):
+    """A caller who does not gate: some tokens of the answer are lost to it, but no length counts a row without a page or
+    beyond the cache, so that later passes read nothing that is another request's."""
+    first = [3, 17, 42]
+    truth, _ = _sequential(dsa, first, 50)
+    m = Model(dsa, 3, nodes)
+    free = (m.refs == 0).nonzero()[:, 0]
+    m.refs[free[20:]] = 1
+    rng, out, last = np.random.default_rng(nodes), [[], [], []], list(first)
+    before, seen = [[0, 0, 0]], []
+
+    def between(step):
+        now = m.seq.tolist()
+        seen.append(m.status.tolist())
+        for r in range(3):
+            assert before[0][r] <= now[r] <= CAP
+            pages = m.table[r, :-(-now[r] // PAGE)]
+            assert ((pages >= 0) & (pages < m.refs.numel())).all()
+            for rows in _rows(m, r, now[r]):                       # every row that is counted was stored (the cache began as NaN)
+                assert torch.isfinite(rows).all()
+        before[0] = now
+        for o in out:
+            del o[40:]                                             # (drafts are taken from a table of 50 tokens)
+
+    _loop(dsa, m, rng, last, out, truth, False, 40, between)
+    assert any(s != [0, 0, 0] for s in seen)
+    assert dsa.dsa_wait_timeouts() == 0
+
+
+def test_a_request_that_reaches_the_end_of_the_cache(dsa):
+    nodes, first = 5, [3, 17]
+    truth, _ = _sequential(dsa, first, CAP)
+    m = Model(dsa, 2, nodes)
+    rng, out, last = np.random.default_rng(2), [[], []], list(first)
+
+    def between(step):
+        assert max(m.seq.tolist()) <= CAP
+        for r in range(2):                                         # (drafts beyond the model's tokens are not looked up)
+            assert len(out[r]) <= len(truth[r])
+
+    _loop(dsa, m, rng, last, out, np.concatenate([truth, np.zeros((2, nodes), truth.dtype)], 1), True, 60, between)
+    for r in range(2):
+        assert int(m.seq[r]) == len(out[r]) > CAP - nodes
+        assert out[r] == truth[r][:len(out[r])].tolist()
+    assert m.status.tolist() != [0, 0] and LAYERS > 1
