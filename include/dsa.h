@@ -594,7 +594,8 @@ DSA_API int32_t dsa_release_pages(const dsa_page_pool *pool, int32_t *block_tabl
  * own; rows within the shared length are not to be written again (moved, or taken back and appended anew) while the
  * other lives.
  * status[i]: 0; 1: no free page was left for it, nothing was changed; 2: refused, nothing was changed:
- * src[i] or dst[i] is no row of the table, or dst[i] is also src or an earlier dst of the same call.
+ * src[i] or dst[i] is no row of the table, a page within src[i]'s length is missing (its entry is outside
+ * [0, num_blocks)), or dst[i] is also src or an earlier dst of the same call.
  * workspace: 16 * n bytes, 256-byte aligned.  num_layers, stride_layer as for dsa_compact_kv.
  */
 DSA_API int32_t dsa_fork_pages(const dsa_page_pool *pool, const dsa_problem *problem, int32_t num_layers,

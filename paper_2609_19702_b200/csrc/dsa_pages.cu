@@ -243,8 +243,9 @@ __device__ __forceinline__ int free_pages(const int* ref_count, int num_blocks, 
 __global__ void __launch_bounds__(kPoolThreads) dsa_fork_plan_kernel(const ForkArgs f) {
     __shared__ int s_warp[32];
     __shared__ int s_src[kPoolThreads], s_dst[kPoolThreads];
+    __shared__ bool s_bad[kPoolThreads];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // fresh pages wanted, in order; an item's rank among them is kept in to_page until the pages are known
     int want = 0;
     for (int i0 = 0; i0 < f.n; i0 += kPoolThreads) {
@@ -261,6 +262,24 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_fork_plan_kernel(const ForkA
             if (ok)
                 for (int j = 0; j < min(kPoolThreads, f.n - j0); ++j) ok = ok && s_src[j] != d && (j0 + j >= i || s_dst[j] != d);
         }
+        // every page within the source's length has to be there: a warp per branch looks its row through
+        __syncthreads();
+        s_src[tid] = s;
+        s_dst[tid] = ok ? len / f.block_size + (len % f.block_size != 0) : 0;
+        __syncthreads();
+        for (int j = warp; j < min(kPoolThreads, f.n - i0); j += 32) {
+            const int* row = f.table + (int64_t)s_src[j] * f.max_blocks;
+            bool bad = false;
+#pragma unroll 4
+            for (int e = lane; e < s_dst[j]; e += 32) {
+                const int id = row[e];
+                bad |= id < 0 || id >= f.num_blocks;
+            }
+            bad = __any_sync(0xffffffffu, bad);
+            if (lane == 0) s_bad[j] = bad;
+        }
+        __syncthreads();
+        ok = ok && !s_bad[tid];
         if (ok) {
             it.tokens = len % f.block_size;
             it.from_page = it.tokens ? f.table[(int64_t)s * f.max_blocks + len / f.block_size] : 0;

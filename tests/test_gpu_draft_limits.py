@@ -55,6 +55,44 @@ def test_lengths_of_long_lists(dsa):
     assert out.tolist() == [800, 799, -1, 2 ** 31 - 1]
 
 
+@pytest.mark.parametrize("rows,m", [(6, 6), (1300, 70)])
+def test_a_source_without_its_pages_is_not_branched(dsa, rows, m):
+    """A page that is missing within the source's length (the part-filled last one, or one in front of it): the branch is
+    refused and nothing changes; what is missing behind the length matters to nobody."""
+    page, hkv = 4, 1
+    held = min(m, 6)                                               # pages that a source has
+    lens = [held * page - 2] * rows + [0] * rows
+    table = np.full((2 * rows, m), -1, np.int32)
+    table[:rows, :held] = np.arange(rows * held).reshape(rows, held)
+    blocks = rows * held + rows
+    c = Cache(dsa, 2 * rows, m, page, blocks=blocks, hkv=hkv, table=table, lens=lens)
+    was = np.array(table)
+    for r, (e, x) in {0: (held - 1, -1), 1: (0, -1), 2: (2, blocks), 3: (1, 10 ** 9), rows - 1: (held - 2, -5)}.items():
+        was[r, e] = x
+    c.table.copy_(torch.from_numpy(was))
+    refs = np.zeros(blocks, np.int32)
+    refs[:rows * held] = 1
+    pool, status = dsa.PagePool(torch.from_numpy(refs).cuda(), page), _int([9] * rows)
+    src, dst = list(range(rows)), list(range(2 * rows - 1, rows - 1, -1))
+    dsa.dsa_fork_pages(pool, c.problem, _int(src), _int(dst), status, dsa.alloc_fork_workspace(status))
+    bad = {0, 1, 2, 3, rows - 1}
+    assert status.tolist() == [2 if r in bad else 0 for r in src]
+    want, fresh = np.array(was), rows * held
+    for r in src:
+        if r in bad:
+            continue
+        want[dst[r], :held] = was[r, :held]
+        want[dst[r], held - 1] = fresh
+        refs[was[r, :held - 1]] += 1
+        refs[fresh] = 1
+        lens[dst[r]] = lens[r]
+        for t in c.host:
+            t[:, fresh, :page - 2] = t[:, was[r, held - 1], :page - 2]
+        fresh += 1
+    assert np.array_equal(c.table.cpu().numpy(), want) and pool.ref_count.tolist() == refs.tolist()
+    assert c.seq.tolist() == lens and c.same()
+
+
 def _loop(dsa, m, rng, last, out, truth, gate, passes, between=None):
     """Passes of the loop; `gate`: nodes without room or pages are left out of node_count."""
     b, n = m.b, m.n
