@@ -557,7 +557,7 @@ DSA_API int32_t dsa_compact_kv(const dsa_problem *problem, int32_t num_layers, i
                                const int32_t *base, const int32_t *keep, const int32_t *keep_count, int32_t max_keep,
                                int32_t *len_out, void *stream);
 
-/* The pages of a paged cache: a page is free while its count is 0.  Pages are taken lowest index first, so
+/* The pages of a paged cache: a page is free while its count is 0 (a negative one is left as it is).  Pages are taken lowest index first, so
  * that equal calls give equal tables.  All arrays on the device; the caller zeroes ref_count to begin with
  * (and fills block tables with -1, the mark of an entry without a page).  Calls on one pool are ordered by
  * the caller: one stream, or events. */

@@ -393,6 +393,10 @@ __global__ void dsa_release_kernel(int* table, int max_blocks, const int* keep_t
     }
 }
 
+// A granted page is marked with its row's entry in its count until the tables are written.  The marks are the lowest
+// numbers there are: a count that is negative already is none of them, and its page is not free either.
+constexpr int kMark = -0x7fffffff - 1;             // + entry, below max_blocks
+
 // Pages for rows that lack some: one block.  Dynamic shared memory: per row its first lacking entry and the
 // running sum of what rows lack (3 ints per row).
 __global__ void __launch_bounds__(kPoolThreads) dsa_reserve_kernel(int* table, int batch, int max_blocks, const int* seq_len,
@@ -484,7 +488,7 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_reserve_kernel(int* table, i
             for (; e < max_blocks - 1; ++e)
                 if (row[e] < 0 && k-- == 0) break;
         }
-        ref_count[page] = -1 - e;                  // (marked; the tables are written when all ranks have counted)
+        ref_count[page] = kMark + e;               // (the tables are written when all ranks have counted)
     });
     __syncthreads();
     // the marked pages are the first `granted` free ones, in order: rank and row again
@@ -495,16 +499,15 @@ __global__ void __launch_bounds__(kPoolThreads) dsa_reserve_kernel(int* table, i
         if (p < num_blocks) {
             eight_counts(ref_count, (int)p, num_blocks, r);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) mine += r[k] < 0;
+            for (int k = 0; k < 8; ++k) mine += r[k] < kMark + max_blocks;
         }
         int n;
         int rank = at + block_prefix(mine, s_warp, n);
         if (p < num_blocks)
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (r[k] < 0) {
-                    const int e = -1 - r[k];       // (a count that was negative to begin with is no mark)
-                    if (rank < granted && e < max_blocks) table[(int64_t)row_of(rank) * max_blocks + e] = (int)p + k;
+                if (r[k] < kMark + max_blocks) {
+                    if (rank < granted) table[(int64_t)row_of(rank) * max_blocks + (r[k] - kMark)] = (int)p + k;
                     ref_count[p + k] = 1;
                     ++rank;
                 }

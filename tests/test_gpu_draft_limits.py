@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests import draft_ref
 from tests.test_gpu_draft_loop import CAP, LAYERS, PAGE, V, Model, _drafts, _rows, _sequential
 from tests.test_gpu_pages import Cache, _int
 
@@ -91,6 +92,26 @@ def test_a_source_without_its_pages_is_not_branched(dsa, rows, m):
         fresh += 1
     assert np.array_equal(c.table.cpu().numpy(), want) and pool.ref_count.tolist() == refs.tolist()
     assert c.seq.tolist() == lens and c.same()
+
+
+@pytest.mark.parametrize("blocks", [40, 20000])
+def test_reserve_passes_over_negative_counts(dsa, blocks):
+    """A count below 0 (a caller's own mark, say) is no free page, stays as it is and shifts nobody's pages."""
+    rng = np.random.default_rng(blocks)
+    rows, m, page = 12, 5, 4
+    refs = np.where(rng.random(blocks) < 0.4, -rng.integers(1, 9, size=blocks), 0).astype(np.int32)
+    refs[0], refs[1], refs[-1] = -1, -(2 ** 31) + m, -3
+    table = np.full((rows, m), -1, np.int32)
+    table[3, 1] = 2                                                # (a row with a hole)
+    refs[2] = 1
+    lens = rng.integers(0, 2 * page, size=rows).tolist()
+    lens[3] = 3 * page
+    pool, dt, status = dsa.PagePool(torch.from_numpy(refs).cuda(), page), torch.from_numpy(table).cuda(), _int([9] * rows)
+    dsa.dsa_reserve_pages(pool, dt, _int(lens), 0, status)
+    model = draft_ref.Pool(refs, table, page)
+    assert status.tolist() == model.reserve(lens, 0)               # (the small pool runs out)
+    assert dt.tolist() == model.table and pool.ref_count.tolist() == model.refs
+    assert (refs < 0).sum() == sum(x < 0 for x in model.refs)
 
 
 def _loop(dsa, m, rng, last, out, truth, gate, passes, between=None):
