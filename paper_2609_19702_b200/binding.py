@@ -208,7 +208,7 @@ def _dtype_code(t: torch.Tensor) -> int:
 @dataclass
 class Problem:
     """Device tensors and host-side sizes of one decode-attention call (see dsa_problem)."""
-    q: torch.Tensor                       # [B, H_q, D] (dsa_tree_step: [B, N, H_q, D])
+    q: torch.Tensor                       # [B, H_q, D] (dsa_tree_step: [B, N, H_q, D]; row and page calls: either)
     k_cache: torch.Tensor                 # any shape; addressed through `strides`
     v_cache: torch.Tensor
     strides: tuple                        # (stride_batch_or_block, stride_token, stride_head), elements
@@ -584,9 +584,11 @@ def _tree_problem(problem: Problem, tree: Tree) -> bytes:
 
 
 def _cache_problem(problem: Problem) -> bytes:
-    b, hq, d = problem.q.shape
-    _rows(problem, b)
-    return problem._packed(b, hq, d)
+    shape = problem.q.shape                      # of one token a request, or of a tree's nodes: its values are not used
+    if len(shape) not in (3, 4):
+        raise ValueError("q must be [batch, heads, head_dim] or [batch, max_nodes, heads, head_dim]")
+    _rows(problem, shape[0])
+    return problem._packed(shape[0], shape[-2], shape[-1])
 
 
 def dsa_tree_workspace_size(problem: Problem, diag: Optional[Diag], tree: Tree) -> int:

@@ -193,3 +193,18 @@ def test_references_by_hand():
     assert draft_ref.verify_reference([0, 0], p, dq, [0.3, 0.6], [-1, 0], 2, "sample") == ([0], 1)
     assert draft_ref.verify_reference([0, 1], p, None, [0.3, 0.6], [-1, 0], 2, "point") == ([0], 0)
     assert draft_ref.verify_reference([0, 1], p, None, None, [-1, 0], 2, "greedy") == ([0], 0)
+
+
+def test_row_and_page_calls_take_a_trees_problem(dsa, monkeypatch):
+    """The problem of a tree call, whose q has a row per node, describes the cache to the calls behind it as well."""
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    cache = torch.zeros((6, 16, 2, 64))
+    monkeypatch.setattr(dsa.Problem, "_packed", lambda self, b, hq, d: (b, hq, d))
+
+    def problem(*shape):
+        return dsa.Problem(q=torch.zeros(shape), k_cache=cache, v_cache=cache, strides=(2048, 128, 64), seq_len=i(3), prompt_len=i(3),
+                           num_kv_heads=2, max_seq_len=32, block_table=i(3, 2), block_size=16, num_blocks=6)
+    assert dsa._cache_problem(problem(3, 5, 4, 64)) == dsa._cache_problem(problem(3, 4, 64)) == (3, 4, 64)
+    for bad in ((3, 64), (2, 3, 5, 4, 64), (4, 5, 4, 64)):
+        with pytest.raises(ValueError):
+            dsa._cache_problem(problem(*bad))

@@ -1,5 +1,8 @@
 """Decoding with drafted tokens where pages or room run out: lengths count nothing that was stored nowhere, and a loop that
 leaves nodes without room out of node_count gives the model's tokens all the same."""
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -223,3 +226,42 @@ def test_a_request_that_reaches_the_end_of_the_cache(dsa):
         assert int(m.seq[r]) == len(out[r]) > CAP - nodes
         assert out[r] == truth[r][:len(out[r])].tolist()
     assert m.status.tolist() != [0, 0] and LAYERS > 1
+
+
+def test_the_documented_loop_runs(dsa):
+    """README's pass with drafted tokens, as it stands there, twice: the second one behind the lengths of the first."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "README.md")).read()
+    code = next(x for x in re.findall(r"```python\n(.*?)```", text, flags=re.S) if "dsa_tree_step" in x)
+    b, n, hq, hkv, d, layers, vocab, s_max = 3, 5, 4, 2, 128, 2, 50, 96
+    blocks = 20
+    g = torch.Generator().manual_seed(0)
+    rand = lambda *s: torch.randn(s, generator=g).bfloat16().cuda()  # noqa: E731
+    k, v = rand(layers, blocks, 16, hkv, d), rand(layers, blocks, 16, hkv, d)
+    seq = _int([30, 16, -1])                                       # (row 2 is free for a branch)
+    table = torch.full((b, s_max // 16), -1, dtype=torch.int32, device="cuda")
+    table[0, :2], table[1, 0] = _int([4, 7]), 2
+    refs = _int([0] * blocks)
+    refs[_int([2, 4, 7]).long()] = 1
+    probs = torch.softmax(torch.randn((b, n, vocab), generator=g) * 3, -1).cuda()
+    names = dict(dsa=dsa, torch=torch, N=n, S_max=s_max, L=layers, layer_stride=k.stride(0), diag=None, block_table=table, seq_len=seq,
+                 ref_count=refs, parent=_int([[-1, 0, 0, 1, 2]] * b), count=_int([0] * b), status=_int([9] * b), k_new=rand(b, n, hkv, d),
+                 v_new=rand(b, n, hkv, d), tokens=_int([[0, 1, 2, 3, 4]] * b), target_probs=probs, draft_probs=probs.roll(1, 0),
+                 uniforms=torch.rand((b, n), generator=g).cuda(), path=_int([[9] * n] * b), accepted=_int([9] * b), next_token=_int([9] * b),
+                 src=_int([0]), dst=_int([2]), forked=_int([9]))
+    names["layers"] = [dsa.Problem(q=rand(b, n, hq, d), k_cache=k[i], v_cache=v[i], strides=k[i].stride()[:3], seq_len=seq,
+                                   prompt_len=_int([0] * b), num_kv_heads=hkv, max_seq_len=s_max, block_table=table, block_size=16,
+                                   num_blocks=blocks) for i in range(layers)]
+    names["out"], names["lse"] = dsa.alloc_tree_outputs(names["layers"][0])
+    names["ws"] = dsa.alloc_tree_workspace(names["layers"][0], None, dsa.Tree(n))
+    for _ in range(2):
+        before = seq.tolist()
+        exec(code, names)
+        torch.cuda.synchronize()
+        stands = names["accepted"].tolist()
+        assert names["status"].tolist() == [0] * b and names["forked"].tolist() == [0] and min(stands[:2]) >= 1 and stands[2] == 0
+        assert seq.tolist() == [before[0] + stands[0], before[1] + stands[1], before[0] + stands[0]]     # (a branch of row 0)
+        assert torch.isfinite(names["out"]).all() and names["next_token"].tolist()[2] == -1 and int(names["next_token"][:2].min()) >= 0
+        dsa.dsa_release_pages(names["pool"], table, torch.where(torch.arange(b).cuda() == 2, 0, -1).int())
+        seq[2] = -1
+    assert dsa.dsa_wait_timeouts() == 0
