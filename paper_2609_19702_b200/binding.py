@@ -571,6 +571,8 @@ class Tree:
 
 def _rows(problem: Problem, b: int) -> None:
     bt = problem.block_table
+    if problem.k_cache.dtype != problem.q.dtype or problem.v_cache.dtype != problem.q.dtype:
+        raise ValueError("k_cache and v_cache must be of q's type")
     if problem.seq_len.shape != (b,) or problem.prompt_len.shape != (b,) or (bt is not None and bt.shape[0] != b):
         raise ValueError("seq_len, prompt_len and block_table must have one row per request")
 

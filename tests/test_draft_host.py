@@ -208,3 +208,34 @@ def test_row_and_page_calls_take_a_trees_problem(dsa, monkeypatch):
     for bad in ((3, 64), (2, 3, 5, 4, 64), (4, 5, 4, 64)):
         with pytest.raises(ValueError):
             dsa._cache_problem(problem(*bad))
+
+
+def _small(dsa, q, cache, v=None, seq=None, prompt=None):
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    return dsa.Problem(q=q, k_cache=cache, v_cache=cache if v is None else v, strides=(2048, 128, 64), seq_len=i(3) if seq is None else seq,
+                       prompt_len=i(3) if prompt is None else prompt, num_kv_heads=2, max_seq_len=32, block_table=i(3, 2), block_size=16,
+                       num_blocks=6)
+
+
+def _every_cache_call(dsa, problem):
+    """The calls that take a problem's cache, each as a function."""
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    one, pool = i(1), dsa.PagePool(i(6), 16)
+    n = 5
+    q = torch.zeros((3, n, 4, 64), dtype=problem.q.dtype)
+    tree = dsa.Problem(**{**problem.__dict__, "q": q})
+    new = torch.zeros((3, n, 2, 64), dtype=q.dtype)
+    yield lambda: dsa.dsa_tree_workspace_size(tree, None, dsa.Tree(n))
+    yield lambda: dsa.dsa_tree_step(tree, None, dsa.Tree(n), new, new, torch.zeros_like(q), torch.zeros((3, n, 4)))
+    yield lambda: dsa.dsa_compact_kv(problem, i(3, n), i(3))
+    yield lambda: dsa.dsa_fork_pages(pool, problem, one, one, one, torch.zeros(16, dtype=torch.uint8))
+    yield lambda: dsa.dsa_copy_pages(problem, one, one)
+
+
+def test_binding_refuses_a_cache_of_another_type(dsa):
+    """q's type says how wide the cache's elements are: with another one every address would be off."""
+    bf, f32 = torch.zeros((6, 16, 2, 64), dtype=torch.bfloat16), torch.zeros((6, 16, 2, 64))
+    for q, k, v in ((torch.float32, bf, bf), (torch.bfloat16, f32, f32), (torch.float32, f32, bf), (torch.bfloat16, f32, bf)):
+        for call in _every_cache_call(dsa, _small(dsa, torch.zeros((3, 4, 64), dtype=q), k, v)):
+            with pytest.raises(ValueError, match="type"):
+                call()
