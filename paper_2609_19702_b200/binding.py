@@ -575,6 +575,8 @@ def _rows(problem: Problem, b: int) -> None:
         raise ValueError("k_cache and v_cache must be of q's type")
     if problem.seq_len.shape != (b,) or problem.prompt_len.shape != (b,) or (bt is not None and bt.shape[0] != b):
         raise ValueError("seq_len, prompt_len and block_table must have one row per request")
+    if not (problem.seq_len.is_contiguous() and problem.prompt_len.is_contiguous()):
+        raise ValueError("seq_len and prompt_len must be contiguous")
 
 
 def _tree_problem(problem: Problem, tree: Tree) -> bytes:

@@ -239,3 +239,14 @@ def test_binding_refuses_a_cache_of_another_type(dsa):
         for call in _every_cache_call(dsa, _small(dsa, torch.zeros((3, 4, 64), dtype=q), k, v)):
             with pytest.raises(ValueError, match="type"):
                 call()
+
+
+def test_binding_refuses_strided_lengths(dsa):
+    """Lengths that are a column of something, or one number for all requests, are not the array that the library reads."""
+    cache = torch.zeros((6, 16, 2, 64))
+    column, one = torch.zeros((3, 2), dtype=torch.int32)[:, 0], torch.zeros((1,), dtype=torch.int32).expand(3)
+    for bad in (column, one):
+        for kw in (dict(seq=bad), dict(prompt=bad)):
+            for call in _every_cache_call(dsa, _small(dsa, torch.zeros((3, 4, 64)), cache, **kw)):
+                with pytest.raises(ValueError, match="contiguous"):
+                    call()
