@@ -541,7 +541,8 @@ DSA_API int32_t dsa_verify_tree(const dsa_verify *verify, const dsa_tree *tree, 
 
 /*
  * Moves kept tokens together: for i < keep_count[b] the K and V rows at position base[b] + keep[b][i] go to
- * position base[b] + i, in place.  keep [B, max_keep] device, ascending without repeats (so keep[b][i] >= i);
+ * position base[b] + i, in place.  keep [B, max_keep] device, ascending without repeats (so keep[b][i] >= i; max_keep at
+ * most 2^30, B * max_keep at most 2^32);
  * keep_count [B] device, clamped to [0, max_keep]; base [B] device, or NULL for 0.  After a verified tree:
  * base = seq_len, keep = path.  To drop tokens for good: base = NULL, keep = the positions that stay.
  * len_out [B] device or NULL: base[b] + (the clamped) keep_count[b], but no further than the first kept row that the

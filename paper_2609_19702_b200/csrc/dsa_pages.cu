@@ -567,7 +567,7 @@ int32_t dsa_compact_kv(const dsa_problem* problem, int32_t num_layers, int64_t s
     int32_t rc = cache_args(problem, num_layers, stride_layer, &c);
     if (rc != DSA_OK) return rc;
     if (max_keep < 0) return DSA_ERR_INVALID_ARG;
-    if ((int64_t)problem->batch * max_keep > (1LL << 32)) return DSA_ERR_UNSUPPORTED;
+    if (max_keep > (1 << 30) || (int64_t)problem->batch * max_keep > (1LL << 32)) return DSA_ERR_UNSUPPORTED;
     if (problem->batch == 0) return DSA_OK;
     if (!keep_count || (max_keep > 0 && !keep)) return DSA_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

@@ -250,3 +250,12 @@ def test_binding_refuses_strided_lengths(dsa):
             for call in _every_cache_call(dsa, _small(dsa, torch.zeros((3, 4, 64)), cache, **kw)):
                 with pytest.raises(ValueError, match="contiguous"):
                     call()
+
+
+def test_sizes_beyond_the_index_arithmetic(dsa):
+    """Refused before anything is launched."""
+    L, a = dsa._lib, ctypes.addressof
+    paged = dict(block_table=FAKE, block_size=16, num_blocks=64, max_blocks=600)
+    p = _problem(dsa, batch=1, **paged)
+    for keep in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 30 + 1):
+        assert L.dsa_compact_kv(a(p), 1, 0, None, FAKE, FAKE, keep, None, None) == UNSUPPORTED
