@@ -645,11 +645,12 @@ int32_t dsa_fork_pages(const dsa_page_pool* pool, const dsa_problem* problem, in
     f.max_seq_len = problem->max_seq_len;
     f.items = reinterpret_cast<ForkItem*>(workspace);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int col_blocks = (c.row_vecs + kCopyThreads - 1) / kCopyThreads;
+    const int64_t blocks = (int64_t)n * num_layers * 2 * col_blocks;
+    if (blocks > 0x7fffffffLL) return DSA_ERR_UNSUPPORTED;   // (before the plan is made: a refused call changes nothing)
     rc = launch(dsa_fork_plan_kernel, 1, kPoolThreads, 0, st, true, f);
     if (rc != DSA_OK) return rc;
-    const int col_blocks = (c.row_vecs + kCopyThreads - 1) / kCopyThreads;
-    return launch(dsa_fork_copy_kernel, (int64_t)n * num_layers * 2 * col_blocks, kCopyThreads, 0, st, true, c, f, col_blocks,
-                  (int)num_layers);
+    return launch(dsa_fork_copy_kernel, blocks, kCopyThreads, 0, st, true, c, f, col_blocks, (int)num_layers);
 }
 
 int32_t dsa_copy_pages(const dsa_problem* problem, int32_t num_layers, int64_t stride_layer, const int32_t* src,

@@ -259,3 +259,8 @@ def test_sizes_beyond_the_index_arithmetic(dsa):
     p = _problem(dsa, batch=1, **paged)
     for keep in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 30 + 1):
         assert L.dsa_compact_kv(a(p), 1, 0, None, FAKE, FAKE, keep, None, None) == UNSUPPORTED
+    # a fork whose copies would be more blocks than a launch has: the plan in front of them is not made either
+    pool = dsa.dsa_page_pool(64, 16, FAKE)
+    for n, layers in ((2 ** 30, 1), (2 ** 22, 2 ** 16), (2 ** 31 - 1, 1)):
+        assert L.dsa_fork_pages(a(pool), a(p), layers, 4096, FAKE, FAKE, n, FAKE, 0x60000, 16 * n, None) == UNSUPPORTED
+        assert L.dsa_copy_pages(a(p), layers, 4096, FAKE, FAKE, n, None) == UNSUPPORTED
