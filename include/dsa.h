@@ -451,9 +451,10 @@ DSA_API int32_t dsa_decode_attention_static_scratch(const dsa_problem *problem, 
  *
  * All conventions above hold.  The calls in this part read nothing that the stream's earlier work may
  * still be writing, and (unlike the attention calls) start none of their successors early before their
- * own predecessors have finished; those that write seq_len, prompt_len or a block table (compact, fork,
- * release, reserve) finish before anything behind them starts, so that a call behind them may make the
- * promise DSA_PLAN_METADATA_STABLE.
+ * own predecessors have finished.  With regard to the promise DSA_PLAN_METADATA_STABLE, those that write
+ * seq_len, prompt_len or a block table (compact, fork, release, reserve) are like dsa_advance_seq_len: the
+ * call directly behind one of them cannot make it, since only a kernel that waits for the launch in front
+ * is certain to see what that has written; the calls behind that one can.
  */
 
 /* The drafted tokens ("nodes") of every request and what hangs on what. */

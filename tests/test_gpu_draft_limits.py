@@ -265,3 +265,79 @@ def test_the_documented_loop_runs(dsa):
         dsa.dsa_release_pages(names["pool"], table, torch.where(torch.arange(b).cuda() == 2, 0, -1).int())
         seq[2] = -1
     assert dsa.dsa_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("last", ["compact", "release", "reserve", "fork"])
+def test_promise_behind_calls_that_write_lengths_and_tables(dsa, last, captured):
+    """Layers of decode steps behind each of the calls that write lengths or block tables: the first without
+    DSA_PLAN_METADATA_STABLE, the others with it.  What comes out is what comes out without it."""
+    b, h, d, page, m, layers, steps = 8, 8, 64, 16, 12, 3, 25
+    rng = np.random.default_rng(3)
+    g = torch.Generator().manual_seed(5)
+    lens = rng.integers(10, (m - 1) * page, size=(steps, b))
+    counts = [_int((x + (x % page == 0)).tolist()) for x in lens]  # (part-filled last pages: the step's token has a place in them)
+    table0 = torch.from_numpy(rng.permutation(3 * b * m)[:b * m].reshape(b, m).astype(np.int32)).cuda()
+    caches = torch.randn((2, layers, 3 * b * m, page, h, d), generator=g).bfloat16()
+    q, kn, vn = (torch.randn((steps, layers, b, h, d), generator=g).bfloat16().cuda() for _ in range(3))
+    diag = dsa.Diag(dsa.DSA_MASK_GRID, 24, 10, 6, 1)
+    keep = torch.arange(m * page, dtype=torch.int32, device="cuda").expand(b, -1).contiguous()
+    whole = _int([(m - 1) * page] * b)
+
+    def run(flag):
+        k, v = (caches[i].cuda() for i in range(2))
+        table, seq, prompt, status = table0.clone(), whole.clone(), _int([9] * b), _int([0] * b)
+        refs = torch.zeros((3 * b * m,), dtype=torch.int32, device="cuda")
+        refs[table.long().flatten()] = 1
+        pool, count = dsa.PagePool(refs, page), counts[0].clone()
+        src, dst = _int([0, 1]), _int([b - 1, b - 2])
+        ws, forked = dsa.alloc_fork_workspace(src), _int([9, 9])
+        give_up = _int([-1] * (b - 2) + [0, 0])
+        qs, ks, vs = (torch.empty_like(t[0]) for t in (q, kn, vn))
+        probs = [dsa.Problem(q=qs[i], k_cache=k[i], v_cache=v[i], strides=k[i].stride()[:3], seq_len=seq, prompt_len=prompt, num_kv_heads=h,
+                             max_seq_len=m * page, max_prompt_len=9, block_table=table, block_size=page, num_blocks=3 * b * m,
+                             plan_flags=dsa.plan_group(4, 1) | (flag if i else 0)) for i in range(layers)]
+        assert dsa.dsa_query_plan(probs[1], diag).block_warps == 4
+        outs = [dsa.alloc_outputs(p) for p in probs]
+        spaces = [dsa.alloc_workspace(p, diag) for p in probs]
+
+        def one_pass():
+            # every call writes what the layers read, `last` right in front of them
+            dsa.dsa_compact_kv(probs[0], keep, whole if last == "reserve" else count, len_out=seq, num_layers=layers, stride_layer=k.stride(0))
+            if last in ("release", "reserve"):
+                dsa.dsa_release_pages(pool, table, count)
+            if last == "reserve":
+                dsa.dsa_compact_kv(probs[0], keep, count, len_out=seq, num_layers=layers, stride_layer=k.stride(0))
+                dsa.dsa_reserve_pages(pool, table, seq, page, status)
+            if last == "fork":
+                dsa.dsa_release_pages(pool, table, give_up)
+                dsa.dsa_fork_pages(pool, probs[0], src, dst, forked, ws, layers, k.stride(0))
+            for p, (out, lse), space, i in zip(probs, outs, spaces, range(layers)):
+                dsa.dsa_decode_step(p, diag, ks[i], vs[i], out, lse, space)
+
+        got, graph = [], None
+        for t in range(steps):
+            for x, y in ((qs, q), (ks, kn), (vs, vn)):
+                x.copy_(y[t])
+            count.copy_(counts[t])
+            if last == "release":                                  # (the pages that a pass gives back are taken again outside it)
+                dsa.dsa_reserve_pages(pool, table, whole, 0, status)
+            if captured and t == 1:
+                dsa.dsa_prepare()
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    one_pass()
+            if graph is not None:
+                graph.replay()
+            else:
+                one_pass()
+            got.append([(out.clone(), lse.clone()) for out, lse in outs] + [seq.clone(), table.clone()])
+        torch.cuda.synchronize()
+        return got
+
+    for a, e in zip(run(dsa.DSA_PLAN_METADATA_STABLE), run(0)):
+        for (o1, l1), (o2, l2) in zip(a[:layers], e[:layers]):
+            assert torch.equal(o1, o2) and torch.equal(l1, l2)
+        assert torch.equal(a[layers], e[layers]) and torch.equal(a[layers + 1], e[layers + 1])
+        assert all(torch.isfinite(o).all() for o, _ in a[:layers])
+    assert dsa.dsa_wait_timeouts() == 0
