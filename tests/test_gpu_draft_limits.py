@@ -341,3 +341,46 @@ def test_promise_behind_calls_that_write_lengths_and_tables(dsa, last, captured)
         assert torch.equal(a[layers], e[layers]) and torch.equal(a[layers + 1], e[layers + 1])
         assert all(torch.isfinite(o).all() for o, _ in a[:layers])
     assert dsa.dsa_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("spare", [2000, 700])
+def test_fork_of_many_entry_by_entry(dsa, spare):
+    """More branches than the planning block has threads: every table entry, count, length and byte of the cache; with too
+    few pages the branches that get none change nothing, and those that need none are made all the same."""
+    n, page, m = 1500, 4, 3
+    rng = np.random.default_rng(spare)
+    lens = [(i * 7) % 12 for i in range(n)] + [0] * n
+    prompts = [min(x, 5) for x in lens]
+    table = np.full((2 * n, m), -1, np.int32)
+    ids, used = rng.permutation(n * m + spare), 0
+    for i in range(n):
+        need = -(-lens[i] // page)
+        table[i, :need] = ids[used:used + need]
+        used += need
+    refs = np.ones(n * m + spare, np.int32)
+    free = np.sort(rng.choice(ids[used:], size=spare, replace=False))
+    refs[free] = 0
+    c = Cache(dsa, 2 * n, m, page, blocks=n * m + spare, hkv=1, layers=2, table=table, lens=lens)
+    c.prompt.copy_(_int(prompts))
+    pool, status = dsa.PagePool(torch.from_numpy(refs).cuda(), page), _int([9] * n)
+    src, dst = rng.integers(0, n, size=n).tolist(), (n + rng.permutation(n)).tolist()
+    dsa.dsa_fork_pages(pool, c.problem, _int(src), _int(dst), status, dsa.alloc_fork_workspace(status), num_layers=2,
+                       stride_layer=c.dev[0].stride(0))
+    left, want = free.tolist(), []
+    for s, d in zip(src, dst):
+        full, part = divmod(lens[s], page)
+        if part and not left:
+            want.append(1)
+            continue
+        want.append(0)
+        refs[table[s, :full]] += 1
+        table[d, :full] = table[s, :full]
+        if part:
+            fresh = left.pop(0)
+            table[d, full], refs[fresh] = fresh, 1
+            for t in c.host:
+                t[:, fresh, :part] = t[:, int(table[s, full]), :part]
+        lens[d], prompts[d] = lens[s], prompts[s]
+    assert want.count(1) == 0 if spare >= n else 0 < want.count(1) < n
+    assert status.tolist() == want and np.array_equal(c.table.cpu().numpy(), table)
+    assert pool.ref_count.tolist() == refs.tolist() and c.seq.tolist() == lens and c.prompt.tolist() == prompts and c.same()
