@@ -2,9 +2,10 @@
 // (dsa_compact_kv, dsa_copy_pages, dsa_fork_pages, dsa_reserve_pages, dsa_release_pages).
 //
 // Rows and pages are moved at copy bandwidth: what bounds them is 2 x the bytes moved.  Measured: 218 MB of kept rows
-// moved up (16 requests, dropped tokens): 78 us, 5.6 TB/s read and written; three accepted rows of 64 requests: 6.5 us for
-// 25 MB; 32 branches with their last pages and the pages given back before: 19 us for 31 MB, of which the planning block
-// and two more launches take 12.  A page pool is one
+// moved up (16 requests, dropped tokens): 78 us, 5.6 TB/s read and written; three accepted rows of 64 requests: 6.9 us for
+// 25 MB; 32 branches with their last pages and the pages given back before: 19.6 us for 31 MB, bound by three launches, the
+// planning block and copies that have one token's rows in flight at a time (201 MB of whole pages: 36.5 us with 16 tokens
+// a page, 78 with 128).  A page pool is one
 // array of counts; a free page is one whose count is 0 and pages are taken lowest index first.  Giving pages
 // back is then nothing but independent decrements, in any order and from any number of blocks, and two runs
 // of the same calls leave the same tables, which a stack of free pages filled by atomics would not.
