@@ -492,9 +492,9 @@ DSA_API int32_t dsa_tree_workspace_size(const dsa_problem *problem, const dsa_di
  *   A node whose page is missing (its entry in the block table is outside [0, num_blocks), after
  *   dsa_reserve_pages found none for instance) is computed, but its rows are stored nowhere.
  *   dsa_verify_tree does not know which nodes have room and pages: a caller whose requests can run out of them
- *   leaves such nodes out of node_count, on the device, between dsa_reserve_pages and this call (none where status[b] is not 0 or
- *   seq_len[b] negative; else at most max_seq_len - seq_len[b]), and gives both calls the same.  dsa_compact_kv counts no
- *   row that is missing.
+ *   leaves such nodes out of node_count, on the device, between dsa_reserve_pages and this call (none where
+ *   status[b] is not 0 or seq_len[b] negative; else at most max_seq_len - seq_len[b]), and gives both calls the
+ *   same.  dsa_compact_kv counts no row that is missing.
  *   Cached rows that no node of the request sees may hold anything (NaN included); a NaN or infinity in
  *   the V row of a token that some node sees reaches the other nodes of the request as well.
  */
@@ -559,8 +559,9 @@ DSA_API int32_t dsa_compact_kv(const dsa_problem *problem, int32_t num_layers, i
                                const int32_t *base, const int32_t *keep, const int32_t *keep_count, int32_t max_keep,
                                int32_t *len_out, void *stream);
 
-/* The pages of a paged cache: a page is free while its count is 0 (a negative one is left as it is).  Pages are taken lowest index first, so
- * that equal calls give equal tables.  All arrays on the device; the caller zeroes ref_count to begin with
+/* The pages of a paged cache: a page is free while its count is 0 (a negative count is left as it is, but for the
+ * lowest max_blocks numbers there are, which dsa_reserve_pages uses while it runs).  Pages are taken lowest index
+ * first, so that equal calls give equal tables.  All arrays on the device; the caller zeroes ref_count to begin with
  * (and fills block tables with -1, the mark of an entry without a page).  Calls on one pool are ordered by
  * the caller: one stream, or events. */
 typedef struct dsa_page_pool {
