@@ -612,6 +612,142 @@ DSA_API int32_t dsa_fork_pages(const dsa_page_pool *pool, const dsa_problem *pro
 DSA_API int32_t dsa_copy_pages(const dsa_problem *problem, int32_t num_layers, int64_t stride_layer,
                                const int32_t *src, const int32_t *dst, int32_t n, void *stream);
 
+/* ==== Latent caches: one shared row a token ==========================================================
+ *
+ * A latent cache holds ONE row a token for all heads: latent_dim numbers c_j that every head's keys and
+ * values are linear maps of, and rope_dim more, r_j, that carry the position (not in the paper).
+ * Two forms of the same attention:
+ *   absorbed  the maps have been multiplied into the query and come off the result afterwards, so that all
+ *             heads attend over the cached rows themselves: dsa_latent_step, for new tokens over a cache;
+ *   expanded  keys and values are computed per head: dsa_latent_prompt, for the tokens of prompts, where that
+ *             costs fewer operations (2 (nope_dim + rope_dim + value_dim) a query and key against
+ *             2 (2 latent_dim + rope_dim)).
+ * dsa_map_tokens says where the tokens of a ragged batch go in a cache (pages from dsa_reserve_pages), and
+ * dsa_store_rows / dsa_gather_rows take their rows there or back.
+ *
+ * All conventions above hold, and those of the drafted-token calls with regard to predecessors, successors
+ * and DSA_PLAN_METADATA_STABLE (dsa_map_tokens and dsa_store_rows write no lengths and no tables).
+ */
+typedef struct dsa_latent {
+    int32_t batch;             /* B                                                                          */
+    int32_t latent_dim;        /* R: 256 or 512                                                              */
+    int32_t rope_dim;          /* P: a multiple of 8 in 8 .. 64                                              */
+    int32_t dtype;             /* dsa_dtype of cache, q, c_new, out                                          */
+    float sm_scale;            /* logit scale, > 0: 1/sqrt of the heads' width BEFORE absorption             */
+    void *cache;               /* rows of R + P contiguous elements [c | r], 16-byte aligned                 */
+    int64_t stride_batch;      /* element strides as in dsa_problem: token s of request b at                 */
+    int64_t stride_token;      /* b*stride_batch + s*stride_token, or with a block_table in page             */
+                               /* block_table[b*max_blocks + s/block_size].  Multiples of 16 bytes           */
+    const int32_t *seq_len;    /* [B] tokens in the cache                                                    */
+    const int32_t *block_table;/* [B, max_blocks] or NULL                                                    */
+    int32_t max_blocks;
+    int32_t block_size;
+    int32_t num_blocks;
+    int32_t max_seq_len;       /* HOST upper bound of seq_len[b]; longer sequences are read as ending there  */
+} dsa_latent;
+
+#define DSA_LATENT_MAX_NEW 64
+
+/* Bytes of workspace dsa_latent_step needs for max_new tokens a request and num_heads heads. */
+DSA_API int32_t dsa_latent_workspace_size(const dsa_latent *latent, int32_t num_heads, int32_t max_new, size_t *bytes);
+
+/*
+ * One pass of up to max_new (N, 1 .. DSA_LATENT_MAX_NEW) new tokens a request: appends their rows to the
+ * cache and lets every token i attend, with all heads, over the S = seq_len[b] cached tokens and the new
+ * tokens 0 .. i.  With the query row of head h split as q = [a | e]:
+ *   x_j = sm_scale * (a . c_j + e . r_j),  lse = ln sum_j e^{x_j},  out = sum_j e^{x_j - lse} c_j.
+ *   q [B, N, num_heads, R + P], c_new [B, N, R + P], out [B, N, num_heads, R], lse [B, N, num_heads] float32:
+ *   contiguous, the first three 16-byte aligned.
+ *   new_count [B] device or NULL: tokens 0 .. new_count[b]-1 of the request exist (clamped to [0, N]); NULL: all N.
+ *   Token i's row goes to position S + i; seq_len is not modified.  Tokens without room (S + i >= max_seq_len)
+ *   are dropped like those at and behind new_count[b]: nothing is appended, out = 0, lse = -inf; their q and
+ *   c_new rows may hold anything.  A negative seq_len drops all.  A token whose page is missing is computed, but
+ *   its row is stored nowhere.  Cached rows behind S may hold anything (NaN included).
+ *   workspace: 256-byte aligned, dsa_latent_workspace_size() bytes.
+ */
+DSA_API int32_t dsa_latent_step(const dsa_latent *latent, int32_t num_heads, int32_t max_new, const void *q,
+                                const void *c_new, const int32_t *new_count, void *out, float *lse,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* A ragged batch of prompts with keys and values expanded per head. */
+typedef struct dsa_prompt {
+    int32_t batch;             /* B                                                                          */
+    int32_t num_heads;         /* H                                                                          */
+    int32_t nope_dim;          /* numbers of a key that each head has for itself: 64 or 128 ...              */
+    int32_t value_dim;         /* ... and of a value: the same                                               */
+    int32_t rope_dim;          /* numbers of a key that all heads share: a multiple of 8 in 8 .. 64          */
+    int32_t dtype;             /* dsa_dtype of q, k_nope, k_rope, v and out                                  */
+    float sm_scale;            /* logit scale; 0 means 1/sqrt(nope_dim + rope_dim)                           */
+    int32_t q_tokens;          /* rows of q, out and lse                                                     */
+    int32_t kv_tokens;         /* rows of k_nope, k_rope and v                                               */
+    int32_t max_q_len;         /* HOST upper bound of a request's queries; sizes the launch.  Queries beyond */
+                               /* it are left out (out and lse stay as they were)                            */
+    /* Rows of a token and head, contiguous, 16-byte aligned, at token*stride_token + head*stride_head
+     * elements (multiples of 16 bytes): q [.., nope_dim + rope_dim], the others as they are named. */
+    const void *q;
+    int64_t q_stride_token, q_stride_head;
+    const void *k_nope;
+    int64_t k_stride_token, k_stride_head;
+    const void *k_rope;        /* one row a token                                                            */
+    int64_t rope_stride_token;
+    const void *v;
+    int64_t v_stride_token, v_stride_head;
+    const int32_t *q_start;    /* device [B + 1], ascending: request b has the query rows                    */
+                               /* q_start[b] .. q_start[b+1]-1 ...                                           */
+    const int32_t *kv_start;   /* ... and the keys kv_start[b] .. kv_start[b+1]-1; NULL: q_start             */
+    int32_t causal;            /* 0: every query sees all keys of its request; else query i of Lq, with Lk   */
+                               /* keys, sees the keys j <= i + Lk - Lq (its own is the last)                 */
+} dsa_prompt;
+
+/*
+ * Attention of the tokens of a ragged batch, per head h:
+ *   x_ij = sm_scale * q_i . [k_nope_j | k_rope_j],  lse_i = ln sum_j e^{x_ij},  out_i = sum_j e^{x_ij - lse_i} v_j
+ * over the keys that query i sees.  out [q_tokens, H, value_dim] (16-byte aligned), lse [q_tokens, H] float32: contiguous.  A query that sees
+ * no key (Lk < Lq) gets out = 0, lse = -inf.  Rows that belong to no request are left as they were.  Starts are
+ * clamped into [0, q_tokens] / [0, kv_tokens].  Keys and values that no query of the request sees may hold anything;
+ * a NaN or infinity in the v row of a key that some query sees may reach the other queries of the request.  No workspace.
+ */
+DSA_API int32_t dsa_latent_prompt(const dsa_prompt *prompt, void *out, float *lse, void *stream);
+
+/* The tokens of a ragged batch and the cache they belong to. */
+typedef struct dsa_token_map {
+    int32_t batch;             /* B                                                                          */
+    int32_t max_tokens;        /* entries of slot, position, request; tokens beyond them are left out        */
+    const int32_t *count;      /* device [B]: tokens of each request in the batch (negative: none)           */
+    const int32_t *base;       /* device [B]: position of its first one (seq_len), or NULL for 0             */
+    const int32_t *block_table;/* device [B, max_blocks], or NULL: request b has the slots                   */
+                               /* b*max_seq_len .. (b+1)*max_seq_len-1                                       */
+    int32_t max_blocks;
+    int32_t block_size;
+    int32_t num_blocks;
+    int32_t max_seq_len;       /* tokens a request has room for                                              */
+} dsa_token_map;
+
+/*
+ * Lays the tokens of the requests end to end: start[b] is the number of tokens before request b, start[B] all of
+ * them (both at most max_tokens), and for its token k (entry t = start[b] + k):
+ *   request[t] = b, position[t] = base[b] + k, slot[t] = page * block_size + position % block_size with the page
+ *   that block_table names, or -1: no room (position outside [0, max_seq_len)) or no page (entry outside [0, num_blocks)).
+ * Entries behind the last token: -1 in all three.  start [B + 1], position and request [max_tokens] int32, slot
+ * [max_tokens] int64; position and request may be NULL.
+ * start is what dsa_prompt takes as q_start / kv_start, slot what the row calls take.  With base NULL and count the
+ * cached lengths the map names the tokens in the cache.
+ */
+DSA_API int32_t dsa_map_tokens(const dsa_token_map *map, int32_t *start, int64_t *slot, int32_t *position,
+                               int32_t *request, void *stream);
+
+/*
+ * Copies rows of R + P elements between a batch and a latent cache: row t, at rows + t*row_stride elements (a multiple of
+ * 16 bytes, 16-byte aligned), goes to (store) or comes from (gather) the token at slot[t], t < count.  slot: device int64,
+ * as dsa_map_tokens gives it: page slot / block_size with a block_table, else request slot / max_seq_len.  Rows whose slot lies
+ * outside the cache are skipped: nothing is stored, or the batch's row stays as it was.  No two rows of a store may have the
+ * same slot.  Of `latent` seq_len, sm_scale and the table's entries are not used.
+ */
+DSA_API int32_t dsa_store_rows(const dsa_latent *latent, const int64_t *slot, int32_t count, const void *rows,
+                               int64_t row_stride, void *stream);
+DSA_API int32_t dsa_gather_rows(const dsa_latent *latent, const int64_t *slot, int32_t count, void *rows,
+                                int64_t row_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

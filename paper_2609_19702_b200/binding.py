@@ -43,7 +43,8 @@ EXPORTS = ["dsa_version", "dsa_status_string", "dsa_last_cuda_error", "dsa_works
            "dsa_decode_attention_host_mapped", "dsa_decode_step", "dsa_advance_seq_len", "dsa_prepare",
            "dsa_wait_timeouts", "dsa_debug_wait_giveup", "dsa_debug_copy_only", "dsa_build_skip_bitmap",
            "dsa_tree_workspace_size", "dsa_tree_step", "dsa_verify_tree", "dsa_compact_kv", "dsa_reserve_pages",
-           "dsa_release_pages", "dsa_fork_pages", "dsa_copy_pages"]
+           "dsa_release_pages", "dsa_fork_pages", "dsa_copy_pages", "dsa_latent_workspace_size", "dsa_latent_step",
+           "dsa_latent_prompt", "dsa_map_tokens", "dsa_store_rows", "dsa_gather_rows"]
 
 
 class dsa_problem(ctypes.Structure):
@@ -101,6 +102,34 @@ class dsa_verify(ctypes.Structure):
 
 class dsa_page_pool(ctypes.Structure):
     _fields_ = [("num_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32), ("ref_count", ctypes.c_void_p)]
+
+
+DSA_LATENT_MAX_NEW = 64
+
+
+class dsa_latent(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("sm_scale", ctypes.c_float), ("cache", ctypes.c_void_p), ("stride_batch", ctypes.c_int64),
+                ("stride_token", ctypes.c_int64), ("seq_len", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("max_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32), ("num_blocks", ctypes.c_int32),
+                ("max_seq_len", ctypes.c_int32)]
+
+
+class dsa_prompt(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("num_heads", ctypes.c_int32), ("nope_dim", ctypes.c_int32), ("value_dim", ctypes.c_int32),
+                ("rope_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("sm_scale", ctypes.c_float), ("q_tokens", ctypes.c_int32),
+                ("kv_tokens", ctypes.c_int32), ("max_q_len", ctypes.c_int32), ("q", ctypes.c_void_p),
+                ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64), ("k_nope", ctypes.c_void_p),
+                ("k_stride_token", ctypes.c_int64), ("k_stride_head", ctypes.c_int64), ("k_rope", ctypes.c_void_p),
+                ("rope_stride_token", ctypes.c_int64), ("v", ctypes.c_void_p), ("v_stride_token", ctypes.c_int64),
+                ("v_stride_head", ctypes.c_int64), ("q_start", ctypes.c_void_p), ("kv_start", ctypes.c_void_p),
+                ("causal", ctypes.c_int32)]
+
+
+class dsa_token_map(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("count", ctypes.c_void_p), ("base", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("max_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32),
+                ("num_blocks", ctypes.c_int32), ("max_seq_len", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -164,13 +193,28 @@ def _load() -> ctypes.CDLL:
     lib.dsa_fork_pages.argtypes = [vp, vp, i32, i64, vp, vp, i32, vp, vp, size, vp]
     lib.dsa_copy_pages.restype = i32
     lib.dsa_copy_pages.argtypes = [vp, i32, i64, vp, vp, i32, vp]
+    lib.dsa_latent_workspace_size.restype = i32
+    lib.dsa_latent_workspace_size.argtypes = [vp, i32, i32, ctypes.POINTER(size)]
+    lib.dsa_latent_step.restype = i32
+    lib.dsa_latent_step.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, size, vp]
+    lib.dsa_latent_prompt.restype = i32
+    lib.dsa_latent_prompt.argtypes = [vp, vp, vp, vp]
+    lib.dsa_map_tokens.restype = i32
+    lib.dsa_map_tokens.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.dsa_store_rows.restype = i32
+    lib.dsa_store_rows.argtypes = [vp, vp, i32, vp, i64, vp]
+    lib.dsa_gather_rows.restype = i32
+    lib.dsa_gather_rows.argtypes = [vp, vp, i32, vp, i64, vp]
     return lib
 
 
 _lib = _load()
 _TREE, _POOL = struct.Struct("@iPP0q"), struct.Struct("@iiP0q")
 _VERIFY = struct.Struct("@iiiPPqPqP0q")
+_LATENT, _MAP = struct.Struct("@4ifPqqPP4i0q"), struct.Struct("@iiPPP4i0q")
+_PROMPT = struct.Struct("@6if3iPqqPqqPqPqqPPi0q")
 assert (_TREE.size, _POOL.size, _VERIFY.size) == tuple(ctypes.sizeof(s) for s in (dsa_tree, dsa_page_pool, dsa_verify))
+assert (_LATENT.size, _MAP.size, _PROMPT.size) == tuple(ctypes.sizeof(s) for s in (dsa_latent, dsa_token_map, dsa_prompt))
 
 
 class DsaError(RuntimeError):
@@ -790,3 +834,187 @@ def dsa_copy_pages(problem: Problem, src: torch.Tensor, dst: torch.Tensor, num_l
     dev = _same_device(problem.q, problem.k_cache, problem.v_cache, problem.block_table, src, dst)
     p = _cache_problem(problem)
     _call(_lib.dsa_copy_pages, dev, stream, p, int(num_layers), int(stride_layer), src.data_ptr(), dst.data_ptr(), n)
+
+
+# ---- latent caches: one shared row a token --------------------------------------------------------------------
+@dataclass
+class Latent:
+    """A cache of one row [latent | rope] a token (see dsa_latent)."""
+    cache: torch.Tensor                           # any shape; addressed through `strides`
+    strides: tuple                                # (stride_batch_or_block, stride_token), elements
+    seq_len: torch.Tensor                         # int32 [B]
+    latent_dim: int
+    rope_dim: int
+    max_seq_len: int
+    sm_scale: float                               # 1/sqrt of the heads' width before their maps were absorbed
+    block_table: Optional[torch.Tensor] = None    # int32 [B, max_blocks]
+    block_size: int = 0
+    num_blocks: int = 0
+
+    def c_struct(self) -> dsa_latent:
+        return dsa_latent.from_buffer_copy(self._packed())
+
+    def _packed(self) -> bytes:
+        seq, bt = self.seq_len, self.block_table
+        b = seq.numel()
+        _int32(seq, (b,), "seq_len")
+        s0, s1 = self.strides
+        if bt is None:
+            return _LATENT.pack(b, self.latent_dim, self.rope_dim, _dtype_code(self.cache), self.sm_scale, self.cache.data_ptr(), s0, s1,
+                                seq.data_ptr(), 0, 0, 0, 0, self.max_seq_len)
+        _, m = _table(bt, b)
+        return _LATENT.pack(b, self.latent_dim, self.rope_dim, _dtype_code(self.cache), self.sm_scale, self.cache.data_ptr(), s0, s1,
+                            seq.data_ptr(), bt.data_ptr(), m, self.block_size, self.num_blocks, self.max_seq_len)
+
+
+def _latent_q(latent: Latent, q: torch.Tensor) -> tuple:
+    if q.dim() != 4 or q.shape[0] != latent.seq_len.numel() or q.shape[3] != latent.latent_dim + latent.rope_dim:
+        raise ValueError("q must be [batch, new tokens, heads, latent_dim + rope_dim]")
+    if q.dtype != latent.cache.dtype or not q.is_contiguous():
+        raise ValueError("q must be contiguous and of the cache's type")
+    return q.shape
+
+
+def dsa_latent_workspace_size(latent: Latent, num_heads: int, max_new: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("dsa_latent_workspace_size",
+           _lib.dsa_latent_workspace_size(latent._packed(), int(num_heads), int(max_new), ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_latent_outputs(latent: Latent, q: torch.Tensor):
+    """out [B, N, H, latent_dim] of q's type, lse [B, N, H] float32."""
+    b, n, h, _ = _latent_q(latent, q)
+    return (torch.empty((b, n, h, latent.latent_dim), dtype=q.dtype, device=q.device),
+            torch.empty((b, n, h), dtype=torch.float32, device=q.device))
+
+
+def alloc_latent_workspace(latent: Latent, q: torch.Tensor) -> Optional[torch.Tensor]:
+    _, n, h, _ = _latent_q(latent, q)
+    with torch.cuda.device(q.device):
+        size = dsa_latent_workspace_size(latent, h, n)
+    return None if size == 0 else torch.empty(size, dtype=torch.uint8, device=q.device)
+
+
+def dsa_latent_step(latent: Latent, q: torch.Tensor, c_new: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                    workspace: Optional[torch.Tensor] = None, new_count: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Append + attention of N new tokens a request over a latent cache (absorbed form): ``q`` [B, N, H, R + P],
+    ``c_new`` [B, N, R + P] the tokens' rows, ``out`` [B, N, H, R], ``lse`` [B, N, H]; ``latent.seq_len`` counts the
+    tokens already cached (it is not advanced), ``new_count`` int32 [B] how many of the N exist (None: all)."""
+    b, n, h, w = _latent_q(latent, q)
+    if c_new.dtype != q.dtype or c_new.shape != (b, n, w) or not c_new.is_contiguous():
+        raise ValueError("c_new must be contiguous [batch, new tokens, latent_dim + rope_dim] of q's type")
+    if out.dtype != q.dtype or out.shape != (b, n, h, latent.latent_dim) or not out.is_contiguous():
+        raise ValueError("out must be contiguous [batch, new tokens, heads, latent_dim] of q's type")
+    if lse.dtype != torch.float32 or lse.shape != (b, n, h) or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor of shape %s" % ((b, n, h),))
+    if new_count is not None:
+        _int32(new_count, (b,), "new_count")
+    dev = _same_device(q, latent.cache, latent.seq_len, latent.block_table, c_new, out, lse, workspace, new_count)
+    ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call(_lib.dsa_latent_step, dev, stream, latent._packed(), h, n, q.data_ptr(), c_new.data_ptr(), _dptr(new_count), out.data_ptr(),
+          lse.data_ptr(), _dptr(workspace), ws_n)
+
+
+@dataclass
+class Prompt:
+    """A ragged batch of prompts with keys and values expanded per head (see dsa_prompt).  Any strides, but contiguous
+    last dimensions: k_nope and v may be the two parts of one product's rows."""
+    q: torch.Tensor                               # [q_tokens, H, nope + rope]
+    k_nope: torch.Tensor                          # [kv_tokens, H, nope]
+    k_rope: torch.Tensor                          # [kv_tokens, rope], shared by the heads
+    v: torch.Tensor                               # [kv_tokens, H, value]
+    q_start: torch.Tensor                         # int32 [B + 1]
+    kv_start: Optional[torch.Tensor] = None       # int32 [B + 1]; None: q_start
+    max_q_len: int = 0                            # upper bound of a request's queries; 0: q_tokens
+    sm_scale: float = 0.0                         # 0: 1/sqrt(nope + rope)
+    causal: bool = True
+
+    def c_struct(self) -> dsa_prompt:
+        return dsa_prompt.from_buffer_copy(self._packed())
+
+    def _packed(self) -> bytes:
+        q, k, r, v = self.q, self.k_nope, self.k_rope, self.v
+        if q.dim() != 3 or k.dim() != 3 or r.dim() != 2 or v.dim() != 3:
+            raise ValueError("q, k_nope, v must be [tokens, heads, width], k_rope [tokens, width]")
+        nq, h, w = q.shape
+        nk, p = r.shape
+        nope = w - p
+        if k.shape != (nk, h, nope) or v.shape[:2] != (nk, h):
+            raise ValueError("q [q_tokens, H, nope + rope], k_nope [kv_tokens, H, nope], k_rope [kv_tokens, rope], v [kv_tokens, H, value]")
+        if k.dtype != q.dtype or r.dtype != q.dtype or v.dtype != q.dtype:
+            raise ValueError("q, k_nope, k_rope and v must be of one type")
+        if q.stride(2) != 1 or k.stride(2) != 1 or r.stride(1) != 1 or v.stride(2) != 1:
+            raise ValueError("the last dimensions of q, k_nope, k_rope and v must be contiguous")
+        b = self.q_start.numel() - 1
+        _int32(self.q_start, (b + 1,), "q_start")
+        ks = self.kv_start
+        if ks is not None:
+            _int32(ks, (b + 1,), "kv_start")
+        return _PROMPT.pack(b, h, nope, v.shape[2], p, _dtype_code(q), self.sm_scale, nq, nk, self.max_q_len or nq, q.data_ptr(), q.stride(0),
+                            q.stride(1), k.data_ptr(), k.stride(0), k.stride(1), r.data_ptr(), r.stride(0), v.data_ptr(), v.stride(0),
+                            v.stride(1), self.q_start.data_ptr(), 0 if ks is None else ks.data_ptr(), 1 if self.causal else 0)
+
+
+def alloc_prompt_outputs(prompt: Prompt):
+    """out [q_tokens, H, value] of q's type, lse [q_tokens, H] float32."""
+    n, h, _ = prompt.q.shape
+    return (torch.empty((n, h, prompt.v.shape[2]), dtype=prompt.q.dtype, device=prompt.q.device),
+            torch.empty((n, h), dtype=torch.float32, device=prompt.q.device))
+
+
+def dsa_latent_prompt(prompt: Prompt, out: torch.Tensor, lse: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Attention of the tokens of a ragged batch of prompts, keys and values expanded per head."""
+    p = prompt._packed()
+    n, h, _ = prompt.q.shape
+    if out.dtype != prompt.q.dtype or out.shape != (n, h, prompt.v.shape[2]) or not out.is_contiguous():
+        raise ValueError("out must be contiguous [q_tokens, heads, value] of q's type")
+    if lse.dtype != torch.float32 or lse.shape != (n, h) or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor of shape %s" % ((n, h),))
+    dev = _same_device(prompt.q, prompt.k_nope, prompt.k_rope, prompt.v, prompt.q_start, prompt.kv_start, out, lse)
+    _call(_lib.dsa_latent_prompt, dev, stream, p, out.data_ptr(), lse.data_ptr())
+
+
+def dsa_map_tokens(count: torch.Tensor, start: torch.Tensor, slot: torch.Tensor, position: Optional[torch.Tensor] = None,
+                   request: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None,
+                   block_table: Optional[torch.Tensor] = None, block_size: int = 0, num_blocks: int = 0, max_seq_len: int = 0,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Lays count[b] tokens of each request end to end: start int32 [B + 1]; slot int64, position and request int32
+    [max_tokens] (-1 behind the last token; slot -1 where a token has no room or no page)."""
+    b, n = count.numel(), slot.numel()
+    _int32(count, (b,), "count")
+    _int32(start, (b + 1,), "start")
+    if slot.dtype != torch.int64 or slot.dim() != 1 or not slot.is_contiguous():
+        raise ValueError("slot must be a contiguous int64 tensor of one dimension")
+    if position is not None:
+        _int32(position, (n,), "position")
+    if request is not None:
+        _int32(request, (n,), "request")
+    if base is not None:
+        _int32(base, (b,), "base")
+    m = 0 if block_table is None else _table(block_table, b)[1]
+    dev = _same_device(count, start, slot, position, request, base, block_table)
+    c = _MAP.pack(b, n, count.data_ptr(), 0 if base is None else base.data_ptr(), 0 if block_table is None else block_table.data_ptr(), m,
+                  block_size, num_blocks, max_seq_len)
+    _call(_lib.dsa_map_tokens, dev, stream, c, start.data_ptr(), slot.data_ptr(), _dptr(position), _dptr(request))
+
+
+def _rows_call(fn, latent: Latent, slot: torch.Tensor, rows: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> None:
+    if rows.dim() != 2 or rows.dtype != latent.cache.dtype or rows.shape[1] != latent.latent_dim + latent.rope_dim or rows.stride(1) != 1:
+        raise ValueError("rows must be [tokens, latent_dim + rope_dim] of the cache's type with a contiguous last dimension")
+    n = rows.shape[0]
+    if slot.dtype != torch.int64 or slot.shape != (n,) or not slot.is_contiguous():
+        raise ValueError("slot must be a contiguous int64 tensor of shape %s" % ((n,),))
+    dev = _same_device(latent.cache, latent.seq_len, latent.block_table, slot, rows)
+    _call(fn, dev, stream, latent._packed(), slot.data_ptr(), n, rows.data_ptr(), rows.stride(0) if n > 1 else rows.shape[1])
+
+
+def dsa_store_rows(latent: Latent, slot: torch.Tensor, rows: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """rows[t] goes to the cache at slot[t] (int64, as dsa_map_tokens gives it); slots outside the cache: nowhere."""
+    _rows_call(_lib.dsa_store_rows, latent, slot, rows, stream)
+
+
+def dsa_gather_rows(latent: Latent, slot: torch.Tensor, rows: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """rows[t] comes from the cache at slot[t]; slots outside the cache leave it as it was."""
+    _rows_call(_lib.dsa_gather_rows, latent, slot, rows, stream)

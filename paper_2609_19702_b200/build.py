@@ -2,8 +2,8 @@
 
 Compiles the translation units under ``csrc/`` for sm_100a with nvcc -- ``dsa_api.cu`` (entry
 points, planner, small kernels), one unit per (element type, head_dim) with the attention kernels,
-and those of the drafted-token calls (``dsa_tree.cu``, ``dsa_verify.cu``, ``dsa_pages.cu``), in
-parallel -- and links them into ``libdsa.so`` beside this file.  nvcc cross-compiles,
+those of the drafted-token calls (``dsa_tree.cu``, ``dsa_verify.cu``, ``dsa_pages.cu``) and those of
+the latent-cache calls (``dsa_latent.cu``, ``dsa_prompt.cu``, ``dsa_rows.cu``), in parallel -- and links them into ``libdsa.so`` beside this file.  nvcc cross-compiles,
 so no GPU is needed to build.
 """
 from __future__ import annotations
@@ -19,7 +19,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdsa.so")
 SOURCES = ["dsa_api.cu", "dsa_kernels_bf16_d128.cu", "dsa_kernels_bf16_d64.cu", "dsa_kernels_f32_d128.cu",
-           "dsa_kernels_f32_d64.cu", "dsa_tree.cu", "dsa_verify.cu", "dsa_pages.cu"]
+           "dsa_kernels_f32_d64.cu", "dsa_tree.cu", "dsa_verify.cu", "dsa_pages.cu", "dsa_latent.cu", "dsa_prompt.cu",
+           "dsa_rows.cu"]
 
 
 def _newest_source_mtime() -> float:

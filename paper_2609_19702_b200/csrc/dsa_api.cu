@@ -9,7 +9,7 @@
 #include <type_traits>
 
 #include "dsa_aux.cuh"
-#include "dsa_host.cuh"
+#include "dsa_latent_host.cuh"
 #include "dsa_launch.cuh"
 
 namespace {
@@ -851,6 +851,8 @@ int32_t dsa_prepare(void) {
     if (e == cudaSuccess) e = kernel_prepare<float, 128>();
     if (e == cudaSuccess) e = tree_prepare();
     if (e == cudaSuccess) e = verify_prepare();
+    if (e == cudaSuccess) e = latent_prepare();
+    if (e == cudaSuccess) e = prompt_prepare();
     void* scratch = nullptr;
     if (e == cudaSuccess) e = static_scratch_address(&scratch);   // (and remember it for this device)
     int* counter = nullptr;

@@ -50,7 +50,7 @@
 // Rows of V that no node sees (behind the sequence, before the window, behind the last node) are zeroed in
 // shared memory before the product: their P is 0, but 0 x NaN is not.
 #pragma once
-#include "dsa_common.cuh"
+#include "dsa_tc.cuh"
 
 namespace dsa {
 
@@ -96,70 +96,6 @@ struct TreeCfg {
     static constexpr int TMEM_COLS = 256;
     static constexpr int COL_S = 0, COL_O = 2 * kTreeTile;
 };
-
-// ---- tcgen05 and tensor-map wrappers ---------------------------------------------------------------
-__device__ __forceinline__ void tma_box4(void* dst, const CUtensorMap* map, int c0, int c1, int c2, int c3,
-                                         unsigned long long* bar) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes "
-                 "[%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void tc_commit(unsigned long long* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
-                 ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// Shared-memory operand descriptors, 128-byte swizzle: atoms of 8 rows x 128 bytes, 1024 bytes from one to the next
-// along the rows; `lead`: bytes from one 64-element column block to the next, where the 64 contiguous elements run
-// along N and the operand is wider than they are.  The upper half is the same for all of them.
-constexpr unsigned kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
-__device__ __forceinline__ unsigned desc_low(unsigned addr, unsigned lead) { return ((addr >> 4) & 0x3fffu) | ((lead >> 4) << 16); }
-// Instruction descriptor: bf16 x bf16 -> fp32, M x N; b_mn: B's contiguous dimension is N, not K.
-__host__ __device__ constexpr unsigned instr_desc(int M, int N, bool b_mn) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((unsigned)(N >> 3) << 17) |
-           ((unsigned)(M >> 4) << 24);
-}
-// D[tmem] (+)= A[smem] B[smem]^T
-__device__ __forceinline__ void tc_mma_ss(unsigned d, unsigned a_low, unsigned b_low, unsigned idesc, bool acc) {
-    asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\n"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}"
-                 ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"((unsigned)acc), "r"(kDescHigh) : "memory");
-}
-// D[tmem] (+)= A[tmem] B[smem]^T
-__device__ __forceinline__ void tc_mma_ts(unsigned d, unsigned a, unsigned b_low, unsigned idesc, bool acc) {
-    asm volatile("{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 b, {%2, %5};\n"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}"
-                 ::"r"(d), "r"(a), "r"(b_low), "r"(idesc), "r"((unsigned)acc), "r"(kDescHigh) : "memory");
-}
-// one lane of the warp, the same every time (products and their commits come from one thread)
-__device__ __forceinline__ bool elect_one() {
-    unsigned yes;
-    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
-    return yes != 0;
-}
-__device__ __forceinline__ void tc_ld32(unsigned (&r)[32], unsigned addr) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(addr));
-}
-__device__ __forceinline__ void tc_st32(unsigned addr, const unsigned (&r)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-                 : "memory");
-}
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ---- what a block works on, in 64-token tiles ---------------------------------------------------------
 // The cached tokens that some node of the request sees: [0, P0) (dense: everything; windowed: prompt and
@@ -245,25 +181,6 @@ __device__ __forceinline__ void tree_write_empty(const TreeArgs& g, int b, int k
     }
 }
 
-// Wait for phase `parity` of `bar`, about a second at most.  False: this wait ran out, or another warp's did
-// (*abort); the block then drains what it has in flight and ends.
-__device__ __forceinline__ bool tree_wait(unsigned long long* bar, unsigned parity, volatile int* abort, int* wait_timeouts,
-                                          int lane) {
-    bool ok = mbar_try_wait(bar, parity);
-    if (!ok) {
-        const long long t0 = clock64();
-        while (!(ok = mbar_try_wait(bar, parity))) {
-            if (*abort) break;
-            if (clock64() - t0 > kMbarWaitCycles) {
-                *abort = 1;
-                if (lane == 0 && wait_timeouts) atomicAdd(wait_timeouts, 1);
-                break;
-            }
-        }
-    }
-    return __all_sync(0xffffffffu, ok);                       // (one answer for the warp)
-}
-
 // ---- thread-block clusters ---------------------------------------------------------------------------
 __device__ __forceinline__ void tree_cluster_barrier() {
     __syncwarp();
@@ -284,34 +201,6 @@ __device__ __forceinline__ float4 tree_peer_f4(unsigned addr) {
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
-    unsigned r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-// two floats in one instruction (each rounded on its own)
-__device__ __forceinline__ unsigned long long pack_f32x2(float lo, float hi) {
-    unsigned long long r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 unpack_f32x2(unsigned long long v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b, unsigned long long c) {
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, unsigned long long b) {
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // ---- dynamic scheduling: a running block takes over blocks that have not been launched yet --------------------
 __device__ __forceinline__ void steal_block(void* response, unsigned long long* bar) {      // one thread
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // (the last response has been read)
