@@ -1,6 +1,7 @@
 // New tokens over a latent cache: argument checks, launch plan and launch (dsa_latent_step).
 #include <algorithm>
 
+#include "dsa_latent.cuh"
 #include "dsa_latent_f32.cuh"
 #include "dsa_latent_host.cuh"
 
@@ -11,9 +12,13 @@ using namespace dsa;
 struct LatentPlan {
     int rows, row_tiles;                           // query rows of a request, blocks of them
     int n_split;                                   // float32: pieces of a request's keys
+    int groups;                                    // bf16: blocks that share the keys of a row tile
     int64_t blocks;
-    size_t ws_out_bytes, ws_total;
+    size_t ws_out_bytes, ws_total;                 // float32: partial outputs, and their log-sums behind them
+    size_t ws_sched_bytes, ws_ml_bytes;            // bf16: the schedule, maxima and sums, and partial outputs behind them
 };
+
+constexpr int kLatMinUnits = 2;                    // tiles that a block takes at least (see LatentTcArgs)
 
 int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, LatentPlan* pl) {
     const int32_t rc = check_latent(l, true);
@@ -23,6 +28,17 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
     if (l->max_seq_len > 0x7fff0000) return DSA_ERR_UNSUPPORTED;     // (positions a tile or N further stay below 2^31)
     *pl = LatentPlan{};
     pl->rows = heads * max_new;
+    if (l->dtype == DSA_BF16) {
+        pl->row_tiles = (pl->rows + kLatRows - 1) / kLatRows;
+        const int64_t units = (int64_t)l->batch * (((int64_t)l->max_seq_len + kLatTile - 1) / kLatTile + 1);
+        if (units > (1 << 30)) return DSA_ERR_UNSUPPORTED;
+        pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(host_sm_count() / pl->row_tiles, units / kLatMinUnits));
+        pl->blocks = (int64_t)pl->groups * pl->row_tiles;
+        pl->ws_sched_bytes = ((size_t)(l->batch + 2) * sizeof(int) + 255) / 256 * 256;
+        pl->ws_ml_bytes = pl->groups > 1 ? (size_t)pl->blocks * 2 * kLatRows * sizeof(float2) : 0;
+        pl->ws_total = pl->ws_sched_bytes + pl->ws_ml_bytes + (pl->groups > 1 ? (size_t)pl->blocks * 2 * kLatRows * l->latent_dim * sizeof(float) : 0);
+        return DSA_OK;
+    }
     pl->row_tiles = (pl->rows + kLatentF32Block - 1) / kLatentF32Block;
     const int64_t items = std::max<int64_t>(1, (int64_t)l->batch * pl->row_tiles);
     const int64_t tiles = ((int64_t)l->max_seq_len + max_new + kStreamTile - 1) / kStreamTile;
@@ -38,25 +54,69 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
     return DSA_OK;
 }
 
-template <typename T, int R>
-cudaError_t configure_f32() {
-    static std::atomic<bool> done[kMaxDevices] = {};
-    return configure_smem(dsa_latent_f32_kernel<T, R>, LatentF32Cfg<R>::SMEM, done);
+// A view of rows of `width` elements for the tensor-map copies: 64 elements (128 bytes) of `box` rows per copy, 128-byte
+// swizzle; what a copy asks for beyond the view arrives as zeros.
+bool encode_rows(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, int64_t width, int64_t rows, int64_t outer,
+                 int64_t row_stride, int64_t outer_stride, int box) {
+    const int64_t most = 0xffffffffLL;
+    if (rows < 1 || rows > most || outer < 1 || outer > most) return false;
+    if (row_stride >= (1LL << 39) || outer_stride <= 0 || outer_stride >= (1LL << 39)) return false;
+    const cuuint64_t n[3] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)outer};
+    const cuuint64_t pitch[2] = {(cuuint64_t)row_stride * 2, (cuuint64_t)outer_stride * 2};
+    const cuuint32_t bx[3] = {64u, (cuuint32_t)box, 1u}, step[3] = {1u, 1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), n, pitch, bx, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-template <typename T, int R>
+
+int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void* q, const void* c_new, LatentTcArgs* g, LatentMaps* m) {
+    const TensorMapEncodeFn encode = host_tensor_map_encoder();
+    if (!encode) return DSA_ERR_UNSUPPORTED;
+    const int64_t W = l->latent_dim + l->rope_dim, tokens = l->block_table ? l->block_size : std::max(l->max_seq_len, 1);
+    // a box of the cache must not cross the end of a page: the largest power of two that divides it
+    g->box_tokens = kLatTile;
+    if (l->block_table)
+        while (l->block_size % g->box_tokens) g->box_tokens /= 2;
+    for (g->box_shift = 0; (1 << g->box_shift) < g->box_tokens;) ++g->box_shift;
+    // division of positions (below 2^31) by the page size: with 2^s >= d the product by ceil(2^(31 + s) / d) is exact
+    const unsigned d = l->block_table ? (unsigned)l->block_size : 1u;
+    for (g->page_shift = 31; (1ull << (g->page_shift - 31)) < d;) ++g->page_shift;
+    g->page_mul = (unsigned)(((1ull << g->page_shift) + d - 1) / d);
+    g->blk_coord = l->stride_batch > 0 ? 1 : 0;    // (a stride of 0: a dimension of one entry)
+    const int64_t outer = g->blk_coord ? (l->block_table ? l->num_blocks : l->batch) : 1;
+    const bool ok = encode_rows(encode, &m->q, q, W, (int64_t)l->batch * pl.rows, 1, W, W, kLatRows) &&
+                    encode_rows(encode, &m->cache, l->cache, W, tokens, outer, l->stride_token, g->blk_coord ? l->stride_batch : l->stride_token,
+                                g->box_tokens) &&
+                    encode_rows(encode, &m->fresh, c_new, W, g->l.N, l->batch, W, (int64_t)g->l.N * W, g->l.N);
+    return ok ? DSA_OK : DSA_ERR_UNSUPPORTED;      // (an extent or stride beyond what a tensor map holds)
+}
+
+template <int R>
+cudaError_t configure() {
+    static std::atomic<bool> done[kMaxDevices] = {}, done_f32[kMaxDevices] = {};
+    cudaError_t e = configure_smem(dsa_latent_kernel<R>, LatentCfg<R>::SMEM, done);
+    if (e == cudaSuccess) e = configure_smem(dsa_latent_f32_kernel<R>, LatentF32Cfg<R>::SMEM, done_f32);
+    return e;
+}
+template <int R>
+cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, int64_t blocks, cudaStream_t st) {
+    cudaError_t e = configure<R>();
+    if (e == cudaSuccess) e = launch_dependent(dsa_latent_kernel<R>, blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
+    if (e == cudaSuccess && g.groups > 1)
+        e = launch_dependent(dsa_latent_merge_kernel<R>, (int64_t)g.l.a.B * g.l.row_tiles * (R / 64), 256, 0, st, g);
+    return e;
+}
+template <int R>
 cudaError_t run_f32(const LatentArgs& g, int64_t blocks, cudaStream_t st) {
-    const cudaError_t e = configure_f32<T, R>();
-    return e != cudaSuccess ? e : launch_dependent(dsa_latent_f32_kernel<T, R>, blocks, kStreamWarps * 32, LatentF32Cfg<R>::SMEM, st, g);
+    const cudaError_t e = configure<R>();
+    return e != cudaSuccess ? e : launch_dependent(dsa_latent_f32_kernel<R>, blocks, kStreamWarps * 32, LatentF32Cfg<R>::SMEM, st, g);
 }
 
 }  // namespace
 
 namespace dsa {
 cudaError_t latent_prepare() {
-    cudaError_t e = configure_f32<float, 256>();
-    if (e == cudaSuccess) e = configure_f32<float, 512>();
-    if (e == cudaSuccess) e = configure_f32<__nv_bfloat16, 256>();
-    if (e == cudaSuccess) e = configure_f32<__nv_bfloat16, 512>();
+    cudaError_t e = configure<256>();
+    if (e == cudaSuccess) e = configure<512>();
     return e;
 }
 }  // namespace dsa
@@ -107,6 +167,27 @@ int32_t dsa_latent_step(const dsa_latent* latent, int32_t num_heads, int32_t max
     g.P = latent->rope_dim;
     g.rows = pl.rows;
     g.row_tiles = pl.row_tiles;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    if (latent->dtype == DSA_BF16) {
+        LatentTcArgs t = {};
+        g.a.out = out;
+        g.a.lse = lse;
+        e = host_wait_timeouts_address(&g.a.wait_timeouts);
+        if (e != cudaSuccess) return host_cuda_fail(e);
+        t.l = g;
+        t.groups = pl.groups;
+        t.min_units = kLatMinUnits;
+        unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+        t.sched = reinterpret_cast<int*>(ws);
+        t.part_ml = reinterpret_cast<float2*>(ws + pl.ws_sched_bytes);
+        t.part_o = reinterpret_cast<float4*>(ws + pl.ws_sched_bytes + pl.ws_ml_bytes);
+        LatentMaps m;
+        const int32_t built = build_latent_maps(latent, pl, q, c_new, &t, &m);
+        if (built != DSA_OK) return built;
+        e = latent->latent_dim == 256 ? run_bf16<256>(t, m, pl.blocks, st) : run_bf16<512>(t, m, pl.blocks, st);
+        return e == cudaSuccess ? DSA_OK : host_cuda_fail(e);
+    }
     if (pl.n_split > 1) {
         g.a.out_part = reinterpret_cast<float*>(workspace);
         g.a.lse_part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(workspace) + pl.ws_out_bytes);
@@ -114,12 +195,7 @@ int32_t dsa_latent_step(const dsa_latent* latent, int32_t num_heads, int32_t max
         g.a.out = out;
         g.a.lse = lse;
     }
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (latent->dtype == DSA_BF16)
-        e = latent->latent_dim == 256 ? run_f32<__nv_bfloat16, 256>(g, pl.blocks, st) : run_f32<__nv_bfloat16, 512>(g, pl.blocks, st);
-    else
-        e = latent->latent_dim == 256 ? run_f32<float, 256>(g, pl.blocks, st) : run_f32<float, 512>(g, pl.blocks, st);
+    e = latent->latent_dim == 256 ? run_f32<256>(g, pl.blocks, st) : run_f32<512>(g, pl.blocks, st);
     if (e != cudaSuccess) return host_cuda_fail(e);
     if (pl.n_split > 1)
         return host_launch_combine(g.a.out_part, g.a.lse_part, (int64_t)latent->batch * pl.rows, latent->latent_dim, pl.n_split, out,

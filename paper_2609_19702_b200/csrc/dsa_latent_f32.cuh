@@ -17,7 +17,7 @@ struct LatentF32Cfg {
     static constexpr int SMEM = 2 * kStreamTile * (R + 64) * 4;
 };
 
-template <typename T, int R>
+template <int R>
 __global__ void __launch_bounds__(kStreamWarps * 32) dsa_latent_f32_kernel(const LatentArgs g) {
     extern __shared__ __align__(16) float s_rows[];
     constexpr int ROWS = kLatentF32Rows, VP = R / 128;
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32) dsa_latent_f32_kernel(const
         const int row = row0 + r, token = row / g.a.H_q;
         limit[r] = row < g.rows && token < n ? S + token + 1 : 0;
         if (limit[r] == 0) continue;
-        const T* q = reinterpret_cast<const T*>(g.a.q) + ((int64_t)b * g.rows + row) * W;
+        const float* q = reinterpret_cast<const float*>(g.a.q) + ((int64_t)b * g.rows + row) * W;
 #pragma unroll
         for (int p = 0; p < VP; ++p) st.q[r][p] = load_piece(q + (lane + 32 * p) * 4);
         if (lane < g.P / 4) st.qr[r] = load_piece(q + R + lane * 4);
@@ -54,10 +54,10 @@ __global__ void __launch_bounds__(kStreamWarps * 32) dsa_latent_f32_kernel(const
         // eight threads a row, every eighth piece each: one address per thread
         const int row = tid >> 3, pos = t * kStreamTile + row;
         const bool there = pos < len;
-        const T* src = reinterpret_cast<const T*>(g.a.k);
+        const float* src = reinterpret_cast<const float*>(g.a.k);
         if (there)
-            src = pos < S ? src + token_offset(g.a, b, 0, pos) : reinterpret_cast<const T*>(g.a.k_new) + ((int64_t)b * g.N + pos - S) * W;
-        for (int c = tid & 7; c < vecs; c += 8) stage_piece(dst + row * (R + 64) + c * 4, src + c * 4, there);
+            src = pos < S ? src + token_offset(g.a, b, 0, pos) : reinterpret_cast<const float*>(g.a.k_new) + ((int64_t)b * g.N + pos - S) * W;
+        for (int c = tid & 7; c < vecs; c += 8) cp_async16(dst + row * (R + 64) + c * 4, src + c * 4, there);
         cp_async_commit();
     };
     if (t0 < t1) stage(t0);
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32) dsa_latent_f32_kernel(const
         __syncthreads();
     }
     cp_async_wait<0>();
-    if (rt == 0) latent_append<T>(g, b, S, n, piece * kStreamWarps + warp, g.a.n_split * kStreamWarps, lane);
+    if (rt == 0) latent_append<float>(g, b, S, n, piece * kStreamWarps + warp, g.a.n_split * kStreamWarps, lane);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const int row = row0 + r;
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32) dsa_latent_f32_kernel(const
             o = st.l[r] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
             const int c = (lane + 32 * p) * 4;
             if (g.a.n_split > 1) store_piece(g.a.out_part + (orow * g.a.n_split + piece) * R + c, o);
-            else store_piece(reinterpret_cast<T*>(g.a.out) + orow * R + c, o);
+            else store_piece(reinterpret_cast<float*>(g.a.out) + orow * R + c, o);
         }
         if (lane == 0) {
             if (g.a.n_split > 1) g.a.lse_part[orow * g.a.n_split + piece] = st.lse(r, g.a.scale_log2);

@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "dsa_latent_host.cuh"
+#include "dsa_prompt.cuh"
 #include "dsa_prompt_f32.cuh"
 
 namespace {
@@ -32,25 +33,44 @@ int32_t check_prompt(const dsa_prompt* p) {
     return DSA_OK;
 }
 
-template <typename T, int D>
-cudaError_t configure_f32() {
-    static std::atomic<bool> done[kMaxDevices] = {};
-    return configure_smem(dsa_prompt_f32_kernel<T, D>, PromptF32Cfg<D>::SMEM, done);
+// A view [tokens][heads][width] for the tensor-map copies: 64 elements (128 bytes) of one head and a tile of tokens per copy,
+// 128-byte swizzle; what a copy asks for beyond the view arrives as zeros.  head: 1, or 0 where all heads read the same rows.
+bool encode_heads(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, int64_t width, int64_t heads, int64_t tokens,
+                  int64_t head_stride, int64_t token_stride, int* head) {
+    const int64_t most = 0xffffffffLL;
+    if (tokens < 1 || tokens > most) return false;
+    if (tokens == 1) token_stride = width + 64;    // (never used: any stride will do)
+    token_stride = (token_stride + 7) / 8 * 8;
+    *head = heads > 1 && head_stride > 0;
+    if (token_stride >= (1LL << 39) || head_stride >= (1LL << 39)) return false;
+    const cuuint64_t n[3] = {(cuuint64_t)width, (cuuint64_t)(*head ? heads : 1), (cuuint64_t)tokens};
+    const cuuint64_t pitch[2] = {(cuuint64_t)(*head ? head_stride : token_stride) * 2, (cuuint64_t)token_stride * 2};
+    const cuuint32_t bx[3] = {64u, 1u, (cuuint32_t)kPrTile}, step[3] = {1u, 1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), n, pitch, bx, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-template <typename T, int D>
-cudaError_t run_f32(const PromptArgs& g, int64_t blocks, cudaStream_t st) {
-    const cudaError_t e = configure_f32<T, D>();
-    return e != cudaSuccess ? e : launch_dependent(dsa_prompt_f32_kernel<T, D>, blocks, kStreamWarps * 32, PromptF32Cfg<D>::SMEM, st, g);
+
+template <int D>
+cudaError_t configure() {
+    static std::atomic<bool> done[kMaxDevices] = {}, done_f32[kMaxDevices] = {};
+    cudaError_t e = configure_smem(dsa_prompt_kernel<D>, PromptCfg<D>::SMEM, done);
+    if (e == cudaSuccess) e = configure_smem(dsa_prompt_f32_kernel<D>, PromptF32Cfg<D>::SMEM, done_f32);
+    return e;
+}
+template <int D>
+cudaError_t run(const PromptArgs& g, const PromptMaps& m, bool bf16, int64_t blocks, cudaStream_t st) {
+    const cudaError_t e = configure<D>();
+    if (e != cudaSuccess) return e;
+    return bf16 ? launch_dependent(dsa_prompt_kernel<D>, blocks, kPrThreads, PromptCfg<D>::SMEM, st, g, m)
+                : launch_dependent(dsa_prompt_f32_kernel<D>, blocks, kStreamWarps * 32, PromptF32Cfg<D>::SMEM, st, g);
 }
 
 }  // namespace
 
 namespace dsa {
 cudaError_t prompt_prepare() {
-    cudaError_t e = configure_f32<float, 64>();
-    if (e == cudaSuccess) e = configure_f32<float, 128>();
-    if (e == cudaSuccess) e = configure_f32<__nv_bfloat16, 64>();
-    if (e == cudaSuccess) e = configure_f32<__nv_bfloat16, 128>();
+    cudaError_t e = configure<64>();
+    if (e == cudaSuccess) e = configure<128>();
     return e;
 }
 }  // namespace dsa
@@ -77,13 +97,28 @@ int32_t dsa_latent_prompt(const dsa_prompt* p, void* out, float* lse, void* stre
     g.out = out;
     g.lse = lse;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const int64_t blocks = ((int64_t)g.max_q_len + kPromptF32Block - 1) / kPromptF32Block * p->num_heads * p->batch;
+    const bool bf16 = p->dtype == DSA_BF16;
+    const int rows = bf16 ? kPrBlock : kPromptF32Block;
+    const int64_t blocks = ((int64_t)g.max_q_len + rows - 1) / rows * p->num_heads * p->batch;
     if (blocks > 0x7fffffffLL) return DSA_ERR_UNSUPPORTED;
+    PromptMaps m = {};
     cudaError_t e;
-    if (p->dtype == DSA_BF16)
-        e = p->nope_dim == 64 ? run_f32<__nv_bfloat16, 64>(g, blocks, st) : run_f32<__nv_bfloat16, 128>(g, blocks, st);
-    else
-        e = p->nope_dim == 64 ? run_f32<float, 64>(g, blocks, st) : run_f32<float, 128>(g, blocks, st);
+    if (bf16) {
+        e = host_wait_timeouts_address(&g.wait_timeouts);
+        if (e != cudaSuccess) return host_cuda_fail(e);
+        const TensorMapEncodeFn encode = host_tensor_map_encoder();
+        if (!encode) return DSA_ERR_UNSUPPORTED;
+        int one;
+        // (without any key no copy of a key is made, and the views may be those of q)
+        const bool keys = p->kv_tokens > 0;
+        const int64_t kv = keys ? p->kv_tokens : 1, W = p->nope_dim + p->rope_dim, H = p->num_heads;
+        const bool ok = encode_heads(encode, &m.q, p->q, W, H, p->q_tokens, p->q_stride_head, p->q_stride_token, &m.q_head) &&
+                        encode_heads(encode, &m.k, keys ? p->k_nope : p->q, p->nope_dim, H, kv, p->k_stride_head, p->k_stride_token, &m.k_head) &&
+                        encode_heads(encode, &m.kr, keys ? p->k_rope : p->q, p->rope_dim, 1, kv, 0, p->rope_stride_token, &one) &&
+                        encode_heads(encode, &m.v, keys ? p->v : p->q, p->value_dim, H, kv, p->v_stride_head, p->v_stride_token, &m.v_head);
+        if (!ok) return DSA_ERR_UNSUPPORTED;       // (an extent or stride beyond what a tensor map holds)
+    }
+    e = p->nope_dim == 64 ? run<64>(g, m, bf16, blocks, st) : run<128>(g, m, bf16, blocks, st);
     return e == cudaSuccess ? DSA_OK : host_cuda_fail(e);
 }
 

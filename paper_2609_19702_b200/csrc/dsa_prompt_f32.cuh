@@ -15,7 +15,7 @@ struct PromptF32Cfg {
     static constexpr int SMEM = 2 * kStreamTile * ROW * 4;
 };
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kStreamWarps * 32) dsa_prompt_f32_kernel(const PromptArgs g) {
     using C = PromptF32Cfg<D>;
     extern __shared__ __align__(16) float s_rows[];
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32) dsa_prompt_f32_kernel(const
         limit[r] = 0;
         if (row0 + r >= nq) continue;
         limit[r] = g.causal ? (int)max((int64_t)0, min((int64_t)nk, (int64_t)row0 + r + 1 + nk - all_q)) : nk;
-        const T* q = reinterpret_cast<const T*>(g.q) + (int64_t)(q0 + row0 + r) * g.q_tok + h * g.q_head;
+        const float* q = reinterpret_cast<const float*>(g.q) + (int64_t)(q0 + row0 + r) * g.q_tok + h * g.q_head;
         if (lane < D / 4) st.q[r][0] = load_piece(q + lane * 4);
         if (lane < g.P / 4) st.qr[r] = load_piece(q + D + lane * 4);
     }
@@ -54,14 +54,14 @@ __global__ void __launch_bounds__(kStreamWarps * 32) dsa_prompt_f32_kernel(const
         float* dst = s_rows + (t & 1) * kStreamTile * C::ROW + row * C::ROW;
         const bool there = pos < len;
         const int64_t tok = there ? k0 + pos : 0;
-        const T* k = reinterpret_cast<const T*>(g.k) + tok * g.k_tok + h * g.k_head;
-        const T* kr = reinterpret_cast<const T*>(g.kr) + tok * g.r_tok;
-        const T* v = reinterpret_cast<const T*>(g.v) + tok * g.v_tok + h * g.v_head;
+        const float* k = reinterpret_cast<const float*>(g.k) + tok * g.k_tok + h * g.k_head;
+        const float* kr = reinterpret_cast<const float*>(g.kr) + tok * g.r_tok;
+        const float* v = reinterpret_cast<const float*>(g.v) + tok * g.v_tok + h * g.v_head;
         for (int c = tid & 7; c < D / 4; c += 8) {
-            stage_piece(dst + c * 4, k + c * 4, there);
-            stage_piece(dst + C::LD_K + c * 4, v + c * 4, there);
+            cp_async16(dst + c * 4, k + c * 4, there);
+            cp_async16(dst + C::LD_K + c * 4, v + c * 4, there);
         }
-        for (int c = tid & 7; c < g.P / 4; c += 8) stage_piece(dst + D + c * 4, kr + c * 4, there);
+        for (int c = tid & 7; c < g.P / 4; c += 8) cp_async16(dst + D + c * 4, kr + c * 4, there);
         cp_async_commit();
     };
     if (tiles > 0) stage(0);
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32) dsa_prompt_f32_kernel(const
         const float inv = st.l[r] == 0.f ? 0.f : 1.f / st.l[r];
         const float4 o = st.o[r][0];
         if (lane < D / 4)
-            store_piece(reinterpret_cast<T*>(g.out) + orow * D + lane * 4,
+            store_piece(reinterpret_cast<float*>(g.out) + orow * D + lane * 4,
                         st.l[r] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
         if (lane == 0) g.lse[orow] = st.lse(r, g.scale_log2);
     }

@@ -14,19 +14,7 @@ constexpr int kStreamWarps = 4;
 constexpr int kStreamTile = 16;                    // keys per shared-memory tile, two of them in flight
 
 __device__ __forceinline__ float4 load_piece(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load_piece(const __nv_bfloat16* p) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
-}
-// four numbers to shared memory, zeros with !there
-__device__ __forceinline__ void stage_piece(float* dst, const float* src, bool there) { cp_async16(dst, src, there); }
-__device__ __forceinline__ void stage_piece(float* dst, const __nv_bfloat16* src, bool there) {
-    *reinterpret_cast<float4*>(dst) = there ? load_piece(src) : make_float4(0.f, 0.f, 0.f, 0.f);
-}
 __device__ __forceinline__ void store_piece(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
-__device__ __forceinline__ void store_piece(__nv_bfloat16* p, float4 x) {
-    p[0] = __float2bfloat16_rn(x.x); p[1] = __float2bfloat16_rn(x.y); p[2] = __float2bfloat16_rn(x.z); p[3] = __float2bfloat16_rn(x.w);
-}
 
 // KP / VP: pieces per lane of the keys' main part and of the values.
 template <int ROWS, int KP, int VP>
