@@ -15,7 +15,7 @@ struct LatentPlan {
     int groups;                                    // bf16: blocks that share the keys of a row tile
     int64_t blocks;
     size_t ws_out_bytes, ws_total;                 // float32: partial outputs, and their log-sums behind them
-    size_t ws_sched_bytes, ws_ml_bytes;            // bf16: the schedule, maxima and sums, and partial outputs behind them
+    size_t ws_ml_bytes;                            // bf16: maxima and sums, and partial outputs behind them
 };
 
 constexpr int kLatMinUnits = 2;                    // tiles that a block takes at least (see LatentTcArgs)
@@ -34,9 +34,10 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
         if (units > (1 << 30)) return DSA_ERR_UNSUPPORTED;
         pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(host_sm_count() / pl->row_tiles, units / kLatMinUnits));
         pl->blocks = (int64_t)pl->groups * pl->row_tiles;
-        pl->ws_sched_bytes = ((size_t)(l->batch + 2) * sizeof(int) + 255) / 256 * 256;
-        pl->ws_ml_bytes = pl->groups > 1 ? (size_t)pl->blocks * 2 * kLatRows * sizeof(float2) : 0;
-        pl->ws_total = pl->ws_sched_bytes + pl->ws_ml_bytes + (pl->groups > 1 ? (size_t)pl->blocks * 2 * kLatRows * l->latent_dim * sizeof(float) : 0);
+        if (pl->groups > 1) {
+            pl->ws_ml_bytes = (size_t)pl->blocks * 2 * kLatRows * sizeof(float2);
+            pl->ws_total = pl->ws_ml_bytes + (size_t)pl->blocks * 2 * kLatRows * l->latent_dim * sizeof(float);
+        }
         return DSA_OK;
     }
     pl->row_tiles = (pl->rows + kLatentF32Block - 1) / kLatentF32Block;
@@ -81,9 +82,10 @@ int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void*
     const unsigned d = l->block_table ? (unsigned)l->block_size : 1u;
     for (g->page_shift = 31; (1ull << (g->page_shift - 31)) < d;) ++g->page_shift;
     g->page_mul = (unsigned)(((1ull << g->page_shift) + d - 1) / d);
+    g->q_rows = std::min(kLatRows, (pl.rows + 7) / 8 * 8);
     g->blk_coord = l->stride_batch > 0 ? 1 : 0;    // (a stride of 0: a dimension of one entry)
     const int64_t outer = g->blk_coord ? (l->block_table ? l->num_blocks : l->batch) : 1;
-    const bool ok = encode_rows(encode, &m->q, q, W, (int64_t)l->batch * pl.rows, 1, W, W, kLatRows) &&
+    const bool ok = encode_rows(encode, &m->q, q, W, (int64_t)l->batch * pl.rows, 1, W, W, g->q_rows) &&
                     encode_rows(encode, &m->cache, l->cache, W, tokens, outer, l->stride_token, g->blk_coord ? l->stride_batch : l->stride_token,
                                 g->box_tokens) &&
                     encode_rows(encode, &m->fresh, c_new, W, g->l.N, l->batch, W, (int64_t)g->l.N * W, g->l.N);
@@ -102,7 +104,7 @@ cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, int64_t blocks,
     cudaError_t e = configure<R>();
     if (e == cudaSuccess) e = launch_dependent(dsa_latent_kernel<R>, blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
     if (e == cudaSuccess && g.groups > 1)
-        e = launch_dependent(dsa_latent_merge_kernel<R>, (int64_t)g.l.a.B * g.l.row_tiles * (R / 64), 256, 0, st, g);
+        e = launch_dependent(dsa_latent_merge_kernel<R>, (int64_t)g.l.a.B * g.l.row_tiles * (R / 64), kLatThreads, 0, st, g);
     return e;
 }
 template <int R>
@@ -179,9 +181,8 @@ int32_t dsa_latent_step(const dsa_latent* latent, int32_t num_heads, int32_t max
         t.groups = pl.groups;
         t.min_units = kLatMinUnits;
         unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
-        t.sched = reinterpret_cast<int*>(ws);
-        t.part_ml = reinterpret_cast<float2*>(ws + pl.ws_sched_bytes);
-        t.part_o = reinterpret_cast<float4*>(ws + pl.ws_sched_bytes + pl.ws_ml_bytes);
+        t.part_ml = reinterpret_cast<float2*>(ws);
+        t.part_o = reinterpret_cast<float4*>(ws + pl.ws_ml_bytes);
         LatentMaps m;
         const int32_t built = build_latent_maps(latent, pl, q, c_new, &t, &m);
         if (built != DSA_OK) return built;

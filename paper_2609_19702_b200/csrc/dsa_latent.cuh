@@ -16,9 +16,9 @@ struct LatentTcArgs {
     int box_tokens, box_shift;                     // tokens per tensor-map box of the cache, and its logarithm
     unsigned page_mul;                             // position / block_size = (position * page_mul) >> page_shift
     int page_shift;
+    int q_rows;                                    // rows of q per copy: fewer than a block's where a request has fewer
     int blk_coord;                                 // 0: the map's outer dimension has one entry (stride 0)
-    int* sched;                                    // workspace: [B + 1] units before each request, then the quota
-    float2* part_ml;                               // [groups * row_tiles * 2][64] maximum (base 2) and sum
+    float2* part_ml;                               // workspace: [groups * row_tiles * 2][64] maximum (base 2) and sum
     float4* part_o;                                // [groups * row_tiles * 2][R / 4][64]
 };
 
@@ -33,7 +33,8 @@ struct LatentCfg {
     static constexpr int SLOT = CH * CHUNK;
     static constexpr int Q_BYTES = CH * kLatRows * 128;
     static constexpr int SLOTS = R == 512 ? 2 : 4;
-    static constexpr int GROUPS = R / 256;                                 // parts of a slot that land and are freed on their own
+    static constexpr int LAND = (CH + 2) / 3;                              // parts of a slot that land on their own: three columns each
+    static constexpr int GROUPS = R / 256;                                 // and that are freed on their own: what a product with V reads
     static constexpr int TAIL = 2048;
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT + TAIL;
     static constexpr int COL_S = R / 2, TMEM_COLS = R == 512 ? 512 : 256;
@@ -44,31 +45,60 @@ __device__ __forceinline__ void tma_box3(void* dst, const CUtensorMap* map, int 
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar)) : "memory");
 }
-// D[tmem] (+)= A[smem] B[smem]^T with 64 rows: the first half of the N columns in lanes 0-63, the second in lanes 64-127
+// D[tmem] (+)= A[smem] B[smem]^T with 64 rows: the first half of the N columns in lanes 0-63, the second in lanes 64-127.  Two
+// forms, because what goes with a predicate costs the issuing lane more than the product costs the tensor pipe (56 against 33
+// cycles with N = 64).
 __device__ __forceinline__ void tc_mma_ws(unsigned d, unsigned a_low, unsigned b_low, unsigned idesc, bool acc) {
     asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\n"
                  "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}"
                  ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"((unsigned)acc), "r"(kDescHigh) : "memory");
 }
-// one look at phase `parity` of the barrier
-__device__ __forceinline__ bool mbar_test(unsigned long long* bar, unsigned parity) {
-    unsigned done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-    return __all_sync(0xffffffffu, done != 0);
+__device__ __forceinline__ void tc_mma_ws_add(unsigned d, unsigned a_low, unsigned b_low, unsigned idesc) {
+    asm volatile("{\n.reg .b64 a, b;\nmov.b64 a, {%1, %4};\nmov.b64 b, {%2, %4};\n"
+                 "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n}"
+                 ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(kDescHigh) : "memory");
 }
 // Units of work of a request: its cached tiles and one for the new tokens (or for having nothing to do).
 __device__ __forceinline__ int latent_units(int S, int n) { return n > 0 ? (S + kLatTile - 1) / kLatTile + 1 : 1; }
+// To begin a request costs a block about as much as two tiles (its q, the last one's results), so where shares are large every
+// request counts that many units more, at its front.
+__device__ __forceinline__ int latent_setup(int total, int groups) { return total >= 8 * groups ? 2 : 0; }
 
-// A block's share of one request: units [t0, t1) of `units`.
+// A block's share of one request: tiles [t0, t1) of `all`, the last of which are the new tokens.
 struct LatentSeg {
-    int b, S, n, t0, t1, units, rows, part;        // b < 0: nothing any more.  rows: query rows of tokens that exist.  part: where the
+    int b, S, n, t0, t1, all, rows, part;          // b < 0: nothing any more.  rows: query rows of tokens that exist.  part: where the
                                                    // partial result goes, -1: the block has the whole request
     __device__ __forceinline__ int tiles() const { return rows > 0 ? t1 - t0 : 0; }
-    __device__ __forceinline__ int count(int t) const {                    // tokens of tile t (of this share)
-        return t0 + t < units - 1 ? min(kLatTile, S - (t0 + t) * kLatTile) : n;
-    }
+    __device__ __forceinline__ bool cached(int t) const { return t0 + t < all - 1; }
+    __device__ __forceinline__ int count(int t) const { return cached(t) ? min(kLatTile, S - (t0 + t) * kLatTile) : n; }   // tokens of its tile t
 };
+
+// The units of the requests before b0 where every thread of a block of kLatThreads calls it with its own stretch [b0, b1) of
+// them, in order; and of all.  s_scan: shared, a number per warp.
+__device__ __forceinline__ int latent_units_before(const LatentArgs& l, int b0, int b1, int* s_scan, int& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int sum = 0;
+    for (int b = b0; b < b1; ++b) {
+        int S, n;
+        latent_lengths(l, b, S, n);
+        sum += latent_units(S, n);
+    }
+    int before = sum;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, before, off);
+        if (lane >= off) before += x;
+    }
+    if (lane == 31) s_scan[warp] = before;
+    before -= sum;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < kLatThreads / 32; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+    }
+    return before;
+}
 
 template <int R>
 __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const LatentTcArgs g, const __grid_constant__ LatentMaps maps) {
@@ -78,10 +108,10 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     unsigned char* s_q = smem;
     unsigned char* s_ring = smem + C::Q_BYTES;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(s_ring + C::SLOTS * C::SLOT);
-    constexpr int PARTS = C::SLOTS * C::GROUPS;
-    unsigned long long* full = bars;                          // [slot][group] has landed
-    unsigned long long* empty = bars + PARTS;                 // [slot][group] the products that read it are done
-    unsigned long long* s_full = bars + 2 * PARTS;            // [2] scores are in TMEM
+    constexpr int LANDS = C::SLOTS * C::LAND, PARTS = C::SLOTS * C::GROUPS;
+    unsigned long long* full = bars;                          // [slot][LAND] has landed
+    unsigned long long* empty = bars + LANDS;                 // [slot][GROUPS] the products that read it are done
+    unsigned long long* s_full = empty + PARTS;               // [2] scores are in TMEM
     unsigned long long* p_ready = s_full + 2;                 // [2] weights are in shared memory
     unsigned long long* pv_done = s_full + 4;                 // [2] O holds the tile
     unsigned long long* info_full = s_full + 6;               // [2] the next share is known
@@ -89,13 +119,13 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     unsigned long long* q_full = s_full + 10;
     unsigned long long* q_empty = s_full + 11;                // the scores of a share's last tile are done
     unsigned long long* o_free = s_full + 12;                 // O has been read
-    unsigned long long* drained = s_full + 13;
-    unsigned long long* pair = s_full + 14;                   // [2] the two warps of a row have written to s_pair
-    LatentSeg* s_info = reinterpret_cast<LatentSeg*>(s_full + 16);             // [2]
+    unsigned long long* drained = s_full + 13;                // [2]
+    unsigned long long* pair = s_full + 15;                   // [2] the two warps of a row have written to s_pair
+    LatentSeg* s_info = reinterpret_cast<LatentSeg*>(s_full + 18);             // [2]
     float* s_pair = reinterpret_cast<float*>(s_info + 2);     // [2][128] maxima and sums that the two halves of a row exchange
-    int* s_misc = reinterpret_cast<int*>(s_pair + 256);       // [0] TMEM address, [1] abort, [2..] first request, units before it, total
+    int* s_misc = reinterpret_cast<int*>(s_pair + 256);       // [0] TMEM address, [1] abort, [2..] first request, its first unit, units, set-up units
     int* s_scan = s_misc + 8;                                 // [8]
-    static_assert((2 * PARTS + 16) * 8 + 2 * sizeof(LatentSeg) + 1024 + 64 <= C::TAIL, "tail of the shared memory");
+    static_assert((LANDS + PARTS + 18) * 8 + 2 * sizeof(LatentSeg) + 1024 + 64 <= C::TAIL, "tail of the shared memory");
     volatile int* abort = s_misc + 1;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -103,21 +133,29 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     const int rt = (int)blockIdx.x % l.row_tiles, group = (int)blockIdx.x / l.row_tiles;
 
     if (warp == 4 && lane == 0) {
-        for (int s = 0; s < 2 * PARTS; ++s) mbar_init(bars + s, 1);
+        for (int s = 0; s < LANDS + PARTS; ++s) mbar_init(bars + s, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
-            mbar_init(info_full + s, 1); mbar_init(info_empty + s, 6);
-            mbar_init(pair + s, 2);
+            mbar_init(info_full + s, 1); mbar_init(info_empty + s, 7);
+            mbar_init(pair + s, 2); mbar_init(drained + s, 1);
         }
-        mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_free, 4); mbar_init(drained, 1);
+        mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_free, 4);
         s_misc[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    } else if (warp == 6) {
+        if (lane < 3)
+            asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &maps.q : lane == 1 ? &maps.cache : &maps.fresh) : "memory");
     } else if (warp == 5) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(smem_u32(s_misc)), "r"((unsigned)C::TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         tc_fence_before();
     }
+    // rows of q that no copy fills: zeros (nobody reads their results, but leftovers would cost power)
+    for (int i = g.q_rows * 8 + tid; i < kLatRows * 8; i += kLatThreads)
+#pragma unroll
+        for (int c = 0; c < C::CH; ++c) *reinterpret_cast<uint4*>(s_q + c * kLatRows * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
@@ -127,43 +165,21 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     // ---- this block's share: the units of all requests end to end, cut into equal pieces -----------------------------
     {
         const int B = l.a.B, per = (B + kLatThreads - 1) / kLatThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-        int sum = 0;
-        for (int b = b0; b < b1; ++b) {
-            int S, n;
-            latent_lengths(l, b, S, n);
-            sum += latent_units(S, n);
-        }
-        int before = sum;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, before, off);
-            if (lane >= off) before += x;
-        }
-        if (lane == 31) s_scan[warp] = before;
-        before -= sum;
-        __syncthreads();
-        int total = 0;
-        for (int w = 0; w < kLatThreads / 32; ++w) {
-            if (w < warp) before += s_scan[w];
-            total += s_scan[w];
-        }
+        int total, before = latent_units_before(l, b0, b1, s_scan, total);
+        const int setup = latent_setup(total, g.groups);
+        total += setup * B;
+        before += setup * b0;
         const int quota = max(g.min_units, (total + g.groups - 1) / g.groups);
         const int first = min(total, group * quota);          // (group * quota < total + groups * min_units)
-        if (tid == 0) {
-            s_misc[2] = -1;
-            s_misc[4] = min(total, first + quota);
-            if (blockIdx.x == 0) { g.sched[B] = total; g.sched[B + 1] = quota; }
-        }
+        if (tid == 0) { s_misc[2] = -1; s_misc[4] = min(total, first + quota) - first; s_misc[5] = setup; }
         __syncthreads();
         for (int b = b0; b < b1; ++b) {
             int S, n;
             latent_lengths(l, b, S, n);
-            const int units = latent_units(S, n);
+            const int units = latent_units(S, n) + setup;
             if (first >= before && first < before + units) { s_misc[2] = b; s_misc[3] = first - before; }
-            if (blockIdx.x == 0) g.sched[b] = before;
             before += units;
         }
-        if (tid == 0) s_misc[5] = first;
     }
     __syncthreads();
 
@@ -178,19 +194,21 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
 
     if (warp == 4) {
         // ---- what to work on; copies of q and of the cached rows ------------------------------------------
-        int b = s_misc[2], at = s_misc[3], left = s_misc[4] - s_misc[5];
+        const int setup = s_misc[5];
+        int b = s_misc[2], at = s_misc[3], left = s_misc[4];
         int slot = 0, round = 0, issued = 0, live = 0;
         bool ok = true;
         for (int i = 0; ok; ++i) {
             sg.b = left > 0 ? b : -1;
             if (sg.b >= 0) {
                 latent_lengths(l, b, sg.S, sg.n);
-                sg.units = latent_units(sg.S, sg.n);
-                sg.t0 = at;
-                sg.t1 = min(sg.units, at + left);
+                const int units = latent_units(sg.S, sg.n) + setup, end = min(units, at + left);
+                sg.all = sg.n > 0 ? units - setup : 0;
+                sg.t0 = min(sg.all, max(0, at - setup));
+                sg.t1 = min(sg.all, max(0, end - setup));
                 sg.rows = max(0, min(kLatRows, sg.n * l.a.H_q - rt * kLatRows));
-                sg.part = sg.t0 == 0 && sg.t1 == sg.units ? -1 : ((int)blockIdx.x * 2 + (sg.t0 > 0 ? 0 : 1));
-                left -= sg.t1 - sg.t0;
+                sg.part = at == 0 && end == units ? -1 : ((int)blockIdx.x * 2 + (at > 0 ? 0 : 1));
+                left -= end - at;
                 at = 0;
                 ++b;
             }
@@ -213,22 +231,32 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                     if (l.a.block_table) {
                         const int bi = (int)(((unsigned long long)(unsigned)pos * g.page_mul) >> g.page_shift);
                         tok[h] = pos - bi * l.a.block_size;
-                        if (box < boxes && sg.t0 + t < sg.units - 1)
+                        if (box < boxes && sg.cached(t))
                             blk[h] = l.a.block_table[(int64_t)sg.b * l.a.max_blocks + min(bi, l.a.max_blocks - 1)];
                     }
                 }
             };
             int blk0[2], tok0[2], blk1[2], tok1[2];
             where(0, blk0, tok0);
-            if (live > 0) ok = tree_wait(q_empty, (live - 1) & 1, abort, l.a.wait_timeouts, lane);
-            if (!ok) break;
-            if (lane == 0) mbar_expect_tx(q_full, (unsigned)C::Q_BYTES);
-            __syncwarp();
-            if (lane < C::CH) tma_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, sg.b * l.rows + rt * kLatRows, 0, q_full);
-            ++live;
+            const int q_before = live;
+            // q is fetched into L2 now, and to its place when the scores of the share before are done: behind the first tile's copies,
+            // which need not wait for that
+            if (lane < C::CH)
+                asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
+                             ::"l"(&maps.q), "r"(64 * lane), "r"(sg.b * l.rows + rt * kLatRows), "r"(0) : "memory");
+            auto copy_q = [&]() -> bool {
+                if (live > 0 && !tree_wait(q_empty, (live - 1) & 1, abort, l.a.wait_timeouts, lane)) return false;
+                if (lane == 0) mbar_expect_tx(q_full, (unsigned)(C::CH * 128 * g.q_rows));
+                __syncwarp();
+                if (lane < C::CH) tma_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, sg.b * l.rows + rt * kLatRows, 0, q_full);
+                __syncwarp();
+                ++live;
+                return true;
+            };
+            if (live == 0) ok = copy_q();
             for (int t = 0; ok && t < tiles; ++t) {
                 if (t + 1 < tiles) where(t + 1, blk1, tok1);
-                const bool cached = sg.t0 + t < sg.units - 1;
+                const bool cached = sg.cached(t);
                 const int used = cached ? (sg.count(t) + g.box_tokens - 1) >> g.box_shift : 1;     // boxes
                 unsigned char* dst = s_ring + slot * C::SLOT;
 #pragma unroll 1
@@ -236,11 +264,12 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                     if (round > 0) ok = tree_wait(empty + slot * C::GROUPS + gr, (round - 1) & 1, abort, l.a.wait_timeouts, lane);
                     if (!ok) break;
                     const int c0 = gr * 4, nch = gr == C::GROUPS - 1 ? C::CH - c0 : 4;
-                    unsigned long long* bar = full + slot * C::GROUPS + gr;
-                    if (lane == 0) mbar_expect_tx(bar, (unsigned)(nch * 128) * (cached ? (unsigned)(used << g.box_shift) : (unsigned)l.N));
+                    unsigned long long* bars_t = full + slot * C::LAND;
+                    if (lane < C::LAND && 3 * lane >= c0 && 3 * lane < c0 + nch)      // parts that begin in this group
+                        mbar_expect_tx(bars_t + lane, (unsigned)(min(3, C::CH - 3 * lane) * 128) * (cached ? (unsigned)(used << g.box_shift) : (unsigned)l.N));
                     __syncwarp();
                     if (!cached) {
-                        if (lane < nch) tma_box3(dst + (c0 + lane) * C::CHUNK, &maps.fresh, 64 * (c0 + lane), 0, sg.b, bar);
+                        if (lane < nch) tma_box3(dst + (c0 + lane) * C::CHUNK, &maps.fresh, 64 * (c0 + lane), 0, sg.b, bars_t + (c0 + lane) / 3);
                     } else {
                         for (int p0 = 0; p0 < used * nch; p0 += 32) {
                             const int p = p0 + lane, box = p / nch, c = c0 + p - box * nch;
@@ -248,13 +277,14 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                             const int blk_h = __shfl_sync(0xffffffffu, blk0[1], box & 31), tok_h = __shfl_sync(0xffffffffu, tok0[1], box & 31);
                             if (box >= 32) { blk = blk_h; tok = tok_h; }
                             if (l.a.block_table) blk = max(0, min(blk, l.a.num_blocks - 1)) * g.blk_coord;
-                            if (p < used * nch) tma_box3(dst + c * C::CHUNK + ((box << g.box_shift) * 128), &maps.cache, 64 * c, tok, blk, bar);
+                            if (p < used * nch) tma_box3(dst + c * C::CHUNK + ((box << g.box_shift) * 128), &maps.cache, 64 * c, tok, blk, bars_t + c / 3);
                         }
                     }
                     __syncwarp();
-                    ++issued;
                 }
+                issued += C::LAND;
                 if (++slot == C::SLOTS) { slot = 0; ++round; }
+                if (ok && t == 0 && live == q_before) ok = copy_q();
 #pragma unroll
                 for (int h = 0; h < 2; ++h) { blk0[h] = blk1[h]; tok0[h] = tok1[h]; }
             }
@@ -262,122 +292,113 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
         // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
         volatile int no_abort = 0;
         if (live > 0) tree_wait(q_full, (live - 1) & 1, &no_abort, nullptr, lane);
-        for (int c = max(0, issued - PARTS); c < issued; ++c)
-            if (!tree_wait(full + c % PARTS, (c / PARTS) & 1, &no_abort, nullptr, lane)) break;
+        for (int c = max(0, issued - LANDS); c < issued; ++c)
+            if (!tree_wait(full + c % LANDS, (c / LANDS) & 1, &no_abort, nullptr, lane)) break;
     } else if (warp == 5) {
-        // ---- products -----------------------------------------------------------------------------------
-        constexpr unsigned kIdescS = instr_desc(kLatRows, kLatTile, false), kIdescO = instr_desc(kLatRows, 256, true);
-        const unsigned q_desc = desc_low(smem_u32(s_q), 16), k_desc = desc_low(smem_u32(s_ring), 16), v_desc = desc_low(smem_u32(s_ring), C::CHUNK);
-        // Scores run up to a tile ahead of the products with V, into the next share if need be: each has its own place in
-        // the shares, and whichever can go on does, scores first.
-        LatentSeg sp = {};                                    // the share of the products with V
-        int si = 0, pi = 0;                                   // shares begun by either
-        int ts = 0, tp = 0, s_tiles = 0, p_tiles = 0;         // tiles of it
-        int gs = 0, gp = 0, gr = 0;                           // tiles in all; the part of a slot that the scores are at
-        int s_slot = 0, s_round = 0, p_slot = 0;
-        int s_live = 0, p_live = 0;                           // shares with tiles
-        bool s_end = false;
-        LatentSeg pend[2];
-        long long idle = clock64();
+        // ---- scores ---------------------------------------------------------------------------------------
+        constexpr unsigned kIdescS = instr_desc(kLatRows, kLatTile, false);
+        const unsigned q_desc = desc_low(smem_u32(s_q), 16), k_desc = desc_low(smem_u32(s_ring), 16);
+        int done = 0, slot = 0, round = 0, live = 0;          // tiles of the shares before this one; shares with tiles
         bool ok = true;
-        while (ok && !(s_end && gp == gs)) {
-            bool moved = false;
-            if (!s_end && ts == s_tiles && si - pi < 2) {     // the scores' next share
-                if (mbar_test(info_full + (si & 1), (si >> 1) & 1)) {
-                    const LatentSeg x = s_info[si & 1];
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(info_empty + (si & 1));
-                    pend[0] = pend[1];
-                    pend[1] = x;
-                    moved = true;
-                    if (x.b < 0) { s_end = true; s_tiles = ts = 0; }
-                    else { sg = x; s_tiles = x.tiles(); ts = 0; ++si; }
-                }
-            }
-            if (tp == p_tiles && pi < si) {                   // the next share of the products with V: the older one that waits
-                sp = si - pi == 2 ? pend[0] : pend[1];
-                if (s_end) sp = pend[0];
-                p_tiles = sp.tiles();
-                tp = 0;
-                ++pi;
-                moved = true;
-            }
-            if (ts < s_tiles && gs <= gp + 1 && mbar_test(full + s_slot * C::GROUPS + gr, s_round & 1) &&
-                (ts > 0 || gr > 0 || mbar_test(q_full, s_live & 1))) {
-                // rows behind the last token, up to where the product with V stops: zero, whatever the cache or the slot held
-                const int c0 = gr * 4, nch = gr == C::GROUPS - 1 ? C::CH - c0 : 4, count = sg.count(ts);
-                if (count & 15) {
-                    const int pieces = (16 - (count & 15)) * 8;
-                    for (int i = lane; i < pieces * nch; i += 32) {
-                        const int c = i / pieces, p = i - c * pieces;
-                        *reinterpret_cast<uint4*>(s_ring + s_slot * C::SLOT + (c0 + c) * C::CHUNK + count * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
+        for (int i = 0; ok && next_seg(i); ++i) {
+            const int tiles = sg.tiles();
+            if (tiles == 0) continue;
+            ok = tree_wait(q_full, live & 1, abort, l.a.wait_timeouts, lane);
+            ++live;
+            for (int t = 0; ok && t < tiles; ++t) {
+                const int gt = done + t, buf = gt & 1;
+                // (this buffer of S has been read)
+                if (gt >= 2) ok = tree_wait(p_ready + buf, ((gt >> 1) - 1) & 1, abort, l.a.wait_timeouts, lane);
+                if (!ok) break;
                 tc_fence_after();
-                const int buf = gs & 1;
-                const bool last = gr == C::GROUPS - 1;
-                if (elect_one()) {
-                    const unsigned ka = k_desc + s_slot * (C::SLOT / 16), d = tmem + C::COL_S + buf * (kLatTile / 2);
-                    for (int c = c0; c < c0 + nch; ++c)
+                const unsigned d = tmem + C::COL_S + buf * (kLatTile / 2);
+                const int count = sg.count(t);
 #pragma unroll
-                        for (int kk = 0; kk < 4; ++kk)
-                            tc_mma_ws(d, q_desc + (c * kLatRows * 128 + kk * 32) / 16, ka + (c * C::CHUNK + kk * 32) / 16, kIdescS, c > 0 || kk > 0);
-                    if (last) {
-                        tc_commit(s_full + buf);
-                        if (ts == s_tiles - 1) tc_commit(q_empty);
+                for (int p = 0; p < C::LAND; ++p) {
+                    constexpr int kCols = 3;
+                    const int c0 = p * kCols, nch = C::CH - c0 < kCols ? C::CH - c0 : kCols;
+                    ok = ok && tree_wait(full + slot * C::LAND + p, round & 1, abort, l.a.wait_timeouts, lane);
+                    if (!ok) break;
+                    // rows behind the last token, up to where the product with V stops: zero, whatever the cache or the slot held
+                    if (count & 15) {
+                        const int pieces = (16 - (count & 15)) * 8;
+                        for (int x = lane; x < pieces * nch; x += 32) {
+                            const int c = x / pieces, at = x - c * pieces;
+                            *reinterpret_cast<uint4*>(s_ring + slot * C::SLOT + (c0 + c) * C::CHUNK + count * 128 + at * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
                     }
-                }
-                __syncwarp();
-                if (last) {
-                    gr = 0;
-                    if (++s_slot == C::SLOTS) { s_slot = 0; ++s_round; }
-                    if (ts == s_tiles - 1) ++s_live;
-                    ++ts;
-                    ++gs;
-                } else {
-                    ++gr;
-                }
-                moved = true;
-            } else if (tp < p_tiles && gp < gs && mbar_test(p_ready + (gp & 1), (gp >> 1) & 1) &&
-                       (tp > 0 || p_live == 0 || mbar_test(o_free, (p_live - 1) & 1))) {
-                tc_fence_after();
-                if (elect_one()) {
-                    const int steps = (sp.count(tp) + 15) / 16;
-                    const unsigned va = v_desc + p_slot * (C::SLOT / 16), pa = k_desc + (p_slot * C::SLOT + (C::CH - 1) * C::CHUNK) / 16;
-                    for (int nb = 0; nb < R / 256; ++nb) {
-                        for (int kk = 0; kk < steps; ++kk)
-                            tc_mma_ws(tmem + nb * 128, pa + kk * 2, va + (nb * 4 * C::CHUNK + kk * 2048) / 16, kIdescO, tp > 0 || kk > 0);
-                        tc_commit(empty + p_slot * C::GROUPS + nb);
+                    if (elect_one()) {
+                        const unsigned qa = q_desc + c0 * kLatRows * 128 / 16, ka = k_desc + (slot * C::SLOT + c0 * C::CHUNK) / 16;
+                        if (p == 0) tc_mma_ws(d, qa, ka, kIdescS, false);
+                        else tc_mma_ws_add(d, qa, ka, kIdescS);
+#pragma unroll
+                        for (int k = 1; k < 4 * kCols; ++k)
+                            if (k / 4 < nch) tc_mma_ws_add(d, qa + ((k / 4) * kLatRows * 128 + (k % 4) * 32) / 16, ka + ((k / 4) * C::CHUNK + (k % 4) * 32) / 16, kIdescS);
+                        if (p == C::LAND - 1) {
+                            tc_commit(s_full + buf);
+                            if (t == tiles - 1) tc_commit(q_empty);
+                        }
                     }
-                    tc_commit(pv_done + (gp & 1));
+                    __syncwarp();
                 }
-                __syncwarp();
-                if (++p_slot == C::SLOTS) p_slot = 0;
-                if (tp == p_tiles - 1) ++p_live;
-                ++tp;
-                ++gp;
-                moved = true;
+                if (++slot == C::SLOTS) { slot = 0; ++round; }
             }
-            if (moved) { idle = clock64(); continue; }
-            const bool late = clock64() - idle > kMbarWaitCycles;
-            if (late && lane == 0) {
-                *abort = 1;
-                if (l.a.wait_timeouts) atomicAdd(l.a.wait_timeouts, 1);
-            }
-            ok = !__any_sync(0xffffffffu, late || *abort);
+            done += tiles;
         }
-        if (__any_sync(0xffffffffu, !ok || *abort)) {         // TMEM is given back only when no product uses it
+        // TMEM is given back only when no product uses it
+        if (__any_sync(0xffffffffu, !ok || *abort)) {
             if (elect_one()) tc_commit(drained);
             __syncwarp();
             volatile int no_abort = 0;
             tree_wait(drained, 0u, &no_abort, nullptr, lane);
         }
+    } else if (warp == 7) {
+        // ---- products with V, by a warp of their own: each of the two goes on as soon as what it needs is there --------
+        constexpr unsigned kIdescO = instr_desc(kLatRows, 256, true);
+        const unsigned ring_desc = desc_low(smem_u32(s_ring), 16), v_desc = desc_low(smem_u32(s_ring), C::CHUNK);
+        int done = 0, slot = 0, live = 0;
+        bool ok = true;
+        for (int i = 0; ok && next_seg(i); ++i) {
+            const int tiles = sg.tiles();
+            if (tiles == 0) continue;
+            // (the first product replaces the last share's O)
+            if (live > 0) ok = tree_wait(o_free, (live - 1) & 1, abort, l.a.wait_timeouts, lane);
+            ++live;
+            for (int t = 0; ok && t < tiles; ++t) {
+                const int gt = done + t, buf = gt & 1;
+                ok = tree_wait(p_ready + buf, (gt >> 1) & 1, abort, l.a.wait_timeouts, lane);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const int steps = (sg.count(t) + 15) / 16;
+                    const unsigned va = v_desc + slot * (C::SLOT / 16), pa = ring_desc + (slot * C::SLOT + (C::CH - 1) * C::CHUNK) / 16;
+#pragma unroll
+                    for (int nb = 0; nb < R / 256; ++nb) {
+                        tc_mma_ws(tmem + nb * 128, pa, va + nb * 4 * C::CHUNK / 16, kIdescO, t > 0);
+#pragma unroll
+                        for (int kk = 1; kk < 4; ++kk)
+                            if (kk < steps) tc_mma_ws_add(tmem + nb * 128, pa + kk * 2, va + (nb * 4 * C::CHUNK + kk * 2048) / 16, kIdescO);
+                        tc_commit(empty + slot * C::GROUPS + nb);
+                    }
+                    tc_commit(pv_done + buf);
+                }
+                __syncwarp();
+                if (++slot == C::SLOTS) slot = 0;
+            }
+            done += tiles;
+        }
+        if (__any_sync(0xffffffffu, !ok || *abort)) {
+            if (elect_one()) tc_commit(drained + 1);
+            __syncwarp();
+            volatile int no_abort = 0;
+            tree_wait(drained + 1, 0u, &no_abort, nullptr, lane);
+        }
     } else if (warp == 6) {
         // ---- the new tokens' rows to the cache, by the blocks that have their unit -----------------------------
         for (int i = 0; next_seg(i); ++i)
-            if (sg.t1 == sg.units) latent_append<T>(l, sg.b, sg.S, sg.n, rt, l.row_tiles, lane);
+            if (sg.t1 == sg.all) latent_append<T>(l, sg.b, sg.S, sg.n, rt, l.row_tiles, lane);
     } else if (warp < 4) {
         // ---- softmax: two threads per query row, half of the tile's keys each -------------------------------
         const int half = warp >> 1, row = (warp & 1) * 32 + lane;
@@ -410,7 +431,7 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                 tc_ld32(x, tmem + lane_base + C::COL_S + buf * (kLatTile / 2));
                 // (a row that does not exist computes along, unmasked, and decides nothing)
                 int seen = kLatTile;
-                if (alive) seen = sg.t0 + t < sg.units - 1 ? sg.count(t) : token + 1;
+                if (alive) seen = sg.cached(t) ? sg.count(t) : token + 1;
                 seen -= half * 32;
                 const unsigned see = seen >= 32 ? ~0u : seen <= 0 ? 0u : (1u << seen) - 1u;
                 tc_wait_ld();
@@ -484,6 +505,8 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
 #pragma unroll 8
                     for (int c = 0; c < R / 16; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
                     if (half == 0) l.a.lse[orow] = -INFINITY;
+                } else if (sg.part >= 0 && half == 0) {
+                    g.part_ml[(int64_t)sg.part * kLatRows + row] = make_float2(-INFINITY, 0.f);
                 }
                 continue;
             }
@@ -497,29 +520,36 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
             total += sum_l;
             const bool none = !alive || total == 0.f;         // nothing seen: zeros and -inf
             const float inv = none ? 0.f : 1.f / total;
-#pragma unroll 1
-            for (int c = 0; c < R / 2; c += 32) {
-                unsigned o[32];
-                tc_ld32(o, tmem + lane_base + c);
-                tc_wait_ld();
-                const int dim = (c >> 7) * 256 + half * 128 + (c & 127);
-                if (sg.part >= 0) {
-                    float4* dst = g.part_o + ((int64_t)sg.part * (R / 4) + dim / 4) * kLatRows + row;
+            const bool mine = sg.part >= 0 ? alive : row < rows_all;       // (of a part nobody reads the other rows)
+            if (__any_sync(0xffffffffu, mine)) {
+                unsigned o[2][32];                            // (the next columns are on their way while these are stored)
+                tc_ld32(o[0], tmem + lane_base);
 #pragma unroll
-                    for (int k = 0; k < 32; k += 4)
-                        dst[(k / 4) * kLatRows] = make_float4(__uint_as_float(o[k]), __uint_as_float(o[k + 1]), __uint_as_float(o[k + 2]), __uint_as_float(o[k + 3]));
-                } else if (row < rows_all) {
-                    float f[32];
+                for (int c = 0; c < R / 2; c += 32) {
+                    const unsigned* x = o[(c / 32) & 1];
+                    tc_wait_ld();
+                    if (c + 32 < R / 2) tc_ld32(o[(c / 32 + 1) & 1], tmem + lane_base + c + 32);
+                    if (!mine) continue;
+                    const int dim = (c >> 7) * 256 + half * 128 + (c & 127);
+                    if (sg.part >= 0) {
+                        float4* dst = g.part_o + ((int64_t)sg.part * (R / 4) + dim / 4) * kLatRows + row;
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) f[k] = none ? 0.f : __uint_as_float(o[k]) * inv;
-                    T* dst = reinterpret_cast<T*>(l.a.out) + orow * R + dim;
+                        for (int k = 0; k < 32; k += 4)
+                            dst[(k / 4) * kLatRows] = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+                    } else {
+                        T* dst = reinterpret_cast<T*>(l.a.out) + orow * R + dim;
 #pragma unroll
-                    for (int k = 0; k < 32; k += 8)
-                        *reinterpret_cast<uint4*>(dst + k) = make_uint4(pack_bf16(f[k], f[k + 1]), pack_bf16(f[k + 2], f[k + 3]),
-                                                                        pack_bf16(f[k + 4], f[k + 5]), pack_bf16(f[k + 6], f[k + 7]));
+                        for (int k = 0; k < 32; k += 8) {
+                            unsigned y[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                y[e] = none ? 0u : pack_bf16(__uint_as_float(x[k + 2 * e]) * inv, __uint_as_float(x[k + 2 * e + 1]) * inv);
+                            *reinterpret_cast<uint4*>(dst + k) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    }
                 }
-                __syncwarp();
             }
+            __syncwarp();
             tc_fence_before();
             if (half == 0) {
                 if (sg.part >= 0) g.part_ml[(int64_t)sg.part * kLatRows + row] = none ? make_float2(-INFINITY, 0.f) : make_float2(m_ref * sl, total);
@@ -538,20 +568,41 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
 
 // Merges the partial results of requests that several blocks share: out = sum_i e^{m_i - M} O_i / sum_i e^{m_i - M} l_i.
 // A block: 64 dims of one (request, row tile); a warp has 8 rows x 4 pieces of four dims, so that it reads and writes whole sectors.
+// Which parts there are is worked out before the wait for the kernel in front, while that still runs: it begins its successors
+// when everything in front of it is done, so the lengths that it has read are there to be read here.
 template <int R>
-__global__ void __launch_bounds__(256) dsa_latent_merge_kernel(const LatentTcArgs g) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;");
+__global__ void __launch_bounds__(kLatThreads) dsa_latent_merge_kernel(const LatentTcArgs g) {
+    __shared__ int s_scan[kLatThreads / 32], s_before;
     const LatentArgs& l = g.l;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int idx = blockIdx.x;
     const int d0 = (idx % (R / 64)) * 64; idx /= R / 64;
     const int rt = idx % l.row_tiles, b = idx / l.row_tiles;
-    const int u0 = g.sched[b], u1 = g.sched[b + 1], quota = g.sched[l.a.B + 1];
-    const int g0 = u0 / quota, g1 = (u1 - 1) / quota;
-    if (g0 == g1) return;
     int S, n;
     latent_lengths(l, b, S, n);
+    int units = latent_units(S, n), before;
+    {
+        const int B = l.a.B, per = (B + kLatThreads - 1) / kLatThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+        int total;
+        before = latent_units_before(l, b0, b1, s_scan, total);
+        if (b >= b0 && b < b1) {
+            for (int i = b0; i < b; ++i) {
+                int Si, ni;
+                latent_lengths(l, i, Si, ni);
+                before += latent_units(Si, ni);
+            }
+            s_before = before;
+        }
+        __syncthreads();
+        const int setup = latent_setup(total, g.groups);
+        idx = max(g.min_units, (total + setup * B + g.groups - 1) / g.groups);
+        units += setup;
+        before = s_before + setup * b;
+    }
+    const int quota = idx, g0 = before / quota, g1 = (before + units - 1) / quota;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    if (g0 == g1) return;
     const int row = warp * 8 + lane / 4, c4 = lane % 4;
     if (rt * kLatRows + row >= l.rows) return;
     const bool alive = row < n * l.a.H_q - rt * kLatRows;
@@ -562,19 +613,21 @@ __global__ void __launch_bounds__(256) dsa_latent_merge_kernel(const LatentTcArg
 #pragma unroll
     for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (alive) {
-        for (int gi = g0; gi <= g1; ++gi) top = fmaxf(top, g.part_ml[part(gi) * kLatRows + row].x);
-#pragma unroll 2
+#pragma unroll 4
         for (int gi = g0; gi <= g1; ++gi) {
             const float2 ml = g.part_ml[part(gi) * kLatRows + row];
-            const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top);
-            sum = fmaf(w, ml.y, sum);
             const float4* o = g.part_o + (part(gi) * (R / 4) + d0 / 4 + c4) * kLatRows + row;
+            float4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = o[k * 4 * kLatRows];
             if (ml.y == 0.f) continue;                        // (a part that saw nothing)
+            const float next = fmaxf(top, ml.x), keep = fast_exp2(top - next), w = fast_exp2(ml.x - next);
+            top = next;
+            sum = fmaf(sum, keep, w * ml.y);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float4 x = o[k * 4 * kLatRows];
-                acc[k].x = fmaf(w, x.x, acc[k].x); acc[k].y = fmaf(w, x.y, acc[k].y);
-                acc[k].z = fmaf(w, x.z, acc[k].z); acc[k].w = fmaf(w, x.w, acc[k].w);
+                acc[k].x = fmaf(acc[k].x, keep, w * x[k].x); acc[k].y = fmaf(acc[k].y, keep, w * x[k].y);
+                acc[k].z = fmaf(acc[k].z, keep, w * x[k].z); acc[k].w = fmaf(acc[k].w, keep, w * x[k].w);
             }
         }
     }
