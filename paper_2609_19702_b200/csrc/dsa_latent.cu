@@ -12,7 +12,7 @@ using namespace dsa;
 struct LatentPlan {
     int rows, row_tiles;                           // query rows of a request, blocks of them
     int n_split;                                   // float32: pieces of a request's keys
-    int groups;                                    // bf16: blocks that share the keys of a row tile
+    int groups;                                    // bf16: shares of the work
     int64_t blocks;
     size_t ws_out_bytes, ws_total;                 // float32: partial outputs, and their log-sums behind them
     size_t ws_ml_bytes;                            // bf16: maxima and sums, and partial outputs behind them
@@ -30,10 +30,11 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
     pl->rows = heads * max_new;
     if (l->dtype == DSA_BF16) {
         pl->row_tiles = (pl->rows + kLatRows - 1) / kLatRows;
-        const int64_t units = (int64_t)l->batch * (((int64_t)l->max_seq_len + kLatTile - 1) / kLatTile + 1);
+        // (an upper bound of the units on the device, and of those that beginnings count for)
+        const int64_t units = (int64_t)l->batch * pl->row_tiles * (((int64_t)l->max_seq_len + kLatTile - 1) / kLatTile + 3);
         if (units > (1 << 30)) return DSA_ERR_UNSUPPORTED;
-        pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(host_sm_count() / pl->row_tiles, units / kLatMinUnits));
-        pl->blocks = (int64_t)pl->groups * pl->row_tiles;
+        pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(host_sm_count(), units / kLatMinUnits));
+        pl->blocks = pl->groups;
         if (pl->groups > 1) {
             pl->ws_ml_bytes = (size_t)pl->blocks * 2 * kLatRows * sizeof(float2);
             pl->ws_total = pl->ws_ml_bytes + (size_t)pl->blocks * 2 * kLatRows * l->latent_dim * sizeof(float);
@@ -104,7 +105,7 @@ cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, int64_t blocks,
     cudaError_t e = configure<R>();
     if (e == cudaSuccess) e = launch_dependent(dsa_latent_kernel<R>, blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
     if (e == cudaSuccess && g.groups > 1)
-        e = launch_dependent(dsa_latent_merge_kernel<R>, (int64_t)g.l.a.B * g.l.row_tiles * (R / 64), kLatThreads, 0, st, g);
+        e = launch_dependent(dsa_latent_merge_kernel<R, kLatTile, kLatRows>, (int64_t)g.l.a.B * g.l.row_tiles * (R / 64), kLatThreads, 0, st, g);
     return e;
 }
 template <int R>

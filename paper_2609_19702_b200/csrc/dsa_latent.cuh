@@ -11,15 +11,15 @@ constexpr int kLatThreads = 256;
 
 struct LatentTcArgs {
     LatentArgs l;
-    int groups;                                    // blocks that share the keys of a row tile
+    int groups;                                    // shares that the work is cut into
     int min_units;                                 // units of work that a block takes at least
     int box_tokens, box_shift;                     // tokens per tensor-map box of the cache, and its logarithm
     unsigned page_mul;                             // position / block_size = (position * page_mul) >> page_shift
     int page_shift;
     int q_rows;                                    // rows of q per copy: fewer than a block's where a request has fewer
     int blk_coord;                                 // 0: the map's outer dimension has one entry (stride 0)
-    float2* part_ml;                               // workspace: [groups * row_tiles * 2][64] maximum (base 2) and sum
-    float4* part_o;                                // [groups * row_tiles * 2][R / 4][64]
+    float2* part_ml;                               // workspace: [blocks * 2][64] maximum (base 2) and sum
+    float4* part_o;                                // [blocks * 2][R / 4][64]
 };
 
 struct LatentMaps {
@@ -58,51 +58,187 @@ __device__ __forceinline__ void tc_mma_ws_add(unsigned d, unsigned a_low, unsign
                  "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n}"
                  ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(kDescHigh) : "memory");
 }
-// Units of work of a request: its cached tiles and one for the new tokens (or for having nothing to do).
-__device__ __forceinline__ int latent_units(int S, int n) { return n > 0 ? (S + kLatTile - 1) / kLatTile + 1 : 1; }
-// To begin a request costs a block about as much as two tiles (its q, the last one's results), so where shares are large every
-// request counts that many units more, at its front.
-__device__ __forceinline__ int latent_setup(int total, int groups) { return total >= 8 * groups ? 2 : 0; }
-
-// A block's share of one request: tiles [t0, t1) of `all`, the last of which are the new tokens.
-struct LatentSeg {
-    int b, S, n, t0, t1, all, rows, part;          // b < 0: nothing any more.  rows: query rows of tokens that exist.  part: where the
-                                                   // partial result goes, -1: the block has the whole request
-    __device__ __forceinline__ int tiles() const { return rows > 0 ? t1 - t0 : 0; }
-    __device__ __forceinline__ bool cached(int t) const { return t0 + t < all - 1; }
-    __device__ __forceinline__ int count(int t) const { return cached(t) ? min(kLatTile, S - (t0 + t) * kLatTile) : n; }   // tokens of its tile t
+// ---- shares -------------------------------------------------------------------------------------------------
+// The work is a list of items: for every request the row tiles (ROWS query rows) that have tokens which exist, for each of them
+// a unit per key tile (KT tokens; the last unit: the new tokens).  End to end they are cut into shares of equal size, one per
+// block (or pair of blocks), so that every one has the same number of tiles whatever the lengths are.  An item that is cut
+// leaves partial results, which the merge kernel joins.
+// To begin an item costs about as much as two tiles (its q, the last one's results), so where shares are large every item counts
+// two units more, at its front.
+template <int KT, int ROWS>
+struct LatentItems {
+    int S, n, items, units;                        // of a request: lengths, items, and units of each
+    __device__ __forceinline__ LatentItems(const LatentArgs& l, int b) {
+        latent_lengths(l, b, S, n);
+        items = n > 0 ? (n * l.a.H_q + ROWS - 1) / ROWS : 1;
+        units = n > 0 ? (S + KT - 1) / KT + 1 : 1;
+    }
 };
 
-// The units of the requests before b0 where every thread of a block of kLatThreads calls it with its own stretch [b0, b1) of
-// them, in order; and of all.  s_scan: shared, a number per warp.
-__device__ __forceinline__ int latent_units_before(const LatentArgs& l, int b0, int b1, int* s_scan, int& total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int sum = 0;
+struct LatentShares {
+    int before, quota, setup;                      // units in front of request `b0`; of a share; that an item counts for its beginning
+};
+
+// By every thread of a block: units in front of request b0, where a thread has the stretch [b0, b1) of them, in order.
+// s_scan: shared, two numbers per warp.
+template <int KT, int ROWS>
+__device__ __forceinline__ LatentShares latent_shares(const LatentArgs& l, int groups, int min_units, int b0, int b1, int2* s_scan) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
+    int sum = 0, items = 0;
     for (int b = b0; b < b1; ++b) {
-        int S, n;
-        latent_lengths(l, b, S, n);
-        sum += latent_units(S, n);
+        const LatentItems<KT, ROWS> x(l, b);
+        sum += x.items * x.units;
+        items += x.items;
     }
-    int before = sum;
+    int before = sum, items_before = items;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, before, off);
-        if (lane >= off) before += x;
+        const int x = __shfl_up_sync(0xffffffffu, before, off), y = __shfl_up_sync(0xffffffffu, items_before, off);
+        if (lane >= off) { before += x; items_before += y; }
     }
-    if (lane == 31) s_scan[warp] = before;
+    if (lane == 31) s_scan[warp] = make_int2(before, items_before);
     before -= sum;
+    items_before -= items;
     __syncthreads();
-    total = 0;
-    for (int w = 0; w < kLatThreads / 32; ++w) {
-        if (w < warp) before += s_scan[w];
-        total += s_scan[w];
+    int total = 0, all = 0;
+    for (int w = 0; w < warps; ++w) {
+        const int2 x = s_scan[w];
+        if (w < warp) { before += x.x; items_before += x.y; }
+        total += x.x;
+        all += x.y;
     }
-    return before;
+    LatentShares r;
+    r.setup = total >= 8 * groups ? 2 : 0;
+    r.before = before + r.setup * items_before;
+    r.quota = max(min_units, (total + r.setup * all + groups - 1) / groups);
+    return r;
+}
+
+// What a share has of one item: tiles [t0, t1) of `all`, the last of which are the new tokens.
+template <int KT>
+struct LatentSeg {
+    int b, rt, S, n, t0, t1, all, rows, part;      // b < 0: nothing any more.  rows: query rows of tokens that exist (of the item's).
+                                                   // part: 0 / 1, the partial result's place; -1: the whole item
+    int zeros;                                     // > 0: the request's query rows from here on have no item, and this share sees to them
+    __device__ __forceinline__ int tiles() const { return t1 - t0; }
+    __device__ __forceinline__ bool cached(int t) const { return t0 + t < all - 1; }
+    __device__ __forceinline__ int count(int t) const { return cached(t) ? min(KT, S - (t0 + t) * KT) : n; }   // tokens of its tile t
+};
+
+// A share's place in the list, moved on from item to item by one warp.
+template <int KT, int ROWS>
+struct LatentCursor {
+    int b, at, left;                               // request, unit of it, units left
+    __device__ __forceinline__ LatentSeg<KT> next(const LatentArgs& l, int setup) {
+        LatentSeg<KT> sg = {};
+        sg.b = -1;
+        if (left <= 0) return sg;
+        const LatentItems<KT, ROWS> x(l, b);
+        const int units = x.units + setup, pos = at % units, end = min(units, pos + left);
+        sg.b = b;
+        sg.rt = at / units;
+        sg.S = x.S;
+        sg.n = x.n;
+        sg.all = x.n > 0 ? x.units : 0;
+        sg.t0 = min(sg.all, max(0, pos - setup));
+        sg.t1 = min(sg.all, max(0, end - setup));
+        sg.rows = min(ROWS, x.n * l.a.H_q - sg.rt * ROWS);
+        sg.part = pos == 0 && end == units ? -1 : pos > 0 ? 0 : 1;
+        sg.zeros = at == 0 && x.items * ROWS < l.rows ? x.items * ROWS : 0;
+        left -= end - pos;
+        at += end - pos;
+        if (at == x.items * units) { ++b; at = 0; }
+        return sg;
+    }
+};
+
+// By a whole block: where share `share` begins.  place: shared; request (-1: it is empty), unit of it, units, set-up units.
+template <int KT, int ROWS>
+__device__ __forceinline__ void latent_first(const LatentTcArgs& g, int share, int2* s_scan, int* place) {
+    const LatentArgs& l = g.l;
+    const int tid = threadIdx.x, B = l.a.B, per = (B + (int)blockDim.x - 1) / (int)blockDim.x, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+    if (tid == 0) { place[0] = -1; place[2] = 0; }
+    const LatentShares sh = latent_shares<KT, ROWS>(l, g.groups, g.min_units, b0, b1, s_scan);      // (has a barrier)
+    const int first = share * sh.quota;                       // (below 2^31: see the host's bound of the units)
+    int before = sh.before;
+    for (int b = b0; b < b1; ++b) {
+        const LatentItems<KT, ROWS> x(l, b);
+        const int units = x.items * (x.units + sh.setup);
+        if (first >= before && first < before + units) { place[0] = b; place[1] = first - before; }
+        // (units left in the list: the last request knows)
+        if (b == B - 1) place[2] = max(0, min(sh.quota, before + units - first));
+        before += units;
+    }
+    if (tid == 0) place[3] = sh.setup;
+    __syncthreads();
+}
+
+// What is left to one warp of a share: the new tokens' rows to the cache (by the shares that have their tile: tokens first,
+// first + step, ...), and zeros for the query rows that no item has.
+template <int R, int ROWS, int KT>
+__device__ __forceinline__ void latent_rest(const LatentArgs& l, const LatentSeg<KT>& sg, int first, int step, int lane) {
+    if (sg.t1 == sg.all) latent_append<__nv_bfloat16>(l, sg.b, sg.S, sg.n, first, step, lane);
+    if (sg.zeros > 0) {
+        uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(l.a.out) + ((int64_t)sg.b * l.rows + sg.zeros) * R);
+        const int pieces = (l.rows - sg.zeros) * (R / 8);
+        for (int i = lane; i < pieces; i += 32) out[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (int r = sg.zeros + lane; r < l.rows; r += 32) l.a.lse[(int64_t)sg.b * l.rows + r] = -INFINITY;
+    }
+}
+
+// The results of 64 query rows by the four warps that have their TMEM lanes, two threads a row (half 0 / 1: dims 0-127 / 128-255 of
+// every 256): to out and lse, or, part >= 0, what the merge needs.  m: maximum in base-2 units, total: the row's sum.
+template <int R>
+__device__ __forceinline__ void latent_results(const LatentTcArgs& g, unsigned tmem, int64_t orow, int rows_all, int row, int half, int part,
+                                               bool any, bool alive, float m, float total) {
+    const LatentArgs& l = g.l;
+    const bool none = !alive || total == 0.f;                 // nothing seen: zeros and -inf
+    const float inv = none ? 0.f : 1.f / total;
+    const bool mine = part >= 0 ? alive && any : row < rows_all;           // (of a part nobody reads the other rows)
+    if (__any_sync(0xffffffffu, mine)) {
+        unsigned o[2][32];                                    // (the next columns are on their way while these are stored)
+        if (any) tc_ld32(o[0], tmem);
+#pragma unroll
+        for (int c = 0; c < R / 2; c += 32) {
+            const unsigned* x = o[(c / 32) & 1];
+            if (any) {
+                tc_wait_ld();
+                if (c + 32 < R / 2) tc_ld32(o[(c / 32 + 1) & 1], tmem + c + 32);
+            }
+            if (mine) {
+                const int dim = (c >> 7) * 256 + half * 128 + (c & 127);
+                if (part >= 0) {
+                    float4* dst = g.part_o + ((int64_t)part * (R / 4) + dim / 4) * kLatRows + row;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        dst[(k / 4) * kLatRows] = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+                } else {
+                    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(l.a.out) + orow * R + dim;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8) {
+                        unsigned y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[e] = none ? 0u : pack_bf16(__uint_as_float(x[k + 2 * e]) * inv, __uint_as_float(x[k + 2 * e + 1]) * inv);
+                        *reinterpret_cast<uint4*>(dst + k) = make_uint4(y[0], y[1], y[2], y[3]);
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        tc_fence_before();
+    }
+    if (half == 0) {
+        if (part >= 0) g.part_ml[(int64_t)part * kLatRows + row] = none ? make_float2(-INFINITY, 0.f) : make_float2(m, total);
+        else if (row < rows_all) l.a.lse[orow] = none ? -INFINITY : (m + log2f(total)) * LN2;
+    }
+    __syncwarp();
 }
 
 template <int R>
 __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const LatentTcArgs g, const __grid_constant__ LatentMaps maps) {
     using C = LatentCfg<R>;
+    using Seg = LatentSeg<kLatTile>;
     using T = __nv_bfloat16;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* s_q = smem;
@@ -121,16 +257,16 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     unsigned long long* o_free = s_full + 12;                 // O has been read
     unsigned long long* drained = s_full + 13;                // [2]
     unsigned long long* pair = s_full + 15;                   // [2] the two warps of a row have written to s_pair
-    LatentSeg* s_info = reinterpret_cast<LatentSeg*>(s_full + 18);             // [2]
+    Seg* s_info = reinterpret_cast<Seg*>(s_full + 18);        // [2]
     float* s_pair = reinterpret_cast<float*>(s_info + 2);     // [2][128] maxima and sums that the two halves of a row exchange
     int* s_misc = reinterpret_cast<int*>(s_pair + 256);       // [0] TMEM address, [1] abort, [2..] first request, its first unit, units, set-up units
-    int* s_scan = s_misc + 8;                                 // [8]
-    static_assert((LANDS + PARTS + 18) * 8 + 2 * sizeof(LatentSeg) + 1024 + 64 <= C::TAIL, "tail of the shared memory");
+    int2* s_scan = reinterpret_cast<int2*>(s_misc + 8);       // [8]
+    static_assert((LANDS + PARTS + 18) * 8 + 2 * sizeof(Seg) + 1024 + 96 <= C::TAIL, "tail of the shared memory");
     volatile int* abort = s_misc + 1;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const LatentArgs& l = g.l;
-    const int rt = (int)blockIdx.x % l.row_tiles, group = (int)blockIdx.x / l.row_tiles;
+    const int share = (int)blockIdx.x;
 
     if (warp == 4 && lane == 0) {
         for (int s = 0; s < LANDS + PARTS; ++s) mbar_init(bars + s, 1);
@@ -162,28 +298,9 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
 
-    // ---- this block's share: the units of all requests end to end, cut into equal pieces -----------------------------
-    {
-        const int B = l.a.B, per = (B + kLatThreads - 1) / kLatThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-        int total, before = latent_units_before(l, b0, b1, s_scan, total);
-        const int setup = latent_setup(total, g.groups);
-        total += setup * B;
-        before += setup * b0;
-        const int quota = max(g.min_units, (total + g.groups - 1) / g.groups);
-        const int first = min(total, group * quota);          // (group * quota < total + groups * min_units)
-        if (tid == 0) { s_misc[2] = -1; s_misc[4] = min(total, first + quota) - first; s_misc[5] = setup; }
-        __syncthreads();
-        for (int b = b0; b < b1; ++b) {
-            int S, n;
-            latent_lengths(l, b, S, n);
-            const int units = latent_units(S, n) + setup;
-            if (first >= before && first < before + units) { s_misc[2] = b; s_misc[3] = first - before; }
-            before += units;
-        }
-    }
-    __syncthreads();
+    latent_first<kLatTile, kLatRows>(g, share, s_scan, s_misc + 2);
 
-    LatentSeg sg;
+    Seg sg;
     auto next_seg = [&](int i) -> bool {
         if (!tree_wait(info_full + (i & 1), (i >> 1) & 1, abort, l.a.wait_timeouts, lane)) return false;
         sg = s_info[i & 1];
@@ -195,23 +312,11 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     if (warp == 4) {
         // ---- what to work on; copies of q and of the cached rows ------------------------------------------
         const int setup = s_misc[5];
-        int b = s_misc[2], at = s_misc[3], left = s_misc[4];
+        LatentCursor<kLatTile, kLatRows> cur = {s_misc[2], s_misc[3], s_misc[4]};
         int slot = 0, round = 0, issued = 0, live = 0;
         bool ok = true;
         for (int i = 0; ok; ++i) {
-            sg.b = left > 0 ? b : -1;
-            if (sg.b >= 0) {
-                latent_lengths(l, b, sg.S, sg.n);
-                const int units = latent_units(sg.S, sg.n) + setup, end = min(units, at + left);
-                sg.all = sg.n > 0 ? units - setup : 0;
-                sg.t0 = min(sg.all, max(0, at - setup));
-                sg.t1 = min(sg.all, max(0, end - setup));
-                sg.rows = max(0, min(kLatRows, sg.n * l.a.H_q - rt * kLatRows));
-                sg.part = at == 0 && end == units ? -1 : ((int)blockIdx.x * 2 + (at > 0 ? 0 : 1));
-                left -= end - at;
-                at = 0;
-                ++b;
-            }
+            sg = cur.next(l, setup);
             if (i >= 2) ok = tree_wait(info_empty + (i & 1), ((i >> 1) - 1) & 1, abort, l.a.wait_timeouts, lane);
             if (!ok) break;
             if (lane == 0) s_info[i & 1] = sg;
@@ -243,12 +348,12 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
             // which need not wait for that
             if (lane < C::CH)
                 asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
-                             ::"l"(&maps.q), "r"(64 * lane), "r"(sg.b * l.rows + rt * kLatRows), "r"(0) : "memory");
+                             ::"l"(&maps.q), "r"(64 * lane), "r"(sg.b * l.rows + sg.rt * kLatRows), "r"(0) : "memory");
             auto copy_q = [&]() -> bool {
                 if (live > 0 && !tree_wait(q_empty, (live - 1) & 1, abort, l.a.wait_timeouts, lane)) return false;
                 if (lane == 0) mbar_expect_tx(q_full, (unsigned)(C::CH * 128 * g.q_rows));
                 __syncwarp();
-                if (lane < C::CH) tma_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, sg.b * l.rows + rt * kLatRows, 0, q_full);
+                if (lane < C::CH) tma_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, sg.b * l.rows + sg.rt * kLatRows, 0, q_full);
                 __syncwarp();
                 ++live;
                 return true;
@@ -397,14 +502,12 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
         }
     } else if (warp == 6) {
         // ---- the new tokens' rows to the cache, by the blocks that have their unit -----------------------------
-        for (int i = 0; next_seg(i); ++i)
-            if (sg.t1 == sg.all) latent_append<T>(l, sg.b, sg.S, sg.n, rt, l.row_tiles, lane);
+        for (int i = 0; next_seg(i); ++i) latent_rest<R, kLatRows>(l, sg, sg.rt, (sg.n * l.a.H_q + kLatRows - 1) / kLatRows, lane);
     } else if (warp < 4) {
         // ---- softmax: two threads per query row, half of the tile's keys each -------------------------------
         const int half = warp >> 1, row = (warp & 1) * 32 + lane;
         const unsigned lane_base = (unsigned)(warp * 32) << 16;
         const float sl = l.a.scale_log2;
-        const int token = (rt * kLatRows + row) / l.a.H_q;
         int done = 0, slot = 0, swaps = 0;
         bool ok = true;
         // a number from either thread of a row to the other one
@@ -421,6 +524,7 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
         for (int i = 0; ok && next_seg(i); ++i) {
             const int tiles = sg.tiles();
             const bool alive = row < sg.rows;
+            const int token = (sg.rt * kLatRows + row) / l.a.H_q;
             float m_ref = -INFINITY, sum_l = 0.f;
             for (int t = 0; ok && t < tiles; ++t) {
                 const int gt = done + t, buf = gt & 1;
@@ -497,65 +601,17 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                 if (++slot == C::SLOTS) slot = 0;
             }
             if (!ok) break;
-            const int rows_all = min(kLatRows, l.rows - rt * kLatRows);
-            const int64_t orow = (int64_t)sg.b * l.rows + rt * kLatRows + row;
-            if (tiles == 0) {
-                if (sg.part < 0 && row < rows_all) {          // nothing to attend with: zeros and -inf
-                    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<T*>(l.a.out) + orow * R) + half * (R / 16);
-#pragma unroll 8
-                    for (int c = 0; c < R / 16; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
-                    if (half == 0) l.a.lse[orow] = -INFINITY;
-                } else if (sg.part >= 0 && half == 0) {
-                    g.part_ml[(int64_t)sg.part * kLatRows + row] = make_float2(-INFINITY, 0.f);
-                }
-                continue;
+            float total = 0.f;
+            if (tiles > 0) {
+                done += tiles;
+                ok = tree_wait(pv_done + ((done - 1) & 1), ((done - 1) >> 1) & 1, abort, l.a.wait_timeouts, lane) && swap(sum_l, total);
+                if (!ok) break;
+                tc_fence_after();
+                total += sum_l;
             }
-            done += tiles;
-            ok = tree_wait(pv_done + ((done - 1) & 1), ((done - 1) >> 1) & 1, abort, l.a.wait_timeouts, lane);
-            if (!ok) break;
-            tc_fence_after();
-            float total;
-            ok = swap(sum_l, total);
-            if (!ok) break;
-            total += sum_l;
-            const bool none = !alive || total == 0.f;         // nothing seen: zeros and -inf
-            const float inv = none ? 0.f : 1.f / total;
-            const bool mine = sg.part >= 0 ? alive : row < rows_all;       // (of a part nobody reads the other rows)
-            if (__any_sync(0xffffffffu, mine)) {
-                unsigned o[2][32];                            // (the next columns are on their way while these are stored)
-                tc_ld32(o[0], tmem + lane_base);
-#pragma unroll
-                for (int c = 0; c < R / 2; c += 32) {
-                    const unsigned* x = o[(c / 32) & 1];
-                    tc_wait_ld();
-                    if (c + 32 < R / 2) tc_ld32(o[(c / 32 + 1) & 1], tmem + lane_base + c + 32);
-                    if (!mine) continue;
-                    const int dim = (c >> 7) * 256 + half * 128 + (c & 127);
-                    if (sg.part >= 0) {
-                        float4* dst = g.part_o + ((int64_t)sg.part * (R / 4) + dim / 4) * kLatRows + row;
-#pragma unroll
-                        for (int k = 0; k < 32; k += 4)
-                            dst[(k / 4) * kLatRows] = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
-                    } else {
-                        T* dst = reinterpret_cast<T*>(l.a.out) + orow * R + dim;
-#pragma unroll
-                        for (int k = 0; k < 32; k += 8) {
-                            unsigned y[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                y[e] = none ? 0u : pack_bf16(__uint_as_float(x[k + 2 * e]) * inv, __uint_as_float(x[k + 2 * e + 1]) * inv);
-                            *reinterpret_cast<uint4*>(dst + k) = make_uint4(y[0], y[1], y[2], y[3]);
-                        }
-                    }
-                }
-            }
-            __syncwarp();
-            tc_fence_before();
-            if (half == 0) {
-                if (sg.part >= 0) g.part_ml[(int64_t)sg.part * kLatRows + row] = none ? make_float2(-INFINITY, 0.f) : make_float2(m_ref * sl, total);
-                else if (row < rows_all) l.a.lse[orow] = none ? -INFINITY : (m_ref * sl + log2f(total)) * LN2;
-            }
-            __syncwarp();
+            latent_results<R>(g, tmem + lane_base, (int64_t)sg.b * l.rows + sg.rt * kLatRows + row, min(kLatRows, l.rows - sg.rt * kLatRows), row,
+                              half, sg.part < 0 ? -1 : share * 2 + sg.part, tiles > 0, alive, m_ref * sl, total);
+            if (tiles == 0) continue;
             if (lane == 0) mbar_arrive(o_free);
         }
     }
@@ -566,48 +622,41 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     }
 }
 
-// Merges the partial results of requests that several blocks share: out = sum_i e^{m_i - M} O_i / sum_i e^{m_i - M} l_i.
-// A block: 64 dims of one (request, row tile); a warp has 8 rows x 4 pieces of four dims, so that it reads and writes whole sectors.
+// Merges the partial results of items that several shares have: out = sum_i e^{m_i - M} O_i / sum_i e^{m_i - M} l_i.
+// A block: 64 dims of 64 query rows; a warp has 8 rows x 4 pieces of four dims, so that it reads and writes whole sectors.
 // Which parts there are is worked out before the wait for the kernel in front, while that still runs: it begins its successors
 // when everything in front of it is done, so the lengths that it has read are there to be read here.
-template <int R>
+template <int R, int KT, int ROWS>
 __global__ void __launch_bounds__(kLatThreads) dsa_latent_merge_kernel(const LatentTcArgs g) {
-    __shared__ int s_scan[kLatThreads / 32], s_before;
+    __shared__ int2 s_scan[kLatThreads / 32];
+    __shared__ int s_before;
+    constexpr int PER = ROWS / kLatRows;                      // blocks that have an item's rows
     const LatentArgs& l = g.l;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int idx = blockIdx.x;
     const int d0 = (idx % (R / 64)) * 64; idx /= R / 64;
     const int rt = idx % l.row_tiles, b = idx / l.row_tiles;
-    int S, n;
-    latent_lengths(l, b, S, n);
-    int units = latent_units(S, n), before;
-    {
-        const int B = l.a.B, per = (B + kLatThreads - 1) / kLatThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-        int total;
-        before = latent_units_before(l, b0, b1, s_scan, total);
-        if (b >= b0 && b < b1) {
-            for (int i = b0; i < b; ++i) {
-                int Si, ni;
-                latent_lengths(l, i, Si, ni);
-                before += latent_units(Si, ni);
-            }
-            s_before = before;
+    const int B = l.a.B, per = (B + kLatThreads - 1) / kLatThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+    const LatentShares sh = latent_shares<KT, ROWS>(l, g.groups, g.min_units, b0, b1, s_scan);
+    if (b >= b0 && b < b1) {
+        int before = sh.before;
+        for (int i = b0; i < b; ++i) {
+            const LatentItems<KT, ROWS> x(l, i);
+            before += x.items * (x.units + sh.setup);
         }
-        __syncthreads();
-        const int setup = latent_setup(total, g.groups);
-        idx = max(g.min_units, (total + setup * B + g.groups - 1) / g.groups);
-        units += setup;
-        before = s_before + setup * b;
+        s_before = before;
     }
-    const int quota = idx, g0 = before / quota, g1 = (before + units - 1) / quota;
+    __syncthreads();
+    const LatentItems<KT, ROWS> x(l, b);
+    const int first = s_before + rt / PER * (x.units + sh.setup), g0 = first / sh.quota, g1 = (first + x.units + sh.setup - 1) / sh.quota;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    if (g0 == g1) return;
+    if (g0 == g1 || rt / PER >= x.items) return;
     const int row = warp * 8 + lane / 4, c4 = lane % 4;
     if (rt * kLatRows + row >= l.rows) return;
-    const bool alive = row < n * l.a.H_q - rt * kLatRows;
+    const bool alive = row < x.n * l.a.H_q - rt * kLatRows;
     const int64_t orow = (int64_t)b * l.rows + rt * kLatRows + row;
-    auto part = [&](int gi) { return (int64_t)(gi * l.row_tiles + rt) * 2 + (gi == g0 ? 1 : 0); };
+    auto part = [&](int gi) { return (int64_t)(gi * PER + rt % PER) * 2 + (gi == g0 ? 1 : 0); };
     float top = -INFINITY, sum = 0.f;
     float4 acc[4];
 #pragma unroll
@@ -617,17 +666,17 @@ __global__ void __launch_bounds__(kLatThreads) dsa_latent_merge_kernel(const Lat
         for (int gi = g0; gi <= g1; ++gi) {
             const float2 ml = g.part_ml[part(gi) * kLatRows + row];
             const float4* o = g.part_o + (part(gi) * (R / 4) + d0 / 4 + c4) * kLatRows + row;
-            float4 x[4];
+            float4 y[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = o[k * 4 * kLatRows];
+            for (int k = 0; k < 4; ++k) y[k] = o[k * 4 * kLatRows];
             if (ml.y == 0.f) continue;                        // (a part that saw nothing)
             const float next = fmaxf(top, ml.x), keep = fast_exp2(top - next), w = fast_exp2(ml.x - next);
             top = next;
             sum = fmaf(sum, keep, w * ml.y);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                acc[k].x = fmaf(acc[k].x, keep, w * x[k].x); acc[k].y = fmaf(acc[k].y, keep, w * x[k].y);
-                acc[k].z = fmaf(acc[k].z, keep, w * x[k].z); acc[k].w = fmaf(acc[k].w, keep, w * x[k].w);
+                acc[k].x = fmaf(acc[k].x, keep, w * y[k].x); acc[k].y = fmaf(acc[k].y, keep, w * y[k].y);
+                acc[k].z = fmaf(acc[k].z, keep, w * y[k].z); acc[k].w = fmaf(acc[k].w, keep, w * y[k].w);
             }
         }
     }
