@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "dsa_latent.cuh"
+#include "dsa_latent_pair.cuh"
 #include "dsa_latent_f32.cuh"
 #include "dsa_latent_host.cuh"
 
@@ -12,7 +13,8 @@ using namespace dsa;
 struct LatentPlan {
     int rows, row_tiles;                           // query rows of a request, blocks of them
     int n_split;                                   // float32: pieces of a request's keys
-    int groups;                                    // bf16: shares of the work
+    bool pairs;                                    // bf16: pairs of blocks with 128 query rows
+    int groups;                                    // and shares of the work
     int64_t blocks;
     size_t ws_out_bytes, ws_total;                 // float32: partial outputs, and their log-sums behind them
     size_t ws_ml_bytes;                            // bf16: maxima and sums, and partial outputs behind them
@@ -33,8 +35,10 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
         // (an upper bound of the units on the device, and of those that beginnings count for)
         const int64_t units = (int64_t)l->batch * pl->row_tiles * (((int64_t)l->max_seq_len + kLatTile - 1) / kLatTile + 3);
         if (units > (1 << 30)) return DSA_ERR_UNSUPPORTED;
-        pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(host_sm_count(), units / kLatMinUnits));
-        pl->blocks = pl->groups;
+        pl->pairs = pl->rows > kLatRows;
+        const int per = pl->pairs ? 2 : 1;
+        pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(host_sm_count() / per, units / (per * per * kLatMinUnits)));
+        pl->blocks = (int64_t)pl->groups * per;
         if (pl->groups > 1) {
             pl->ws_ml_bytes = (size_t)pl->blocks * 2 * kLatRows * sizeof(float2);
             pl->ws_total = pl->ws_ml_bytes + (size_t)pl->blocks * 2 * kLatRows * l->latent_dim * sizeof(float);
@@ -96,17 +100,22 @@ int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void*
 template <int R>
 cudaError_t configure() {
     static std::atomic<bool> done[kMaxDevices] = {}, done_f32[kMaxDevices] = {};
+    static std::atomic<bool> done_pair[kMaxDevices] = {};
     cudaError_t e = configure_smem(dsa_latent_kernel<R>, LatentCfg<R>::SMEM, done);
+    if (e == cudaSuccess) e = configure_smem(dsa_latent_pair_kernel<R>, PairCfg<R>::SMEM, done_pair);
     if (e == cudaSuccess) e = configure_smem(dsa_latent_f32_kernel<R>, LatentF32Cfg<R>::SMEM, done_f32);
     return e;
 }
 template <int R>
-cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, int64_t blocks, cudaStream_t st) {
+cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, bool pairs, int64_t blocks, cudaStream_t st) {
     cudaError_t e = configure<R>();
-    if (e == cudaSuccess) e = launch_dependent(dsa_latent_kernel<R>, blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
-    if (e == cudaSuccess && g.groups > 1)
-        e = launch_dependent(dsa_latent_merge_kernel<R, kLatTile, kLatRows>, (int64_t)g.l.a.B * g.l.row_tiles * (R / 64), kLatThreads, 0, st, g);
-    return e;
+    if (e != cudaSuccess) return e;
+    e = pairs ? launch_dependent(dsa_latent_pair_kernel<R>, blocks, kPairThreads, PairCfg<R>::SMEM, st, g, m)
+              : launch_dependent(dsa_latent_kernel<R>, blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
+    if (e != cudaSuccess || g.groups == 1) return e;
+    const int64_t merge = (int64_t)g.l.a.B * g.l.row_tiles * (R / 64);
+    return pairs ? launch_dependent(dsa_latent_merge_kernel<R, kPairTile, kPairRows>, merge, kLatThreads, 0, st, g)
+                 : launch_dependent(dsa_latent_merge_kernel<R, kLatTile, kLatRows>, merge, kLatThreads, 0, st, g);
 }
 template <int R>
 cudaError_t run_f32(const LatentArgs& g, int64_t blocks, cudaStream_t st) {
@@ -187,7 +196,7 @@ int32_t dsa_latent_step(const dsa_latent* latent, int32_t num_heads, int32_t max
         LatentMaps m;
         const int32_t built = build_latent_maps(latent, pl, q, c_new, &t, &m);
         if (built != DSA_OK) return built;
-        e = latent->latent_dim == 256 ? run_bf16<256>(t, m, pl.blocks, st) : run_bf16<512>(t, m, pl.blocks, st);
+        e = latent->latent_dim == 256 ? run_bf16<256>(t, m, pl.pairs, pl.blocks, st) : run_bf16<512>(t, m, pl.pairs, pl.blocks, st);
         return e == cudaSuccess ? DSA_OK : host_cuda_fail(e);
     }
     if (pl.n_split > 1) {
