@@ -33,10 +33,10 @@ int32_t check_prompt(const dsa_prompt* p) {
     return DSA_OK;
 }
 
-// A view [tokens][heads][width] for the tensor-map copies: 64 elements (128 bytes) of one head and a tile of tokens per copy,
+// A view [tokens][heads][width] for the tensor-map copies: 64 elements (128 bytes) of one head and `box` tokens per copy,
 // 128-byte swizzle; what a copy asks for beyond the view arrives as zeros.  head: 1, or 0 where all heads read the same rows.
 bool encode_heads(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, int64_t width, int64_t heads, int64_t tokens,
-                  int64_t head_stride, int64_t token_stride, int* head) {
+                  int64_t head_stride, int64_t token_stride, int box, int* head) {
     const int64_t most = 0xffffffffLL;
     if (tokens < 1 || tokens > most) return false;
     if (tokens == 1) token_stride = width + 64;    // (never used: any stride will do)
@@ -45,7 +45,7 @@ bool encode_heads(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, 
     if (token_stride >= (1LL << 39) || head_stride >= (1LL << 39)) return false;
     const cuuint64_t n[3] = {(cuuint64_t)width, (cuuint64_t)(*head ? heads : 1), (cuuint64_t)tokens};
     const cuuint64_t pitch[2] = {(cuuint64_t)(*head ? head_stride : token_stride) * 2, (cuuint64_t)token_stride * 2};
-    const cuuint32_t bx[3] = {64u, 1u, (cuuint32_t)kPrTile}, step[3] = {1u, 1u, 1u};
+    const cuuint32_t bx[3] = {64u, 1u, (cuuint32_t)box}, step[3] = {1u, 1u, 1u};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), n, pitch, bx, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -112,10 +112,10 @@ int32_t dsa_latent_prompt(const dsa_prompt* p, void* out, float* lse, void* stre
         // (without any key no copy of a key is made, and the views may be those of q)
         const bool keys = p->kv_tokens > 0;
         const int64_t kv = keys ? p->kv_tokens : 1, W = p->nope_dim + p->rope_dim, H = p->num_heads;
-        const bool ok = encode_heads(encode, &m.q, p->q, W, H, p->q_tokens, p->q_stride_head, p->q_stride_token, &m.q_head) &&
-                        encode_heads(encode, &m.k, keys ? p->k_nope : p->q, p->nope_dim, H, kv, p->k_stride_head, p->k_stride_token, &m.k_head) &&
-                        encode_heads(encode, &m.kr, keys ? p->k_rope : p->q, p->rope_dim, 1, kv, 0, p->rope_stride_token, &one) &&
-                        encode_heads(encode, &m.v, keys ? p->v : p->q, p->value_dim, H, kv, p->v_stride_head, p->v_stride_token, &m.v_head);
+        const bool ok = encode_heads(encode, &m.q, p->q, W, H, p->q_tokens, p->q_stride_head, p->q_stride_token, kPrRows, &m.q_head) &&
+                        encode_heads(encode, &m.k, keys ? p->k_nope : p->q, p->nope_dim, H, kv, p->k_stride_head, p->k_stride_token, kPrTile, &m.k_head) &&
+                        encode_heads(encode, &m.kr, keys ? p->k_rope : p->q, p->rope_dim, 1, kv, 0, p->rope_stride_token, kPrTile, &one) &&
+                        encode_heads(encode, &m.v, keys ? p->v : p->q, p->value_dim, H, kv, p->v_stride_head, p->v_stride_token, kPrTile, &m.v_head);
         if (!ok) return DSA_ERR_UNSUPPORTED;       // (an extent or stride beyond what a tensor map holds)
     }
     e = p->nope_dim == 64 ? run<64>(g, m, bf16, blocks, st) : run<128>(g, m, bf16, blocks, st);

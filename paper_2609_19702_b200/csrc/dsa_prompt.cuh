@@ -5,10 +5,10 @@
 
 namespace dsa {
 
-constexpr int kPrTile = 128;                       // keys per tile
+constexpr int kPrTile = 96;                        // keys per tile: two tiles of K and V fit beside 256 queries
 constexpr int kPrRows = 128;                       // query rows per half of a block: the M of the products
 constexpr int kPrBlock = 2 * kPrRows;
-constexpr int kPrThreads = 320;
+constexpr int kPrThreads = 352;
 
 struct PromptMaps {
     CUtensorMap q, k, kr, v;
@@ -18,13 +18,14 @@ struct PromptMaps {
 template <int D>
 struct PromptCfg {
     static constexpr int KC = D / 64 + 1, VC = D / 64;                     // 64-element columns of a key (the last: k_rope), a value
-    static constexpr int COL = kPrTile * 128;                              // bytes of one column of a tile
-    static constexpr int Q_BYTES = 2 * KC * COL;
-    static constexpr int RING = D == 128 ? 8 : 9;
+    static constexpr int COL = kPrTile * 128, Q_COL = kPrRows * 128;       // bytes of one column of a tile, of a half's queries
+    static constexpr int Q_BYTES = 2 * KC * Q_COL;
+    static constexpr int RING = (D == 128 ? 2 : 4) * (KC + VC);            // columns in flight
     static constexpr int TAIL = 1024;
     static constexpr int SMEM = Q_BYTES + RING * COL + TAIL;
     static constexpr int COL_O = 2 * kPrTile, TMEM_COLS = 512;
     static_assert(SMEM <= 232448, "shared memory of an SM");
+    static_assert(RING % (KC + VC) == 0, "a tile's columns lie side by side");
 };
 
 __device__ __forceinline__ void tma_col(void* dst, const CUtensorMap* map, int c0, int c1, int c2, unsigned long long* bar) {
@@ -40,29 +41,29 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     unsigned char* s_q = smem;
     unsigned char* s_ring = smem + C::Q_BYTES;
     unsigned long long* full = reinterpret_cast<unsigned long long*>(s_ring + C::RING * C::COL);   // [RING] a column has landed
-    unsigned long long* empty = full + C::RING;               // [RING] the products that read it are done
+    unsigned long long* empty = full + C::RING;               // [RING] the products of either half that read it are done
     unsigned long long* q_full = empty + C::RING;             // [2] a half's queries
     unsigned long long* s_full = q_full + 2;                  // [2] scores are in TMEM
     unsigned long long* p_ready = q_full + 4;                 // [2] weights are in TMEM
     unsigned long long* pv_done = q_full + 6;                 // [2] O holds the tile
-    unsigned long long* drained = q_full + 8;
-    int* s_misc = reinterpret_cast<int*>(q_full + 9);         // [0] TMEM address, [1] abort
-    static_assert((2 * C::RING + 9) * 8 + 8 <= C::TAIL, "tail of the shared memory");
+    unsigned long long* drained = q_full + 8;                 // [2]
+    unsigned long long* turn = q_full + 10;                   // [2] the other half has issued its products
+    int* s_misc = reinterpret_cast<int*>(q_full + 12);        // [0] TMEM address, [1] abort
+    static_assert((2 * C::RING + 12) * 8 + 8 <= C::TAIL, "tail of the shared memory");
     volatile int* abort = s_misc + 1;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int tiles_q = (g.max_q_len + kPrBlock - 1) / kPrBlock;
     int idx = blockIdx.x;
     const int h = idx % g.H; idx /= g.H;
     const int b = idx % g.batch;
-    const int first = (tiles_q - 1 - idx / g.batch) * kPrBlock;            // (the rows with the most keys first)
+    const int from_end = idx / g.batch;                       // (the rows with the most keys first)
 
     if (warp == 8 && lane == 0) {
-        for (int s = 0; s < 2 * C::RING; ++s) mbar_init(full + s, 1);
+        for (int s = 0; s < C::RING; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 2); }
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + s, 1); mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
+            mbar_init(drained + s, 1); mbar_init(turn + s, 1);
         }
-        mbar_init(drained, 1);
         s_misc[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     } else if (warp == 9) {
@@ -79,6 +80,9 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
 
     int q0, nq, k0, nk;
     prompt_range(g, b, q0, nq, k0, nk);
+    // the request's last rows are in blocks of kPrBlock from the end; the first rows, with the fewest keys, are what is left
+    const int tiles_r = (nq + kPrBlock - 1) / kPrBlock, tile = tiles_r - 1 - from_end;
+    const int first = tile <= 0 ? 0 : nq - (from_end + 1) * kPrBlock, n_rows = tile < 0 ? 0 : tile == 0 ? nq - from_end * kPrBlock : kPrBlock;
     // (the starts of the whole request decide which keys a query sees, whatever max_q_len leaves out)
     const int all_q = max(0, min(g.q_start[b + 1], g.q_tokens) - q0);
     // keys that query i sees: the first `limit(i)`
@@ -86,7 +90,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     int rows[2], len[2], tiles[2];                            // of either half: queries, keys that any of them sees, tiles of those
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        rows[s] = max(0, min(kPrRows, nq - first - s * kPrRows));
+        rows[s] = max(0, min(kPrRows, n_rows - s * kPrRows));
         len[s] = rows[s] > 0 ? limit(first + s * kPrRows + rows[s] - 1) : 0;
         tiles[s] = (len[s] + kPrTile - 1) / kPrTile;
     }
@@ -100,9 +104,9 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
 #pragma unroll 1
             for (int s = 0; s < 2; ++s)
                 if (tiles[s] > 0) {
-                    mbar_expect_tx(q_full + s, (unsigned)(C::KC * C::COL));
+                    mbar_expect_tx(q_full + s, (unsigned)(C::KC * C::Q_COL));
                     for (int c = 0; c < C::KC; ++c)
-                        tma_col(s_q + (s * C::KC + c) * C::COL, &maps.q, 64 * c, h * maps.q_head, q0 + first + s * kPrRows, q_full + s);
+                        tma_col(s_q + (s * C::KC + c) * C::Q_COL, &maps.q, 64 * c, h * maps.q_head, q0 + first + s * kPrRows, q_full + s);
                 }
         __syncwarp();
         for (int j = 0; ok && j < n_tiles; ++j)
@@ -128,88 +132,83 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
             if (tiles[s] > 0) tree_wait(q_full + s, 0u, &no_abort, nullptr, lane);
         for (int c = max(0, issued - C::RING); c < issued; ++c)
             if (!tree_wait(full + c % C::RING, (c / C::RING) & 1, &no_abort, nullptr, lane)) break;
-    } else if (warp == 9) {
-        // ---- products: O_A += P_A V(j), S_A = Q_A K(j + 1), and the same for B ------------------------------
-        constexpr unsigned kIdescS = instr_desc(kPrRows, kPrTile, false), kIdescO = instr_desc(kPrRows, D, true), kIdescO64 = instr_desc(kPrRows, 64, true);
-        const unsigned q_desc = desc_low(smem_u32(s_q), 16), k_desc = desc_low(smem_u32(s_ring), 16), v_desc = desc_low(smem_u32(s_ring), C::COL);
+    } else if (warp >= 9) {
+        // ---- products of a half: O += P V(j), S = Q K(j + 1).  A warp for either half, so that what the one waits for and works
+        // out is behind the other's products.
+        constexpr unsigned kIdescS = instr_desc(kPrRows, kPrTile, false), kIdescO = instr_desc(kPrRows, D, true);
+        const int s = warp - 9;
+        const unsigned q_desc = desc_low(smem_u32(s_q), 16) + s * C::KC * (C::Q_COL / 16), k_desc = desc_low(smem_u32(s_ring), 16);
+        const unsigned v_desc = desc_low(smem_u32(s_ring), C::COL), s_addr = tmem + s * kPrTile, o_addr = tmem + C::COL_O + s * D;
+        int slot = 0, round = 0;                              // of the ring: the next column, in the order of the copies
         bool ok = true;
-        // a tile's columns: (KC + VC) j + c in the order of the copies
-        auto wait_col = [&](int c) { return tree_wait(full + c % C::RING, (c / C::RING) & 1, abort, g.wait_timeouts, lane); };
-        auto free_cols = [&](int c, int n) {
-            if (elect_one())
-                for (int i = 0; i < n; ++i) tc_commit(empty + (c + i) % C::RING);
-            __syncwarp();
+        auto step_on = [&](int n) {
+            slot += n;
+            if (slot >= C::RING) { slot -= C::RING; ++round; }
         };
-        auto scores = [&](int s, int j) -> bool {
-            const int c0 = (C::KC + C::VC) * j;
-            if (j == 0 && !tree_wait(q_full + s, 0u, abort, g.wait_timeouts, lane)) return false;
-#pragma unroll
-            for (int c = 0; c < C::KC; ++c) {
-                if (!wait_col(c0 + c)) return false;
-                tc_fence_after();
-                if (elect_one()) {
-                    const unsigned qa = q_desc + (s * C::KC + c) * (C::COL / 16), ka = k_desc + ((c0 + c) % C::RING) * (C::COL / 16);
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) tc_mma_ss(tmem + s * kPrTile, qa + kk * 2, ka + kk * 2, kIdescS, c > 0 || kk > 0);
-                    if (c == C::KC - 1) tc_commit(s_full + s);
-                }
-                __syncwarp();
-            }
-            return true;
+        auto wait_col = [&](int c) {                          // the c-th column from here
+            const bool wrap = slot + c >= C::RING;
+            return tree_wait(full + (wrap ? slot + c - C::RING : slot + c), (round + wrap) & 1, abort, g.wait_timeouts, lane);
         };
-        auto values = [&](int s, int j) -> bool {
-            const int c0 = (C::KC + C::VC) * j + C::KC;
-            if (!tree_wait(p_ready + s, j & 1, abort, g.wait_timeouts, lane)) return false;
-#pragma unroll
-            for (int c = 0; c < C::VC; ++c)
-                if (!wait_col(c0 + c)) return false;
-            // values behind the request's last key, up to where the product stops: zero, whatever they were
-            const int count = min(kPrTile, len[s] - j * kPrTile), there = nk - j * kPrTile;
-            const int steps = (count + 15) / 16;
-            if (there < steps * 16) {
-                const int pieces = (steps * 16 - there) * 8;
-                for (int i = lane; i < pieces * C::VC; i += 32) {
-                    const int c = i / pieces, p = i - c * pieces;
-                    *reinterpret_cast<uint4*>(s_ring + ((c0 + c) % C::RING) * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
+        auto at_col = [&](int c) { return slot + c >= C::RING ? slot + c - C::RING : slot + c; };
+        // Step j: O += P V(j) and S = Q K(j + 1), issued in one go.  The halves take turns, so that one's softmax runs while the
+        // other's products do; left to themselves they fall in step, and the tensor pipe waits for both.
+        for (int j = -1; ok && j < n_tiles; ++j) {
+            const bool pv = j >= 0 && j < tiles[s], next = j + 1 < tiles[s];
+            const int nv = j >= 0 ? C::VC : 0, nk_cols = j + 1 < n_tiles ? C::KC : 0;
+            if (j < 0 && next) ok = tree_wait(q_full + s, 0u, abort, g.wait_timeouts, lane);
+            for (int c = 0; ok && c < nv + nk_cols; ++c) ok = wait_col(c);
+            if (!ok) break;
+            const int count = min(kPrTile, len[s] - j * kPrTile), there = nk - j * kPrTile, steps = (count + 15) / 16;
+            if (pv) {
+                // values behind the request's last key, up to where the product stops: zero, whatever they were
+                if (there < steps * 16) {
+                    const int pieces = (steps * 16 - there) * 8;
+                    for (int i = lane; i < pieces * C::VC; i += 32) {
+                        const int c = i / pieces, p = i - c * pieces;
+                        *reinterpret_cast<uint4*>(s_ring + at_col(c) * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
+                ok = tree_wait(p_ready + s, j & 1, abort, g.wait_timeouts, lane);
             }
+            if (ok && (s == 1 || j >= 0)) ok = tree_wait(turn + s, (s == 1 ? j + 1 : j) & 1, abort, g.wait_timeouts, lane);
+            if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-                const unsigned o = tmem + C::COL_O + s * D, p = tmem + s * kPrTile;
-                const int slot = c0 % C::RING;
-                if (C::VC == 1 || slot + 1 < C::RING) {
-                    const unsigned va = v_desc + slot * (C::COL / 16);
-                    for (int kk = 0; kk < steps; ++kk) tc_mma_ts(o, p + kk * 8, va + kk * (2048 / 16), kIdescO, j > 0 || kk > 0);
-                } else {                                      // the two columns are the ring's last and first
-                    for (int c = 0; c < C::VC; ++c) {
-                        const unsigned va = v_desc + ((c0 + c) % C::RING) * (C::COL / 16);
-                        for (int kk = 0; kk < steps; ++kk) tc_mma_ts(o + c * 64, p + kk * 8, va + kk * (2048 / 16), kIdescO64, j > 0 || kk > 0);
+                if (pv) {
+                    const unsigned va = v_desc + slot * (C::COL / 16);           // (a tile's columns never span the ring's end)
+                    tc_mma_ts(o_addr, s_addr, va, kIdescO, j > 0);
+                    if (steps == kPrTile / 16) {
+#pragma unroll
+                        for (int kk = 1; kk < kPrTile / 16; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
+                    } else {
+                        for (int kk = 1; kk < steps; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
                     }
+                    tc_commit(pv_done + s);
                 }
-                tc_commit(pv_done + s);
+                if (next) {
+#pragma unroll
+                    for (int c = 0; c < C::KC; ++c) {
+                        const unsigned qa = q_desc + c * (C::Q_COL / 16), ka = k_desc + at_col(nv + c) * (C::COL / 16);
+                        if (c == 0) tc_mma_ss(s_addr, qa, ka, kIdescS, false);
+                        else tc_mma_ss_add(s_addr, qa, ka, kIdescS);
+#pragma unroll
+                        for (int kk = 1; kk < 4; ++kk) tc_mma_ss_add(s_addr, qa + kk * 2, ka + kk * 2, kIdescS);
+                    }
+                    tc_commit(s_full + s);
+                }
+                mbar_arrive(turn + 1 - s);
+                for (int c = 0; c < nv + nk_cols; ++c) tc_commit(empty + at_col(c));
             }
             __syncwarp();
-            return true;
-        };
-        for (int s = 0; ok && s < 2; ++s)
-            if (tiles[s] > 0) ok = scores(s, 0);
-        if (ok && n_tiles > 0) free_cols(0, C::KC);
-        for (int j = 0; ok && j < n_tiles; ++j) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                if (ok && j < tiles[s]) ok = values(s, j);
-                if (ok && s == 1) free_cols((C::KC + C::VC) * j + C::KC, C::VC);
-                if (ok && j + 1 < tiles[s]) ok = scores(s, j + 1);
-                if (ok && s == 1 && j + 1 < n_tiles) free_cols((C::KC + C::VC) * (j + 1), C::KC);
-            }
+            step_on(nv + nk_cols);
         }
         if (__any_sync(0xffffffffu, !ok || *abort)) {         // TMEM is given back only when no product uses it
-            if (elect_one()) tc_commit(drained);
+            if (elect_one()) tc_commit(drained + s);
             __syncwarp();
             volatile int no_abort = 0;
-            tree_wait(drained, 0u, &no_abort, nullptr, lane);
+            tree_wait(drained + s, 0u, &no_abort, nullptr, lane);
         }
     } else {
         // ---- softmax: one thread per query row, four warps per half -----------------------------------------
@@ -225,24 +224,24 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
             ok = tree_wait(s_full + s, j & 1, abort, g.wait_timeouts, lane);
             if (!ok) break;
             tc_fence_after();
-            unsigned x[4][32];
+            unsigned x[3][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tc_ld32(x[c], s_addr + 32 * c);
+            for (int c = 0; c < 3; ++c) tc_ld32(x[c], s_addr + 32 * c);
             tc_wait_ld();
             const int seen = sees - j * kPrTile;
             if (__any_sync(0xffffffffu, seen < kPrTile)) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 3; ++c)
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
                         if (c * 32 + k >= seen) x[c][k] = 0xff800000u;
             }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float mx[3] = {-INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int k = 0; k < 32; k += 2)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][k])), __uint_as_float(x[c][k + 1]));
-            const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                for (int c = 0; c < 3; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][k])), __uint_as_float(x[c][k + 1]));
+            const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), mx[2]);
             // (-inf - -inf is NaN: compares false, nothing to rescale)
             if (__any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f)) {
                 const float m_new = fmaxf(m_ref, m_tile);
@@ -268,17 +267,16 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
             const unsigned long long sl2 = pack_f32x2(sl, sl), sub2 = pack_f32x2(-sub, -sub);
             unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                unsigned pk[32];
+            for (int c = 0; c < 3; ++c) {
+                unsigned pk[16];
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    const unsigned* from = x[half * 2 + k / 16] + (k % 16) * 2;
-                    const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(from[0]), __uint_as_float(from[1])), sl2, sub2));
+                for (int k = 0; k < 16; ++k) {
+                    const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), sl2, sub2));
                     const float p0 = fast_exp2(y.x), p1 = fast_exp2(y.y);
                     sum[k & 1] = add_f32x2(sum[k & 1], pack_f32x2(p0, p1));
                     pk[k] = pack_bf16(p0, p1);
                 }
-                tc_st32(s_addr + 32 * half, pk);
+                tc_st16(s_addr + 16 * c, pk);
             }
             const float2 both = unpack_f32x2(add_f32x2(sum[0], sum[1]));
             sum_l += both.x + both.y;

@@ -40,6 +40,17 @@ __device__ __forceinline__ void tc_mma_ts(unsigned d, unsigned a, unsigned b_low
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}"
                  ::"r"(d), "r"(a), "r"(b_low), "r"(idesc), "r"((unsigned)acc), "r"(kDescHigh) : "memory");
 }
+// The same, always adding: a predicate costs the issuing lane more than a small product costs the tensor pipe.
+__device__ __forceinline__ void tc_mma_ss_add(unsigned d, unsigned a_low, unsigned b_low, unsigned idesc) {
+    asm volatile("{\n.reg .b64 a, b;\nmov.b64 a, {%1, %4};\nmov.b64 b, {%2, %4};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n}"
+                 ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts_add(unsigned d, unsigned a, unsigned b_low, unsigned idesc) {
+    asm volatile("{\n.reg .b64 b;\nmov.b64 b, {%2, %4};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, 1;\n}"
+                 ::"r"(d), "r"(a), "r"(b_low), "r"(idesc), "r"(kDescHigh) : "memory");
+}
 // one lane of the warp, the same every time (products and their commits come from one thread)
 __device__ __forceinline__ bool elect_one() {
     unsigned yes;
@@ -64,6 +75,12 @@ __device__ __forceinline__ void tc_st32(unsigned addr, const unsigned (&r)[32]) 
                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
                    "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tc_st16(unsigned addr, const unsigned (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                   "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
