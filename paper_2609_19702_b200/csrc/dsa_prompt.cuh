@@ -20,12 +20,11 @@ struct PromptCfg {
     static constexpr int KC = D / 64 + 1, VC = D / 64;                     // 64-element columns of a key (the last: k_rope), a value
     static constexpr int COL = kPrTile * 128, Q_COL = kPrRows * 128;       // bytes of one column of a tile, of a half's queries
     static constexpr int Q_BYTES = 2 * KC * Q_COL;
-    static constexpr int RING = (D == 128 ? 2 : 4) * (KC + VC);            // columns in flight
+    static constexpr int SLOTS = D == 128 ? 2 : 4, RING = SLOTS * (KC + VC);   // tiles in flight, and their columns
     static constexpr int TAIL = 1024;
     static constexpr int SMEM = Q_BYTES + RING * COL + TAIL;
     static constexpr int COL_O = 2 * kPrTile, TMEM_COLS = 512;
     static_assert(SMEM <= 232448, "shared memory of an SM");
-    static_assert(RING % (KC + VC) == 0, "a tile's columns lie side by side");
 };
 
 __device__ __forceinline__ void tma_col(void* dst, const CUtensorMap* map, int c0, int c1, int c2, unsigned long long* bar) {
@@ -40,16 +39,16 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* s_q = smem;
     unsigned char* s_ring = smem + C::Q_BYTES;
-    unsigned long long* full = reinterpret_cast<unsigned long long*>(s_ring + C::RING * C::COL);   // [RING] a column has landed
-    unsigned long long* empty = full + C::RING;               // [RING] the products of either half that read it are done
-    unsigned long long* q_full = empty + C::RING;             // [2] a half's queries
+    unsigned long long* full = reinterpret_cast<unsigned long long*>(s_ring + C::RING * C::COL);   // [SLOTS][2] a tile's K / V has landed
+    unsigned long long* empty = full + 2 * C::SLOTS;          // [SLOTS][2] the products of either half that read it are done
+    unsigned long long* q_full = empty + 2 * C::SLOTS;             // [2] a half's queries
     unsigned long long* s_full = q_full + 2;                  // [2] scores are in TMEM
     unsigned long long* p_ready = q_full + 4;                 // [2] weights are in TMEM
     unsigned long long* pv_done = q_full + 6;                 // [2] O holds the tile
     unsigned long long* drained = q_full + 8;                 // [2]
     unsigned long long* turn = q_full + 10;                   // [2] the other half has issued its products
     int* s_misc = reinterpret_cast<int*>(q_full + 12);        // [0] TMEM address, [1] abort
-    static_assert((2 * C::RING + 12) * 8 + 8 <= C::TAIL, "tail of the shared memory");
+    static_assert((4 * C::SLOTS + 12) * 8 + 8 <= C::TAIL, "tail of the shared memory");
     volatile int* abort = s_misc + 1;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -59,7 +58,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     const int from_end = idx / g.batch;                       // (the rows with the most keys first)
 
     if (warp == 8 && lane == 0) {
-        for (int s = 0; s < C::RING; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 2); }
+        for (int s = 0; s < 2 * C::SLOTS; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 2); }
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + s, 1); mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
             mbar_init(drained + s, 1); mbar_init(turn + s, 1);
@@ -97,8 +96,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     const int n_tiles = max(tiles[0], tiles[1]);
 
     if (warp == 8) {
-        // ---- copies: the columns of K(0), V(0), K(1), V(1), ... -------------------------------------------
-        int slot = 0, round = 0, issued = 0;
+        // ---- copies: K(0), V(0), K(1), V(1), ... -----------------------------------------------------------
+        int issued = 0;
         bool ok = true;
         if (lane == 0)
 #pragma unroll 1
@@ -109,29 +108,33 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
                         tma_col(s_q + (s * C::KC + c) * C::Q_COL, &maps.q, 64 * c, h * maps.q_head, q0 + first + s * kPrRows, q_full + s);
                 }
         __syncwarp();
-        for (int j = 0; ok && j < n_tiles; ++j)
-#pragma unroll 1
-            for (int c = 0; ok && c < C::KC + C::VC; ++c) {
-                if (round > 0) ok = tree_wait(empty + slot, (round - 1) & 1, abort, g.wait_timeouts, lane);
+        for (int j = 0; ok && j < n_tiles; ++j) {
+            const int slot = j % C::SLOTS, round = j / C::SLOTS, tok = k0 + j * kPrTile;
+            unsigned char* dst = s_ring + slot * (C::KC + C::VC) * C::COL;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                unsigned long long* bar = full + 2 * slot + v;
+                if (ok && round > 0) ok = tree_wait(empty + 2 * slot + v, (round - 1) & 1, abort, g.wait_timeouts, lane);
                 if (!ok) break;
                 if (lane == 0) {
-                    unsigned char* dst = s_ring + slot * C::COL;
-                    mbar_expect_tx(full + slot, (unsigned)C::COL);
-                    const int tok = k0 + j * kPrTile;
-                    if (c < C::KC - 1) tma_col(dst, &maps.k, 64 * c, h * maps.k_head, tok, full + slot);
-                    else if (c == C::KC - 1) tma_col(dst, &maps.kr, 0, 0, tok, full + slot);
-                    else tma_col(dst, &maps.v, 64 * (c - C::KC), h * maps.v_head, tok, full + slot);
+                    mbar_expect_tx(bar, (unsigned)((v ? C::VC : C::KC) * C::COL));
+                    if (v == 0) {
+                        for (int c = 0; c < C::KC - 1; ++c) tma_col(dst + c * C::COL, &maps.k, 64 * c, h * maps.k_head, tok, bar);
+                        tma_col(dst + (C::KC - 1) * C::COL, &maps.kr, 0, 0, tok, bar);
+                    } else {
+                        for (int c = 0; c < C::VC; ++c) tma_col(dst + (C::KC + c) * C::COL, &maps.v, 64 * c, h * maps.v_head, tok, bar);
+                    }
                 }
                 __syncwarp();
                 ++issued;
-                if (++slot == C::RING) { slot = 0; ++round; }
             }
+        }
         // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
         volatile int no_abort = 0;
         for (int s = 0; s < 2; ++s)
             if (tiles[s] > 0) tree_wait(q_full + s, 0u, &no_abort, nullptr, lane);
-        for (int c = max(0, issued - C::RING); c < issued; ++c)
-            if (!tree_wait(full + c % C::RING, (c / C::RING) & 1, &no_abort, nullptr, lane)) break;
+        for (int c = max(0, issued - 2 * C::SLOTS); c < issued; ++c)
+            if (!tree_wait(full + c % (2 * C::SLOTS), (c / (2 * C::SLOTS)) & 1, &no_abort, nullptr, lane)) break;
     } else if (warp >= 9) {
         // ---- products of a half: O += P V(j), S = Q K(j + 1).  A warp for either half, so that what the one waits for and works
         // out is behind the other's products.
@@ -139,45 +142,35 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         const int s = warp - 9;
         const unsigned q_desc = desc_low(smem_u32(s_q), 16) + s * C::KC * (C::Q_COL / 16), k_desc = desc_low(smem_u32(s_ring), 16);
         const unsigned v_desc = desc_low(smem_u32(s_ring), C::COL), s_addr = tmem + s * kPrTile, o_addr = tmem + C::COL_O + s * D;
-        int slot = 0, round = 0;                              // of the ring: the next column, in the order of the copies
         bool ok = true;
-        auto step_on = [&](int n) {
-            slot += n;
-            if (slot >= C::RING) { slot -= C::RING; ++round; }
-        };
-        auto wait_col = [&](int c) {                          // the c-th column from here
-            const bool wrap = slot + c >= C::RING;
-            return tree_wait(full + (wrap ? slot + c - C::RING : slot + c), (round + wrap) & 1, abort, g.wait_timeouts, lane);
-        };
-        auto at_col = [&](int c) { return slot + c >= C::RING ? slot + c - C::RING : slot + c; };
         // Step j: O += P V(j) and S = Q K(j + 1), issued in one go.  The halves take turns, so that one's softmax runs while the
-        // other's products do; left to themselves they fall in step, and the tensor pipe waits for both.
+        // other's products do; left to themselves they fall in step, and the tensor pipe waits for both.  The weights, which come
+        // last, are waited for last: every look at a barrier costs some 250 cycles behind the products that are still queued.
         for (int j = -1; ok && j < n_tiles; ++j) {
-            const bool pv = j >= 0 && j < tiles[s], next = j + 1 < tiles[s];
-            const int nv = j >= 0 ? C::VC : 0, nk_cols = j + 1 < n_tiles ? C::KC : 0;
-            if (j < 0 && next) ok = tree_wait(q_full + s, 0u, abort, g.wait_timeouts, lane);
-            for (int c = 0; ok && c < nv + nk_cols; ++c) ok = wait_col(c);
+            const bool pv = j >= 0 && j < tiles[s], next = j + 1 < tiles[s], last = j + 1 >= n_tiles;
+            const int vs = j < 0 ? 0 : j % C::SLOTS, ks = (j + 1) % C::SLOTS;
+            if (!last) ok = tree_wait(full + 2 * ks, ((j + 1) / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
+            if (ok && j >= 0) ok = tree_wait(full + 2 * vs + 1, (j / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
+            if (ok && j < 0 && next) ok = tree_wait(q_full + s, 0u, abort, g.wait_timeouts, lane);
             if (!ok) break;
             const int count = min(kPrTile, len[s] - j * kPrTile), there = nk - j * kPrTile, steps = (count + 15) / 16;
-            if (pv) {
-                // values behind the request's last key, up to where the product stops: zero, whatever they were
-                if (there < steps * 16) {
-                    const int pieces = (steps * 16 - there) * 8;
-                    for (int i = lane; i < pieces * C::VC; i += 32) {
-                        const int c = i / pieces, p = i - c * pieces;
-                        *reinterpret_cast<uint4*>(s_ring + at_col(c) * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
+            // values behind the request's last key, up to where the product stops: zero, whatever they were
+            if (pv && there < steps * 16) {
+                const int pieces = (steps * 16 - there) * 8;
+                for (int i = lane; i < pieces * C::VC; i += 32) {
+                    const int c = i / pieces, p = i - c * pieces;
+                    *reinterpret_cast<uint4*>(s_ring + (vs * (C::KC + C::VC) + C::KC + c) * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
-                ok = tree_wait(p_ready + s, j & 1, abort, g.wait_timeouts, lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
             }
-            if (ok && (s == 1 || j >= 0)) ok = tree_wait(turn + s, (s == 1 ? j + 1 : j) & 1, abort, g.wait_timeouts, lane);
+            if (s == 1 || j >= 0) ok = tree_wait(turn + s, (s == 1 ? j + 1 : j) & 1, abort, g.wait_timeouts, lane);
+            if (ok && pv) ok = tree_wait(p_ready + s, j & 1, abort, g.wait_timeouts, lane);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
                 if (pv) {
-                    const unsigned va = v_desc + slot * (C::COL / 16);           // (a tile's columns never span the ring's end)
+                    const unsigned va = v_desc + (vs * (C::KC + C::VC) + C::KC) * (C::COL / 16);
                     tc_mma_ts(o_addr, s_addr, va, kIdescO, j > 0);
                     if (steps == kPrTile / 16) {
 #pragma unroll
@@ -190,7 +183,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
                 if (next) {
 #pragma unroll
                     for (int c = 0; c < C::KC; ++c) {
-                        const unsigned qa = q_desc + c * (C::Q_COL / 16), ka = k_desc + at_col(nv + c) * (C::COL / 16);
+                        const unsigned qa = q_desc + c * (C::Q_COL / 16), ka = k_desc + (ks * (C::KC + C::VC) + c) * (C::COL / 16);
                         if (c == 0) tc_mma_ss(s_addr, qa, ka, kIdescS, false);
                         else tc_mma_ss_add(s_addr, qa, ka, kIdescS);
 #pragma unroll
@@ -199,10 +192,10 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
                     tc_commit(s_full + s);
                 }
                 mbar_arrive(turn + 1 - s);
-                for (int c = 0; c < nv + nk_cols; ++c) tc_commit(empty + at_col(c));
+                if (j >= 0) tc_commit(empty + 2 * vs + 1);
+                if (!last) tc_commit(empty + 2 * ks);
             }
             __syncwarp();
-            step_on(nv + nk_cols);
         }
         if (__any_sync(0xffffffffu, !ok || *abort)) {         // TMEM is given back only when no product uses it
             if (elect_one()) tc_commit(drained + s);
