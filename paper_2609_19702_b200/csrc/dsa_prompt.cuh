@@ -32,6 +32,13 @@ __device__ __forceinline__ void tma_col(void* dst, const CUtensorMap* map, int c
                  ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar)) : "memory");
 }
 
+// What a block works on: 256 queries of one (request, head), in two halves.
+struct PromptItem {
+    int h, row0, k0, nk, n_tiles;                  // head (< 0: nothing any more), first query's row, first key, keys, key tiles that any query sees
+    int shift;                                     // query i of the item sees the first clamp(i + shift, 0, nk) keys
+    int rows[2], len[2], tiles[2];                 // of either half: queries, keys that any of them sees, tiles of those
+};
+
 template <int D>
 __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptArgs g, const __grid_constant__ PromptMaps maps) {
     using C = PromptCfg<D>;
@@ -41,28 +48,33 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     unsigned char* s_ring = smem + C::Q_BYTES;
     unsigned long long* full = reinterpret_cast<unsigned long long*>(s_ring + C::RING * C::COL);   // [SLOTS][2] a tile's K / V has landed
     unsigned long long* empty = full + 2 * C::SLOTS;          // [SLOTS][2] the products of either half that read it are done
-    unsigned long long* q_full = empty + 2 * C::SLOTS;             // [2] a half's queries
+    unsigned long long* q_full = empty + 2 * C::SLOTS;        // [2] a half's queries
     unsigned long long* s_full = q_full + 2;                  // [2] scores are in TMEM
     unsigned long long* p_ready = q_full + 4;                 // [2] weights are in TMEM
     unsigned long long* pv_done = q_full + 6;                 // [2] O holds the tile
     unsigned long long* drained = q_full + 8;                 // [2]
     unsigned long long* turn = q_full + 10;                   // [2] the other half has issued its products
-    int* s_misc = reinterpret_cast<int*>(q_full + 12);        // [0] TMEM address, [1] abort
-    static_assert((4 * C::SLOTS + 12) * 8 + 8 <= C::TAIL, "tail of the shared memory");
+    unsigned long long* q_empty = q_full + 12;                // [2] the scores of an item's last tile are done
+    unsigned long long* o_free = q_full + 14;                 // [2] O has been read
+    unsigned long long* info_full = q_full + 16;              // [2] the next item is known
+    unsigned long long* info_empty = q_full + 18;             // [2] every warp has read it
+    unsigned long long* stolen = q_full + 20;
+    uint4* s_response = reinterpret_cast<uint4*>(q_full + 22);
+    PromptItem* s_info = reinterpret_cast<PromptItem*>(q_full + 24);           // [2]
+    int* s_misc = reinterpret_cast<int*>(s_info + 2);         // [0] TMEM address, [1] abort
+    static_assert((4 * C::SLOTS + 24) * 8 + 2 * sizeof(PromptItem) + 8 <= C::TAIL, "tail of the shared memory");
+    static_assert((4 * C::SLOTS + 22) % 2 == 0, "the response lies on 16 bytes");
     volatile int* abort = s_misc + 1;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int idx = blockIdx.x;
-    const int h = idx % g.H; idx /= g.H;
-    const int b = idx % g.batch;
-    const int from_end = idx / g.batch;                       // (the rows with the most keys first)
-
     if (warp == 8 && lane == 0) {
         for (int s = 0; s < 2 * C::SLOTS; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 2); }
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + s, 1); mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
-            mbar_init(drained + s, 1); mbar_init(turn + s, 1);
+            mbar_init(drained + s, 1); mbar_init(turn + s, 1); mbar_init(q_empty + s, 1); mbar_init(o_free + s, 4);
+            mbar_init(info_full + s, 1); mbar_init(info_empty + s, 10);
         }
+        mbar_init(stolen, 1);
         s_misc[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     } else if (warp == 9) {
@@ -77,64 +89,116 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
 
-    int q0, nq, k0, nk;
-    prompt_range(g, b, q0, nq, k0, nk);
-    // the request's last rows are in blocks of kPrBlock from the end; the first rows, with the fewest keys, are what is left
-    const int tiles_r = (nq + kPrBlock - 1) / kPrBlock, tile = tiles_r - 1 - from_end;
-    const int first = tile <= 0 ? 0 : nq - (from_end + 1) * kPrBlock, n_rows = tile < 0 ? 0 : tile == 0 ? nq - from_end * kPrBlock : kPrBlock;
-    // (the starts of the whole request decide which keys a query sees, whatever max_q_len leaves out)
-    const int all_q = max(0, min(g.q_start[b + 1], g.q_tokens) - q0);
-    // keys that query i sees: the first `limit(i)`
-    auto limit = [&](int i) { return g.causal ? (int)max((int64_t)0, min((int64_t)nk, (int64_t)i + 1 + nk - all_q)) : nk; };
-    int rows[2], len[2], tiles[2];                            // of either half: queries, keys that any of them sees, tiles of those
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        rows[s] = max(0, min(kPrRows, n_rows - s * kPrRows));
-        len[s] = rows[s] > 0 ? limit(first + s * kPrRows + rows[s] - 1) : 0;
-        tiles[s] = (len[s] + kPrTile - 1) / kPrTile;
-    }
-    const int n_tiles = max(tiles[0], tiles[1]);
+    // item number `i` of this block, once the copying warp has found it; nullptr: give up
+    auto item = [&](int i) -> const PromptItem* {
+        return tree_wait(info_full + (i & 1), (i >> 1) & 1, abort, g.wait_timeouts, lane) ? s_info + (i & 1) : nullptr;
+    };
+    auto item_read = [&](int i) {                             // this warp needs item i's description no longer
+        __syncwarp();
+        if (lane == 0) mbar_arrive(info_empty + (i & 1));
+    };
 
     if (warp == 8) {
-        // ---- copies: K(0), V(0), K(1), V(1), ... -----------------------------------------------------------
-        int issued = 0;
+        // ---- what to work on; copies of q, K(0), V(0), K(1), V(1), ... ----------------------------------------
+        // Blocks are persistent: a running one takes over the next that has not been launched yet, and begins its copies while
+        // the products of the last one run.  Those with the most keys come first.
+        PromptItem it = {};
+        int issued = 0, live[2] = {0, 0}, idx = (int)blockIdx.x, asked = 0;
         bool ok = true;
-        if (lane == 0)
-#pragma unroll 1
-            for (int s = 0; s < 2; ++s)
-                if (tiles[s] > 0) {
-                    mbar_expect_tx(q_full + s, (unsigned)(C::KC * C::Q_COL));
-                    for (int c = 0; c < C::KC; ++c)
-                        tma_col(s_q + (s * C::KC + c) * C::Q_COL, &maps.q, 64 * c, h * maps.q_head, q0 + first + s * kPrRows, q_full + s);
-                }
-        __syncwarp();
-        for (int j = 0; ok && j < n_tiles; ++j) {
-            const int slot = j % C::SLOTS, round = j / C::SLOTS, tok = k0 + j * kPrTile;
-            unsigned char* dst = s_ring + slot * (C::KC + C::VC) * C::COL;
+        auto ask = [&]() { if (lane == 0) steal_block(s_response, stolen); __syncwarp(); ++asked; };
+        auto answer = [&]() -> bool {
+            volatile int no_abort = 0;                        // (the response is waited for whatever else has happened)
+            if (!tree_wait(stolen, (asked - 1) & 1, &no_abort, g.wait_timeouts, lane)) { *abort = 1; return false; }
+            idx = stolen_block(s_response);
+            return true;
+        };
+        for (int i = 0; ok; ++i) {
+            it.h = -1;
+            while (ok && idx >= 0) {                          // (blocks without a query are passed over)
+                int x = idx, q0, nq, nk;
+                const int h = x % g.H; x /= g.H;
+                const int b = x % g.batch, from_end = x / g.batch;
+                prompt_range(g, b, q0, nq, it.k0, nk);
+                // the request's last rows are in blocks of kPrBlock from the end; the first rows, with the fewest keys, are what is left
+                const int tile = (nq + kPrBlock - 1) / kPrBlock - 1 - from_end;
+                if (tile >= 0) {
+                    const int first = tile == 0 ? 0 : nq - (from_end + 1) * kPrBlock, n_rows = tile == 0 ? nq - from_end * kPrBlock : kPrBlock;
+                    // (the starts of the whole request decide which keys a query sees, whatever max_q_len leaves out)
+                    const int all_q = max(0, min(g.q_start[b + 1], g.q_tokens) - q0);
+                    it.h = h;
+                    it.row0 = q0 + first;
+                    it.nk = nk;
+                    it.shift = g.causal ? nk - (all_q - first - 1) : nk;
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                unsigned long long* bar = full + 2 * slot + v;
-                if (ok && round > 0) ok = tree_wait(empty + 2 * slot + v, (round - 1) & 1, abort, g.wait_timeouts, lane);
-                if (!ok) break;
-                if (lane == 0) {
-                    mbar_expect_tx(bar, (unsigned)((v ? C::VC : C::KC) * C::COL));
-                    if (v == 0) {
-                        for (int c = 0; c < C::KC - 1; ++c) tma_col(dst + c * C::COL, &maps.k, 64 * c, h * maps.k_head, tok, bar);
-                        tma_col(dst + (C::KC - 1) * C::COL, &maps.kr, 0, 0, tok, bar);
-                    } else {
-                        for (int c = 0; c < C::VC; ++c) tma_col(dst + (C::KC + c) * C::COL, &maps.v, 64 * c, h * maps.v_head, tok, bar);
+                    for (int s = 0; s < 2; ++s) {
+                        it.rows[s] = max(0, min(kPrRows, n_rows - s * kPrRows));
+                        const int last = g.causal ? s * kPrRows + it.rows[s] - 1 : 0;
+                        it.len[s] = it.rows[s] > 0 ? max(0, min(nk, last + it.shift)) : 0;
+                        it.tiles[s] = (it.len[s] + kPrTile - 1) / kPrTile;
                     }
+                    it.n_tiles = max(it.tiles[0], it.tiles[1]);
+                    break;
                 }
-                __syncwarp();
+                ask();
+                ok = answer();
+            }
+            if (!ok) break;
+            if (i >= 2) ok = tree_wait(info_empty + (i & 1), ((i >> 1) - 1) & 1, abort, g.wait_timeouts, lane);
+            if (!ok) break;
+            if (lane == 0) s_info[i & 1] = it;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(info_full + (i & 1));
+            if (it.h < 0) break;
+            const int h = it.h;
+            auto copy_q = [&]() {
+#pragma unroll
+                for (int s = 0; ok && s < 2; ++s) {
+                    if (it.tiles[s] == 0) continue;
+                    if (live[s] > 0) ok = tree_wait(q_empty + s, (live[s] - 1) & 1, abort, g.wait_timeouts, lane);
+                    if (!ok) break;
+                    ++live[s];
+                    if (lane == 0) {
+                        mbar_expect_tx(q_full + s, (unsigned)(C::KC * C::Q_COL));
+                        for (int c = 0; c < C::KC; ++c)
+                            tma_col(s_q + (s * C::KC + c) * C::Q_COL, &maps.q, 64 * c, h * maps.q_head, it.row0 + s * kPrRows, q_full + s);
+                    }
+                    __syncwarp();
+                }
+            };
+            if (i == 0) copy_q();
+            for (int j = 0; ok && j < it.n_tiles; ++j) {
+                const int slot = issued % C::SLOTS, round = issued / C::SLOTS, tok = it.k0 + j * kPrTile;
+                unsigned char* dst = s_ring + slot * (C::KC + C::VC) * C::COL;
+                if (j + 1 == it.n_tiles) ask();               // late, so that it goes to whoever has room for it
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    unsigned long long* bar = full + 2 * slot + v;
+                    if (ok && round > 0) ok = tree_wait(empty + 2 * slot + v, (round - 1) & 1, abort, g.wait_timeouts, lane);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(bar, (unsigned)((v ? C::VC : C::KC) * C::COL));
+                        if (v == 0) {
+                            for (int c = 0; c < C::KC - 1; ++c) tma_col(dst + c * C::COL, &maps.k, 64 * c, h * maps.k_head, tok, bar);
+                            tma_col(dst + (C::KC - 1) * C::COL, &maps.kr, 0, 0, tok, bar);
+                        } else {
+                            for (int c = 0; c < C::VC; ++c) tma_col(dst + (C::KC + c) * C::COL, &maps.v, 64 * c, h * maps.v_head, tok, bar);
+                        }
+                    }
+                    __syncwarp();
+                    if (v == 0 && j == 0 && i > 0) copy_q();  // (behind the first keys, which need not wait for the last item's scores)
+                }
                 ++issued;
             }
+            if (it.n_tiles == 0) ask();
+            if (ok) ok = answer();
         }
         // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
         volatile int no_abort = 0;
         for (int s = 0; s < 2; ++s)
-            if (tiles[s] > 0) tree_wait(q_full + s, 0u, &no_abort, nullptr, lane);
-        for (int c = max(0, issued - 2 * C::SLOTS); c < issued; ++c)
-            if (!tree_wait(full + c % (2 * C::SLOTS), (c / (2 * C::SLOTS)) & 1, &no_abort, nullptr, lane)) break;
+            if (live[s] > 0) tree_wait(q_full + s, (live[s] - 1) & 1, &no_abort, nullptr, lane);
+        for (int c = max(0, issued - C::SLOTS); c < issued; ++c)
+            for (int v = 0; v < 2; ++v)
+                if (ok && !tree_wait(full + 2 * (c % C::SLOTS) + v, (c / C::SLOTS) & 1, &no_abort, nullptr, lane)) break;
     } else if (warp >= 9) {
         // ---- products of a half: O += P V(j), S = Q K(j + 1).  A warp for either half, so that what the one waits for and works
         // out is behind the other's products.
@@ -143,59 +207,73 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         const unsigned q_desc = desc_low(smem_u32(s_q), 16) + s * C::KC * (C::Q_COL / 16), k_desc = desc_low(smem_u32(s_ring), 16);
         const unsigned v_desc = desc_low(smem_u32(s_ring), C::COL), s_addr = tmem + s * kPrTile, o_addr = tmem + C::COL_O + s * D;
         bool ok = true;
+        int first = 0, mine = 0, live = 0, step = 0;          // tiles of the items before this one, this half's of them; items that it had tiles of; steps
         // Step j: O += P V(j) and S = Q K(j + 1), issued in one go.  The halves take turns, so that one's softmax runs while the
         // other's products do; left to themselves they fall in step, and the tensor pipe waits for both.  The weights, which come
         // last, are waited for last: every look at a barrier costs some 250 cycles behind the products that are still queued.
-        for (int j = -1; ok && j < n_tiles; ++j) {
-            const bool pv = j >= 0 && j < tiles[s], next = j + 1 < tiles[s], last = j + 1 >= n_tiles;
-            const int vs = j < 0 ? 0 : j % C::SLOTS, ks = (j + 1) % C::SLOTS;
-            if (!last) ok = tree_wait(full + 2 * ks, ((j + 1) / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
-            if (ok && j >= 0) ok = tree_wait(full + 2 * vs + 1, (j / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
-            if (ok && j < 0 && next) ok = tree_wait(q_full + s, 0u, abort, g.wait_timeouts, lane);
-            if (!ok) break;
-            const int count = min(kPrTile, len[s] - j * kPrTile), there = nk - j * kPrTile, steps = (count + 15) / 16;
-            // values behind the request's last key, up to where the product stops: zero, whatever they were
-            if (pv && there < steps * 16) {
-                const int pieces = (steps * 16 - there) * 8;
-                for (int i = lane; i < pieces * C::VC; i += 32) {
-                    const int c = i / pieces, p = i - c * pieces;
-                    *reinterpret_cast<uint4*>(s_ring + (vs * (C::KC + C::VC) + C::KC + c) * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; ok; ++i) {
+            const PromptItem* it = item(i);
+            if (!it || it->h < 0) break;
+            const int tiles = it->tiles[s], n_tiles = it->n_tiles, len = it->len[s], nk = it->nk;
+            item_read(i);
+            if (n_tiles == 0) continue;
+            for (int j = -1; ok && j < n_tiles; ++j, ++step) {
+                const bool pv = j >= 0 && j < tiles, next = j + 1 < tiles, last = j + 1 >= n_tiles;
+                const int vt = first + j, kt = vt + 1, vs = j < 0 ? 0 : vt % C::SLOTS, ks = kt % C::SLOTS;
+                if (!last) ok = tree_wait(full + 2 * ks, (kt / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
+                if (ok && j >= 0) ok = tree_wait(full + 2 * vs + 1, (vt / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
+                if (ok && j < 0 && next) ok = tree_wait(q_full + s, live & 1, abort, g.wait_timeouts, lane);
+                // (the first product replaces the last item's O)
+                if (ok && j == 0 && pv && live > 0) ok = tree_wait(o_free + s, (live - 1) & 1, abort, g.wait_timeouts, lane);
+                if (!ok) break;
+                const int count = min(kPrTile, len - j * kPrTile), there = nk - j * kPrTile, steps = (count + 15) / 16;
+                // values behind the request's last key, up to where the product stops: zero, whatever they were
+                if (pv && there < steps * 16) {
+                    const int pieces = (steps * 16 - there) * 8;
+                    for (int x = lane; x < pieces * C::VC; x += 32) {
+                        const int c = x / pieces, p = x - c * pieces;
+                        *reinterpret_cast<uint4*>(s_ring + (vs * (C::KC + C::VC) + C::KC + c) * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                if (s == 1 || step > 0) ok = tree_wait(turn + s, (s == 1 ? step : step - 1) & 1, abort, g.wait_timeouts, lane);
+                if (ok && pv) ok = tree_wait(p_ready + s, (mine + j) & 1, abort, g.wait_timeouts, lane);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    if (pv) {
+                        const unsigned va = v_desc + (vs * (C::KC + C::VC) + C::KC) * (C::COL / 16);
+                        tc_mma_ts(o_addr, s_addr, va, kIdescO, j > 0);
+                        if (steps == kPrTile / 16) {
+#pragma unroll
+                            for (int kk = 1; kk < kPrTile / 16; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
+                        } else {
+                            for (int kk = 1; kk < steps; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
+                        }
+                        tc_commit(pv_done + s);
+                    }
+                    if (next) {
+#pragma unroll
+                        for (int c = 0; c < C::KC; ++c) {
+                            const unsigned qa = q_desc + c * (C::Q_COL / 16), ka = k_desc + (ks * (C::KC + C::VC) + c) * (C::COL / 16);
+                            if (c == 0) tc_mma_ss(s_addr, qa, ka, kIdescS, false);
+                            else tc_mma_ss_add(s_addr, qa, ka, kIdescS);
+#pragma unroll
+                            for (int kk = 1; kk < 4; ++kk) tc_mma_ss_add(s_addr, qa + kk * 2, ka + kk * 2, kIdescS);
+                        }
+                        tc_commit(s_full + s);
+                        if (j + 2 == tiles) tc_commit(q_empty + s);
+                    }
+                    mbar_arrive(turn + 1 - s);
+                    if (j >= 0) tc_commit(empty + 2 * vs + 1);
+                    if (!last) tc_commit(empty + 2 * ks);
+                }
                 __syncwarp();
             }
-            if (s == 1 || j >= 0) ok = tree_wait(turn + s, (s == 1 ? j + 1 : j) & 1, abort, g.wait_timeouts, lane);
-            if (ok && pv) ok = tree_wait(p_ready + s, j & 1, abort, g.wait_timeouts, lane);
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-                if (pv) {
-                    const unsigned va = v_desc + (vs * (C::KC + C::VC) + C::KC) * (C::COL / 16);
-                    tc_mma_ts(o_addr, s_addr, va, kIdescO, j > 0);
-                    if (steps == kPrTile / 16) {
-#pragma unroll
-                        for (int kk = 1; kk < kPrTile / 16; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
-                    } else {
-                        for (int kk = 1; kk < steps; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
-                    }
-                    tc_commit(pv_done + s);
-                }
-                if (next) {
-#pragma unroll
-                    for (int c = 0; c < C::KC; ++c) {
-                        const unsigned qa = q_desc + c * (C::Q_COL / 16), ka = k_desc + (ks * (C::KC + C::VC) + c) * (C::COL / 16);
-                        if (c == 0) tc_mma_ss(s_addr, qa, ka, kIdescS, false);
-                        else tc_mma_ss_add(s_addr, qa, ka, kIdescS);
-#pragma unroll
-                        for (int kk = 1; kk < 4; ++kk) tc_mma_ss_add(s_addr, qa + kk * 2, ka + kk * 2, kIdescS);
-                    }
-                    tc_commit(s_full + s);
-                }
-                mbar_arrive(turn + 1 - s);
-                if (j >= 0) tc_commit(empty + 2 * vs + 1);
-                if (!last) tc_commit(empty + 2 * ks);
-            }
-            __syncwarp();
+            first += n_tiles;
+            mine += tiles;
+            if (tiles > 0) ++live;
         }
         if (__any_sync(0xffffffffu, !ok || *abort)) {         // TMEM is given back only when no product uses it
             if (elect_one()) tc_commit(drained + s);
@@ -209,104 +287,122 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         const unsigned lane_base = (unsigned)((warp & 3) * 32) << 16;
         const unsigned s_addr = tmem + lane_base + s * kPrTile, o_addr = tmem + lane_base + C::COL_O + s * D;
         const float sl = g.scale_log2;
-        const bool alive = row < rows[s];
-        const int sees = alive ? limit(first + s * kPrRows + row) : 0x7fffffff;   // (a row that does not exist computes along and decides nothing)
-        float m_ref = -INFINITY, sum_l = 0.f;
+        int done = 0;                                         // tiles of the items before this one
         bool ok = true;
-        for (int j = 0; ok && j < tiles[s]; ++j) {
-            ok = tree_wait(s_full + s, j & 1, abort, g.wait_timeouts, lane);
-            if (!ok) break;
-            tc_fence_after();
-            unsigned x[3][32];
+        for (int i = 0; ok; ++i) {
+            const PromptItem* it = item(i);
+            if (!it || it->h < 0) break;
+            const int tiles = it->tiles[s], rows = it->rows[s], h = it->h, row0 = it->row0 + s * kPrRows;
+            const bool alive = row < rows;
+            // (a row that does not exist computes along and decides nothing)
+            const int sees = alive ? max(0, min(it->nk, it->shift + (g.causal ? s * kPrRows + row : 0))) : 0x7fffffff;
+            item_read(i);
+            float m_ref = -INFINITY, sum_l = 0.f;
+            for (int j = 0; ok && j < tiles; ++j) {
+                const int gt = done + j;
+                ok = tree_wait(s_full + s, gt & 1, abort, g.wait_timeouts, lane);
+                if (!ok) break;
+                tc_fence_after();
+                unsigned x[3][32];
 #pragma unroll
-            for (int c = 0; c < 3; ++c) tc_ld32(x[c], s_addr + 32 * c);
-            tc_wait_ld();
-            const int seen = sees - j * kPrTile;
-            if (__any_sync(0xffffffffu, seen < kPrTile)) {
+                for (int c = 0; c < 3; ++c) tc_ld32(x[c], s_addr + 32 * c);
+                tc_wait_ld();
+                const int seen = sees - j * kPrTile;
+                if (__any_sync(0xffffffffu, seen < kPrTile)) {
 #pragma unroll
-                for (int c = 0; c < 3; ++c)
+                    for (int c = 0; c < 3; ++c)
 #pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (c * 32 + k >= seen) x[c][k] = 0xff800000u;
-            }
-            float mx[3] = {-INFINITY, -INFINITY, -INFINITY};
+                        for (int k = 0; k < 32; ++k)
+                            if (c * 32 + k >= seen) x[c][k] = 0xff800000u;
+                }
+                float mx[3] = {-INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int k = 0; k < 32; k += 2)
+                for (int k = 0; k < 32; k += 2)
 #pragma unroll
-                for (int c = 0; c < 3; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][k])), __uint_as_float(x[c][k + 1]));
-            const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), mx[2]);
-            // (-inf - -inf is NaN: compares false, nothing to rescale)
-            if (__any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f)) {
-                const float m_new = fmaxf(m_ref, m_tile);
-                const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m_ref - m_new) * sl);
-                m_ref = m_new;
-                sum_l *= alpha;
-                if (j > 0) {
-                    ok = tree_wait(pv_done + s, (j - 1) & 1, abort, g.wait_timeouts, lane);
-                    if (!ok) break;
-                    tc_fence_after();
+                    for (int c = 0; c < 3; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][k])), __uint_as_float(x[c][k + 1]));
+                const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), mx[2]);
+                // (-inf - -inf is NaN: compares false, nothing to rescale)
+                if (__any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f)) {
+                    const float m_new = fmaxf(m_ref, m_tile);
+                    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m_ref - m_new) * sl);
+                    m_ref = m_new;
+                    sum_l *= alpha;
+                    if (j > 0) {
+                        ok = tree_wait(pv_done + s, (gt - 1) & 1, abort, g.wait_timeouts, lane);
+                        if (!ok) break;
+                        tc_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
-                        unsigned o[32];
-                        tc_ld32(o, o_addr + c);
-                        tc_wait_ld();
+                        for (int c = 0; c < D; c += 16) {     // (16 columns at a time: the scores hold 96 registers)
+                            unsigned o[16];
+                            tc_ld16(o, o_addr + c);
+                            tc_wait_ld();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
-                        tc_st32(o_addr + c, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                            tc_st16(o_addr + c, o);
+                        }
                     }
                 }
-            }
-            const float sub = m_ref == -INFINITY ? 0.f : m_ref * sl;
-            const unsigned long long sl2 = pack_f32x2(sl, sl), sub2 = pack_f32x2(-sub, -sub);
-            unsigned long long sum[2] = {0ull, 0ull};
+                const float sub = m_ref == -INFINITY ? 0.f : m_ref * sl;
+                const unsigned long long sl2 = pack_f32x2(sl, sl), sub2 = pack_f32x2(-sub, -sub);
+                unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
-            for (int c = 0; c < 3; ++c) {
-                unsigned pk[16];
+                for (int c = 0; c < 3; ++c) {
+                    unsigned pk[16];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), sl2, sub2));
-                    const float p0 = fast_exp2(y.x), p1 = fast_exp2(y.y);
-                    sum[k & 1] = add_f32x2(sum[k & 1], pack_f32x2(p0, p1));
-                    pk[k] = pack_bf16(p0, p1);
+                    for (int k = 0; k < 16; ++k) {
+                        const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), sl2, sub2));
+                        const float p0 = fast_exp2(y.x), p1 = fast_exp2(y.y);
+                        sum[k & 1] = add_f32x2(sum[k & 1], pack_f32x2(p0, p1));
+                        pk[k] = pack_bf16(p0, p1);
+                    }
+                    tc_st16(s_addr + 16 * c, pk);
                 }
-                tc_st16(s_addr + 16 * c, pk);
-            }
-            const float2 both = unpack_f32x2(add_f32x2(sum[0], sum[1]));
-            sum_l += both.x + both.y;
-            tc_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_ready + s);
-        }
-        // ---- results ------------------------------------------------------------------------------------
-        if (ok && tiles[s] > 0) ok = tree_wait(pv_done + s, (tiles[s] - 1) & 1, abort, g.wait_timeouts, lane);
-        tc_fence_after();
-        if (ok && (warp & 3) * 32 < rows[s]) {
-            const bool none = sum_l == 0.f;                    // nothing seen: zeros and -inf
-            const float inv = none ? 0.f : 1.f / sum_l;
-            const int64_t orow = (int64_t)(q0 + first + s * kPrRows + row) * g.H + h;
-            T* dst = reinterpret_cast<T*>(g.out) + orow * D;
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-                unsigned o[32];
-                if (tiles[s] > 0) {
-                    tc_ld32(o, o_addr + c);
-                    tc_wait_ld();
-                }
-                if (alive) {
-                    float f[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) f[k] = none ? 0.f : __uint_as_float(o[k]) * inv;
-#pragma unroll
-                    for (int k = 0; k < 32; k += 8)
-                        *reinterpret_cast<uint4*>(dst + c + k) = make_uint4(pack_bf16(f[k], f[k + 1]), pack_bf16(f[k + 2], f[k + 3]),
-                                                                            pack_bf16(f[k + 4], f[k + 5]), pack_bf16(f[k + 6], f[k + 7]));
-                }
+                const float2 both = unpack_f32x2(add_f32x2(sum[0], sum[1]));
+                sum_l += both.x + both.y;
+                tc_wait_st();
+                tc_fence_before();
                 __syncwarp();
+                if (lane == 0) mbar_arrive(p_ready + s);
             }
-            if (alive) g.lse[orow] = none ? -INFINITY : (m_ref * sl + log2f(sum_l)) * LN2;
+            // ---- results ----------------------------------------------------------------------------------------
+            if (!ok) break;
+            if (tiles > 0) {
+                done += tiles;
+                ok = tree_wait(pv_done + s, (done - 1) & 1, abort, g.wait_timeouts, lane);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            if ((warp & 3) * 32 < rows) {
+                const bool none = sum_l == 0.f;                    // nothing seen: zeros and -inf
+                const float inv = none ? 0.f : 1.f / sum_l;
+                const int64_t orow = (int64_t)(row0 + row) * g.H + h;
+                T* dst = reinterpret_cast<T*>(g.out) + orow * D;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    unsigned x[32];
+                    if (tiles > 0) {
+                        tc_ld32(x, o_addr + c);
+                        tc_wait_ld();
+                    }
+                    if (alive)
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) {
+                            unsigned y[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                y[e] = none ? 0u : pack_bf16(__uint_as_float(x[k + 2 * e]) * inv, __uint_as_float(x[k + 2 * e + 1]) * inv);
+                            *reinterpret_cast<uint4*>(dst + c + k) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    __syncwarp();
+                }
+                if (alive) g.lse[orow] = none ? -INFINITY : (m_ref * sl + log2f(sum_l)) * LN2;
+            }
+            if (tiles > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(o_free + s);
+            }
         }
-        tc_fence_before();
     }
     __syncthreads();                                          // (every role has come to its end)
     if (warp == 9) {

@@ -77,6 +77,12 @@ __device__ __forceinline__ void tc_st32(unsigned addr, const unsigned (&r)[32]) 
                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
                  : "memory");
 }
+__device__ __forceinline__ void tc_ld16(unsigned (&r)[16], unsigned addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+}
 __device__ __forceinline__ void tc_st16(unsigned addr, const unsigned (&r)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                  ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
@@ -131,6 +137,26 @@ __device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, un
     unsigned long long r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+
+// ---- dynamic scheduling: a running block takes over blocks that have not been launched yet --------------------
+__device__ __forceinline__ void steal_block(void* response, unsigned long long* bar) {      // one thread
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // (the last response has been read)
+    mbar_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(smem_u32(response)), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ int stolen_block(const void* response) {         // its index, or -1: there is none any more
+    unsigned ok;
+    int x;
+    asm volatile("{\n.reg .b128 r;\n.reg .pred p;\n"
+                 "ld.shared.b128 r, [%2];\n"
+                 "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
+                 "selp.u32 %0, 1, 0, p;\n"
+                 "mov.b32 %1, 0;\n"
+                 "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
+                 : "=r"(ok), "=r"(x) : "r"(smem_u32(response)) : "memory");
+    return ok ? x : -1;
 }
 
 }  // namespace dsa

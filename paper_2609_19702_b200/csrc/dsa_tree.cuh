@@ -201,26 +201,6 @@ __device__ __forceinline__ float4 tree_peer_f4(unsigned addr) {
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
-// ---- dynamic scheduling: a running block takes over blocks that have not been launched yet --------------------
-__device__ __forceinline__ void steal_block(void* response, unsigned long long* bar) {      // one thread
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // (the last response has been read)
-    mbar_expect_tx(bar, 16);
-    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
-                 ::"r"(smem_u32(response)), "r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ int stolen_block(const void* response) {         // its index, or -1: there is none any more
-    unsigned ok;
-    int x;
-    asm volatile("{\n.reg .b128 r;\n.reg .pred p;\n"
-                 "ld.shared.b128 r, [%2];\n"
-                 "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
-                 "selp.u32 %0, 1, 0, p;\n"
-                 "mov.b32 %1, 0;\n"
-                 "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
-                 : "=r"(ok), "=r"(x) : "r"(smem_u32(response)) : "memory");
-    return ok ? x : -1;
-}
-
 // What a block works on: the piece `piece` of the tiles that the nodes of row tile `rt` of (b, kvh) see.
 struct TreeItem {
     int index, b, kvh, rt, piece, S, L_p, n;                  // index < 0: nothing any more
