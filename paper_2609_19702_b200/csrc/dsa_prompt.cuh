@@ -5,7 +5,7 @@
 
 namespace dsa {
 
-constexpr int kPrTile = 96;                        // keys per tile: two tiles of K and V fit beside 256 queries
+constexpr int kPrTile = 80;                        // keys per tile: scores, weights and O of 256 queries fill the tensor memory
 constexpr int kPrRows = 128;                       // query rows per half of a block: the M of the products
 constexpr int kPrBlock = 2 * kPrRows;
 constexpr int kPrThreads = 352;
@@ -20,10 +20,12 @@ struct PromptCfg {
     static constexpr int KC = D / 64 + 1, VC = D / 64;                     // 64-element columns of a key (the last: k_rope), a value
     static constexpr int COL = kPrTile * 128, Q_COL = kPrRows * 128;       // bytes of one column of a tile, of a half's queries
     static constexpr int Q_BYTES = 2 * KC * Q_COL;
-    static constexpr int SLOTS = D == 128 ? 2 : 4, RING = SLOTS * (KC + VC);   // tiles in flight, and their columns
+    static constexpr int K_SLOTS = D == 128 ? 3 : 4, V_SLOTS = D == 128 ? 2 : 4;   // tiles in flight
+    static constexpr int K_SLOT = KC * COL, V_SLOT = VC * COL, RING_BYTES = K_SLOTS * K_SLOT + V_SLOTS * V_SLOT;
     static constexpr int TAIL = 1024;
-    static constexpr int SMEM = Q_BYTES + RING * COL + TAIL;
-    static constexpr int COL_O = 2 * kPrTile, TMEM_COLS = 512;
+    static constexpr int SMEM = Q_BYTES + RING_BYTES + TAIL;
+    static constexpr int COL_P = kPrTile, COL_HALF = 128, COL_O = 256, TMEM_COLS = 512;    // a half: scores, then weights; O of both
+    static_assert(COL_P + kPrTile / 2 <= COL_HALF, "tensor memory");
     static_assert(SMEM <= 232448, "shared memory of an SM");
 };
 
@@ -46,14 +48,18 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* s_q = smem;
     unsigned char* s_ring = smem + C::Q_BYTES;
-    unsigned long long* full = reinterpret_cast<unsigned long long*>(s_ring + C::RING * C::COL);   // [SLOTS][2] a tile's K / V has landed
-    unsigned long long* empty = full + 2 * C::SLOTS;          // [SLOTS][2] the products of either half that read it are done
-    unsigned long long* q_full = empty + 2 * C::SLOTS;        // [2] a half's queries
+    unsigned char* s_vring = s_ring + C::K_SLOTS * C::K_SLOT;
+    constexpr int SLOTS = C::K_SLOTS + C::V_SLOTS;
+    unsigned long long* k_full = reinterpret_cast<unsigned long long*>(s_ring + C::RING_BYTES);    // a tile's K has landed
+    unsigned long long* v_full = k_full + C::K_SLOTS;
+    unsigned long long* k_empty = k_full + SLOTS;             // the products of either half that read it are done
+    unsigned long long* v_empty = k_empty + C::K_SLOTS;
+    unsigned long long* q_full = k_full + 2 * SLOTS;          // [2] a half's queries
     unsigned long long* s_full = q_full + 2;                  // [2] scores are in TMEM
     unsigned long long* p_ready = q_full + 4;                 // [2] weights are in TMEM
     unsigned long long* pv_done = q_full + 6;                 // [2] O holds the tile
     unsigned long long* drained = q_full + 8;                 // [2]
-    unsigned long long* turn = q_full + 10;                   // [2] the other half has issued its products
+    unsigned long long* s_read = q_full + 10;                 // [2] the scores have been read
     unsigned long long* q_empty = q_full + 12;                // [2] the scores of an item's last tile are done
     unsigned long long* o_free = q_full + 14;                 // [2] O has been read
     unsigned long long* info_full = q_full + 16;              // [2] the next item is known
@@ -62,16 +68,16 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     uint4* s_response = reinterpret_cast<uint4*>(q_full + 22);
     PromptItem* s_info = reinterpret_cast<PromptItem*>(q_full + 24);           // [2]
     int* s_misc = reinterpret_cast<int*>(s_info + 2);         // [0] TMEM address, [1] abort
-    static_assert((4 * C::SLOTS + 24) * 8 + 2 * sizeof(PromptItem) + 8 <= C::TAIL, "tail of the shared memory");
-    static_assert((4 * C::SLOTS + 22) % 2 == 0, "the response lies on 16 bytes");
+    static_assert((2 * SLOTS + 24) * 8 + 2 * sizeof(PromptItem) + 8 <= C::TAIL, "tail of the shared memory");
+    static_assert((2 * SLOTS + 22) % 2 == 0, "the response lies on 16 bytes");
     volatile int* abort = s_misc + 1;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (warp == 8 && lane == 0) {
-        for (int s = 0; s < 2 * C::SLOTS; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, 2); }
+        for (int s = 0; s < SLOTS; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 2); }
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + s, 1); mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
-            mbar_init(drained + s, 1); mbar_init(turn + s, 1); mbar_init(q_empty + s, 1); mbar_init(o_free + s, 4);
+            mbar_init(drained + s, 1); mbar_init(s_read + s, 4); mbar_init(q_empty + s, 1); mbar_init(o_free + s, 4);
             mbar_init(info_full + s, 1); mbar_init(info_empty + s, 10);
         }
         mbar_init(stolen, 1);
@@ -103,7 +109,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         // Blocks are persistent: a running one takes over the next that has not been launched yet, and begins its copies while
         // the products of the last one run.  Those with the most keys come first.
         PromptItem it = {};
-        int issued = 0, live[2] = {0, 0}, idx = (int)blockIdx.x, asked = 0;
+        int issued = 0, k_issued = 0, live[2] = {0, 0}, idx = (int)blockIdx.x, asked = 0;
         bool ok = true;
         auto ask = [&]() { if (lane == 0) steal_block(s_response, stolen); __syncwarp(); ++asked; };
         auto answer = [&]() -> bool {
@@ -167,27 +173,26 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
             };
             if (i == 0) copy_q();
             for (int j = 0; ok && j < it.n_tiles; ++j) {
-                const int slot = issued % C::SLOTS, round = issued / C::SLOTS, tok = it.k0 + j * kPrTile;
-                unsigned char* dst = s_ring + slot * (C::KC + C::VC) * C::COL;
+                const int ks = issued % C::K_SLOTS, k_round = issued / C::K_SLOTS, vs = issued % C::V_SLOTS, v_round = issued / C::V_SLOTS;
+                const int tok = it.k0 + j * kPrTile;
                 if (j + 1 == it.n_tiles) ask();               // late, so that it goes to whoever has room for it
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    unsigned long long* bar = full + 2 * slot + v;
-                    if (ok && round > 0) ok = tree_wait(empty + 2 * slot + v, (round - 1) & 1, abort, g.wait_timeouts, lane);
-                    if (!ok) break;
-                    if (lane == 0) {
-                        mbar_expect_tx(bar, (unsigned)((v ? C::VC : C::KC) * C::COL));
-                        if (v == 0) {
-                            for (int c = 0; c < C::KC - 1; ++c) tma_col(dst + c * C::COL, &maps.k, 64 * c, h * maps.k_head, tok, bar);
-                            tma_col(dst + (C::KC - 1) * C::COL, &maps.kr, 0, 0, tok, bar);
-                        } else {
-                            for (int c = 0; c < C::VC; ++c) tma_col(dst + (C::KC + c) * C::COL, &maps.v, 64 * c, h * maps.v_head, tok, bar);
-                        }
-                    }
-                    __syncwarp();
-                    if (v == 0 && j == 0 && i > 0) copy_q();  // (behind the first keys, which need not wait for the last item's scores)
+                if (k_round > 0) ok = tree_wait(k_empty + ks, (k_round - 1) & 1, abort, g.wait_timeouts, lane);
+                if (ok && lane == 0) {
+                    mbar_expect_tx(k_full + ks, (unsigned)C::K_SLOT);
+                    for (int c = 0; c < C::KC - 1; ++c) tma_col(s_ring + ks * C::K_SLOT + c * C::COL, &maps.k, 64 * c, h * maps.k_head, tok, k_full + ks);
+                    tma_col(s_ring + ks * C::K_SLOT + (C::KC - 1) * C::COL, &maps.kr, 0, 0, tok, k_full + ks);
                 }
-                ++issued;
+                __syncwarp();
+                if (!ok) break;
+                ++k_issued;
+                if (j == 0 && i > 0) copy_q();                // (behind the first keys, which need not wait for the last item's scores)
+                if (ok && v_round > 0) ok = tree_wait(v_empty + vs, (v_round - 1) & 1, abort, g.wait_timeouts, lane);
+                if (ok && lane == 0) {
+                    mbar_expect_tx(v_full + vs, (unsigned)C::V_SLOT);
+                    for (int c = 0; c < C::VC; ++c) tma_col(s_vring + vs * C::V_SLOT + c * C::COL, &maps.v, 64 * c, h * maps.v_head, tok, v_full + vs);
+                }
+                __syncwarp();
+                if (ok) ++issued;
             }
             if (it.n_tiles == 0) ask();
             if (ok) ok = answer();
@@ -196,78 +201,88 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         volatile int no_abort = 0;
         for (int s = 0; s < 2; ++s)
             if (live[s] > 0) tree_wait(q_full + s, (live[s] - 1) & 1, &no_abort, nullptr, lane);
-        for (int c = max(0, issued - C::SLOTS); c < issued; ++c)
-            for (int v = 0; v < 2; ++v)
-                if (ok && !tree_wait(full + 2 * (c % C::SLOTS) + v, (c / C::SLOTS) & 1, &no_abort, nullptr, lane)) break;
+        for (int c = max(0, k_issued - C::K_SLOTS); c < k_issued; ++c)
+            if (!tree_wait(k_full + c % C::K_SLOTS, (c / C::K_SLOTS) & 1, &no_abort, nullptr, lane)) break;
+        for (int c = max(0, issued - C::V_SLOTS); c < issued; ++c)
+            if (!tree_wait(v_full + c % C::V_SLOTS, (c / C::V_SLOTS) & 1, &no_abort, nullptr, lane)) break;
     } else if (warp >= 9) {
-        // ---- products of a half: O += P V(j), S = Q K(j + 1).  A warp for either half, so that what the one waits for and works
-        // out is behind the other's products.
+        // ---- products of a half, S = Q K(j) and O += P V(j), a warp for either half ------------------------------
+        // Scores have columns of their own, so those of tile j + 1 are computed as soon as tile j's have been read, while their
+        // weights are worked out: the softmax of a half never waits for a product, and the tensor pipe never for a softmax.
         constexpr unsigned kIdescS = instr_desc(kPrRows, kPrTile, false), kIdescO = instr_desc(kPrRows, D, true);
         const int s = warp - 9;
         const unsigned q_desc = desc_low(smem_u32(s_q), 16) + s * C::KC * (C::Q_COL / 16), k_desc = desc_low(smem_u32(s_ring), 16);
-        const unsigned v_desc = desc_low(smem_u32(s_ring), C::COL), s_addr = tmem + s * kPrTile, o_addr = tmem + C::COL_O + s * D;
+        const unsigned v_desc = desc_low(smem_u32(s_vring), C::COL);
+        const unsigned s_addr = tmem + s * C::COL_HALF, p_addr = s_addr + C::COL_P, o_addr = tmem + C::COL_O + s * D;
         bool ok = true;
-        int first = 0, mine = 0, live = 0, step = 0;          // tiles of the items before this one, this half's of them; items that it had tiles of; steps
-        // Step j: O += P V(j) and S = Q K(j + 1), issued in one go.  The halves take turns, so that one's softmax runs while the
-        // other's products do; left to themselves they fall in step, and the tensor pipe waits for both.  The weights, which come
-        // last, are waited for last: every look at a barrier costs some 250 cycles behind the products that are still queued.
+        int first = 0, mine = 0, live = 0;                    // tiles of the items before this one, this half's of them; items that it had tiles of
         for (int i = 0; ok; ++i) {
             const PromptItem* it = item(i);
             if (!it || it->h < 0) break;
             const int tiles = it->tiles[s], n_tiles = it->n_tiles, len = it->len[s], nk = it->nk;
             item_read(i);
-            if (n_tiles == 0) continue;
-            for (int j = -1; ok && j < n_tiles; ++j, ++step) {
-                const bool pv = j >= 0 && j < tiles, next = j + 1 < tiles, last = j + 1 >= n_tiles;
-                const int vt = first + j, kt = vt + 1, vs = j < 0 ? 0 : vt % C::SLOTS, ks = kt % C::SLOTS;
-                if (!last) ok = tree_wait(full + 2 * ks, (kt / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
-                if (ok && j >= 0) ok = tree_wait(full + 2 * vs + 1, (vt / C::SLOTS) & 1, abort, g.wait_timeouts, lane);
-                if (ok && j < 0 && next) ok = tree_wait(q_full + s, live & 1, abort, g.wait_timeouts, lane);
-                // (the first product replaces the last item's O)
-                if (ok && j == 0 && pv && live > 0) ok = tree_wait(o_free + s, (live - 1) & 1, abort, g.wait_timeouts, lane);
-                if (!ok) break;
-                const int count = min(kPrTile, len - j * kPrTile), there = nk - j * kPrTile, steps = (count + 15) / 16;
-                // values behind the request's last key, up to where the product stops: zero, whatever they were
-                if (pv && there < steps * 16) {
-                    const int pieces = (steps * 16 - there) * 8;
-                    for (int x = lane; x < pieces * C::VC; x += 32) {
-                        const int c = x / pieces, p = x - c * pieces;
-                        *reinterpret_cast<uint4*>(s_ring + (vs * (C::KC + C::VC) + C::KC + c) * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
+            for (int j = 0; ok && j <= n_tiles && n_tiles > 0; ++j) {
+                if (j < n_tiles) {                            // scores of tile j
+                    const int slot = (first + j) % C::K_SLOTS;
+                    ok = tree_wait(k_full + slot, ((first + j) / C::K_SLOTS) & 1, abort, g.wait_timeouts, lane);
+                    if (ok && j < tiles) {
+                        if (j == 0) ok = tree_wait(q_full + s, live & 1, abort, g.wait_timeouts, lane);
+                        if (ok && mine + j > 0) ok = tree_wait(s_read + s, (mine + j - 1) & 1, abort, g.wait_timeouts, lane);
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        if (j < tiles) {
+#pragma unroll
+                            for (int c = 0; c < C::KC; ++c) {
+                                const unsigned qa = q_desc + c * (C::Q_COL / 16), ka = k_desc + (slot * C::K_SLOT + c * C::COL) / 16;
+                                if (c == 0) tc_mma_ss(s_addr, qa, ka, kIdescS, false);
+                                else tc_mma_ss_add(s_addr, qa, ka, kIdescS);
+#pragma unroll
+                                for (int kk = 1; kk < 4; ++kk) tc_mma_ss_add(s_addr, qa + kk * 2, ka + kk * 2, kIdescS);
+                            }
+                            tc_commit(s_full + s);
+                            if (j + 1 == tiles) tc_commit(q_empty + s);
+                        }
+                        tc_commit(k_empty + slot);
+                    }
                     __syncwarp();
                 }
-                if (s == 1 || step > 0) ok = tree_wait(turn + s, (s == 1 ? step : step - 1) & 1, abort, g.wait_timeouts, lane);
-                if (ok && pv) ok = tree_wait(p_ready + s, (mine + j) & 1, abort, g.wait_timeouts, lane);
+                if (j == 0) continue;
+                const int v = j - 1, slot = (first + v) % C::V_SLOTS;        // values of the tile before
+                ok = tree_wait(v_full + slot, ((first + v) / C::V_SLOTS) & 1, abort, g.wait_timeouts, lane);
                 if (!ok) break;
+                const int count = min(kPrTile, len - v * kPrTile), there = nk - v * kPrTile, steps = (count + 15) / 16;
+                if (v < tiles) {
+                    // values behind the request's last key, up to where the product stops: zero, whatever they were
+                    if (there < steps * 16) {
+                        const int pieces = (steps * 16 - there) * 8;
+                        for (int x = lane; x < pieces * C::VC; x += 32) {
+                            const int c = x / pieces, p = x - c * pieces;
+                            *reinterpret_cast<uint4*>(s_vring + slot * C::V_SLOT + c * C::COL + there * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    // (the first product replaces the last item's O)
+                    if (v == 0 && live > 0) ok = tree_wait(o_free + s, (live - 1) & 1, abort, g.wait_timeouts, lane);
+                    if (ok) ok = tree_wait(p_ready + s, (mine + v) & 1, abort, g.wait_timeouts, lane);
+                    if (!ok) break;
+                }
                 tc_fence_after();
                 if (elect_one()) {
-                    if (pv) {
-                        const unsigned va = v_desc + (vs * (C::KC + C::VC) + C::KC) * (C::COL / 16);
-                        tc_mma_ts(o_addr, s_addr, va, kIdescO, j > 0);
+                    if (v < tiles) {
+                        const unsigned va = v_desc + slot * (C::V_SLOT / 16);
+                        tc_mma_ts(o_addr, p_addr, va, kIdescO, v > 0);
                         if (steps == kPrTile / 16) {
 #pragma unroll
-                            for (int kk = 1; kk < kPrTile / 16; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
+                            for (int kk = 1; kk < kPrTile / 16; ++kk) tc_mma_ts_add(o_addr, p_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
                         } else {
-                            for (int kk = 1; kk < steps; ++kk) tc_mma_ts_add(o_addr, s_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
+                            for (int kk = 1; kk < steps; ++kk) tc_mma_ts_add(o_addr, p_addr + kk * 8, va + kk * (2048 / 16), kIdescO);
                         }
                         tc_commit(pv_done + s);
                     }
-                    if (next) {
-#pragma unroll
-                        for (int c = 0; c < C::KC; ++c) {
-                            const unsigned qa = q_desc + c * (C::Q_COL / 16), ka = k_desc + (ks * (C::KC + C::VC) + c) * (C::COL / 16);
-                            if (c == 0) tc_mma_ss(s_addr, qa, ka, kIdescS, false);
-                            else tc_mma_ss_add(s_addr, qa, ka, kIdescS);
-#pragma unroll
-                            for (int kk = 1; kk < 4; ++kk) tc_mma_ss_add(s_addr, qa + kk * 2, ka + kk * 2, kIdescS);
-                        }
-                        tc_commit(s_full + s);
-                        if (j + 2 == tiles) tc_commit(q_empty + s);
-                    }
-                    mbar_arrive(turn + 1 - s);
-                    if (j >= 0) tc_commit(empty + 2 * vs + 1);
-                    if (!last) tc_commit(empty + 2 * ks);
+                    tc_commit(v_empty + slot);
                 }
                 __syncwarp();
             }
@@ -285,7 +300,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         // ---- softmax: one thread per query row, four warps per half -----------------------------------------
         const int s = warp >> 2, row = tid & 127;
         const unsigned lane_base = (unsigned)((warp & 3) * 32) << 16;
-        const unsigned s_addr = tmem + lane_base + s * kPrTile, o_addr = tmem + lane_base + C::COL_O + s * D;
+        const unsigned s_addr = tmem + lane_base + s * C::COL_HALF, p_addr = s_addr + C::COL_P, o_addr = tmem + lane_base + C::COL_O + s * D;
         const float sl = g.scale_log2;
         int done = 0;                                         // tiles of the items before this one
         bool ok = true;
@@ -303,24 +318,35 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
                 ok = tree_wait(s_full + s, gt & 1, abort, g.wait_timeouts, lane);
                 if (!ok) break;
                 tc_fence_after();
-                unsigned x[3][32];
+                constexpr int PARTS = kPrTile / 16;
+                unsigned x[PARTS][16];
 #pragma unroll
-                for (int c = 0; c < 3; ++c) tc_ld32(x[c], s_addr + 32 * c);
+                for (int c = 0; c < PARTS; ++c) tc_ld16(x[c], s_addr + 16 * c);
                 tc_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_read + s);
                 const int seen = sees - j * kPrTile;
                 if (__any_sync(0xffffffffu, seen < kPrTile)) {
 #pragma unroll
-                    for (int c = 0; c < 3; ++c)
+                    for (int c = 0; c < PARTS; ++c)
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (c * 32 + k >= seen) x[c][k] = 0xff800000u;
+                        for (int k = 0; k < 16; ++k)
+                            if (c * 16 + k >= seen) x[c][k] = 0xff800000u;
                 }
-                float mx[3] = {-INFINITY, -INFINITY, -INFINITY};
+                float mx[PARTS];
 #pragma unroll
-                for (int k = 0; k < 32; k += 2)
+                for (int c = 0; c < PARTS; ++c) mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
 #pragma unroll
-                    for (int c = 0; c < 3; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][k])), __uint_as_float(x[c][k + 1]));
-                const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), mx[2]);
+                for (int k = 2; k < 16; k += 2)
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][k])), __uint_as_float(x[c][k + 1]));
+                float m_tile = mx[0];
+#pragma unroll
+                for (int c = 1; c < PARTS; ++c) m_tile = fmaxf(m_tile, mx[c]);
+                // O holds the tile before, and its weights may be written over
+                if (gt > 0) ok = tree_wait(pv_done + s, (gt - 1) & 1, abort, g.wait_timeouts, lane);
+                if (!ok) break;
                 // (-inf - -inf is NaN: compares false, nothing to rescale)
                 if (__any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f)) {
                     const float m_new = fmaxf(m_ref, m_tile);
@@ -328,11 +354,9 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
                     m_ref = m_new;
                     sum_l *= alpha;
                     if (j > 0) {
-                        ok = tree_wait(pv_done + s, (gt - 1) & 1, abort, g.wait_timeouts, lane);
-                        if (!ok) break;
                         tc_fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {     // (16 columns at a time: the scores hold 96 registers)
+                        for (int c = 0; c < D; c += 16) {     // (few columns at a time: the scores hold 80 registers)
                             unsigned o[16];
                             tc_ld16(o, o_addr + c);
                             tc_wait_ld();
@@ -346,16 +370,16 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
                 const unsigned long long sl2 = pack_f32x2(sl, sl), sub2 = pack_f32x2(-sub, -sub);
                 unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
-                for (int c = 0; c < 3; ++c) {
-                    unsigned pk[16];
+                for (int c = 0; c < PARTS; ++c) {
+                    unsigned pk[8];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
+                    for (int k = 0; k < 8; ++k) {
                         const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), sl2, sub2));
                         const float p0 = fast_exp2(y.x), p1 = fast_exp2(y.y);
                         sum[k & 1] = add_f32x2(sum[k & 1], pack_f32x2(p0, p1));
                         pk[k] = pack_bf16(p0, p1);
                     }
-                    tc_st16(s_addr + 16 * c, pk);
+                    tc_st8(p_addr + 8 * c, pk);
                 }
                 const float2 both = unpack_f32x2(add_f32x2(sum[0], sum[1]));
                 sum_l += both.x + both.y;
