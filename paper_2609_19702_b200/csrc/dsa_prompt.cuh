@@ -344,43 +344,45 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
                 float m_tile = mx[0];
 #pragma unroll
                 for (int c = 1; c < PARTS; ++c) m_tile = fmaxf(m_tile, mx[c]);
-                // O holds the tile before, and its weights may be written over
-                if (gt > 0) ok = tree_wait(pv_done + s, (gt - 1) & 1, abort, g.wait_timeouts, lane);
-                if (!ok) break;
                 // (-inf - -inf is NaN: compares false, nothing to rescale)
-                if (__any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f)) {
+                const bool grow = __any_sync(0xffffffffu, alive && (m_tile - m_ref) * sl > 8.f);
+                float alpha = 1.f;
+                if (grow) {
                     const float m_new = fmaxf(m_ref, m_tile);
-                    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((m_ref - m_new) * sl);
+                    if (m_new != -INFINITY) alpha = fast_exp2((m_ref - m_new) * sl);
                     m_ref = m_new;
                     sum_l *= alpha;
-                    if (j > 0) {
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {     // (few columns at a time: the scores hold 80 registers)
-                            unsigned o[16];
-                            tc_ld16(o, o_addr + c);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
-                            tc_st16(o_addr + c, o);
-                        }
-                    }
                 }
                 const float sub = m_ref == -INFINITY ? 0.f : m_ref * sl;
                 const unsigned long long sl2 = pack_f32x2(sl, sl), sub2 = pack_f32x2(-sub, -sub);
                 unsigned long long sum[2] = {0ull, 0ull};
+                unsigned pk[PARTS][8];
 #pragma unroll
-                for (int c = 0; c < PARTS; ++c) {
-                    unsigned pk[8];
+                for (int c = 0; c < PARTS; ++c)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), sl2, sub2));
                         const float p0 = fast_exp2(y.x), p1 = fast_exp2(y.y);
                         sum[k & 1] = add_f32x2(sum[k & 1], pack_f32x2(p0, p1));
-                        pk[k] = pack_bf16(p0, p1);
+                        pk[c][k] = pack_bf16(p0, p1);
                     }
-                    tc_st8(p_addr + 8 * c, pk);
+                // only now: O holds the tile before, and that tile's weights may be written over
+                if (gt > 0) ok = tree_wait(pv_done + s, (gt - 1) & 1, abort, g.wait_timeouts, lane);
+                if (!ok) break;
+                tc_fence_after();
+                if (grow && j > 0) {
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        unsigned o[16];
+                        tc_ld16(o, o_addr + c);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                        tc_st16(o_addr + c, o);
+                    }
                 }
+#pragma unroll
+                for (int c = 0; c < PARTS; ++c) tc_st8(p_addr + 8 * c, pk[c]);
                 const float2 both = unpack_f32x2(add_f32x2(sum[0], sum[1]));
                 sum_l += both.x + both.y;
                 tc_wait_st();
