@@ -45,9 +45,9 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
         }
         return DSA_OK;
     }
-    pl->row_tiles = (pl->rows + kLatentF32Block - 1) / kLatentF32Block;
+    pl->row_tiles = (pl->rows + kTileRows - 1) / kTileRows;
     const int64_t items = std::max<int64_t>(1, (int64_t)l->batch * pl->row_tiles);
-    const int64_t tiles = ((int64_t)l->max_seq_len + max_new + kStreamTile - 1) / kStreamTile;
+    const int64_t tiles = ((int64_t)l->max_seq_len + max_new + kTileKeys - 1) / kTileKeys;
     const int64_t places = 3 * (int64_t)host_sm_count();
     pl->n_split = (int)std::max<int64_t>(1, std::min<int64_t>({(places + items / 2) / items, tiles / 2, (int64_t)kMaxSplits}));
     pl->blocks = items * pl->n_split;
@@ -120,7 +120,7 @@ cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, bool pairs, int
 template <int R>
 cudaError_t run_f32(const LatentArgs& g, int64_t blocks, cudaStream_t st) {
     const cudaError_t e = configure<R>();
-    return e != cudaSuccess ? e : launch_dependent(dsa_latent_f32_kernel<R>, blocks, kStreamWarps * 32, LatentF32Cfg<R>::SMEM, st, g);
+    return e != cudaSuccess ? e : launch_dependent(dsa_latent_f32_kernel<R>, blocks, kTileThreads, LatentF32Cfg<R>::SMEM, st, g);
 }
 
 }  // namespace

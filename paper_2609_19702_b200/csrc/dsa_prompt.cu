@@ -62,7 +62,7 @@ cudaError_t run(const PromptArgs& g, const PromptMaps& m, bool bf16, int64_t blo
     const cudaError_t e = configure<D>();
     if (e != cudaSuccess) return e;
     return bf16 ? launch_dependent(dsa_prompt_kernel<D>, blocks, kPrThreads, PromptCfg<D>::SMEM, st, g, m)
-                : launch_dependent(dsa_prompt_f32_kernel<D>, blocks, kStreamWarps * 32, PromptF32Cfg<D>::SMEM, st, g);
+                : launch_dependent(dsa_prompt_f32_kernel<D>, blocks, kTileThreads, PromptF32Cfg<D>::SMEM, st, g);
 }
 
 }  // namespace
@@ -98,7 +98,7 @@ int32_t dsa_latent_prompt(const dsa_prompt* p, void* out, float* lse, void* stre
     g.lse = lse;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool bf16 = p->dtype == DSA_BF16;
-    const int rows = bf16 ? kPrBlock : kPromptF32Block;
+    const int rows = bf16 ? kPrBlock : kTileRows;
     const int64_t blocks = ((int64_t)g.max_q_len + rows - 1) / rows * p->num_heads * p->batch;
     if (blocks > 0x7fffffffLL) return DSA_ERR_UNSUPPORTED;
     PromptMaps m = {};
