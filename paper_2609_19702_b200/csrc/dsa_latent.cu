@@ -14,7 +14,8 @@ struct LatentPlan {
     int rows, row_tiles;                           // query rows of a request, blocks of them
     int n_split;                                   // float32: pieces of a request's keys
     bool pairs;                                    // bf16: pairs of blocks with 128 query rows
-    int groups;                                    // and shares of the work
+    int groups;                                    // and shares of the work, or
+    int cluster;                                   // blocks of a cluster with an item to itself (0: shares)
     int64_t blocks;
     size_t ws_out_bytes, ws_total;                 // float32: partial outputs, and their log-sums behind them
     size_t ws_ml_bytes;                            // bf16: maxima and sums, and partial outputs behind them
@@ -33,12 +34,34 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
     if (l->dtype == DSA_BF16) {
         pl->row_tiles = (pl->rows + kLatRows - 1) / kLatRows;
         // (an upper bound of the units on the device, and of those that beginnings count for)
-        const int64_t units = (int64_t)l->batch * pl->row_tiles * (((int64_t)l->max_seq_len + kLatTile - 1) / kLatTile + 3);
+        const int64_t tiles = ((int64_t)l->max_seq_len + kLatTile - 1) / kLatTile + 1, items = std::max<int64_t>(1, (int64_t)l->batch * pl->row_tiles);
+        const int64_t units = items * (tiles + 2), sms = std::max(host_sm_count(), 1);
         if (units > (1 << 30)) return DSA_ERR_UNSUPPORTED;
         pl->pairs = pl->rows > kLatRows;
         const int per = pl->pairs ? 2 : 1;
-        pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(host_sm_count() / per, units / (per * per * kLatMinUnits)));
+        pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(sms / per, units / (per * per * kLatMinUnits)));
         pl->blocks = (int64_t)pl->groups * per;
+        // Few items, or items of few tiles: a cluster has each of them to itself and merges on chip, without partial results in HBM
+        // or a second launch.  In us, with `tiles` the bound of an item's tiles: a launch and 1.5 a tile of a block, and the
+        // merge's rounds; against shares, which are of one size whatever the lengths, but start later, write parts and need the
+        // merge kernel.  Measured, shares / best cluster (lengths spread up to the bound): 16 heads, 9 requests, 17 tiles: 23.1 /
+        // 14.1 (8 blocks), 65 tiles: 33.1 / 21.5; 18 requests, 33 tiles: 28.5 / 22.5 (4), 65: 34.0 / 36.5; 64 requests, 10 tiles:
+        // 23.9 / 20.3 (2), 65: 48.0 / 64.5; 128 heads, 4 requests, 65 tiles: 35.1 / 23.9 (8); 18 requests, 10 tiles: 23.6 / 25.6 (2).
+        const float t = (float)tiles, all = (float)(items * tiles) / (float)sms;
+        float best = pl->pairs ? 13.f + std::min(5.f, t / 2.5f) + 0.7f * all + 8.f * std::min(1.f, all / 4.f)
+                               : 14.f + std::min(4.f, t / 4.f) + 1.1f * all + 6.f * std::min(1.f, all / 2.f);
+        const int rounds = std::min(pl->rows, kLatRows) * l->latent_dim / 128;               // of the merge, by eight warps a block
+        // (clusters that are on the device at once: an SM holds one block, and a cluster's SMs lie close together)
+        const int64_t most[4] = {sms, sms * 7 / 15, sms * 7 / 33, sms / 10};
+        for (int i = 0, c = 1; i < 4; ++i, c *= 2) {
+            const float cost = 11.f + 1.5f * (float)((tiles + c - 1) / c) + (c > 1 ? 0.35f * (float)((rounds + 8 * c - 1) / (8 * c)) : 0.f);
+            if (items <= most[i] && cost < best) { best = cost; pl->cluster = c; }
+        }
+        if (pl->cluster) {
+            pl->pairs = false;
+            pl->groups = 1;
+            pl->blocks = items * pl->cluster;
+        }
         if (pl->groups > 1) {
             pl->ws_ml_bytes = (size_t)pl->blocks * 2 * kLatRows * sizeof(float2);
             pl->ws_total = pl->ws_ml_bytes + (size_t)pl->blocks * 2 * kLatRows * l->latent_dim * sizeof(float);
@@ -74,6 +97,15 @@ bool encode_rows(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, i
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same as a matrix that single rows are gathered from.
+bool encode_matrix(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, int64_t width, int64_t rows, int64_t row_stride) {
+    if (row_stride >= (1LL << 39)) return false;
+    const cuuint64_t n[2] = {(cuuint64_t)width, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)row_stride * 2};
+    const cuuint32_t bx[2] = {64u, 1u}, step[2] = {1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), n, pitch, bx, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void* q, const void* c_new, LatentTcArgs* g, LatentMaps* m) {
     const TensorMapEncodeFn encode = host_tensor_map_encoder();
     if (!encode) return DSA_ERR_UNSUPPORTED;
@@ -82,6 +114,12 @@ int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void*
     g->box_tokens = kLatTile;
     if (l->block_table)
         while (l->block_size % g->box_tokens) g->box_tokens /= 2;
+    // Boxes of one or two tokens: rows gathered four by four instead, where the pool is a matrix of token rows.  (A copy costs some
+    // 70-90 cycles however little it brings: 64 x 16 heads over pages of 1 / 2 / 4 tokens: 604 / 323 / 184 us by boxes, 212 gathered.)
+    const int64_t page_rows = l->stride_token > 0 && l->stride_batch % l->stride_token == 0 ? l->stride_batch / l->stride_token : 0;
+    const int64_t pool_rows = l->block_table ? (l->num_blocks - 1) * page_rows + l->block_size : 0;
+    g->gather = l->block_table && g->box_tokens < 4 && page_rows > 0 && pool_rows < 0x7fffffff;
+    if (g->gather) { g->box_tokens = 4; g->page_rows = (int)page_rows; }
     for (g->box_shift = 0; (1 << g->box_shift) < g->box_tokens;) ++g->box_shift;
     // division of positions (below 2^31) by the page size: with 2^s >= d the product by ceil(2^(31 + s) / d) is exact
     const unsigned d = l->block_table ? (unsigned)l->block_size : 1u;
@@ -91,8 +129,9 @@ int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void*
     g->blk_coord = l->stride_batch > 0 ? 1 : 0;    // (a stride of 0: a dimension of one entry)
     const int64_t outer = g->blk_coord ? (l->block_table ? l->num_blocks : l->batch) : 1;
     const bool ok = encode_rows(encode, &m->q, q, W, (int64_t)l->batch * pl.rows, 1, W, W, g->q_rows) &&
-                    encode_rows(encode, &m->cache, l->cache, W, tokens, outer, l->stride_token, g->blk_coord ? l->stride_batch : l->stride_token,
-                                g->box_tokens) &&
+                    (g->gather ? encode_matrix(encode, &m->cache, l->cache, W, pool_rows, l->stride_token)
+                               : encode_rows(encode, &m->cache, l->cache, W, tokens, outer, l->stride_token,
+                                             g->blk_coord ? l->stride_batch : l->stride_token, g->box_tokens)) &&
                     encode_rows(encode, &m->fresh, c_new, W, g->l.N, l->batch, W, (int64_t)g->l.N * W, g->l.N);
     return ok ? DSA_OK : DSA_ERR_UNSUPPORTED;      // (an extent or stride beyond what a tensor map holds)
 }
@@ -111,7 +150,7 @@ cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, bool pairs, int
     cudaError_t e = configure<R>();
     if (e != cudaSuccess) return e;
     e = pairs ? launch_dependent(dsa_latent_pair_kernel<R>, blocks, kPairThreads, PairCfg<R>::SMEM, st, g, m)
-              : launch_dependent(dsa_latent_kernel<R>, blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
+              : launch_clusters(dsa_latent_kernel<R>, std::max(g.cluster, 1), blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
     if (e != cudaSuccess || g.groups == 1) return e;
     const int64_t merge = (int64_t)g.l.a.B * g.l.row_tiles * (R / 64);
     return pairs ? launch_dependent(dsa_latent_merge_kernel<R, kPairTile, kPairRows>, merge, kLatThreads, 0, st, g)
@@ -189,6 +228,7 @@ int32_t dsa_latent_step(const dsa_latent* latent, int32_t num_heads, int32_t max
         if (e != cudaSuccess) return host_cuda_fail(e);
         t.l = g;
         t.groups = pl.groups;
+        t.cluster = pl.cluster;
         t.min_units = kLatMinUnits;
         unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
         t.part_ml = reinterpret_cast<float2*>(ws);

@@ -11,9 +11,12 @@ constexpr int kLatThreads = 256;
 
 struct LatentTcArgs {
     LatentArgs l;
-    int groups;                                    // shares that the work is cut into
+    int groups;                                    // shares that the work is cut into, or
+    int cluster;                                   // > 0: blocks of a cluster that have one item to themselves
     int min_units;                                 // units of work that a block takes at least
-    int box_tokens, box_shift;                     // tokens per tensor-map box of the cache, and its logarithm
+    int box_tokens, box_shift;                     // tokens per tensor-map copy of the cache, and its logarithm
+    int gather;                                    // 1: a copy is four single rows of the cache as a matrix, for pages too small for boxes
+    int page_rows;                                 // its rows from one page to the next
     unsigned page_mul;                             // position / block_size = (position * page_mul) >> page_shift
     int page_shift;
     int q_rows;                                    // rows of q per copy: fewer than a block's where a request has fewer
@@ -37,6 +40,8 @@ struct LatentCfg {
     static constexpr int GROUPS = R / 256;                                 // and that are freed on their own: what a product with V reads
     static constexpr int TAIL = 2048;
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT + TAIL;
+    static constexpr int PART_LD = R + 4;                                  // row of a partial result in shared memory, in floats
+    static_assert(kLatRows * PART_LD * 4 <= SLOTS * SLOT, "the partial result takes the ring's place");
     static constexpr int COL_S = R / 2, TMEM_COLS = R == 512 ? 512 : 256;
     static_assert(SMEM <= 232448, "shared memory of an SM");
 };
@@ -58,6 +63,63 @@ __device__ __forceinline__ void tc_mma_ws_add(unsigned d, unsigned a_low, unsign
                  "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n}"
                  ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(kDescHigh) : "memory");
 }
+// four rows of a matrix, 128 bytes of each
+__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int x, int y0, int y1, int y2, int y3, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y0), "r"(y1), "r"(y2), "r"(y3), "r"(smem_u32(bar)) : "memory");
+}
+
+// Where the 64 cached tokens from position `pos` on lie, as far as a lane sees to it: of boxes lane and lane + 32 (page or request,
+// token in it), or, where single rows are gathered, the rows of tokens lane and lane + 32.  Looked up tiles ahead of the copies.
+struct LatentWhere {
+    int blk[2], tok[2];
+};
+__device__ __forceinline__ void latent_where(const LatentTcArgs& g, int b, int pos, bool cached, int lane, LatentWhere& w) {
+    const AttnArgs& a = g.l.a;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int i = lane + 32 * e, shift = g.gather ? 0 : g.box_shift, at = pos + (i << shift);
+        w.blk[e] = g.blk_coord ? b : 0;
+        w.tok[e] = at;
+        if (a.block_table) {
+            const int bi = (int)(((unsigned long long)(unsigned)at * g.page_mul) >> g.page_shift);
+            w.tok[e] = at - bi * a.block_size;
+            // (as the table has it: put into range when the copy is made, so that nobody waits for it here)
+            if ((i << shift) < 64 && cached) w.blk[e] = a.block_table[(int64_t)b * a.max_blocks + min(bi, a.max_blocks - 1)];
+        }
+    }
+}
+// Copies `used` times box_tokens tokens, `nch` 128-byte columns of each, to dst: column(i) of the rows to place(i).
+// box(dst, x, token, page, i) and rows(dst, x, y0, y1, y2, y3, i) make one copy, for the i-th column.
+template <class Column, class Place, class Box, class Rows>
+__device__ __forceinline__ void latent_copy(const LatentTcArgs& g, const LatentWhere& w, int used, int nch, unsigned char* dst, int lane,
+                                            Column column, Place place, Box box, Rows rows) {
+    const AttnArgs& a = g.l.a;
+    auto page = [&](int blk) { return a.block_table ? max(0, min(blk, a.num_blocks - 1)) * g.blk_coord : blk; };
+    LatentWhere v = w;
+    if (g.gather)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v.tok[e] += page(v.blk[e]) * g.page_rows;
+    for (int p0 = 0; p0 < used * nch; p0 += 32) {
+        const int p = p0 + lane, n = p / nch, i = p - n * nch;
+        unsigned char* to = dst + place(i) * (kLatTile * 128) + ((n << g.box_shift) * 128);
+        if (g.gather) {
+            int y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int lo = __shfl_sync(0xffffffffu, v.tok[0], (4 * n + e) & 31), hi = __shfl_sync(0xffffffffu, v.tok[1], (4 * n + e) & 31);
+                y[e] = 4 * n < 32 ? lo : hi;
+            }
+            if (p < used * nch) rows(to, 64 * column(i), y[0], y[1], y[2], y[3], i);
+        } else {
+            const int blk0 = __shfl_sync(0xffffffffu, v.blk[0], n & 31), tok0 = __shfl_sync(0xffffffffu, v.tok[0], n & 31);
+            const int blk1 = __shfl_sync(0xffffffffu, v.blk[1], n & 31), tok1 = __shfl_sync(0xffffffffu, v.tok[1], n & 31);
+            if (p < used * nch) box(to, 64 * column(i), n < 32 ? tok0 : tok1, page(n < 32 ? blk0 : blk1), i);
+        }
+    }
+    __syncwarp();
+}
+
 // ---- shares -------------------------------------------------------------------------------------------------
 // The work is a list of items: for every request the row tiles (ROWS query rows) that have tokens which exist, for each of them
 // a unit per key tile (KT tokens; the last unit: the new tokens).  End to end they are cut into shares of equal size, one per
@@ -187,10 +249,10 @@ __device__ __forceinline__ void latent_rest(const LatentArgs& l, const LatentSeg
 }
 
 // The results of 64 query rows by the four warps that have their TMEM lanes, two threads a row (half 0 / 1: dims 0-127 / 128-255 of
-// every 256): to out and lse, or, part >= 0, what the merge needs.  m: maximum in base-2 units, total: the row's sum.
+// every 256): to out and lse, or, part >= 0, what the merge needs (in s_part and s_ml, where the blocks of a cluster merge).  m: maximum in base-2 units, total: the row's sum.
 template <int R>
 __device__ __forceinline__ void latent_results(const LatentTcArgs& g, unsigned tmem, int64_t orow, int rows_all, int row, int half, int part,
-                                               bool any, bool alive, float m, float total) {
+                                               bool any, bool alive, float m, float total, float* s_part = nullptr, float2* s_ml = nullptr) {
     const LatentArgs& l = g.l;
     const bool none = !alive || total == 0.f;                 // nothing seen: zeros and -inf
     const float inv = none ? 0.f : 1.f / total;
@@ -207,7 +269,12 @@ __device__ __forceinline__ void latent_results(const LatentTcArgs& g, unsigned t
             }
             if (mine) {
                 const int dim = (c >> 7) * 256 + half * 128 + (c & 127);
-                if (part >= 0) {
+                if (part >= 0 && s_part) {
+                    float4* dst = reinterpret_cast<float4*>(s_part + row * LatentCfg<R>::PART_LD + dim);
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        dst[k / 4] = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+                } else if (part >= 0) {
                     float4* dst = g.part_o + ((int64_t)part * (R / 4) + dim / 4) * kLatRows + row;
 #pragma unroll
                     for (int k = 0; k < 32; k += 4)
@@ -229,7 +296,7 @@ __device__ __forceinline__ void latent_results(const LatentTcArgs& g, unsigned t
         tc_fence_before();
     }
     if (half == 0) {
-        if (part >= 0) g.part_ml[(int64_t)part * kLatRows + row] = none ? make_float2(-INFINITY, 0.f) : make_float2(m, total);
+        if (part >= 0) (s_ml ? s_ml + row : g.part_ml + (int64_t)part * kLatRows + row)[0] = none ? make_float2(-INFINITY, 0.f) : make_float2(m, total);
         else if (row < rows_all) l.a.lse[orow] = none ? -INFINITY : (m + log2f(total)) * LN2;
     }
     __syncwarp();
@@ -267,6 +334,9 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const LatentArgs& l = g.l;
     const int share = (int)blockIdx.x;
+    // a cluster's merge: O of this block's part (rows padded against bank conflicts) and per row (maximum in base-2 units, sum)
+    float* s_part = reinterpret_cast<float*>(s_ring);
+    float2* s_ml = reinterpret_cast<float2*>(s_q);
 
     if (warp == 4 && lane == 0) {
         for (int s = 0; s < LANDS + PARTS; ++s) mbar_init(bars + s, 1);
@@ -298,7 +368,21 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
 
-    latent_first<kLatTile, kLatRows>(g, share, s_scan, s_misc + 2);
+    bool merged = false;                                      // several blocks of the cluster have parts of the item
+    int item_b = 0, item_rt = 0;
+    if (g.cluster > 0) {
+        const int rank = share % g.cluster, item = share / g.cluster;
+        item_b = item / l.row_tiles;
+        item_rt = item % l.row_tiles;
+        const LatentItems<kLatTile, kLatRows> x(l, item_b);
+        const int per = (x.units + g.cluster - 1) / g.cluster, left = item_rt < x.items ? max(0, min(per, x.units - rank * per)) : 0;
+        merged = item_rt < x.items && x.units > per;
+        if (tid == 0) { s_misc[2] = item_b; s_misc[3] = item_rt * x.units + rank * per; s_misc[4] = left; s_misc[5] = 0; }
+        if (merged && left == 0 && tid < kLatRows) s_ml[tid] = make_float2(-INFINITY, 0.f);
+        __syncthreads();
+    } else {
+        latent_first<kLatTile, kLatRows>(g, share, s_scan, s_misc + 2);
+    }
 
     Seg sg;
     auto next_seg = [&](int i) -> bool {
@@ -325,24 +409,8 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
             if (sg.b < 0) break;
             const int tiles = sg.tiles();
             if (tiles == 0) continue;
-            // where this lane's boxes of a tile come from: (page or request, token in it)
-            const int boxes = kLatTile >> g.box_shift;
-            auto where = [&](int t, int (&blk)[2], int (&tok)[2]) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int box = lane + 32 * h, pos = (sg.t0 + t) * kLatTile + (box << g.box_shift);
-                    blk[h] = g.blk_coord ? sg.b : 0;
-                    tok[h] = pos;
-                    if (l.a.block_table) {
-                        const int bi = (int)(((unsigned long long)(unsigned)pos * g.page_mul) >> g.page_shift);
-                        tok[h] = pos - bi * l.a.block_size;
-                        if (box < boxes && sg.cached(t))
-                            blk[h] = l.a.block_table[(int64_t)sg.b * l.a.max_blocks + min(bi, l.a.max_blocks - 1)];
-                    }
-                }
-            };
-            int blk0[2], tok0[2], blk1[2], tok1[2];
-            where(0, blk0, tok0);
+            LatentWhere at0, at1;
+            latent_where(g, sg.b, sg.t0 * kLatTile, sg.cached(0), lane, at0);
             const int q_before = live;
             // q is fetched into L2 now, and to its place when the scores of the share before are done: behind the first tile's copies,
             // which need not wait for that
@@ -360,7 +428,7 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
             };
             if (live == 0) ok = copy_q();
             for (int t = 0; ok && t < tiles; ++t) {
-                if (t + 1 < tiles) where(t + 1, blk1, tok1);
+                if (t + 1 < tiles) latent_where(g, sg.b, (sg.t0 + t + 1) * kLatTile, sg.cached(t + 1), lane, at1);
                 const bool cached = sg.cached(t);
                 const int used = cached ? (sg.count(t) + g.box_tokens - 1) >> g.box_shift : 1;     // boxes
                 unsigned char* dst = s_ring + slot * C::SLOT;
@@ -376,22 +444,16 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                     if (!cached) {
                         if (lane < nch) tma_box3(dst + (c0 + lane) * C::CHUNK, &maps.fresh, 64 * (c0 + lane), 0, sg.b, bars_t + (c0 + lane) / 3);
                     } else {
-                        for (int p0 = 0; p0 < used * nch; p0 += 32) {
-                            const int p = p0 + lane, box = p / nch, c = c0 + p - box * nch;
-                            int blk = __shfl_sync(0xffffffffu, blk0[0], box & 31), tok = __shfl_sync(0xffffffffu, tok0[0], box & 31);
-                            const int blk_h = __shfl_sync(0xffffffffu, blk0[1], box & 31), tok_h = __shfl_sync(0xffffffffu, tok0[1], box & 31);
-                            if (box >= 32) { blk = blk_h; tok = tok_h; }
-                            if (l.a.block_table) blk = max(0, min(blk, l.a.num_blocks - 1)) * g.blk_coord;
-                            if (p < used * nch) tma_box3(dst + c * C::CHUNK + ((box << g.box_shift) * 128), &maps.cache, 64 * c, tok, blk, bars_t + c / 3);
-                        }
+                        latent_copy(g, at0, used, nch, dst, lane, [&](int c) { return c0 + c; }, [&](int c) { return c0 + c; },
+                                    [&](unsigned char* to, int x, int tok, int page, int c) { tma_box3(to, &maps.cache, x, tok, page, bars_t + (c0 + c) / 3); },
+                                    [&](unsigned char* to, int x, int y0, int y1, int y2, int y3, int c) { tma_gather4(to, &maps.cache, x, y0, y1, y2, y3, bars_t + (c0 + c) / 3); });
                     }
                     __syncwarp();
                 }
                 issued += C::LAND;
                 if (++slot == C::SLOTS) { slot = 0; ++round; }
                 if (ok && t == 0 && live == q_before) ok = copy_q();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) { blk0[h] = blk1[h]; tok0[h] = tok1[h]; }
+                at0 = at1;
             }
         }
         // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
@@ -610,12 +672,51 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                 total += sum_l;
             }
             latent_results<R>(g, tmem + lane_base, (int64_t)sg.b * l.rows + sg.rt * kLatRows + row, min(kLatRows, l.rows - sg.rt * kLatRows), row,
-                              half, sg.part < 0 ? -1 : share * 2 + sg.part, tiles > 0, alive, m_ref * sl, total);
+                              half, sg.part < 0 ? -1 : share * 2 + sg.part, tiles > 0, alive, m_ref * sl, total, g.cluster > 0 ? s_part : nullptr,
+                              g.cluster > 0 ? s_ml : nullptr);
             if (tiles == 0) continue;
             if (lane == 0) mbar_arrive(o_free);
         }
     }
     __syncthreads();                                          // (every role has come to its end)
+    if (g.cluster > 1 && merged) {
+        // out = sum_i e^{m_i - M} O_i / sum_i e^{m_i - M} l_i over the cluster's blocks, which share the rows
+        tree_cluster_barrier();
+        constexpr int PIECES = R / 128;                       // of a row, a warp each: every lane has four dims, of all blocks at once
+        const int rank = share % g.cluster, tasks = min(kLatRows, l.rows - item_rt * kLatRows) * PIECES;
+        for (int task = rank * (kLatThreads / 32) + warp; task < tasks; task += kLatThreads / 32 * g.cluster) {
+            const int r = task / PIECES, c = task % PIECES * 128 + lane * 4;
+            float2 ml[8];
+            float4 o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                ml[i] = make_float2(-INFINITY, 0.f);
+                if (i < g.cluster) {
+                    ml[i] = tree_peer_f2(tree_peer(s_ml + r, i));
+                    o[i] = tree_peer_f4(tree_peer(s_part + r * C::PART_LD + c, i));
+                }
+            }
+            float top = -INFINITY, sum = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (ml[i].y == 0.f) continue;                 // (a part that saw nothing has no O either)
+                const float w = fast_exp2(ml[i].x - top);
+                sum = fmaf(w, ml[i].y, sum);
+                acc.x = fmaf(w, o[i].x, acc.x); acc.y = fmaf(w, o[i].y, acc.y);
+                acc.z = fmaf(w, o[i].z, acc.z); acc.w = fmaf(w, o[i].w, acc.w);
+            }
+            const bool none = sum == 0.f;
+            const float inv = none ? 0.f : 1.f / sum;
+            const int64_t orow = (int64_t)item_b * l.rows + item_rt * kLatRows + r;
+            *reinterpret_cast<uint2*>(reinterpret_cast<T*>(l.a.out) + orow * R + c) =
+                none ? make_uint2(0u, 0u) : make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+            if (c == 0) l.a.lse[orow] = none ? -INFINITY : (top + log2f(sum)) * LN2;
+        }
+        tree_cluster_barrier();                               // nobody leaves while its shared memory may be read
+    }
     if (warp == 5) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((unsigned)C::TMEM_COLS));

@@ -28,18 +28,26 @@ inline int32_t check_latent(const dsa_latent* l, bool step) {
 
 // A launch that may begin while the one in front ends (its kernel waits for that one's writes itself).
 template <class Kern, class... Args>
-cudaError_t launch_dependent(Kern kern, int64_t blocks, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+cudaError_t launch_clusters(Kern kern, int cluster, int64_t blocks, int threads, size_t smem, cudaStream_t st, const Args&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+template <class Kern, class... Args>
+cudaError_t launch_dependent(Kern kern, int64_t blocks, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+    return launch_clusters(kern, 1, blocks, threads, smem, st, args...);
 }
 
 cudaError_t latent_prepare();                                // configure the kernels for the current device

@@ -18,11 +18,6 @@ struct PairCfg {
     static_assert(SMEM <= 232448, "shared memory of an SM");
 };
 
-__device__ __forceinline__ unsigned pair_peer(const void* p, unsigned rank) {   // p in the shared memory of block `rank` of the pair
-    unsigned r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
-    return r;
-}
 __device__ __forceinline__ void pair_arrive(unsigned bar) {                     // on a barrier of either block
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -30,6 +25,11 @@ __device__ __forceinline__ void pair_arrive(unsigned bar) {                     
 __device__ __forceinline__ void pair_box3(void* dst, const CUtensorMap* map, int c0, int c1, int c2, unsigned bar) {
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_gather4(void* dst, const CUtensorMap* map, int x, int y0, int y1, int y2, int y3, unsigned bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y0), "r"(y1), "r"(y2), "r"(y3), "r"(bar) : "memory");
 }
 // one arrival on the barrier at this offset in both blocks when the products issued so far are done
 __device__ __forceinline__ void pair_commit(unsigned long long* bar) {
@@ -47,11 +47,6 @@ __device__ __forceinline__ void tc_mma_pair_add(unsigned d, unsigned a_low, unsi
                  "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, 1;\n}"
                  ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void pair_barrier() {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 template <int R>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa_latent_pair_kernel(const LatentTcArgs g, const __grid_constant__ LatentMaps maps) {
     using W = LatentCfg<R>;
@@ -114,7 +109,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
         tc_fence_before();
     }
     __syncthreads();
-    pair_barrier();                                           // (the other block's barriers are there)
+    tree_cluster_barrier();                                           // (the other block's barriers are there)
     tc_fence_after();
     const unsigned tmem = (unsigned)*reinterpret_cast<volatile int*>(s_misc);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -131,42 +126,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
     };
     // tokens of tile t that block h of the pair has
     auto half_count = [&](int t, int h) { return max(0, min(kLatTile, sg.count(t) - h * kLatTile)); };
-    // where a lane's boxes of block h's keys of tile t come from: (page or request, token in it)
-    const int boxes = kLatTile >> g.box_shift;
-    auto where = [&](int t, int h, int (&blk)[2], int (&tok)[2]) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int box = lane + 32 * e, pos = (sg.t0 + t) * kPairTile + h * kLatTile + (box << g.box_shift);
-            blk[e] = g.blk_coord ? sg.b : 0;
-            tok[e] = pos;
-            if (l.a.block_table) {
-                const int bi = (int)(((unsigned long long)(unsigned)pos * g.page_mul) >> g.page_shift);
-                tok[e] = pos - bi * l.a.block_size;
-                if (box < boxes && sg.cached(t))
-                    blk[e] = l.a.block_table[(int64_t)sg.b * l.a.max_blocks + min(bi, l.a.max_blocks - 1)];
-            }
-        }
-    };
+    auto where = [&](int t, int h, LatentWhere& w) { latent_where(g, sg.b, (sg.t0 + t) * kPairTile + h * kLatTile, sg.cached(t), lane, w); };
     // boxes of block h's keys of tile t, and their rows; a tile of new tokens is one box of N rows, the first block's
     auto used_boxes = [&](int t, int h) { return sg.cached(t) ? (half_count(t, h) + g.box_tokens - 1) >> g.box_shift : h == 0 ? 1 : 0; };
     auto used_rows = [&](int t, int h) { return sg.cached(t) ? used_boxes(t, h) << g.box_shift : h == 0 ? l.N : 0; };
-    // one 64-element column after the other of `nch` (column(i) of the row to place(i) of the slot), all boxes
-    auto copy_cols = [&](int t, int h, const int (&blk)[2], const int (&tok)[2], unsigned char* dst, int nch, auto column, auto place, auto bar) {
+    // `nch` columns, column(i) of the rows to place(i) of the slot, of block h's keys of tile t
+    auto copy_cols = [&](int t, int h, const LatentWhere& w, unsigned char* dst, int nch, auto column, auto place, auto bar) {
         const int used = used_boxes(t, h);
         if (!sg.cached(t)) {
             if (lane < nch && used > 0) pair_box3(dst + place(lane) * W::CHUNK, &maps.fresh, 64 * column(lane), 0, sg.b, bar(lane));
+            __syncwarp();
         } else {
-            for (int p0 = 0; p0 < used * nch; p0 += 32) {
-                const int p = p0 + lane, box = p / nch, i = p - box * nch;
-                int bk = __shfl_sync(0xffffffffu, blk[0], box & 31), tk = __shfl_sync(0xffffffffu, tok[0], box & 31);
-                const int bk_h = __shfl_sync(0xffffffffu, blk[1], box & 31), tk_h = __shfl_sync(0xffffffffu, tok[1], box & 31);
-                if (box >= 32) { bk = bk_h; tk = tk_h; }
-                if (l.a.block_table) bk = max(0, min(bk, l.a.num_blocks - 1)) * g.blk_coord;
-                if (p < used * nch)
-                    pair_box3(dst + place(i) * W::CHUNK + ((box << g.box_shift) * 128), &maps.cache, 64 * column(i), tk, bk, bar(i));
-            }
+            latent_copy(g, w, used, nch, dst, lane, column, place,
+                        [&](unsigned char* to, int x, int tok, int page, int i) { pair_box3(to, &maps.cache, x, tok, page, bar(i)); },
+                        [&](unsigned char* to, int x, int y0, int y1, int y2, int y3, int i) { pair_gather4(to, &maps.cache, x, y0, y1, y2, y3, bar(i)); });
         }
-        __syncwarp();
     };
 
     if (warp == 4) {
@@ -186,8 +160,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
             const int tiles = sg.tiles();
             if (tiles == 0) continue;
             const int q_row = sg.b * l.rows + sg.rt * kPairRows + (int)rank * kLatRows;
-            int blk0[2], tok0[2], blk1[2], tok1[2];
-            where(0, (int)rank, blk0, tok0);
+            LatentWhere at0, at1;
+            where(0, (int)rank, at0);
             const int q_before = live;
             if (lane < W::CH)
                 asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
@@ -196,14 +170,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
                 if (live > 0 && !tree_wait(q_empty, (live - 1) & 1, abort, l.a.wait_timeouts, lane)) return false;
                 if (leader && lane == 0) mbar_expect_tx(q_full, (unsigned)(2 * W::Q_BYTES));
                 __syncwarp();
-                if (lane < W::CH) pair_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, q_row, 0, pair_peer(q_full, 0));
+                if (lane < W::CH) pair_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, q_row, 0, tree_peer(q_full, 0));
                 __syncwarp();
                 ++live;
                 return true;
             };
             if (live == 0) ok = copy_q();
             for (int t = 0; ok && t < tiles; ++t) {
-                if (t + 1 < tiles) where(t + 1, (int)rank, blk1, tok1);
+                if (t + 1 < tiles) where(t + 1, (int)rank, at1);
                 const unsigned rows = (unsigned)(used_rows(t, 0) + used_rows(t, 1));
                 unsigned char* dst = s_ring + slot * W::SLOT;
 #pragma unroll 1
@@ -214,14 +188,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
                     if (leader && lane < W::LAND && 3 * lane >= c0 && 3 * lane < c0 + nch)    // parts that begin in this group
                         mbar_expect_tx(full + slot * W::LAND + lane, (unsigned)(min(3, W::CH - 3 * lane) * 128) * rows);
                     __syncwarp();
-                    copy_cols(t, (int)rank, blk0, tok0, dst, nch, [&](int c) { return c0 + c; }, [&](int c) { return c0 + c; },
-                              [&](int c) { return pair_peer(full + slot * W::LAND + (c0 + c) / 3, 0); });
+                    copy_cols(t, (int)rank, at0, dst, nch, [&](int c) { return c0 + c; }, [&](int c) { return c0 + c; },
+                              [&](int c) { return tree_peer(full + slot * W::LAND + (c0 + c) / 3, 0); });
                 }
                 issued += W::LAND;
                 if (++slot == W::SLOTS) { slot = 0; ++round; }
                 if (ok && t == 0 && live == q_before) ok = copy_q();
-#pragma unroll
-                for (int e = 0; e < 2; ++e) { blk0[e] = blk1[e]; tok0[e] = tok1[e]; }
+                at0 = at1;
             }
         }
         // no copy is in flight when the pair ends (in a healthy run the products have waited for all of them)
@@ -246,10 +219,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
         for (int i = 0; ok && next_seg(i); ++i) {
             const int tiles = sg.tiles();
             if (tiles == 0) continue;
-            int blk0[2], tok0[2], blk1[2], tok1[2];
-            where(0, other, blk0, tok0);
+            LatentWhere at0, at1;
+            where(0, other, at0);
             for (int t = 0; ok && t < tiles; ++t) {
-                if (t + 1 < tiles) where(t + 1, other, blk1, tok1);
+                if (t + 1 < tiles) where(t + 1, other, at1);
                 const int gt = done + t, buf = gt & 1, rows = used_rows(t, other);
                 ok = tree_wait(s_full + buf, (gt >> 1) & 1, abort, l.a.wait_timeouts, lane);
                 if (!ok) break;
@@ -257,7 +230,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
                 if (rows > 0) {
                     if (lane == 0) mbar_expect_tx(v_land, (unsigned)(COLS * 128 * rows));
                     __syncwarp();
-                    copy_cols(t, other, blk0, tok0, dst, COLS, [&](int c) { return pick(c, from); }, [&](int c) { return pick(c, to); },
+                    copy_cols(t, other, at0, dst, COLS, [&](int c) { return pick(c, from); }, [&](int c) { return pick(c, to); },
                               [&](int) { return smem_u32(v_land); });
                 }
                 // rows behind the last token, up to where the product stops: zero, whatever the cache or the slot held
@@ -278,10 +251,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
                     zero(half_count(t, other), to);
                 }
                 __syncwarp();
-                if (lane == 0) pair_arrive(pair_peer(v_ready + buf, 0));
+                if (lane == 0) pair_arrive(tree_peer(v_ready + buf, 0));
                 if (++slot == W::SLOTS) slot = 0;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) { blk0[e] = blk1[e]; tok0[e] = tok1[e]; }
+                at0 = at1;
             }
             done += tiles;
         }
@@ -490,7 +462,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
                 sum_l += both.x + both.y;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) pair_arrive(pair_peer(p_ready + buf, 0));
+                if (lane == 0) pair_arrive(tree_peer(p_ready + buf, 0));
                 if (++slot == W::SLOTS) slot = 0;
             }
             if (!ok) break;
@@ -506,11 +478,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
             latent_results<R>(g, tmem + lane_base, (int64_t)sg.b * l.rows + first + row, max(0, min(kLatRows, l.rows - first)), row, half,
                               sg.part < 0 ? -1 : (share * 2 + (int)rank) * 2 + sg.part, tiles > 0, alive, m_ref * sl, total);
             if (tiles == 0) continue;
-            if (lane == 0) pair_arrive(pair_peer(o_free, 0));
+            if (lane == 0) pair_arrive(tree_peer(o_free, 0));
         }
     }
     __syncthreads();                                          // (every role has come to its end)
-    pair_barrier();                                           // nobody leaves while its shared memory or barriers may be used
+    tree_cluster_barrier();                                           // nobody leaves while its shared memory or barriers may be used
     if (warp == 5) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((unsigned)C::TMEM_COLS));

@@ -181,26 +181,6 @@ __device__ __forceinline__ void tree_write_empty(const TreeArgs& g, int b, int k
     }
 }
 
-// ---- thread-block clusters ---------------------------------------------------------------------------
-__device__ __forceinline__ void tree_cluster_barrier() {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ unsigned tree_peer(const void* p, unsigned rank) {   // p in the shared memory of block `rank`
-    unsigned r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ float2 tree_peer_f2(unsigned addr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 tree_peer_f4(unsigned addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
 // What a block works on: the piece `piece` of the tiles that the nodes of row tile `rt` of (b, kvh) see.
 struct TreeItem {
     int index, b, kvh, rt, piece, S, L_p, n;                  // index < 0: nothing any more

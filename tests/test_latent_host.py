@@ -21,8 +21,8 @@ def dsa():
 
 
 def _latent(dsa, **kw):
-    base = dict(batch=4, latent_dim=512, rope_dim=64, dtype=dsa.DSA_BF16, sm_scale=0.1, cache=FAKE, stride_batch=16 * 576, stride_token=576,
-                seq_len=FAKE, block_table=FAKE, max_blocks=64, block_size=16, num_blocks=300, max_seq_len=1000)
+    base = dict(batch=64, latent_dim=512, rope_dim=64, dtype=dsa.DSA_BF16, sm_scale=0.1, cache=FAKE, stride_batch=16 * 576, stride_token=576,
+                seq_len=FAKE, block_table=FAKE, max_blocks=500, block_size=16, num_blocks=300, max_seq_len=8000)
     base.update(kw)
     x = dsa.dsa_latent()
     for k, v in base.items():
@@ -43,7 +43,7 @@ BAD_LATENTS = [(dict(batch=-1), INVALID), (dict(dtype=7), UNSUPPORTED), (dict(la
                (dict(rope_dim=0), UNSUPPORTED), (dict(rope_dim=72), UNSUPPORTED), (dict(rope_dim=12), UNSUPPORTED), (dict(cache=None), INVALID),
                (dict(cache=FAKE + 8), INVALID), (dict(stride_token=568), INVALID), (dict(stride_token=580), INVALID), (dict(stride_batch=-8), INVALID),
                (dict(stride_batch=12), INVALID), (dict(max_seq_len=-1), INVALID), (dict(block_size=0), INVALID), (dict(num_blocks=0), INVALID),
-               (dict(max_blocks=62), INVALID)]
+               (dict(max_blocks=499), INVALID)]
 
 
 def test_step_refusals(dsa):
