@@ -763,21 +763,28 @@ __global__ void __launch_bounds__(kLatThreads) dsa_latent_merge_kernel(const Lat
 #pragma unroll
     for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (alive) {
-#pragma unroll 4
-        for (int gi = g0; gi <= g1; ++gi) {
-            const float2 ml = g.part_ml[part(gi) * kLatRows + row];
-            const float4* o = g.part_o + (part(gi) * (R / 4) + d0 / 4 + c4) * kLatRows + row;
-            float4 y[4];
+        for (int from = g0; from <= g1; from += 2) {          // (the loads of two parts at a time)
+            float2 ml[2];
+            float4 y[2][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = o[k * 4 * kLatRows];
-            if (ml.y == 0.f) continue;                        // (a part that saw nothing)
-            const float next = fmaxf(top, ml.x), keep = fast_exp2(top - next), w = fast_exp2(ml.x - next);
-            top = next;
-            sum = fmaf(sum, keep, w * ml.y);
+            for (int j = 0; j < 2; ++j) {
+                const int64_t p = part(min(from + j, g1));
+                ml[j] = g.part_ml[p * kLatRows + row];
+                const float4* o = g.part_o + (p * (R / 4) + d0 / 4 + c4) * kLatRows + row;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                acc[k].x = fmaf(acc[k].x, keep, w * y[k].x); acc[k].y = fmaf(acc[k].y, keep, w * y[k].y);
-                acc[k].z = fmaf(acc[k].z, keep, w * y[k].z); acc[k].w = fmaf(acc[k].w, keep, w * y[k].w);
+                for (int k = 0; k < 4; ++k) y[j][k] = o[k * 4 * kLatRows];
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (from + j > g1 || ml[j].y == 0.f) continue;    // (a part that saw nothing)
+                const float next = fmaxf(top, ml[j].x), keep = fast_exp2(top - next), w = fast_exp2(ml[j].x - next);
+                top = next;
+                sum = fmaf(sum, keep, w * ml[j].y);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    acc[k].x = fmaf(acc[k].x, keep, w * y[j][k].x); acc[k].y = fmaf(acc[k].y, keep, w * y[j][k].y);
+                    acc[k].z = fmaf(acc[k].z, keep, w * y[j][k].z); acc[k].w = fmaf(acc[k].w, keep, w * y[j][k].w);
+                }
             }
         }
     }
