@@ -158,8 +158,12 @@ cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, bool pairs, int
 }
 template <int R>
 cudaError_t run_f32(const LatentArgs& g, int64_t blocks, cudaStream_t st) {
-    const cudaError_t e = configure<R>();
-    return e != cudaSuccess ? e : launch_dependent(dsa_latent_f32_kernel<R>, blocks, kTileThreads, LatentF32Cfg<R>::SMEM, st, g);
+    cudaError_t e = configure<R>();
+    if (e != cudaSuccess) return e;
+    e = launch_dependent(dsa_latent_f32_kernel<R>, blocks, kTileThreads, LatentF32Cfg<R>::SMEM, st, g);
+    if (e != cudaSuccess || g.a.n_split == 1) return e;
+    const int64_t rows = (int64_t)g.a.B * g.rows, warps = rows * (R / 128);
+    return launch_dependent(dsa_latent_f32_merge_kernel<R>, (warps + kLatF32MergeWarps - 1) / kLatF32MergeWarps, kLatF32MergeWarps * 32, 0, st, g, rows);
 }
 
 }  // namespace
@@ -242,16 +246,11 @@ int32_t dsa_latent_step(const dsa_latent* latent, int32_t num_heads, int32_t max
     if (pl.n_split > 1) {
         g.a.out_part = reinterpret_cast<float*>(workspace);
         g.a.lse_part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(workspace) + pl.ws_out_bytes);
-    } else {
-        g.a.out = out;
-        g.a.lse = lse;
     }
+    g.a.out = out;
+    g.a.lse = lse;
     e = latent->latent_dim == 256 ? run_f32<256>(g, pl.blocks, st) : run_f32<512>(g, pl.blocks, st);
-    if (e != cudaSuccess) return host_cuda_fail(e);
-    if (pl.n_split > 1)
-        return host_launch_combine(g.a.out_part, g.a.lse_part, (int64_t)latent->batch * pl.rows, latent->latent_dim, pl.n_split, out,
-                                   lse, latent->dtype, st);
-    return DSA_OK;
+    return e == cudaSuccess ? DSA_OK : host_cuda_fail(e);
 }
 
 }  // extern "C"

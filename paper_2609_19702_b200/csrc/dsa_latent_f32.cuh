@@ -1,7 +1,7 @@
 // Attention of new tokens over a latent cache, float32 (dsa_latent_step), by CUDA cores: see dsa_tile_f32.cuh.
 //
 // A block has 32 of a request's query rows (token, head) and one piece of its keys, the cached tokens and the new ones as one
-// sequence; pieces are merged by the combine kernel.  Every staged row of R + P floats is key and value at once.
+// sequence; pieces are merged by the kernel behind it.  Every staged row of R + P floats is key and value at once.
 #pragma once
 #include "dsa_latent_args.cuh"
 #include "dsa_tile_f32.cuh"
@@ -70,6 +70,47 @@ __global__ void __launch_bounds__(kTileThreads, R == 256 ? 2 : 1) dsa_latent_f32
                    if (parts) g.a.lse_part[orow * g.a.n_split + piece] = lse;
                    else g.a.lse[orow] = lse;
                });
+}
+
+// The pieces of a row joined: a warp has 128 of its dims, the weights exp(lse_i - max) over their sum from 32 lanes at a time.
+// Bound by reading the pieces (rows x n_split x R floats, from L2), eight of them in flight.
+constexpr int kLatF32MergeWarps = 4;
+
+template <int R>
+__global__ void __launch_bounds__(kLatF32MergeWarps * 32) dsa_latent_f32_merge_kernel(const LatentArgs g, int64_t rows) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int lane = threadIdx.x & 31, n = g.a.n_split;
+    const int64_t at = (int64_t)blockIdx.x * kLatF32MergeWarps + (threadIdx.x >> 5), row = at / (R / 128);
+    const int col = (int)(at % (R / 128)) * 128 + lane * 4;
+    if (row >= rows) return;
+    const float* lp = g.a.lse_part + row * n;
+    float top = -INFINITY;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, lp[i]);
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    float sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const float v = i0 + lane < n ? lp[i0 + lane] : -INFINITY;
+        const float w = v == -INFINITY ? 0.f : expf(v - top);         // (a piece without a number makes the row one)
+        sum += w;
+        const int m = min(32, n - i0);
+        const float* op = g.a.out_part + (row * n + i0) * R + col;
+#pragma unroll 8
+        for (int j = 0; j < m; ++j) {
+            const float wj = __shfl_sync(0xffffffffu, w, j);
+            const float4 y = *reinterpret_cast<const float4*>(op + (int64_t)j * R);
+            acc.x = fmaf(wj, y.x, acc.x); acc.y = fmaf(wj, y.y, acc.y); acc.z = fmaf(wj, y.z, acc.z); acc.w = fmaf(wj, y.w, acc.w);
+        }
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    const bool none = sum == 0.f;
+    const float inv = none ? 0.f : 1.f / sum;
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(g.a.out) + row * R + col) =
+        none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    if (col == 0) g.a.lse[row] = none ? -INFINITY : top + logf(sum);
 }
 
 }  // namespace dsa
