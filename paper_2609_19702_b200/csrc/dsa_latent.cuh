@@ -1,4 +1,24 @@
 // Attention of new tokens over a latent cache, bf16 (dsa_latent_step).
+//
+// A cached row is key and value of all heads at once, so the query rows (token, head) of a request are the M of two products over the
+// same tile of keys in shared memory: S = Q K^T over the R + P numbers of a row, and O += W V with V the first R of them and
+// W = 2^(x - m), x the scores in base-2 units.  m, a row's reference, follows its running maximum only when that has grown by more
+// than 8: a weight is then at most 2^8, O and the sums are float32 and bear that, and O is seldom rescaled.  W is rounded to bf16,
+// the type that V has in the product (relative error of half a step whatever m is); the sum that divides O is of the weights
+// before that rounding, in float32.
+//
+// What bounds it: reading the rows once.  A tile of 64 keys is 73.7 KB (R 512, P 64): 1.7 us of one SM's share of HBM, and about
+// 1800 cycles, 1 us, of its tensor pipe (36 products of N 64 at 33 cycles, 8 of N 256 at 80).  So 64 query rows fit under the
+// copies, and few rows cost the same; more than 64 are the pair kernel's.  The M of 64 is the .ws form: a half of the N
+// columns in either half of the tensor memory's lanes, so that four warps have two threads a row, for softmax and results.
+// Shared memory holds q (73.7 KB) and two tiles (four with R 256); what a slot cannot wait for is cut up: a tile lands
+// in parts of three 128-byte columns, the scores of each part begin as it lands, and its halves are freed one by one as the products
+// with V have read them.  W takes the place of the slot's r column, which only the scores read.  Scores and products with V are
+// issued by a warp each, because every look at a barrier costs an issuing warp some 250 cycles behind queued products.
+//
+// Measured: 64 requests x 16 heads, lengths up to 8190 (304 MB of rows, 47 us at the measured copy rate): 68.0 us, 4.5 TB/s.  Some
+// 4 us go by before the first tile has landed (lengths, then pages, then rows), 5 in the merge of the parts and its launch, the
+// rest in begun and ended items.  One request of about 600 tokens: 13.1 us, four dependent reads and one launch.
 #pragma once
 #include "dsa_latent_args.cuh"
 #include "dsa_tc.cuh"
@@ -127,11 +147,11 @@ __device__ __forceinline__ void latent_copy(const LatentTcArgs& g, const LatentW
 // leaves partial results, which the merge kernel joins.
 // To begin an item costs about as much as two tiles (its q, the last one's results), so where shares are large every item counts
 // two units more, at its front.
-template <int KT, int ROWS>
+template <int KT, int ROWS, bool L2 = false>
 struct LatentItems {
     int S, n, items, units;                        // of a request: lengths, items, and units of each
     __device__ __forceinline__ LatentItems(const LatentArgs& l, int b) {
-        latent_lengths(l, b, S, n);
+        latent_lengths<L2>(l, b, S, n);
         items = n > 0 ? (n * l.a.H_q + ROWS - 1) / ROWS : 1;
         units = n > 0 ? (S + KT - 1) / KT + 1 : 1;
     }
@@ -143,12 +163,12 @@ struct LatentShares {
 
 // By every thread of a block: units in front of request b0, where a thread has the stretch [b0, b1) of them, in order.
 // s_scan: shared, two numbers per warp.
-template <int KT, int ROWS>
+template <int KT, int ROWS, bool L2 = false>
 __device__ __forceinline__ LatentShares latent_shares(const LatentArgs& l, int groups, int min_units, int b0, int b1, int2* s_scan) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
     int sum = 0, items = 0;
     for (int b = b0; b < b1; ++b) {
-        const LatentItems<KT, ROWS> x(l, b);
+        const LatentItems<KT, ROWS, L2> x(l, b);
         sum += x.items * x.units;
         items += x.items;
     }
@@ -249,7 +269,8 @@ __device__ __forceinline__ void latent_rest(const LatentArgs& l, const LatentSeg
 }
 
 // The results of 64 query rows by the four warps that have their TMEM lanes, two threads a row (half 0 / 1: dims 0-127 / 128-255 of
-// every 256): to out and lse, or, part >= 0, what the merge needs (in s_part and s_ml, where the blocks of a cluster merge).  m: maximum in base-2 units, total: the row's sum.
+// every 256): to out and lse, or, part >= 0, what the merge needs (in s_part and s_ml, where the blocks of a cluster merge).  m: the
+// reference in base-2 units, total: the row's sum.
 template <int R>
 __device__ __forceinline__ void latent_results(const LatentTcArgs& g, unsigned tmem, int64_t orow, int rows_all, int row, int half, int part,
                                                bool any, bool alive, float m, float total, float* s_part = nullptr, float2* s_ml = nullptr) {
@@ -738,17 +759,17 @@ __global__ void __launch_bounds__(kLatThreads) dsa_latent_merge_kernel(const Lat
     const int d0 = (idx % (R / 64)) * 64; idx /= R / 64;
     const int rt = idx % l.row_tiles, b = idx / l.row_tiles;
     const int B = l.a.B, per = (B + kLatThreads - 1) / kLatThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-    const LatentShares sh = latent_shares<KT, ROWS>(l, g.groups, g.min_units, b0, b1, s_scan);
+    const LatentItems<KT, ROWS, true> x(l, b);
+    const LatentShares sh = latent_shares<KT, ROWS, true>(l, g.groups, g.min_units, b0, b1, s_scan);
     if (b >= b0 && b < b1) {
         int before = sh.before;
         for (int i = b0; i < b; ++i) {
-            const LatentItems<KT, ROWS> x(l, i);
+            const LatentItems<KT, ROWS, true> x(l, i);
             before += x.items * (x.units + sh.setup);
         }
         s_before = before;
     }
     __syncthreads();
-    const LatentItems<KT, ROWS> x(l, b);
     const int first = s_before + rt / PER * (x.units + sh.setup), g0 = first / sh.quota, g1 = (first + x.units + sh.setup - 1) / sh.quota;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");

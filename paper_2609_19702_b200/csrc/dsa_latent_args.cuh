@@ -12,11 +12,13 @@ struct LatentArgs {
     int row_tiles;                                 // blocks of query rows per request
 };
 
-// Lengths of request b: cached tokens, and new ones that exist and have room.
+// Lengths of request b: cached tokens, and new ones that exist and have room.  L2: read past an SM's L1, by who reads them before it
+// waits for the kernel in front, so that nothing else keeps older ones from being found there.
+template <bool L2 = false>
 __device__ __forceinline__ void latent_lengths(const LatentArgs& g, int b, int& S, int& n) {
-    const int raw = g.a.seq_len[b];
+    const int raw = L2 ? __ldcg(g.a.seq_len + b) : g.a.seq_len[b];
     S = max(0, min(raw, g.a.max_seq_len));
-    n = g.new_count ? max(0, min(g.new_count[b], g.N)) : g.N;
+    n = g.new_count ? max(0, min(L2 ? __ldcg(g.new_count + b) : g.new_count[b], g.N)) : g.N;
     n = raw < 0 ? 0 : min(n, g.a.max_seq_len - S);
 }
 

@@ -2,6 +2,10 @@
 //
 // A block has 32 of a request's query rows (token, head) and one piece of its keys, the cached tokens and the new ones as one
 // sequence; pieces are merged by the kernel behind it.  Every staged row of R + P floats is key and value at once.
+//
+// Meant for checking a model in single precision, where the tensor cores have no exact form: bound by the multiply-adds of
+// dsa_tile_f32.cuh and, for few rows, by the launch, the dependent reads and the merge.  4 requests x 20 heads x 3 tokens, R 256, lengths up to
+// 1144: 19 us, of which the bytes would take 2.
 #pragma once
 #include "dsa_latent_args.cuh"
 #include "dsa_tile_f32.cuh"

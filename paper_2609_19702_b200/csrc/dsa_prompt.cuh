@@ -1,4 +1,23 @@
 // Attention of the tokens of prompts with expanded keys and values, bf16 (dsa_latent_prompt).
+//
+// S = Q [K | K_rope]^T over D + 64 numbers (what K_rope has fewer arrives as zeros), O += W V, with the lagging reference and the
+// roundings of dsa_latent.cuh.  K_rope's rows are one column of a tile, read once for all heads from where they lie; k_nope and v
+// are read through their strides, so the two parts of one product's rows need no copy.
+//
+// What bounds it: the tensor pipe, 2 (D + 64 + D) operations a query and key, and beside it the softmax, an exponential for each.
+// A block has 256 queries as two halves of 128 (M 128, one thread a row), each with a warp that issues its products, so that one
+// half's softmax runs under the other's products.  A half has 80 columns of scores and 40 of weights of its own beside O's (2 x
+// 128 + 256 = 512 columns with D 128): the scores of tile j + 1 are there when the softmax of tile j is done, and 80 keys are the
+// most that leaves room for.  Weights go back through tensor memory (A of the second product), not through shared memory, whose bytes
+// the products need: K and V of a tile are read by either half, q with every tile.  Tiles of 96 keys whose weights
+// take the scores' columns: 84 us for the prompt below instead of 81, and 75 instead of 68 for the batch.
+// Blocks are persistent and take over those not launched yet, the ones with most keys first, so that an item's first
+// copies run under the last one's products and a ragged batch leaves no SM behind; the rows that do not fill a block are the
+// request's first ones, which see the fewest keys.
+//
+// Measured: one prompt of 4160 tokens, 16 heads: 80 us, 1.1 PFLOP/s or 65 % of the measured matrix rate (which is for bursts: in a row of such
+// calls the power limit holds the clock at 1650 MHz, 92 us).  24 prompts of up to 600 tokens behind prefixes of up to 512, 16 heads:
+// 66 us, where keys and values alone (185 MB) would take 29: halves that are not full, and beginnings and ends of short items.
 #pragma once
 #include "dsa_prompt_args.cuh"
 #include "dsa_tc.cuh"
@@ -109,11 +128,12 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         // Blocks are persistent: a running one takes over the next that has not been launched yet, and begins its copies while
         // the products of the last one run.  Those with the most keys come first.
         PromptItem it = {};
-        int issued = 0, k_issued = 0, live[2] = {0, 0}, idx = (int)blockIdx.x, asked = 0;
+        int issued = 0, k_issued = 0, live[2] = {0, 0}, idx = (int)blockIdx.x, asked = 0, answered = 0;
         bool ok = true;
         auto ask = [&]() { if (lane == 0) steal_block(s_response, stolen); __syncwarp(); ++asked; };
         auto answer = [&]() -> bool {
             volatile int no_abort = 0;                        // (the response is waited for whatever else has happened)
+            ++answered;
             if (!tree_wait(stolen, (asked - 1) & 1, &no_abort, g.wait_timeouts, lane)) { *abort = 1; return false; }
             idx = stolen_block(s_response);
             return true;
@@ -198,6 +218,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
             if (ok) ok = answer();
         }
         // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
+        if (asked > answered) answer();
         volatile int no_abort = 0;
         for (int s = 0; s < 2; ++s)
             if (live[s] > 0) tree_wait(q_full + s, (live[s] - 1) & 1, &no_abort, nullptr, lane);

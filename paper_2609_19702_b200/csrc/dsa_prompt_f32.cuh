@@ -1,5 +1,7 @@
 // Attention of the tokens of prompts with expanded keys and values, float32 (dsa_latent_prompt), by CUDA cores: see
 // dsa_tile_f32.cuh.  A block has 32 queries of one (request, head) and takes the keys that they see tile by tile.
+// Bound by the multiply-adds (see there): 4 prompts of up to 300 tokens, 8 heads of 64 + 32 numbers: 29 us, whose bytes
+// would take 2.
 #pragma once
 #include "dsa_prompt_args.cuh"
 #include "dsa_tile_f32.cuh"
