@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kTileThreads, R == 256 ? 2 : 1) dsa_latent_f32
         cp_async_commit();
         cp_async_wait<0>();
         __syncthreads();
-        st.tile(s_q, s_k, s_k, C::LD, C::LD, W, g.a.scale_log2, scratch, [&](int) { return limit - t * kTileKeys; });
+        st.tile(s_q, s_k, s_k, C::LD, C::LD, W, g.a.scale_log2, scratch, [&](int) { return limit - t * kTileKeys; }, [] {}, [] {});
     }
     if (rt == 0) latent_append<float>(g, b, S, n, piece * (kTileThreads / 32) + warp, g.a.n_split * (kTileThreads / 32), lane);
     const bool parts = g.a.n_split > 1;

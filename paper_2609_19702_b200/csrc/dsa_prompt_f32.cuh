@@ -43,24 +43,34 @@ __global__ void __launch_bounds__(kTileThreads, 2) dsa_prompt_f32_kernel(const P
         for (int c = tid & 7; c < (D + g.P) / 4; c += 8) cp_async16(s_q + row * C::LD + c * 4, src + c * 4, there);
     }
     const int mine = first + row < nq ? limit(first + row) : 0, len = limit(min(first + kTileRows, nq) - 1);
-    TileF32<D> st;
-    st.clear();
-    for (int t = 0; t * kTileKeys < len; ++t) {
-        const int pos = t * kTileKeys + row;
-        const bool there = pos < len;
-        const int64_t tok = there ? k0 + pos : 0;
+    // K of a tile is on its way while the weights and the product of the tile before are worked out, V while the scores are
+    auto copy_k = [&](int t) {
+        const bool there = t * kTileKeys + row < len;
+        const int64_t tok = there ? k0 + t * kTileKeys + row : 0;
         const float* k = reinterpret_cast<const float*>(g.k) + tok * g.k_tok + h * g.k_head;
         const float* kr = reinterpret_cast<const float*>(g.kr) + tok * g.r_tok;
-        const float* v = reinterpret_cast<const float*>(g.v) + tok * g.v_tok + h * g.v_head;
-        for (int c = tid & 7; c < D / 4; c += 8) {
-            cp_async16(s_k + row * C::LD + c * 4, k + c * 4, there);
-            cp_async16(s_v + row * C::LD_V + c * 4, v + c * 4, there);
-        }
+        for (int c = tid & 7; c < D / 4; c += 8) cp_async16(s_k + row * C::LD + c * 4, k + c * 4, there);
         for (int c = tid & 7; c < g.P / 4; c += 8) cp_async16(s_k + row * C::LD + D + c * 4, kr + c * 4, there);
-        cp_async_commit();
-        cp_async_wait<0>();
+    };
+    auto copy_v = [&](int t) {
+        const bool there = t * kTileKeys + row < len;
+        const float* v = reinterpret_cast<const float*>(g.v) + (there ? k0 + t * kTileKeys + row : (int64_t)0) * g.v_tok + h * g.v_head;
+        for (int c = tid & 7; c < D / 4; c += 8) cp_async16(s_v + row * C::LD_V + c * 4, v + c * 4, there);
+    };
+    TileF32<D> st;
+    st.clear();
+    const int tiles = (len + kTileKeys - 1) / kTileKeys;
+    if (tiles > 0) copy_k(0);
+    cp_async_commit();
+    if (tiles > 0) copy_v(0);
+    cp_async_commit();
+    for (int t = 0; t < tiles; ++t) {
+        cp_async_wait<1>();
         __syncthreads();
-        st.tile(s_q, s_k, s_v, C::LD, C::LD_V, D + g.P, g.scale_log2, scratch, [&](int) { return mine - t * kTileKeys; });
+        st.tile(s_q, s_k, s_v, C::LD, C::LD_V, D + g.P, g.scale_log2, scratch, [&](int) { return mine - t * kTileKeys; },
+                [&] { if (t + 1 < tiles) copy_k(t + 1); cp_async_commit(); }, [] { cp_async_wait<1>(); });
+        if (t + 1 < tiles) copy_v(t + 1);
+        cp_async_commit();
     }
     cp_async_wait<0>();
     st.results(g.scale_log2, scratch,

@@ -34,9 +34,11 @@ struct TileF32 {
     }
 
     // One tile, by the whole block: q and k [32][ld] with `width` floats a row, v [32][ld_v]; row r sees the keys below seen(r).
-    // Between its barriers nobody writes q, k or v; when it returns they may be written again.
-    template <class Seen>
-    __device__ __forceinline__ void tile(const float* q, const float* k, const float* v, int ld, int ld_v, int width, float sl, float* scratch, Seen seen) {
+    // Nobody writes q, k or v before it returns, but for k, which may be written from scores_done() on (where k is not v as well);
+    // values() waits for this thread's copies of v.
+    template <class Seen, class ScoresDone, class Values>
+    __device__ __forceinline__ void tile(const float* q, const float* k, const float* v, int ld, int ld_v, int width, float sl, float* scratch, Seen seen, ScoresDone scores_done,
+                                         Values values) {
         float* s_s = scratch;
         float* s_p = scratch + 4 * kTileRows * LS;
         float* s_alpha = s_p + kTileKeys * LS;
@@ -65,6 +67,7 @@ struct TileF32 {
                 }
         }
         __syncthreads();
+        scores_done();
         {
             const int row = tid >> 3, key = (tid & 7) * 4, limit = seen(row);
             float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -95,6 +98,7 @@ struct TileF32 {
             l = fmaf(l, alpha, sum);
             if ((tid & 7) == 0) s_alpha[row] = alpha;
         }
+        values();
         __syncthreads();
         {
             const int dg = tid % DG, r0 = tid / DG * RPT;
