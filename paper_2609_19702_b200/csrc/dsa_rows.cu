@@ -13,9 +13,10 @@ using namespace dsa;
 // Every block adds up the counts of all requests itself (a few reads per thread; no second launch, no wait on another
 // block), keeps the starts in shared memory, and looks the requests of its own stretch of tokens up there by bisection.
 // What bounds it is the chain of dependent reads -- counts, base, table -- for small batches and 16 written bytes a token
-// for large ones.  Measured: 8 requests, one token each: 2.4 us in a row of replayed calls; 256 requests of up to 512: 5.3.
+// for large ones.  Measured: 8 requests, one token each: 2.4 us in a row of replayed calls; 256 requests of up to 512: 3.1 (with 1024
+// tokens a block 5.3).
 constexpr int kMapThreads = 256;
-constexpr int kMapTokens = 1024;                   // of a block
+constexpr int kMapTokens = 256;                    // of a block
 constexpr int kMapBatch = 8192;                    // requests, at most: their starts lie in shared memory
 
 struct MapArgs {
