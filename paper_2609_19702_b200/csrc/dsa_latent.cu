@@ -153,8 +153,8 @@ cudaError_t run_bf16(const LatentTcArgs& g, const LatentMaps& m, bool pairs, int
               : launch_clusters(dsa_latent_kernel<R>, std::max(g.cluster, 1), blocks, kLatThreads, LatentCfg<R>::SMEM, st, g, m);
     if (e != cudaSuccess || g.groups == 1) return e;
     const int64_t merge = (int64_t)g.l.a.B * g.l.row_tiles * (R / 64);
-    return pairs ? launch_dependent(dsa_latent_merge_kernel<R, kPairTile, kPairRows>, merge, kLatThreads, 0, st, g)
-                 : launch_dependent(dsa_latent_merge_kernel<R, kLatTile, kLatRows>, merge, kLatThreads, 0, st, g);
+    return pairs ? launch_dependent(dsa_latent_merge_kernel<R, kPairTile, kPairRows>, merge, kLatMergeThreads, 0, st, g)
+                 : launch_dependent(dsa_latent_merge_kernel<R, kLatTile, kLatRows>, merge, kLatMergeThreads, 0, st, g);
 }
 template <int R>
 cudaError_t run_f32(const LatentArgs& g, int64_t blocks, cudaStream_t st) {

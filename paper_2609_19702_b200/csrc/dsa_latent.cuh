@@ -27,7 +27,9 @@ namespace dsa {
 
 constexpr int kLatTile = 64;                       // tokens per tile
 constexpr int kLatRows = 64;                       // query rows per block: the M of the products
-constexpr int kLatThreads = 256;
+constexpr int kLatThreads = 384;
+constexpr int kRowLoaders = 128;                   // of them: copy rows of the cache
+constexpr int kLatMergeThreads = 256;
 
 struct LatentTcArgs {
     LatentArgs l;
@@ -348,8 +350,8 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     Seg* s_info = reinterpret_cast<Seg*>(s_full + 18);        // [2]
     float* s_pair = reinterpret_cast<float*>(s_info + 2);     // [2][128] maxima and sums that the two halves of a row exchange
     int* s_misc = reinterpret_cast<int*>(s_pair + 256);       // [0] TMEM address, [1] abort, [2..] first request, its first unit, units, set-up units
-    int2* s_scan = reinterpret_cast<int2*>(s_misc + 8);       // [8]
-    static_assert((LANDS + PARTS + 18) * 8 + 2 * sizeof(Seg) + 1024 + 96 <= C::TAIL, "tail of the shared memory");
+    int2* s_scan = reinterpret_cast<int2*>(s_misc + 8);       // [kLatThreads / 32]
+    static_assert((LANDS + PARTS + 18) * 8 + 2 * sizeof(Seg) + 1024 + 32 + kLatThreads / 4 <= C::TAIL, "tail of the shared memory");
     volatile int* abort = s_misc + 1;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -360,18 +362,18 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     float2* s_ml = reinterpret_cast<float2*>(s_q);
 
     if (warp == 4 && lane == 0) {
-        for (int s = 0; s < LANDS + PARTS; ++s) mbar_init(bars + s, 1);
+        for (int s = 0; s < LANDS; ++s) mbar_init(full + s, kRowLoaders);
+        for (int s = 0; s < PARTS; ++s) mbar_init(empty + s, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
-            mbar_init(info_full + s, 1); mbar_init(info_empty + s, 7);
+            mbar_init(info_full + s, 1); mbar_init(info_empty + s, kLatThreads / 32 - 1);
             mbar_init(pair + s, 2); mbar_init(drained + s, 1);
         }
         mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_free, 4);
         s_misc[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     } else if (warp == 6) {
-        if (lane < 3)
-            asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &maps.q : lane == 1 ? &maps.cache : &maps.fresh) : "memory");
+        if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q) : "memory");
     } else if (warp == 5) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(smem_u32(s_misc)), "r"((unsigned)C::TMEM_COLS) : "memory");
@@ -415,10 +417,10 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     };
 
     if (warp == 4) {
-        // ---- what to work on; copies of q and of the cached rows ------------------------------------------
+        // ---- what to work on; copies of q ---------------------------------------------------------------------
         const int setup = s_misc[5];
         LatentCursor<kLatTile, kLatRows> cur = {s_misc[2], s_misc[3], s_misc[4]};
-        int slot = 0, round = 0, issued = 0, live = 0;
+        int live = 0;
         bool ok = true;
         for (int i = 0; ok; ++i) {
             sg = cur.next(l, setup);
@@ -428,60 +430,22 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
             __syncwarp();
             if (lane == 0) mbar_arrive(info_full + (i & 1));
             if (sg.b < 0) break;
-            const int tiles = sg.tiles();
-            if (tiles == 0) continue;
-            LatentWhere at0, at1;
-            latent_where(g, sg.b, sg.t0 * kLatTile, sg.cached(0), lane, at0);
-            const int q_before = live;
-            // q is fetched into L2 now, and to its place when the scores of the share before are done: behind the first tile's copies,
-            // which need not wait for that
+            if (sg.tiles() == 0) continue;
+            // q is fetched into L2 now, and to its place when the scores of the share before are done
             if (lane < C::CH)
                 asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
                              ::"l"(&maps.q), "r"(64 * lane), "r"(sg.b * l.rows + sg.rt * kLatRows), "r"(0) : "memory");
-            auto copy_q = [&]() -> bool {
-                if (live > 0 && !tree_wait(q_empty, (live - 1) & 1, abort, l.a.wait_timeouts, lane)) return false;
-                if (lane == 0) mbar_expect_tx(q_full, (unsigned)(C::CH * 128 * g.q_rows));
-                __syncwarp();
-                if (lane < C::CH) tma_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, sg.b * l.rows + sg.rt * kLatRows, 0, q_full);
-                __syncwarp();
-                ++live;
-                return true;
-            };
-            if (live == 0) ok = copy_q();
-            for (int t = 0; ok && t < tiles; ++t) {
-                if (t + 1 < tiles) latent_where(g, sg.b, (sg.t0 + t + 1) * kLatTile, sg.cached(t + 1), lane, at1);
-                const bool cached = sg.cached(t);
-                const int used = cached ? (sg.count(t) + g.box_tokens - 1) >> g.box_shift : 1;     // boxes
-                unsigned char* dst = s_ring + slot * C::SLOT;
-#pragma unroll 1
-                for (int gr = 0; ok && gr < C::GROUPS; ++gr) {
-                    if (round > 0) ok = tree_wait(empty + slot * C::GROUPS + gr, (round - 1) & 1, abort, l.a.wait_timeouts, lane);
-                    if (!ok) break;
-                    const int c0 = gr * 4, nch = gr == C::GROUPS - 1 ? C::CH - c0 : 4;
-                    unsigned long long* bars_t = full + slot * C::LAND;
-                    if (lane < C::LAND && 3 * lane >= c0 && 3 * lane < c0 + nch)      // parts that begin in this group
-                        mbar_expect_tx(bars_t + lane, (unsigned)(min(3, C::CH - 3 * lane) * 128) * (cached ? (unsigned)(used << g.box_shift) : (unsigned)l.N));
-                    __syncwarp();
-                    if (!cached) {
-                        if (lane < nch) tma_box3(dst + (c0 + lane) * C::CHUNK, &maps.fresh, 64 * (c0 + lane), 0, sg.b, bars_t + (c0 + lane) / 3);
-                    } else {
-                        latent_copy(g, at0, used, nch, dst, lane, [&](int c) { return c0 + c; }, [&](int c) { return c0 + c; },
-                                    [&](unsigned char* to, int x, int tok, int page, int c) { tma_box3(to, &maps.cache, x, tok, page, bars_t + (c0 + c) / 3); },
-                                    [&](unsigned char* to, int x, int y0, int y1, int y2, int y3, int c) { tma_gather4(to, &maps.cache, x, y0, y1, y2, y3, bars_t + (c0 + c) / 3); });
-                    }
-                    __syncwarp();
-                }
-                issued += C::LAND;
-                if (++slot == C::SLOTS) { slot = 0; ++round; }
-                if (ok && t == 0 && live == q_before) ok = copy_q();
-                at0 = at1;
-            }
+            if (live > 0) ok = tree_wait(q_empty, (live - 1) & 1, abort, l.a.wait_timeouts, lane);
+            if (!ok) break;
+            if (lane == 0) mbar_expect_tx(q_full, (unsigned)(C::CH * 128 * g.q_rows));
+            __syncwarp();
+            if (lane < C::CH) tma_box3(s_q + lane * kLatRows * 128, &maps.q, 64 * lane, sg.b * l.rows + sg.rt * kLatRows, 0, q_full);
+            __syncwarp();
+            ++live;
         }
         // no copy is in flight when the block ends (in a healthy run the products have waited for all of them)
         volatile int no_abort = 0;
         if (live > 0) tree_wait(q_full, (live - 1) & 1, &no_abort, nullptr, lane);
-        for (int c = max(0, issued - LANDS); c < issued; ++c)
-            if (!tree_wait(full + c % LANDS, (c / LANDS) & 1, &no_abort, nullptr, lane)) break;
     } else if (warp == 5) {
         // ---- scores ---------------------------------------------------------------------------------------
         constexpr unsigned kIdescS = instr_desc(kLatRows, kLatTile, false);
@@ -500,23 +464,13 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                 if (!ok) break;
                 tc_fence_after();
                 const unsigned d = tmem + C::COL_S + buf * (kLatTile / 2);
-                const int count = sg.count(t);
 #pragma unroll
                 for (int p = 0; p < C::LAND; ++p) {
                     constexpr int kCols = 3;
                     const int c0 = p * kCols, nch = C::CH - c0 < kCols ? C::CH - c0 : kCols;
                     ok = ok && tree_wait(full + slot * C::LAND + p, round & 1, abort, l.a.wait_timeouts, lane);
                     if (!ok) break;
-                    // rows behind the last token, up to where the product with V stops: zero, whatever the cache or the slot held
-                    if (count & 15) {
-                        const int pieces = (16 - (count & 15)) * 8;
-                        for (int x = lane; x < pieces * nch; x += 32) {
-                            const int c = x / pieces, at = x - c * pieces;
-                            *reinterpret_cast<uint4*>(s_ring + slot * C::SLOT + (c0 + c) * C::CHUNK + count * 128 + at * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // (what was copied by threads, to the products)
                     if (elect_one()) {
                         const unsigned qa = q_desc + c0 * kLatRows * 128 / 16, ka = k_desc + (slot * C::SLOT + c0 * C::CHUNK) / 16;
                         if (p == 0) tc_mma_ws(d, qa, ka, kIdescS, false);
@@ -586,6 +540,69 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
     } else if (warp == 6) {
         // ---- the new tokens' rows to the cache, by the blocks that have their unit -----------------------------
         for (int i = 0; next_seg(i); ++i) latent_rest<R, kLatRows>(l, sg, sg.rt, (sg.n * l.a.H_q + kLatRows - 1) / kLatRows, lane);
+    } else if (warp >= 8) {
+        // ---- copies of rows, cached and new ones, 16 of a tile by each warp ---------------------------------------
+        // Eight lanes have 128 bytes of a row, so that a warp's copy of 16 bytes a lane is four whole lines in either memory.  Rows
+        // behind the last token arrive as zeros.
+        const int first = (warp - 8) * 16, piece = lane & 7, vecs_r = l.P / 8;
+        const T* cache = reinterpret_cast<const T*>(l.a.k);
+        const T* fresh = reinterpret_cast<const T*>(l.a.k_new);
+        // the row of token first + lane % 16 of tile t, looked up a tile ahead
+        auto find = [&](int t, int& page, int& token) {
+            token = (sg.t0 + t) * kLatTile + first + (lane & 15);
+            page = sg.b;
+            if (!l.a.block_table || !sg.cached(t)) return;
+            const int bi = (int)(((unsigned long long)(unsigned)token * g.page_mul) >> g.page_shift);
+            token -= bi * l.a.block_size;
+            page = l.a.block_table[(int64_t)sg.b * l.a.max_blocks + min(bi, l.a.max_blocks - 1)];
+        };
+        unsigned to[4];                                       // of the four rows that this lane has pieces of
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = first + 4 * k + (lane >> 3);
+            to[k] = smem_u32(s_ring) + r * 128 + ((piece ^ (r & 7)) * 16);
+        }
+        int slot = 0, round = 0;
+        bool ok = true;
+        for (int i = 0; ok && next_seg(i); ++i) {
+            const int tiles = sg.tiles();
+            if (tiles == 0) continue;
+            int page, token;
+            find(0, page, token);
+            for (int t = 0; ok && t < tiles; ++t) {
+                const int count = sg.count(t);
+                if (l.a.block_table) page = max(0, min(page, l.a.num_blocks - 1));
+                const T* mine = sg.cached(t) ? cache + page * l.a.stride_b + token * l.a.stride_tok
+                                             : fresh + ((int64_t)sg.b * l.N + first + (lane & 15)) * (l.R + l.P);
+                if (t + 1 < tiles) find(t + 1, page, token);
+                const T* from[4];
+                bool there[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = 4 * k + (lane >> 3);
+                    from[k] = reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), r)) + piece * 8;
+                    there[k] = first + r < count;
+                    if (!there[k]) from[k] = cache;           // (an address that is there; nothing is read)
+                }
+#pragma unroll
+                for (int c = 0; c < C::CH; ++c) {
+                    if (c % 4 == 0 && c / 4 < C::GROUPS) {
+                        if (round > 0) ok = ok && tree_wait(empty + slot * C::GROUPS + c / 4, (round - 1) & 1, abort, l.a.wait_timeouts, lane);
+                        if (!ok) break;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool some = there[k] && (c < C::CH - 1 || piece < vecs_r);
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                                     ::"r"(to[k] + slot * C::SLOT + c * C::CHUNK), "l"(some ? from[k] + c * 64 : cache), "r"(some ? 16 : 0) : "memory");
+                    }
+                    if (c % 3 == 2 || c == C::CH - 1)
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(full + slot * C::LAND + c / 3)) : "memory");
+                }
+                if (++slot == C::SLOTS) { slot = 0; ++round; }
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp < 4) {
         // ---- softmax: two threads per query row, half of the tile's keys each -------------------------------
         const int half = warp >> 1, row = (warp & 1) * 32 + lane;
@@ -749,8 +766,8 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
 // Which parts there are is worked out before the wait for the kernel in front, while that still runs: it begins its successors
 // when everything in front of it is done, so the lengths that it has read are there to be read here.
 template <int R, int KT, int ROWS>
-__global__ void __launch_bounds__(kLatThreads) dsa_latent_merge_kernel(const LatentTcArgs g) {
-    __shared__ int2 s_scan[kLatThreads / 32];
+__global__ void __launch_bounds__(kLatMergeThreads) dsa_latent_merge_kernel(const LatentTcArgs g) {
+    __shared__ int2 s_scan[kLatMergeThreads / 32];
     __shared__ int s_before;
     constexpr int PER = ROWS / kLatRows;                      // blocks that have an item's rows
     const LatentArgs& l = g.l;
@@ -758,7 +775,7 @@ __global__ void __launch_bounds__(kLatThreads) dsa_latent_merge_kernel(const Lat
     int idx = blockIdx.x;
     const int d0 = (idx % (R / 64)) * 64; idx /= R / 64;
     const int rt = idx % l.row_tiles, b = idx / l.row_tiles;
-    const int B = l.a.B, per = (B + kLatThreads - 1) / kLatThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+    const int B = l.a.B, per = (B + kLatMergeThreads - 1) / kLatMergeThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
     const LatentItems<KT, ROWS, true> x(l, b);
     const LatentShares sh = latent_shares<KT, ROWS, true>(l, g.groups, g.min_units, b0, b1, s_scan);
     if (b >= b0 && b < b1) {
