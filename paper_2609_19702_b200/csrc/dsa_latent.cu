@@ -23,6 +23,14 @@ struct LatentPlan {
 
 constexpr int kLatMinUnits = 2;                    // tiles that a block takes at least (see LatentTcArgs)
 
+// Tokens per tensor-map copy of the cache: a box must not cross the end of a page, so the largest power of two that divides it.
+int latent_box(const dsa_latent* l) {
+    int box = kLatTile;
+    if (l->block_table)
+        while (l->block_size % box) box /= 2;
+    return box;
+}
+
 int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, LatentPlan* pl) {
     const int32_t rc = check_latent(l, true);
     if (rc != DSA_OK) return rc;
@@ -37,7 +45,10 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
         const int64_t tiles = ((int64_t)l->max_seq_len + kLatTile - 1) / kLatTile + 1, items = std::max<int64_t>(1, (int64_t)l->batch * pl->row_tiles);
         const int64_t units = items * (tiles + 2), sms = std::max(host_sm_count(), 1);
         if (units > (1 << 30)) return DSA_ERR_UNSUPPORTED;
-        pl->pairs = pl->rows > kLatRows;
+        // More than 64 query rows: pairs, but where a page allows only boxes of less than 16 tokens, whose copies cost 70 to 90 cycles
+        // each however little they bring.  32 x 128 heads, pairs / blocks of 64 rows, whose threads copy row by row: pages of 64:
+        // 61 / 77 us, 16: 67 / 78, 24: 87 / 78, 1: 146 / 79.
+        pl->pairs = pl->rows > kLatRows && latent_box(l) >= 16;
         const int per = pl->pairs ? 2 : 1;
         pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(sms / per, units / (per * per * kLatMinUnits)));
         pl->blocks = (int64_t)pl->groups * per;
@@ -97,30 +108,12 @@ bool encode_rows(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, i
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The same as a matrix that single rows are gathered from.
-bool encode_matrix(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, int64_t width, int64_t rows, int64_t row_stride) {
-    if (row_stride >= (1LL << 39)) return false;
-    const cuuint64_t n[2] = {(cuuint64_t)width, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)row_stride * 2};
-    const cuuint32_t bx[2] = {64u, 1u}, step[2] = {1u, 1u};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), n, pitch, bx, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void* q, const void* c_new, LatentTcArgs* g, LatentMaps* m) {
     const TensorMapEncodeFn encode = host_tensor_map_encoder();
     if (!encode) return DSA_ERR_UNSUPPORTED;
     const int64_t W = l->latent_dim + l->rope_dim, tokens = l->block_table ? l->block_size : std::max(l->max_seq_len, 1);
-    // a box of the cache must not cross the end of a page: the largest power of two that divides it
-    g->box_tokens = kLatTile;
-    if (l->block_table)
-        while (l->block_size % g->box_tokens) g->box_tokens /= 2;
-    // Boxes of one or two tokens: rows gathered four by four instead, where the pool is a matrix of token rows.  (A copy costs some
-    // 70-90 cycles however little it brings: 64 x 16 heads over pages of 1 / 2 / 4 tokens: 604 / 323 / 184 us by boxes, 212 gathered.)
-    const int64_t page_rows = l->stride_token > 0 && l->stride_batch % l->stride_token == 0 ? l->stride_batch / l->stride_token : 0;
-    const int64_t pool_rows = l->block_table ? (l->num_blocks - 1) * page_rows + l->block_size : 0;
-    g->gather = l->block_table && g->box_tokens < 4 && page_rows > 0 && pool_rows < 0x7fffffff;
-    if (g->gather) { g->box_tokens = 4; g->page_rows = (int)page_rows; }
-    for (g->box_shift = 0; (1 << g->box_shift) < g->box_tokens;) ++g->box_shift;
+    const int box = latent_box(l);
+    for (g->box_shift = 0; (1 << g->box_shift) < box;) ++g->box_shift;
     // division of positions (below 2^31) by the page size: with 2^s >= d the product by ceil(2^(31 + s) / d) is exact
     const unsigned d = l->block_table ? (unsigned)l->block_size : 1u;
     for (g->page_shift = 31; (1ull << (g->page_shift - 31)) < d;) ++g->page_shift;
@@ -128,11 +121,10 @@ int32_t build_latent_maps(const dsa_latent* l, const LatentPlan& pl, const void*
     g->q_rows = std::min(kLatRows, (pl.rows + 7) / 8 * 8);
     g->blk_coord = l->stride_batch > 0 ? 1 : 0;    // (a stride of 0: a dimension of one entry)
     const int64_t outer = g->blk_coord ? (l->block_table ? l->num_blocks : l->batch) : 1;
-    const bool ok = encode_rows(encode, &m->q, q, W, (int64_t)l->batch * pl.rows, 1, W, W, g->q_rows) &&
-                    (g->gather ? encode_matrix(encode, &m->cache, l->cache, W, pool_rows, l->stride_token)
-                               : encode_rows(encode, &m->cache, l->cache, W, tokens, outer, l->stride_token,
-                                             g->blk_coord ? l->stride_batch : l->stride_token, g->box_tokens)) &&
-                    encode_rows(encode, &m->fresh, c_new, W, g->l.N, l->batch, W, (int64_t)g->l.N * W, g->l.N);
+    bool ok = encode_rows(encode, &m->q, q, W, (int64_t)l->batch * pl.rows, 1, W, W, g->q_rows);
+    if (pl.pairs)
+        ok = ok && encode_rows(encode, &m->cache, l->cache, W, tokens, outer, l->stride_token, g->blk_coord ? l->stride_batch : l->stride_token, box) &&
+             encode_rows(encode, &m->fresh, c_new, W, g->l.N, l->batch, W, (int64_t)g->l.N * W, g->l.N);
     return ok ? DSA_OK : DSA_ERR_UNSUPPORTED;      // (an extent or stride beyond what a tensor map holds)
 }
 

@@ -36,13 +36,11 @@ struct LatentTcArgs {
     int groups;                                    // shares that the work is cut into, or
     int cluster;                                   // > 0: blocks of a cluster that have one item to themselves
     int min_units;                                 // units of work that a block takes at least
-    int box_tokens, box_shift;                     // tokens per tensor-map copy of the cache, and its logarithm
-    int gather;                                    // 1: a copy is four single rows of the cache as a matrix, for pages too small for boxes
-    int page_rows;                                 // its rows from one page to the next
+    int box_shift;                                 // pairs: logarithm of the tokens per tensor-map copy of the cache
     unsigned page_mul;                             // position / block_size = (position * page_mul) >> page_shift
     int page_shift;
     int q_rows;                                    // rows of q per copy: fewer than a block's where a request has fewer
-    int blk_coord;                                 // 0: the map's outer dimension has one entry (stride 0)
+    int blk_coord;                                 // pairs: 0: the map's outer dimension has one entry (stride 0)
     float2* part_ml;                               // workspace: [blocks * 2][64] maximum (base 2) and sum
     float4* part_o;                                // [blocks * 2][R / 4][64]
 };
@@ -85,63 +83,6 @@ __device__ __forceinline__ void tc_mma_ws_add(unsigned d, unsigned a_low, unsign
                  "tcgen05.mma.ws.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n}"
                  ::"r"(d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(kDescHigh) : "memory");
 }
-// four rows of a matrix, 128 bytes of each
-__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int x, int y0, int y1, int y2, int y3, unsigned long long* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y0), "r"(y1), "r"(y2), "r"(y3), "r"(smem_u32(bar)) : "memory");
-}
-
-// Where the 64 cached tokens from position `pos` on lie, as far as a lane sees to it: of boxes lane and lane + 32 (page or request,
-// token in it), or, where single rows are gathered, the rows of tokens lane and lane + 32.  Looked up tiles ahead of the copies.
-struct LatentWhere {
-    int blk[2], tok[2];
-};
-__device__ __forceinline__ void latent_where(const LatentTcArgs& g, int b, int pos, bool cached, int lane, LatentWhere& w) {
-    const AttnArgs& a = g.l.a;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int i = lane + 32 * e, shift = g.gather ? 0 : g.box_shift, at = pos + (i << shift);
-        w.blk[e] = g.blk_coord ? b : 0;
-        w.tok[e] = at;
-        if (a.block_table) {
-            const int bi = (int)(((unsigned long long)(unsigned)at * g.page_mul) >> g.page_shift);
-            w.tok[e] = at - bi * a.block_size;
-            // (as the table has it: put into range when the copy is made, so that nobody waits for it here)
-            if ((i << shift) < 64 && cached) w.blk[e] = a.block_table[(int64_t)b * a.max_blocks + min(bi, a.max_blocks - 1)];
-        }
-    }
-}
-// Copies `used` times box_tokens tokens, `nch` 128-byte columns of each, to dst: column(i) of the rows to place(i).
-// box(dst, x, token, page, i) and rows(dst, x, y0, y1, y2, y3, i) make one copy, for the i-th column.
-template <class Column, class Place, class Box, class Rows>
-__device__ __forceinline__ void latent_copy(const LatentTcArgs& g, const LatentWhere& w, int used, int nch, unsigned char* dst, int lane,
-                                            Column column, Place place, Box box, Rows rows) {
-    const AttnArgs& a = g.l.a;
-    auto page = [&](int blk) { return a.block_table ? max(0, min(blk, a.num_blocks - 1)) * g.blk_coord : blk; };
-    LatentWhere v = w;
-    if (g.gather)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) v.tok[e] += page(v.blk[e]) * g.page_rows;
-    for (int p0 = 0; p0 < used * nch; p0 += 32) {
-        const int p = p0 + lane, n = p / nch, i = p - n * nch;
-        unsigned char* to = dst + place(i) * (kLatTile * 128) + ((n << g.box_shift) * 128);
-        if (g.gather) {
-            int y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int lo = __shfl_sync(0xffffffffu, v.tok[0], (4 * n + e) & 31), hi = __shfl_sync(0xffffffffu, v.tok[1], (4 * n + e) & 31);
-                y[e] = 4 * n < 32 ? lo : hi;
-            }
-            if (p < used * nch) rows(to, 64 * column(i), y[0], y[1], y[2], y[3], i);
-        } else {
-            const int blk0 = __shfl_sync(0xffffffffu, v.blk[0], n & 31), tok0 = __shfl_sync(0xffffffffu, v.tok[0], n & 31);
-            const int blk1 = __shfl_sync(0xffffffffu, v.blk[1], n & 31), tok1 = __shfl_sync(0xffffffffu, v.tok[1], n & 31);
-            if (p < used * nch) box(to, 64 * column(i), n < 32 ? tok0 : tok1, page(n < 32 ? blk0 : blk1), i);
-        }
-    }
-    __syncwarp();
-}
-
 // ---- shares -------------------------------------------------------------------------------------------------
 // The work is a list of items: for every request the row tiles (ROWS query rows) that have tokens which exist, for each of them
 // a unit per key tile (KT tokens; the last unit: the new tokens).  End to end they are cut into shares of equal size, one per
@@ -325,6 +266,66 @@ __device__ __forceinline__ void latent_results(const LatentTcArgs& g, unsigned t
     __syncwarp();
 }
 
+// Copies of 16 rows of a tile by one warp, straight from where each of them lies.  Eight lanes have 128 bytes (a column) of a row, so that a copy of
+// 16 bytes by every lane is four whole lines in either memory; rows behind the last token arrive as zeros.  A tile's
+// rows cost 16 such copies a column with addresses that are worked out once, about what a tensor-map copy of the same bytes takes,
+// and it is the same whatever the pages are.
+template <int R>
+struct LatentRows {
+    static constexpr int ROWS = kLatTile / (kRowLoaders / 32), K = ROWS / 4;
+    const LatentArgs& l;
+    int first, piece, row4;                                   // first row; this lane's piece of a column, its row of every four
+    unsigned to[K];                                           // its places in a tile
+    const __nv_bfloat16* from[K];
+    bool there[K];
+    __device__ __forceinline__ LatentRows(const LatentArgs& args, unsigned char* ring, int w, int lane) : l(args), first(w * ROWS), piece(lane & 7), row4(lane >> 3) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int r = first + 4 * k + row4;
+            to[k] = smem_u32(ring) + r * 128 + ((piece ^ (r & 7)) * 16);
+        }
+    }
+    // What a lane sees to: row first + lane % 16 of tile t: its page (or request) and token.  Ahead of at().
+    __device__ __forceinline__ void find(const LatentTcArgs& g, const LatentSeg<kLatTile>& sg, int t, int& page, int& token) const {
+        page = sg.b;
+        token = (sg.t0 + t) * kLatTile + first + ((int)threadIdx.x & (ROWS - 1));
+        if (!l.a.block_table || !sg.cached(t)) return;
+        const int bi = (int)(((unsigned long long)(unsigned)token * g.page_mul) >> g.page_shift);
+        token -= bi * l.a.block_size;
+        page = l.a.block_table[(int64_t)sg.b * l.a.max_blocks + min(bi, l.a.max_blocks - 1)];
+    }
+    // The rows of tile t, which find() has looked up.
+    __device__ __forceinline__ void at(const LatentTcArgs& g, const LatentSeg<kLatTile>& sg, int t, int page, int token) {
+        using T = __nv_bfloat16;
+        const T* cache = reinterpret_cast<const T*>(l.a.k);
+        if (l.a.block_table) page = max(0, min(page, l.a.num_blocks - 1));
+        const T* mine = sg.cached(t) ? cache + page * l.a.stride_b + token * l.a.stride_tok
+                                     : reinterpret_cast<const T*>(l.a.k_new) + ((int64_t)sg.b * l.N + first + ((int)threadIdx.x & (ROWS - 1))) * (l.R + l.P);
+        const int count = sg.count(t) - first;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int r = 4 * k + row4;
+            const T* x = reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), r)) + piece * 8;
+            there[k] = r < count;
+            from[k] = there[k] ? x : cache;                   // (an address that is there; nothing is read)
+        }
+    }
+    // Column c of the rows to a slot.
+    __device__ __forceinline__ void copy(int slot, int c) const {
+        using C = LatentCfg<R>;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const bool some = there[k] && (c < C::CH - 1 || piece < l.P / 8);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                         ::"r"(to[k] + slot * C::SLOT + c * C::CHUNK), "l"(some ? from[k] + c * 64 : from[k]), "r"(some ? 16 : 0) : "memory");
+        }
+    }
+    // One arrival by this thread when its copies so far have landed.
+    __device__ __forceinline__ void arrive(unsigned long long* bar) const {
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    }
+};
+
 template <int R>
 __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const LatentTcArgs g, const __grid_constant__ LatentMaps maps) {
     using C = LatentCfg<R>;
@@ -366,7 +367,7 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
         for (int s = 0; s < PARTS; ++s) mbar_init(empty + s, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(s_full + s, 1); mbar_init(p_ready + s, 4); mbar_init(pv_done + s, 1);
-            mbar_init(info_full + s, 1); mbar_init(info_empty + s, kLatThreads / 32 - 1);
+            mbar_init(info_full + s, 1); mbar_init(info_empty + s, 7);
             mbar_init(pair + s, 2); mbar_init(drained + s, 1);
         }
         mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_free, 4);
@@ -542,62 +543,27 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
         for (int i = 0; next_seg(i); ++i) latent_rest<R, kLatRows>(l, sg, sg.rt, (sg.n * l.a.H_q + kLatRows - 1) / kLatRows, lane);
     } else if (warp >= 8) {
         // ---- copies of rows, cached and new ones, 16 of a tile by each warp ---------------------------------------
-        // Eight lanes have 128 bytes of a row, so that a warp's copy of 16 bytes a lane is four whole lines in either memory.  Rows
-        // behind the last token arrive as zeros.
-        const int first = (warp - 8) * 16, piece = lane & 7, vecs_r = l.P / 8;
-        const T* cache = reinterpret_cast<const T*>(l.a.k);
-        const T* fresh = reinterpret_cast<const T*>(l.a.k_new);
-        // the row of token first + lane % 16 of tile t, looked up a tile ahead
-        auto find = [&](int t, int& page, int& token) {
-            token = (sg.t0 + t) * kLatTile + first + (lane & 15);
-            page = sg.b;
-            if (!l.a.block_table || !sg.cached(t)) return;
-            const int bi = (int)(((unsigned long long)(unsigned)token * g.page_mul) >> g.page_shift);
-            token -= bi * l.a.block_size;
-            page = l.a.block_table[(int64_t)sg.b * l.a.max_blocks + min(bi, l.a.max_blocks - 1)];
-        };
-        unsigned to[4];                                       // of the four rows that this lane has pieces of
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int r = first + 4 * k + (lane >> 3);
-            to[k] = smem_u32(s_ring) + r * 128 + ((piece ^ (r & 7)) * 16);
-        }
+        // (by a place in the list of their own, since they are ahead of those who learn of the items from one another)
+        LatentRows<R> rows(l, s_ring, warp - 8, lane);
+        LatentCursor<kLatTile, kLatRows> cur = {s_misc[2], s_misc[3], s_misc[4]};
+        const int setup = s_misc[5];
         int slot = 0, round = 0;
         bool ok = true;
-        for (int i = 0; ok && next_seg(i); ++i) {
+        while (ok && (sg = cur.next(l, setup)).b >= 0) {
             const int tiles = sg.tiles();
             if (tiles == 0) continue;
             int page, token;
-            find(0, page, token);
+            rows.find(g, sg, 0, page, token);
             for (int t = 0; ok && t < tiles; ++t) {
-                const int count = sg.count(t);
-                if (l.a.block_table) page = max(0, min(page, l.a.num_blocks - 1));
-                const T* mine = sg.cached(t) ? cache + page * l.a.stride_b + token * l.a.stride_tok
-                                             : fresh + ((int64_t)sg.b * l.N + first + (lane & 15)) * (l.R + l.P);
-                if (t + 1 < tiles) find(t + 1, page, token);
-                const T* from[4];
-                bool there[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = 4 * k + (lane >> 3);
-                    from[k] = reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), r)) + piece * 8;
-                    there[k] = first + r < count;
-                    if (!there[k]) from[k] = cache;           // (an address that is there; nothing is read)
-                }
+                rows.at(g, sg, t, page, token);
+                if (t + 1 < tiles) rows.find(g, sg, t + 1, page, token);
 #pragma unroll
                 for (int c = 0; c < C::CH; ++c) {
-                    if (c % 4 == 0 && c / 4 < C::GROUPS) {
-                        if (round > 0) ok = ok && tree_wait(empty + slot * C::GROUPS + c / 4, (round - 1) & 1, abort, l.a.wait_timeouts, lane);
-                        if (!ok) break;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const bool some = there[k] && (c < C::CH - 1 || piece < vecs_r);
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                                     ::"r"(to[k] + slot * C::SLOT + c * C::CHUNK), "l"(some ? from[k] + c * 64 : cache), "r"(some ? 16 : 0) : "memory");
-                    }
-                    if (c % 3 == 2 || c == C::CH - 1)
-                        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(full + slot * C::LAND + c / 3)) : "memory");
+                    if (c % 4 == 0 && c / 4 < C::GROUPS && round > 0)
+                        ok = ok && tree_wait(empty + slot * C::GROUPS + c / 4, (round - 1) & 1, abort, l.a.wait_timeouts, lane);
+                    if (!ok) break;
+                    rows.copy(slot, c);
+                    if (c % 3 == 2 || c == C::CH - 1) rows.arrive(full + slot * C::LAND + c / 3);
                 }
                 if (++slot == C::SLOTS) { slot = 0; ++round; }
             }

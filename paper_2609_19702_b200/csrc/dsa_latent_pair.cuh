@@ -39,10 +39,21 @@ __device__ __forceinline__ void pair_box3(void* dst, const CUtensorMap* map, int
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void pair_gather4(void* dst, const CUtensorMap* map, int x, int y0, int y1, int y2, int y3, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
-                 "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y0), "r"(y1), "r"(y2), "r"(y3), "r"(bar) : "memory");
+// Where the 64 cached tokens from position `pos` on lie, as far as a lane sees to it: of box `lane` (page or request, token in
+// it).  Looked up tiles ahead of the copies.
+struct PairWhere {
+    int blk, tok;
+};
+__device__ __forceinline__ PairWhere pair_where(const LatentTcArgs& g, int b, int pos, bool cached, int lane) {
+    const AttnArgs& a = g.l.a;
+    PairWhere w = {g.blk_coord ? b : 0, pos + (lane << g.box_shift)};
+    if (a.block_table) {
+        const int bi = (int)(((unsigned long long)(unsigned)w.tok * g.page_mul) >> g.page_shift);
+        w.tok -= bi * a.block_size;
+        // (as the table has it: put into range when the copy is made, so that nobody waits for it here)
+        if ((lane << g.box_shift) < kLatTile && cached) w.blk = a.block_table[(int64_t)b * a.max_blocks + min(bi, a.max_blocks - 1)];
+    }
+    return w;
 }
 // one arrival on the barrier at this offset in both blocks when the products issued so far are done
 __device__ __forceinline__ void pair_commit(unsigned long long* bar) {
@@ -139,21 +150,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
     };
     // tokens of tile t that block h of the pair has
     auto half_count = [&](int t, int h) { return max(0, min(kLatTile, sg.count(t) - h * kLatTile)); };
-    auto where = [&](int t, int h, LatentWhere& w) { latent_where(g, sg.b, (sg.t0 + t) * kPairTile + h * kLatTile, sg.cached(t), lane, w); };
+    auto where = [&](int t, int h) { return pair_where(g, sg.b, (sg.t0 + t) * kPairTile + h * kLatTile, sg.cached(t), lane); };
     // boxes of block h's keys of tile t, and their rows; a tile of new tokens is one box of N rows, the first block's
-    auto used_boxes = [&](int t, int h) { return sg.cached(t) ? (half_count(t, h) + g.box_tokens - 1) >> g.box_shift : h == 0 ? 1 : 0; };
+    auto used_boxes = [&](int t, int h) { return sg.cached(t) ? (half_count(t, h) + (1 << g.box_shift) - 1) >> g.box_shift : h == 0 ? 1 : 0; };
     auto used_rows = [&](int t, int h) { return sg.cached(t) ? used_boxes(t, h) << g.box_shift : h == 0 ? l.N : 0; };
     // `nch` columns, column(i) of the rows to place(i) of the slot, of block h's keys of tile t
-    auto copy_cols = [&](int t, int h, const LatentWhere& w, unsigned char* dst, int nch, auto column, auto place, auto bar) {
+    auto copy_cols = [&](int t, int h, const PairWhere& w, unsigned char* dst, int nch, auto column, auto place, auto bar) {
         const int used = used_boxes(t, h);
         if (!sg.cached(t)) {
             if (lane < nch && used > 0) pair_box3(dst + place(lane) * W::CHUNK, &maps.fresh, 64 * column(lane), 0, sg.b, bar(lane));
-            __syncwarp();
         } else {
-            latent_copy(g, w, used, nch, dst, lane, column, place,
-                        [&](unsigned char* to, int x, int tok, int page, int i) { pair_box3(to, &maps.cache, x, tok, page, bar(i)); },
-                        [&](unsigned char* to, int x, int y0, int y1, int y2, int y3, int i) { pair_gather4(to, &maps.cache, x, y0, y1, y2, y3, bar(i)); });
+            for (int p0 = 0; p0 < used * nch; p0 += 32) {
+                const int p = p0 + lane, n = p / nch, i = p - n * nch;
+                int blk = __shfl_sync(0xffffffffu, w.blk, n & 31);
+                const int tok = __shfl_sync(0xffffffffu, w.tok, n & 31);
+                if (l.a.block_table) blk = max(0, min(blk, l.a.num_blocks - 1)) * g.blk_coord;
+                if (p < used * nch) pair_box3(dst + place(i) * W::CHUNK + ((n << g.box_shift) * 128), &maps.cache, 64 * column(i), tok, blk, bar(i));
+            }
         }
+        __syncwarp();
     };
 
     if (warp == 4) {
@@ -173,8 +188,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
             const int tiles = sg.tiles();
             if (tiles == 0) continue;
             const int q_row = sg.b * l.rows + sg.rt * kPairRows + (int)rank * kLatRows;
-            LatentWhere at0, at1;
-            where(0, (int)rank, at0);
+            PairWhere at0, at1;
+            at0 = where(0, (int)rank);
             const int q_before = live;
             if (lane < W::CH)
                 asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
@@ -190,7 +205,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
             };
             if (live == 0) ok = copy_q();
             for (int t = 0; ok && t < tiles; ++t) {
-                if (t + 1 < tiles) where(t + 1, (int)rank, at1);
+                if (t + 1 < tiles) at1 = where(t + 1, (int)rank);
                 const unsigned rows = (unsigned)(used_rows(t, 0) + used_rows(t, 1));
                 unsigned char* dst = s_ring + slot * W::SLOT;
 #pragma unroll 1
@@ -232,10 +247,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) dsa
         for (int i = 0; ok && next_seg(i); ++i) {
             const int tiles = sg.tiles();
             if (tiles == 0) continue;
-            LatentWhere at0, at1;
-            where(0, other, at0);
+            PairWhere at0, at1;
+            at0 = where(0, other);
             for (int t = 0; ok && t < tiles; ++t) {
-                if (t + 1 < tiles) where(t + 1, other, at1);
+                if (t + 1 < tiles) at1 = where(t + 1, other);
                 const int gt = done + t, buf = gt & 1, rows = used_rows(t, other);
                 ok = tree_wait(s_full + buf, (gt >> 1) & 1, abort, l.a.wait_timeouts, lane);
                 if (!ok) break;
