@@ -53,19 +53,20 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
         pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(sms / per, units / (per * per * kLatMinUnits)));
         pl->blocks = (int64_t)pl->groups * per;
         // Few items, or items of few tiles: a cluster has each of them to itself and merges on chip, without partial results in HBM
-        // or a second launch.  In us, with `tiles` the bound of an item's tiles: a launch and 1.5 a tile of a block, and the
-        // merge's rounds; against shares, which are of one size whatever the lengths, but start later, write parts and need the
-        // merge kernel.  Measured, shares / best cluster (lengths spread up to the bound): 16 heads, 9 requests, 17 tiles: 23.1 /
-        // 14.1 (8 blocks), 65 tiles: 33.1 / 21.5; 18 requests, 33 tiles: 28.5 / 22.5 (4), 65: 34.0 / 36.5; 64 requests, 10 tiles:
-        // 23.9 / 20.3 (2), 65: 48.0 / 64.5; 128 heads, 4 requests, 65 tiles: 35.1 / 23.9 (8); 18 requests, 10 tiles: 23.6 / 25.6 (2).
+        // or a second launch.  In us, with `t` the bound of an item's tiles: a launch, 1.4 to 1.5 a tile of a block, and the merge's
+        // reads; against shares, which are of one size whatever the lengths, but start later, write parts (the more of an item,
+        // the longer its merge) and need the merge kernel.  Measured, shares / best cluster (lengths spread up to the bound): 16
+        // heads, 9 requests, 17 tiles: 17.2 / 12.4 (8 blocks), 65 tiles: 24.8 / 20.1 (8); 18 requests, 33 tiles: 20.6 / 20.3 (4), 65:
+        // 26.6 / 34.3; 64 requests, 2 tiles: 12.6 / 9.0 (1), 5: 15.8 / 13.2 (2), 17: 21.9 / 23.9, 65: 42.2 / 60.3; 128 heads, one
+        // request, 33 tiles: 14.7 / 17.1 (8), 9 requests, 17 tiles: 20.6 / 18.5 (4); 37 requests, 10 tiles: 25.6 / 22.8 (1).
         const float t = (float)tiles, all = (float)(items * tiles) / (float)sms;
-        float best = pl->pairs ? 13.f + std::min(5.f, t / 2.5f) + 0.7f * all + 8.f * std::min(1.f, all / 4.f)
-                               : 14.f + std::min(4.f, t / 4.f) + 1.1f * all + 6.f * std::min(1.f, all / 2.f);
-        const int rounds = std::min(pl->rows, kLatRows) * l->latent_dim / 128;               // of the merge, by eight warps a block
+        float best = pl->pairs ? 13.f + 10.f * all / (all + 1.f) + 0.7f * all
+                               : 10.5f + std::min(3.f, t / 2.f) + 1.03f * all + 0.35f * std::min(t / 2.f, (float)sms / (float)items);
+        const float merge = 0.018f * (float)(std::min(pl->rows, kLatRows) * l->latent_dim / 128);
         // (clusters that are on the device at once: an SM holds one block, and a cluster's SMs lie close together)
         const int64_t most[4] = {sms, sms * 7 / 15, sms * 7 / 33, sms / 10};
         for (int i = 0, c = 1; i < 4; ++i, c *= 2) {
-            const float cost = 11.f + 1.5f * (float)((tiles + c - 1) / c) + (c > 1 ? 0.35f * (float)((rounds + 8 * c - 1) / (8 * c)) : 0.f);
+            const float cost = (c > 1 ? 8.f + merge : 6.5f) + (c > 2 ? 1.35f : 1.5f) * (float)((tiles + c - 1) / c);
             if (items <= most[i] && cost < best) { best = cost; pl->cluster = c; }
         }
         if (pl->cluster) {

@@ -15,10 +15,13 @@
 // in parts of three 128-byte columns, the scores of each part begin as it lands, and its halves are freed one by one as the products
 // with V have read them.  W takes the place of the slot's r column, which only the scores read.  Scores and products with V are
 // issued by a warp each, because every look at a barrier costs an issuing warp some 250 cycles behind queued products.
+// Rows are copied by 128 threads, 16 bytes at a time: tensor-map copies, with boxes within a page, take 70 to 90 cycles each at
+// the least and arrive later (64 x 16 heads, threads / tensor maps: pages of 64: 64.7 / 68 us, 16: 65 / 81, 24: 65 / 118, 1: 69 / 212,
+// one request of 600 tokens 11.3 / 13.1).
 //
-// Measured: 64 requests x 16 heads, lengths up to 8190 (304 MB of rows, 47 us at the measured copy rate): 68.0 us, 4.5 TB/s.  Some
-// 4 us go by before the first tile has landed (lengths, then pages, then rows), 5 in the merge of the parts and its launch, the
-// rest in begun and ended items.  One request of about 600 tokens: 13.1 us, four dependent reads and one launch.
+// Measured: 64 requests x 16 heads, lengths up to 8190 (304 MB of rows, 47 us at the measured copy rate): 64.7 us, 4.7 TB/s.  Some
+// 4 us go by before the first tile has landed (lengths, then pages, then rows), 3 to 5 in the merge of the parts and its launch, the
+// rest in begun and ended items.  One request of about 600 tokens: 11 us, four dependent reads and one launch.
 #pragma once
 #include "dsa_latent_args.cuh"
 #include "dsa_tc.cuh"

@@ -9,9 +9,10 @@
 // 3 / 2 of its keys' bytes that way, against 2 / 1 with a block for each half of the rows.
 //
 // Measured: 32 requests x 128 heads, lengths 1024 to 8190 (179 MB of rows, 28 us at the measured copy rate; 41 GFLOP, 24 at
-// the matrix rate): 61 us; with blocks of 64
-// rows 90.  16 x 128 heads with up to four tokens: 50 us, from 71.  A tile takes as long as its chain of landing, scores,
-// softmax, the other keys' values, products: two tiles in flight are all that fits beside q, and do not cover all of it.
+// the matrix rate): 61 us, with blocks of 64 rows 77.  16 x 128 heads with up to four tokens: 50 us, and 57.  Copies by threads, as the
+// blocks of 64 rows have them, take 74 here: their arrivals have to be passed on to the other block.  A tile takes as long as
+// its chain of landing, scores, softmax, the other keys' values, products: two tiles in flight are all that fits beside q,
+// and do not cover all of it.
 #pragma once
 #include "dsa_latent.cuh"
 
