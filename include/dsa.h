@@ -662,7 +662,8 @@ DSA_API int32_t dsa_latent_workspace_size(const dsa_latent *latent, int32_t num_
  *   Token i's row goes to position S + i; seq_len is not modified.  Tokens without room (S + i >= max_seq_len)
  *   are dropped like those at and behind new_count[b]: nothing is appended, out = 0, lse = -inf; their q and
  *   c_new rows may hold anything.  A negative seq_len drops all.  A token whose page is missing is computed, but
- *   its row is stored nowhere.  Cached rows behind S may hold anything (NaN included).
+ *   its row is stored nowhere.  Cached rows behind S may hold anything (NaN included); a NaN or infinity in a row
+ *   that some of the request's new tokens see may reach the other ones.  num_heads: at most 1024.
  *   workspace: 256-byte aligned, dsa_latent_workspace_size() bytes.
  */
 DSA_API int32_t dsa_latent_step(const dsa_latent *latent, int32_t num_heads, int32_t max_new, const void *q,
@@ -702,10 +703,11 @@ typedef struct dsa_prompt {
 /*
  * Attention of the tokens of a ragged batch, per head h:
  *   x_ij = sm_scale * q_i . [k_nope_j | k_rope_j],  lse_i = ln sum_j e^{x_ij},  out_i = sum_j e^{x_ij - lse_i} v_j
- * over the keys that query i sees.  out [q_tokens, H, value_dim] (16-byte aligned), lse [q_tokens, H] float32: contiguous.  A query that sees
- * no key (Lk < Lq) gets out = 0, lse = -inf.  Rows that belong to no request are left as they were.  Starts are
- * clamped into [0, q_tokens] / [0, kv_tokens].  Keys and values that no query of the request sees may hold anything;
- * a NaN or infinity in the v row of a key that some query sees may reach the other queries of the request.  No workspace.
+ * over the keys that query i sees.  out [q_tokens, H, value_dim] (16-byte aligned), lse [q_tokens, H] float32: contiguous.
+ * A query that sees no key (Lk < Lq) gets out = 0, lse = -inf.  Rows that belong to no request are left as they were.  Starts
+ * are clamped into [0, q_tokens] / [0, kv_tokens].  Keys and values that no query of the request sees may hold anything; a NaN
+ * or infinity in the v row of a key that some query sees may reach the other queries of the request.  num_heads: at most 1024,
+ * batch 2^20.  No workspace.
  */
 DSA_API int32_t dsa_latent_prompt(const dsa_prompt *prompt, void *out, float *lse, void *stream);
 

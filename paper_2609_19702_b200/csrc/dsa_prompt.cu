@@ -101,6 +101,9 @@ int32_t dsa_latent_prompt(const dsa_prompt* p, void* out, float* lse, void* stre
     const int rows = bf16 ? kPrBlock : kTileRows;
     const int64_t blocks = ((int64_t)g.max_q_len + rows - 1) / rows * p->num_heads * p->batch;
     if (blocks > 0x7fffffffLL) return DSA_ERR_UNSUPPORTED;
+    // Several requests and more blocks than places: sorted, so that none of the long ones is begun last (24 prompts of up to 600
+    // tokens behind prefixes of up to 512, 16 heads: 66 -> 63.7 us).  One request's are in order already, and very many even out.
+    g.sorted = p->batch > 1 && blocks > host_sm_count() && blocks / p->num_heads <= kPrSorted;
     PromptMaps m = {};
     cudaError_t e;
     if (bf16) {

@@ -11,13 +11,13 @@
 // most that leaves room for.  Weights go back through tensor memory (A of the second product), not through shared memory, whose bytes
 // the products need: K and V of a tile are read by either half, q with every tile.  Tiles of 96 keys whose weights
 // take the scores' columns: 84 us for the prompt below instead of 81, and 75 instead of 68 for the batch.
-// Blocks are persistent and take over those not launched yet, the ones with most keys first, so that an item's first
+// Blocks are persistent and take over those not launched yet, the dearest first, so that an item's first
 // copies run under the last one's products and a ragged batch leaves no SM behind; the rows that do not fill a block are the
 // request's first ones, which see the fewest keys.
 //
 // Measured: one prompt of 4160 tokens, 16 heads: 80 us, 1.1 PFLOP/s or 65 % of the measured matrix rate (which is for bursts: in a row of such
 // calls the power limit holds the clock at 1650 MHz, 92 us).  24 prompts of up to 600 tokens behind prefixes of up to 512, 16 heads:
-// 66 us, where keys and values alone (185 MB) would take 29: halves that are not full, and beginnings and ends of short items.
+// 64 us, where keys and values alone (185 MB) would take 29: halves that are not full, and beginnings and ends of short items.
 #pragma once
 #include "dsa_prompt_args.cuh"
 #include "dsa_tc.cuh"
@@ -28,6 +28,8 @@ constexpr int kPrTile = 80;                        // keys per tile: scores, wei
 constexpr int kPrRows = 128;                       // query rows per half of a block: the M of the products
 constexpr int kPrBlock = 2 * kPrRows;
 constexpr int kPrThreads = 352;
+constexpr int kPrSorted = 256;                     // entries of a batch that are sorted, at most
+static_assert(kPrSorted <= kPrThreads && kPrSorted <= 256, "one entry a thread, one byte a number");
 
 struct PromptMaps {
     CUtensorMap q, k, kr, v;
@@ -87,7 +89,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     uint4* s_response = reinterpret_cast<uint4*>(q_full + 22);
     PromptItem* s_info = reinterpret_cast<PromptItem*>(q_full + 24);           // [2]
     int* s_misc = reinterpret_cast<int*>(s_info + 2);         // [0] TMEM address, [1] abort
-    static_assert((2 * SLOTS + 24) * 8 + 2 * sizeof(PromptItem) + 8 <= C::TAIL, "tail of the shared memory");
+    unsigned char* s_order = reinterpret_cast<unsigned char*>(s_misc + 2);     // [kPrSorted] where that is wanted: the numbers of items, dearest first
+    static_assert((2 * SLOTS + 24) * 8 + 2 * sizeof(PromptItem) + 8 + kPrSorted <= C::TAIL, "tail of the shared memory");
     static_assert((2 * SLOTS + 22) % 2 == 0, "the response lies on 16 bytes");
     volatile int* abort = s_misc + 1;
 
@@ -114,6 +117,50 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
 
+    // Rows of 256 queries are numbered from the requests' ends, e = number * batch + request: those with most keys tend to come first.
+    // false: the request has none of this number.
+    auto describe = [&](int e, PromptItem& it) -> bool {
+        const int b = e % g.batch, from_end = e / g.batch;
+        int q0, nq, nk;
+        prompt_range(g, b, q0, nq, it.k0, nk);
+        // the request's last rows are in blocks of kPrBlock from the end; the first rows, with the fewest keys, are what is left
+        const int tile = (nq + kPrBlock - 1) / kPrBlock - 1 - from_end;
+        if (tile < 0) return false;
+        const int first = tile == 0 ? 0 : nq - (from_end + 1) * kPrBlock, n_rows = tile == 0 ? nq - from_end * kPrBlock : kPrBlock;
+        // (the starts of the whole request decide which keys a query sees, whatever max_q_len leaves out)
+        const int all_q = max(0, min(g.q_start[b + 1], g.q_tokens) - q0);
+        it.row0 = q0 + first;
+        it.nk = nk;
+        it.shift = g.causal ? nk - (all_q - first - 1) : nk;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            it.rows[s] = max(0, min(kPrRows, n_rows - s * kPrRows));
+            const int last = g.causal ? s * kPrRows + it.rows[s] - 1 : 0;
+            it.len[s] = it.rows[s] > 0 ? max(0, min(nk, last + it.shift)) : 0;
+            it.tiles[s] = (it.len[s] + kPrTile - 1) / kPrTile;
+        }
+        it.n_tiles = max(it.tiles[0], it.tiles[1]);
+        return true;
+    };
+    if (g.sorted) {
+        // By what they cost, the dearest first: a tile of both halves some 2500 cycles, of one 1400, the ends of an item 3000.
+        // (one entry a thread; a batch has at most as many as there are bytes in s_order)
+        int* s_cost = reinterpret_cast<int*>(smem);
+        const int n = (g.max_q_len + kPrBlock - 1) / kPrBlock * g.batch;
+        PromptItem it = {};
+        if (tid < n) s_cost[tid] = describe(tid, it) ? 6 + 3 * it.n_tiles + 2 * min(it.tiles[0], it.tiles[1]) : 0;
+        __syncthreads();
+        if (tid < n) {
+            const int mine = s_cost[tid];
+            int place = 0;
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) place += s_cost[k] > mine || (s_cost[k] == mine && k < tid);
+            s_order[place] = (unsigned char)tid;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // (copies take s_cost's place)
+        __syncthreads();
+    }
+
     // item number `i` of this block, once the copying warp has found it; nullptr: give up
     auto item = [&](int i) -> const PromptItem* {
         return tree_wait(info_full + (i & 1), (i >> 1) & 1, abort, g.wait_timeouts, lane) ? s_info + (i & 1) : nullptr;
@@ -126,7 +173,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     if (warp == 8) {
         // ---- what to work on; copies of q, K(0), V(0), K(1), V(1), ... ----------------------------------------
         // Blocks are persistent: a running one takes over the next that has not been launched yet, and begins its copies while
-        // the products of the last one run.  Those with the most keys come first.
+        // the products of the last one run.
         PromptItem it = {};
         int issued = 0, k_issued = 0, live[2] = {0, 0}, idx = (int)blockIdx.x, asked = 0, answered = 0;
         bool ok = true;
@@ -141,30 +188,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         for (int i = 0; ok; ++i) {
             it.h = -1;
             while (ok && idx >= 0) {                          // (blocks without a query are passed over)
-                int x = idx, q0, nq, nk;
-                const int h = x % g.H; x /= g.H;
-                const int b = x % g.batch, from_end = x / g.batch;
-                prompt_range(g, b, q0, nq, it.k0, nk);
-                // the request's last rows are in blocks of kPrBlock from the end; the first rows, with the fewest keys, are what is left
-                const int tile = (nq + kPrBlock - 1) / kPrBlock - 1 - from_end;
-                if (tile >= 0) {
-                    const int first = tile == 0 ? 0 : nq - (from_end + 1) * kPrBlock, n_rows = tile == 0 ? nq - from_end * kPrBlock : kPrBlock;
-                    // (the starts of the whole request decide which keys a query sees, whatever max_q_len leaves out)
-                    const int all_q = max(0, min(g.q_start[b + 1], g.q_tokens) - q0);
-                    it.h = h;
-                    it.row0 = q0 + first;
-                    it.nk = nk;
-                    it.shift = g.causal ? nk - (all_q - first - 1) : nk;
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        it.rows[s] = max(0, min(kPrRows, n_rows - s * kPrRows));
-                        const int last = g.causal ? s * kPrRows + it.rows[s] - 1 : 0;
-                        it.len[s] = it.rows[s] > 0 ? max(0, min(nk, last + it.shift)) : 0;
-                        it.tiles[s] = (it.len[s] + kPrTile - 1) / kPrTile;
-                    }
-                    it.n_tiles = max(it.tiles[0], it.tiles[1]);
-                    break;
-                }
+                const int e = idx / g.H;
+                if (describe(g.sorted ? s_order[e] : e, it)) { it.h = idx % g.H; break; }
                 ask();
                 ok = answer();
             }

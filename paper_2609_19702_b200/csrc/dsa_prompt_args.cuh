@@ -15,6 +15,7 @@ struct PromptArgs {
     int batch, H, P;
     int q_tokens, kv_tokens, max_q_len;
     int causal;
+    int sorted;                                    // bf16: blocks take the items in order of what they cost
     float scale_log2;
     void* out;                                     // [q_tokens, H, value_dim]
     float* lse;                                    // [q_tokens, H]
