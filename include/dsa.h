@@ -663,7 +663,8 @@ DSA_API int32_t dsa_latent_workspace_size(const dsa_latent *latent, int32_t num_
  *   are dropped like those at and behind new_count[b]: nothing is appended, out = 0, lse = -inf; their q and
  *   c_new rows may hold anything.  A negative seq_len drops all.  A token whose page is missing is computed, but
  *   its row is stored nowhere.  Cached rows behind S may hold anything (NaN included); a NaN or infinity in a row
- *   that some of the request's new tokens see may reach the other ones.  num_heads: at most 1024.
+ *   that some of the request's new tokens see may reach the other ones.  num_heads: at most 1024.  bf16: bounds that
+ *   allow a block more than 2^24 tokens of one sequence are unsupported (a wait in the kernel could pass its limit).
  *   workspace: 256-byte aligned, dsa_latent_workspace_size() bytes.
  */
 DSA_API int32_t dsa_latent_step(const dsa_latent *latent, int32_t num_heads, int32_t max_new, const void *q,
@@ -707,7 +708,7 @@ typedef struct dsa_prompt {
  * A query that sees no key (Lk < Lq) gets out = 0, lse = -inf.  Rows that belong to no request are left as they were.  Starts
  * are clamped into [0, q_tokens] / [0, kv_tokens].  Keys and values that no query of the request sees may hold anything; a NaN
  * or infinity in the v row of a key that some query sees may reach the other queries of the request.  num_heads: at most 1024,
- * batch 2^20.  No workspace.
+ * batch 2^20, kv_tokens 2^25 (bf16; a wait in the kernel could pass its limit).  No workspace.
  */
 DSA_API int32_t dsa_latent_prompt(const dsa_prompt *prompt, void *out, float *lse, void *stream);
 

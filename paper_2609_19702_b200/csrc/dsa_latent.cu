@@ -52,6 +52,8 @@ int32_t make_latent_plan(const dsa_latent* l, int32_t heads, int32_t max_new, La
         const int per = pl->pairs ? 2 : 1;
         pl->groups = (int)std::max<int64_t>(1, std::min<int64_t>(sms / per, units / (per * per * kLatMinUnits)));
         pl->blocks = (int64_t)pl->groups * per;
+        // (waits of up to one item's share: 2^18 tiles take half of the second that a wait may)
+        if (std::min(tiles, units / pl->groups) > (1 << 18)) return DSA_ERR_UNSUPPORTED;
         // Few items, or items of few tiles: a cluster has each of them to itself and merges on chip, without partial results in HBM
         // or a second launch.  In us, with `t` the bound of an item's tiles: a launch, 1.4 to 1.5 a tile of a block, and the merge's
         // reads; against shares, which are of one size whatever the lengths, but start later, write parts (the more of an item,

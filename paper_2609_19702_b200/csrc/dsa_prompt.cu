@@ -26,6 +26,8 @@ int32_t check_prompt(const dsa_prompt* p) {
     if ((p->q_tokens > 1 && p->q_stride_token < p->nope_dim + p->rope_dim) ||
         (p->kv_tokens > 1 && (p->k_stride_token < p->nope_dim || p->rope_stride_token < p->rope_dim || p->v_stride_token < p->value_dim)))
         return DSA_ERR_INVALID_ARG;
+    // (a half without queries waits while the other half goes through a request's keys: 2^25 take half of the second that a wait may)
+    if (p->dtype == DSA_BF16 && p->kv_tokens > (1 << 25)) return DSA_ERR_UNSUPPORTED;
     if (p->batch == 0 || p->q_tokens == 0 || p->max_q_len == 0) return DSA_OK;
     if (!p->q || !p->q_start || !aligned16(p->q)) return DSA_ERR_INVALID_ARG;
     if (p->kv_tokens > 0 && (!p->k_nope || !p->k_rope || !p->v)) return DSA_ERR_INVALID_ARG;

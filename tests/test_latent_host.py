@@ -51,9 +51,11 @@ def test_step_refusals(dsa):
     assert _size(dsa, None)[0] == INVALID
     for kw, rc in BAD_LATENTS + [(dict(sm_scale=0.0), INVALID), (dict(sm_scale=-1.0), INVALID), (dict(sm_scale=math.inf), INVALID),
                                  (dict(sm_scale=math.nan), INVALID), (dict(seq_len=None), INVALID),
-                                 (dict(block_table=None, max_seq_len=2 ** 31 - 1), UNSUPPORTED)]:
+                                 (dict(block_table=None, max_seq_len=2 ** 31 - 1), UNSUPPORTED),
+                                 (dict(block_table=None, max_seq_len=2 ** 24 + 2 ** 20, batch=1024), UNSUPPORTED)]:     # (a whole request for a block)
         assert _size(dsa, _latent(dsa, **kw))[0] == rc, kw
         assert _step(dsa, _latent(dsa, **kw)) == rc, kw
+    assert _size(dsa, _latent(dsa, block_table=None, max_seq_len=2 ** 24 + 2 ** 20))[0] == 0           # (64 requests: cut into smaller pieces)
     x = _latent(dsa)
     for heads, new, rc in [(0, 1, INVALID), (1, 0, INVALID), (1025, 1, UNSUPPORTED), (1, 65, UNSUPPORTED), (1024, 64, 0)]:
         assert _size(dsa, x, heads, new)[0] == rc
@@ -87,7 +89,7 @@ def test_prompt_refusals(dsa):
                    (dict(v=None), INVALID), (dict(q_start=None), INVALID), (dict(q=FAKE + 8), INVALID), (dict(k_nope=FAKE + 2), INVALID),
                    (dict(k_rope=FAKE + 8), INVALID), (dict(v=FAKE + 4), INVALID), (dict(q_stride_token=100), INVALID), (dict(q_stride_token=184), INVALID),
                    (dict(k_stride_head=-8), INVALID), (dict(v_stride_head=4), INVALID), (dict(rope_stride_token=56), INVALID),
-                   (dict(v_stride_token=0), INVALID)]:
+                   (dict(v_stride_token=0), INVALID), (dict(kv_tokens=2 ** 25 + 1), UNSUPPORTED)]:
         assert call(_prompt(dsa, **kw)) == rc, kw
     x = _prompt(dsa)
     assert call(x, out=None) == INVALID and call(x, lse=None) == INVALID and call(x, out=FAKE + 8) == INVALID
