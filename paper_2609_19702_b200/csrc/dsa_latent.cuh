@@ -323,10 +323,6 @@ struct LatentRows {
                          ::"r"(to[k] + slot * C::SLOT + c * C::CHUNK), "l"(some ? from[k] + c * 64 : from[k]), "r"(some ? 16 : 0) : "memory");
         }
     }
-    // One arrival by this thread when its copies so far have landed.
-    __device__ __forceinline__ void arrive(unsigned long long* bar) const {
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-    }
 };
 
 template <int R>
@@ -566,7 +562,7 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
                         ok = ok && tree_wait(empty + slot * C::GROUPS + c / 4, (round - 1) & 1, abort, l.a.wait_timeouts, lane);
                     if (!ok) break;
                     rows.copy(slot, c);
-                    if (c % 3 == 2 || c == C::CH - 1) rows.arrive(full + slot * C::LAND + c / 3);
+                    if (c % 3 == 2 || c == C::CH - 1) cp_async_arrive_on(full + slot * C::LAND + c / 3);
                 }
                 if (++slot == C::SLOTS) { slot = 0; ++round; }
             }
