@@ -775,10 +775,12 @@ class PagePool:
 
 
 def _table(block_table: torch.Tensor, rows: Optional[int] = None) -> tuple:
-    if block_table.dim() != 2:
+    shape = block_table.shape
+    if len(shape) != 2:
         raise ValueError("block_table must be [rows, max_blocks]")
-    _int32(block_table, (block_table.shape[0] if rows is None else rows, block_table.shape[1]), "block_table")
-    return block_table.shape
+    if block_table.dtype != torch.int32 or (rows is not None and shape[0] != rows) or not block_table.is_contiguous():
+        raise ValueError("block_table must be a contiguous int32 tensor of shape %s" % ((shape[0] if rows is None else rows, shape[1]),))
+    return shape
 
 
 def dsa_reserve_pages(pool: PagePool, block_table: torch.Tensor, seq_len: torch.Tensor, extra_tokens: int,
