@@ -101,11 +101,19 @@ int32_t dsa_latent_prompt(const dsa_prompt* p, void* out, float* lse, void* stre
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool bf16 = p->dtype == DSA_BF16;
     const int rows = bf16 ? kPrBlock : kTileRows;
-    const int64_t blocks = ((int64_t)g.max_q_len + rows - 1) / rows * p->num_heads * p->batch;
+    // Blocks of a head: max_q_len's for every request, or, in a list, what the tokens fill and one a request more.  bf16 lists what a
+    // thread a request and an entry can name, and sorts it, so that none of the long items is begun last (24 prompts of up to 600
+    // tokens behind prefixes of up to 512, 16 heads: 66 -> 63.7 us; 64 of up to 300 with a bound of all tokens: 198 -> 56);
+    // very many even out.  float32 lists where that saves half of the blocks, since each of them has to look for its place (200 of
+    // up to 20 with a bound of all tokens: 383 -> 85, with a tight one 79, and 84 listed).
+    const int64_t grid = ((int64_t)g.max_q_len + rows - 1) / rows * p->batch, filled = (int64_t)p->q_tokens / rows + p->batch;
+    int64_t entries = std::min(grid, filled);
+    if (p->batch == 1 || p->batch > kPrListed) entries = grid;
+    else if (bf16 ? entries <= kPrListed && (entries * p->num_heads > host_sm_count() || entries < grid) : 2 * entries <= grid)
+        g.entries = (int)entries;
+    else entries = grid;
+    const int64_t blocks = entries * p->num_heads;
     if (blocks > 0x7fffffffLL) return DSA_ERR_UNSUPPORTED;
-    // Several requests and more blocks than places: sorted, so that none of the long ones is begun last (24 prompts of up to 600
-    // tokens behind prefixes of up to 512, 16 heads: 66 -> 63.7 us).  One request's are in order already, and very many even out.
-    g.sorted = p->batch > 1 && blocks > host_sm_count() && blocks / p->num_heads <= kPrSorted;
     PromptMaps m = {};
     cudaError_t e;
     if (bf16) {

@@ -28,8 +28,7 @@ constexpr int kPrTile = 80;                        // keys per tile: scores, wei
 constexpr int kPrRows = 128;                       // query rows per half of a block: the M of the products
 constexpr int kPrBlock = 2 * kPrRows;
 constexpr int kPrThreads = 352;
-constexpr int kPrSorted = 256;                     // entries of a batch that are sorted, at most
-static_assert(kPrSorted <= kPrThreads && kPrSorted <= 256, "one entry a thread, one byte a number");
+static_assert(kPrListed <= kPrThreads && kPrListed <= 256, "a request and an entry a thread, a byte for either in a name");
 
 struct PromptMaps {
     CUtensorMap q, k, kr, v;
@@ -89,8 +88,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     uint4* s_response = reinterpret_cast<uint4*>(q_full + 22);
     PromptItem* s_info = reinterpret_cast<PromptItem*>(q_full + 24);           // [2]
     int* s_misc = reinterpret_cast<int*>(s_info + 2);         // [0] TMEM address, [1] abort
-    unsigned char* s_order = reinterpret_cast<unsigned char*>(s_misc + 2);     // [kPrSorted] where that is wanted: the numbers of items, dearest first
-    static_assert((2 * SLOTS + 24) * 8 + 2 * sizeof(PromptItem) + 8 + kPrSorted <= C::TAIL, "tail of the shared memory");
+    unsigned short* s_list = reinterpret_cast<unsigned short*>(s_misc + 2);    // [kPrListed] request | number << 8; 0xffff: nothing
+    static_assert((2 * SLOTS + 24) * 8 + 2 * sizeof(PromptItem) + 8 + 2 * kPrListed <= C::TAIL, "tail of the shared memory");
     static_assert((2 * SLOTS + 22) % 2 == 0, "the response lies on 16 bytes");
     volatile int* abort = s_misc + 1;
 
@@ -117,10 +116,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
 
-    // Rows of 256 queries are numbered from the requests' ends, e = number * batch + request: those with most keys tend to come first.
-    // false: the request has none of this number.
-    auto describe = [&](int e, PromptItem& it) -> bool {
-        const int b = e % g.batch, from_end = e / g.batch;
+    // Rows of 256 queries are numbered from the requests' ends.  false: the request has none of this number.
+    auto describe = [&](int b, int from_end, PromptItem& it) -> bool {
         int q0, nq, nk;
         prompt_range(g, b, q0, nq, it.k0, nk);
         // the request's last rows are in blocks of kPrBlock from the end; the first rows, with the fewest keys, are what is left
@@ -142,20 +139,34 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         it.n_tiles = max(it.tiles[0], it.tiles[1]);
         return true;
     };
-    if (g.sorted) {
-        // By what they cost, the dearest first: a tile of both halves some 2500 cycles, of one 1400, the ends of an item 3000.
-        // (one entry a thread; a batch has at most as many as there are bytes in s_order)
+    if (g.entries > 0) {
+        // A list of the items of one head, without gaps and by what they cost, the dearest first: a tile of both halves takes some 2500
+        // cycles, of one 1400, the ends of an item 3000.  (a request a thread, then an entry a thread)
         int* s_cost = reinterpret_cast<int*>(smem);
-        const int n = (g.max_q_len + kPrBlock - 1) / kPrBlock * g.batch;
+        int* s_name = s_cost + kPrListed;
+        int* s_warp = s_name + kPrListed;
+        int q0, nq, k0, nk, rows = 0;
+        if (tid < kPrListed) {
+            s_cost[tid] = -1;
+            if (tid < g.batch) {
+                prompt_range(g, tid, q0, nq, k0, nk);
+                rows = (nq + kPrBlock - 1) / kPrBlock;
+            }
+        }
+        const int first = prompt_before(rows, s_warp);
         PromptItem it = {};
-        if (tid < n) s_cost[tid] = describe(tid, it) ? 6 + 3 * it.n_tiles + 2 * min(it.tiles[0], it.tiles[1]) : 0;
+        for (int k = 0; k < rows && first + k < g.entries; ++k) {
+            describe(tid, k, it);
+            s_cost[first + k] = 6 + 3 * it.n_tiles + 2 * min(it.tiles[0], it.tiles[1]);
+            s_name[first + k] = tid | k << 8;
+        }
         __syncthreads();
-        if (tid < n) {
+        if (tid < g.entries) {
             const int mine = s_cost[tid];
             int place = 0;
 #pragma unroll 8
-            for (int k = 0; k < n; ++k) place += s_cost[k] > mine || (s_cost[k] == mine && k < tid);
-            s_order[place] = (unsigned char)tid;
+            for (int k = 0; k < g.entries; ++k) place += s_cost[k] > mine || (s_cost[k] == mine && k < tid);
+            s_list[place] = mine < 0 ? 0xffff : (unsigned short)s_name[tid];
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // (copies take s_cost's place)
         __syncthreads();
@@ -188,8 +199,11 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         for (int i = 0; ok; ++i) {
             it.h = -1;
             while (ok && idx >= 0) {                          // (blocks without a query are passed over)
-                const int e = idx / g.H;
-                if (describe(g.sorted ? s_order[e] : e, it)) { it.h = idx % g.H; break; }
+                const int e = idx / g.H, name = g.entries > 0 ? s_list[e] : 0;
+                if (name != 0xffff && (g.entries > 0 ? describe(name & 255, name >> 8, it) : describe(e % g.batch, e / g.batch, it))) {
+                    it.h = idx % g.H;
+                    break;
+                }
                 ask();
                 ok = answer();
             }

@@ -282,3 +282,13 @@ def test_steps_one_behind_the_other(dsa):
             o, l, tol, ltol = latent_ref.step_expected(qs[i, r].double(), rows.double(), news[i, r].double(), 1, 512, c.scale, True)
             latent_ref.assert_near(outs[i][0][r], o, tol, "step %d of request %d" % (i, r))
             latent_ref.assert_near(outs[i][1][r], l, ltol, "lse of step %d of request %d" % (i, r))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,bound", [([3] * 200, 600), ([0, 700, 0, 1, 257, 256, 0], 1214), ([5] * 256, 1280), ([5] * 257, 1285), ([0] * 40, 1),
+                                        ([0] * 255 + [300], 300), ([90, 400] * 10, 250), ([1], 1), ([1, 1], 2), ([2000, 10, 3, 900], 2913)])
+def test_prompt_bounds_that_are_loose(dsa, dtype, lens, bound):
+    """Upper bounds of the queries far above what most requests have (all tokens, say), and below what some have."""
+    run_case(dsa, dtype, 2, 64, 32, lens, max_q=bound, seed=len(lens))
+    if sum(lens) < 1500:
+        run_case(dsa, dtype, 1, 128, 64, lens, [2 * n + 1 for n in lens], max_q=bound, seed=len(lens), causal=len(lens) % 2 == 0)
