@@ -397,6 +397,11 @@ __global__ void __launch_bounds__(kLatThreads, 1) dsa_latent_kernel(const Latent
         const int rank = share % g.cluster, item = share / g.cluster;
         item_b = item / l.row_tiles;
         item_rt = item % l.row_tiles;
+        // (the request's pages are fetched into L2 while its lengths are read: from cold caches 17.6 -> 17.1 us, one request of 600 tokens)
+        if (l.a.block_table && warp >= 8) {
+            const int at = (tid - 256) * 32;
+            if (at < l.a.max_blocks) asm volatile("prefetch.global.L2 [%0];" ::"l"(l.a.block_table + (int64_t)item_b * l.a.max_blocks + at) : "memory");
+        }
         const LatentItems<kLatTile, kLatRows> x(l, item_b);
         const int per = (x.units + g.cluster - 1) / g.cluster, left = item_rt < x.items ? max(0, min(per, x.units - rank * per)) : 0;
         merged = item_rt < x.items && x.units > per;
