@@ -3,8 +3,10 @@
 // Per tile: scores, a running maximum and sum per row, O rescaled and added to.  The scores' dims are dealt out to four groups
 // of 64 threads, each thread with 4 x 4 scores, so that 8 reads of 16 bytes from shared memory feed 64 multiply-adds; the
 // groups' sums meet in shared memory, where eight threads a row take the softmax.  For O every thread has some rows x some
-// dims.  What bounds it: the multiply-adds of 128 lanes an SM and clock, at about half their rate, and the three barriers of a
-// tile.  Rows lie W + 4 floats apart, an odd number of 16-byte pieces, so that eight of them are read without a conflict.
+// dims, two at a time.  What bounds it: the multiply-adds of 128 lanes an SM and clock, at 48 % of their rate where there are
+// many blocks (one prompt of 1280 tokens, 32 heads of 128 + 64: 490 us); where there are few, reads, sums and three barriers
+// one behind the other, 2.2 us a tile of 64-wide heads and 3.5 of 128-wide ones.
+// Rows lie W + 4 floats apart, an odd number of 16-byte pieces, so that eight of them are read without a conflict.
 #pragma once
 #include "dsa_tc.cuh"
 
@@ -21,7 +23,7 @@ struct TileF32 {
     static constexpr int LS = 36;                                          // row of the scores and weights, in floats
     static constexpr int SCRATCH = 4 * kTileRows * LS + kTileKeys * LS + 2 * kTileRows;   // floats of shared memory beside q and the keys
 
-    float4 o[RPT][F4];
+    ulonglong2 o[RPT][F4];                                                 // pairs of floats
     float m, l;                                                            // of row tid / 8 (the same in its eight threads)
 
     __device__ __forceinline__ void clear() {
@@ -30,7 +32,7 @@ struct TileF32 {
 #pragma unroll
         for (int r = 0; r < RPT; ++r)
 #pragma unroll
-            for (int f = 0; f < F4; ++f) o[r][f] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int f = 0; f < F4; ++f) o[r][f] = make_ulonglong2(0ull, 0ull);
     }
 
     // One tile, by the whole block: q and k [32][ld] with `width` floats a row, v [32][ld_v]; row r sees the keys below seen(r).
@@ -105,30 +107,28 @@ struct TileF32 {
 #pragma unroll
             for (int r = 0; r < RPT; ++r) {
                 const float alpha = s_alpha[r0 + r];
+                const unsigned long long two = pack_f32x2(alpha, alpha);
 #pragma unroll
-                for (int f = 0; f < F4; ++f) { o[r][f].x *= alpha; o[r][f].y *= alpha; o[r][f].z *= alpha; o[r][f].w *= alpha; }
+                for (int f = 0; f < F4; ++f) { o[r][f].x = fma_f32x2(o[r][f].x, two, 0ull); o[r][f].y = fma_f32x2(o[r][f].y, two, 0ull); }
             }
 #pragma unroll 4
             for (int j = 0; j < kTileKeys; ++j) {
-                float p[RPT];
+                unsigned long long p[RPT];                     // (a weight twice)
                 if constexpr (RPT >= 4) {
 #pragma unroll
                     for (int r = 0; r < RPT; r += 4) {
                         const float4 y = *reinterpret_cast<const float4*>(s_p + j * LS + r0 + r);
-                        p[r] = y.x; p[r + 1] = y.y; p[r + 2] = y.z; p[r + 3] = y.w;
+                        p[r] = pack_f32x2(y.x, y.x); p[r + 1] = pack_f32x2(y.y, y.y); p[r + 2] = pack_f32x2(y.z, y.z); p[r + 3] = pack_f32x2(y.w, y.w);
                     }
                 } else {
                     const float2 y = *reinterpret_cast<const float2*>(s_p + j * LS + r0);
-                    p[0] = y.x; p[1] = y.y;
+                    p[0] = pack_f32x2(y.x, y.x); p[1] = pack_f32x2(y.y, y.y);
                 }
 #pragma unroll
                 for (int f = 0; f < F4; ++f) {
-                    const float4 y = *reinterpret_cast<const float4*>(v + j * ld_v + (dg + f * DG) * 4);
+                    const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(v + j * ld_v + (dg + f * DG) * 4);
 #pragma unroll
-                    for (int r = 0; r < RPT; ++r) {
-                        o[r][f].x = fmaf(p[r], y.x, o[r][f].x); o[r][f].y = fmaf(p[r], y.y, o[r][f].y);
-                        o[r][f].z = fmaf(p[r], y.z, o[r][f].z); o[r][f].w = fmaf(p[r], y.w, o[r][f].w);
-                    }
+                    for (int r = 0; r < RPT; ++r) { o[r][f].x = fma_f32x2(p[r], y.x, o[r][f].x); o[r][f].y = fma_f32x2(p[r], y.y, o[r][f].y); }
                 }
             }
         }
@@ -151,9 +151,11 @@ struct TileF32 {
             const float inv = scratch[r0 + r];
             if (dst)
 #pragma unroll
-                for (int f = 0; f < F4; ++f)
+                for (int f = 0; f < F4; ++f) {
+                    const float2 a = unpack_f32x2(o[r][f].x), b = unpack_f32x2(o[r][f].y);
                     *reinterpret_cast<float4*>(dst + (dg + f * DG) * 4) =
-                        inv == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[r][f].x * inv, o[r][f].y * inv, o[r][f].z * inv, o[r][f].w * inv);
+                        inv == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x * inv, a.y * inv, b.x * inv, b.y * inv);
+                }
         }
     }
 };
