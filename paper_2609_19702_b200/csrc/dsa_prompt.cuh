@@ -188,7 +188,12 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         PromptItem it = {};
         int issued = 0, k_issued = 0, live[2] = {0, 0}, idx = (int)blockIdx.x, asked = 0, answered = 0;
         bool ok = true;
-        auto ask = [&]() { if (lane == 0) steal_block(s_response, stolen); __syncwarp(); ++asked; };
+        auto ask = [&]() {
+            __syncwarp();                                     // (every lane has read the last response, whose place the next one takes)
+            if (lane == 0) steal_block(s_response, stolen);
+            __syncwarp();
+            ++asked;
+        };
         auto answer = [&]() -> bool {
             volatile int no_abort = 0;                        // (the response is waited for whatever else has happened)
             ++answered;

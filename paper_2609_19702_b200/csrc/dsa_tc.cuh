@@ -145,8 +145,9 @@ __device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, un
 }
 
 // ---- dynamic scheduling: a running block takes over blocks that have not been launched yet --------------------
-__device__ __forceinline__ void steal_block(void* response, unsigned long long* bar) {      // one thread
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // (the last response has been read)
+// By one thread, behind a warp barrier that follows every lane's reading of the last response: the next one is written to its place.
+__device__ __forceinline__ void steal_block(void* response, unsigned long long* bar) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // (those reads come before the write, which is asynchronous)
     mbar_expect_tx(bar, 16);
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
                  ::"r"(smem_u32(response)), "r"(smem_u32(bar)) : "memory");
