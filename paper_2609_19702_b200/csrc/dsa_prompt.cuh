@@ -28,6 +28,7 @@ constexpr int kPrTile = 80;                        // keys per tile: scores, wei
 constexpr int kPrRows = 128;                       // query rows per half of a block: the M of the products
 constexpr int kPrBlock = 2 * kPrRows;
 constexpr int kPrThreads = 352;
+constexpr int kPrPassed = 4096;                    // blocks without a query that a running block passes over before it says so
 static_assert(kPrListed <= kPrThreads && kPrListed <= 256, "a request and an entry a thread, a byte for either in a name");
 
 struct PromptMaps {
@@ -203,10 +204,17 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         };
         for (int i = 0; ok; ++i) {
             it.h = -1;
+            int passed = 0;
             while (ok && idx >= 0) {                          // (blocks without a query are passed over)
                 const int e = idx / g.H, name = g.entries > 0 ? s_list[e] : 0;
                 if (name != 0xffff && (g.entries > 0 ? describe(name & 255, name >> 8, it) : describe(e % g.batch, e / g.batch, it))) {
                     it.h = idx % g.H;
+                    break;
+                }
+                // Nobody waits for the end of a long run of them, which a batch of 2^20 requests and 1024 heads could make longer than a wait
+                // may take (some 0.5 us a block): now and then the others get an item without a row.
+                if (++passed == kPrPassed) {
+                    it = PromptItem{};
                     break;
                 }
                 ask();

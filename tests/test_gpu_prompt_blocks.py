@@ -23,3 +23,11 @@ def test_runs_of_requests_without_a_token(dsa):
     for _ in range(10):
         again = run_case(dsa, "bf16", 8, 64, 8, lens)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_a_run_longer_than_a_wait_may_take(dsa):
+    """A million requests of 1024 heads, hardly any with a token: what a block finds behind seconds of nothing is computed too."""
+    lens = [0] * 2 ** 20
+    for b, n in ((0, 1), (2 ** 19 + 3, 2), (2 ** 20 - 1, 3)):
+        lens[b] = n
+    run_case(dsa, "bf16", 1024, 64, 8, lens)
