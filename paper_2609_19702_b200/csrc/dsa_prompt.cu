@@ -52,19 +52,32 @@ bool encode_heads(TensorMapEncodeFn encode, CUtensorMap* map, const void* base, 
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <int D, int BLOCKS>
+cudaError_t configure_bf16() {
+    static std::atomic<bool> done[kMaxDevices] = {};
+    return configure_smem(dsa_prompt_kernel<D, BLOCKS>, PromptCfg<D>::SMEM, done);
+}
+template <int D>
+cudaError_t configure_f32() {
+    static std::atomic<bool> done[kMaxDevices] = {};
+    return configure_smem(dsa_prompt_f32_kernel<D>, PromptF32Cfg<D>::SMEM, done);
+}
 template <int D>
 cudaError_t configure() {
-    static std::atomic<bool> done[kMaxDevices] = {}, done_f32[kMaxDevices] = {};
-    cudaError_t e = configure_smem(dsa_prompt_kernel<D>, PromptCfg<D>::SMEM, done);
-    if (e == cudaSuccess) e = configure_smem(dsa_prompt_f32_kernel<D>, PromptF32Cfg<D>::SMEM, done_f32);
+    cudaError_t e = configure_bf16<D, kPrByBound>();
+    if (e == cudaSuccess) e = configure_bf16<D, kPrByNumber>();
+    if (e == cudaSuccess) e = configure_bf16<D, kPrByList>();
+    if (e == cudaSuccess) e = configure_f32<D>();
     return e;
 }
 template <int D>
 cudaError_t run(const PromptArgs& g, const PromptMaps& m, bool bf16, int64_t blocks, cudaStream_t st) {
     const cudaError_t e = configure<D>();
     if (e != cudaSuccess) return e;
-    return bf16 ? launch_dependent(dsa_prompt_kernel<D>, blocks, kPrThreads, PromptCfg<D>::SMEM, st, g, m)
-                : launch_dependent(dsa_prompt_f32_kernel<D>, blocks, kTileThreads, PromptF32Cfg<D>::SMEM, st, g);
+    if (!bf16) return launch_dependent(dsa_prompt_f32_kernel<D>, blocks, kTileThreads, PromptF32Cfg<D>::SMEM, st, g);
+    if (g.blocks == kPrByList) return launch_dependent(dsa_prompt_kernel<D, kPrByList>, blocks, kPrThreads, PromptCfg<D>::SMEM, st, g, m);
+    if (g.blocks == kPrByNumber) return launch_dependent(dsa_prompt_kernel<D, kPrByNumber>, blocks, kPrThreads, PromptCfg<D>::SMEM, st, g, m);
+    return launch_dependent(dsa_prompt_kernel<D, kPrByBound>, blocks, kPrThreads, PromptCfg<D>::SMEM, st, g, m);
 }
 
 }  // namespace
@@ -101,17 +114,23 @@ int32_t dsa_latent_prompt(const dsa_prompt* p, void* out, float* lse, void* stre
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool bf16 = p->dtype == DSA_BF16;
     const int rows = bf16 ? kPrBlock : kTileRows;
-    // Blocks of a head: max_q_len's for every request, or, in a list, what the tokens fill and one a request more.  bf16 lists what a
-    // thread a request and an entry can name, and sorts it, so that none of the long items is begun last (24 prompts of up to 600
-    // tokens behind prefixes of up to 512, 16 heads: 66 -> 63.7 us; 64 of up to 300 with a bound of all tokens: 198 -> 56);
-    // very many even out.  float32 lists where that saves half of the blocks, since each of them has to look for its place (200 of
-    // up to 20 with a bound of all tokens: 383 -> 85, with a tight one 79, and 84 listed).
+    // Blocks of a head: max_q_len's for every request, or, found by their numbers, what the tokens fill and one a request.  The first
+    // where it is not many more: it takes no search and puts the long items first, but a block without a query costs half a
+    // microsecond.  In us, by bound / by number: bf16, 1000 prompts of up to 300, 4 heads, 1.3 times as many: 169 / 175, 1.9
+    // times: 184 / 175; 40 of up to 3000, 8 heads, 1.7 times: 359 / 320; 300 of up to 130, 128 heads, 66 times: 12249 / 885.
+    // float32, 600 of up to 100, 16 heads, 1.6 times: 730 / 760, 2.7 times: 778 / 760.
     const int64_t grid = ((int64_t)g.max_q_len + rows - 1) / rows * p->batch, filled = (int64_t)p->q_tokens / rows + p->batch;
-    int64_t entries = std::min(grid, filled);
-    if (p->batch == 1 || p->batch > kPrListed) entries = grid;
-    else if (bf16 ? entries <= kPrListed && (entries * p->num_heads > host_sm_count() || entries < grid) : 2 * entries <= grid)
-        g.entries = (int)entries;
-    else entries = grid;
+    g.blocks = (bf16 ? 2 * grid >= 3 * filled : grid >= 2 * filled) || grid * p->num_heads > 0x7fffffffLL ? kPrByNumber : kPrByBound;
+    int64_t entries = g.blocks == kPrByNumber ? filled : grid;
+    // bf16 lists what a thread a request and an entry can name, and sorts it, so that none of the long items is begun last (24
+    // prompts of up to 600 tokens behind prefixes of up to 512, 16 heads: 66 -> 63.7 us; 64 of up to 300 with a bound of all
+    // tokens: 198 -> 56); very many even out.
+    const int64_t listed = std::min(grid, filled);
+    if (bf16 && p->batch > 1 && p->batch <= kPrListed && listed <= kPrListed && (listed * p->num_heads > host_sm_count() || listed < grid)) {
+        g.blocks = kPrByList;
+        g.entries = (int)listed;
+        entries = listed;
+    }
     const int64_t blocks = entries * p->num_heads;
     if (blocks > 0x7fffffffLL) return DSA_ERR_UNSUPPORTED;
     PromptMaps m = {};

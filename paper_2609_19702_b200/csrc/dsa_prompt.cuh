@@ -62,7 +62,8 @@ struct PromptItem {
     int rows[2], len[2], tiles[2];                 // of either half: queries, keys that any of them sees, tiles of those
 };
 
-template <int D>
+// BLOCKS: how a block finds its work (forms of their own, because what one of them does not need cost it 2 to 5 % with short prompts)
+template <int D, int BLOCKS>
 __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptArgs g, const __grid_constant__ PromptMaps maps) {
     using C = PromptCfg<D>;
     using T = __nv_bfloat16;
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
         it.n_tiles = max(it.tiles[0], it.tiles[1]);
         return true;
     };
-    if (g.entries > 0) {
+    if constexpr (BLOCKS == kPrByList) {
         // A list of the items of one head, without gaps and by what they cost, the dearest first: a tile of both halves takes some 2500
         // cycles, of one 1400, the ends of an item 3000.  (a request a thread, then an entry a thread)
         int* s_cost = reinterpret_cast<int*>(smem);
@@ -206,20 +207,27 @@ __global__ void __launch_bounds__(kPrThreads, 1) dsa_prompt_kernel(const PromptA
             it.h = -1;
             int passed = 0;
             while (ok && idx >= 0) {                          // (blocks without a query are passed over)
-                const int e = idx / g.H, name = g.entries > 0 ? s_list[e] : 0;
-                if (name != 0xffff && (g.entries > 0 ? describe(name & 255, name >> 8, it) : describe(e % g.batch, e / g.batch, it))) {
+                const int e = idx / g.H;
+                int2 at;                                      // request (-1: none), which of its blocks
+                if constexpr (BLOCKS == kPrByList) {
+                    const int name = s_list[e];
+                    at = make_int2(name == 0xffff ? -1 : name & 255, name >> 8);
+                } else if constexpr (BLOCKS == kPrByNumber) {
+                    at = prompt_find(g.q_start, g.q_tokens, g.batch, kPrBlock, e);
+                } else {
+                    at = make_int2(e % g.batch, e / g.batch);
+                }
+                if (at.x >= 0 && describe(at.x, at.y, it)) {
                     it.h = idx % g.H;
                     break;
                 }
-                // Nobody waits for the end of a long run of them, which a batch of 2^20 requests and 1024 heads could make longer than a wait
-                // may take (some 0.5 us a block): now and then the others get an item without a row.
-                if (++passed == kPrPassed) {
-                    it = PromptItem{};
-                    break;
-                }
+                if (BLOCKS != kPrByList && ++passed == kPrPassed) break;         // (a list is short)
                 ask();
                 ok = answer();
             }
+            // Nobody waits for the end of a long run of blocks without a query, which a batch of 2^20 requests and 1024 heads could make
+            // longer than a wait may take (some 0.5 us a block): now and then the others get an item without a row.
+            if (BLOCKS != kPrByList && passed == kPrPassed) it = PromptItem{};
             if (!ok) break;
             if (i >= 2) ok = tree_wait(info_empty + (i & 1), ((i >> 1) - 1) & 1, abort, g.wait_timeouts, lane);
             if (!ok) break;

@@ -30,20 +30,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) dsa_prompt_f32_kernel(const P
     const int h = idx % g.H; idx /= g.H;
     int b = idx % g.batch, first = (tiles_q - 1 - idx / g.batch) * kTileRows;      // (the longest rows first)
     int q0, nq, k0, nk;
-    if (g.entries > 0) {
-        __shared__ int s_warp[kTileThreads / 32], s_name[2];
-        int rows = 0;
-        if (tid < g.batch) {
-            prompt_range(g, tid, q0, nq, k0, nk);
-            rows = (nq + kTileRows - 1) / kTileRows;
-        }
-        if (tid == 0) s_name[0] = -1;
-        const int before = prompt_before(rows, s_warp);
-        if (idx >= before && idx < before + rows) { s_name[0] = tid; s_name[1] = (rows - 1 - (idx - before)) * kTileRows; }
-        __syncthreads();
-        b = s_name[0];
-        first = s_name[1];
+    if (g.blocks == kPrByNumber) {
+        const int2 at = prompt_find(g.q_start, g.q_tokens, g.batch, kTileRows, idx);
+        b = at.x;
         if (b < 0) return;
+        prompt_range(g, b, q0, nq, k0, nk);
+        first = ((nq + kTileRows - 1) / kTileRows - 1 - at.y) * kTileRows;
+        if (first < 0) return;
     }
     prompt_range(g, b, q0, nq, k0, nk);
     // (the starts of the whole request decide which keys a query sees, whatever max_q_len leaves out)
