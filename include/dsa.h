@@ -682,7 +682,8 @@ typedef struct dsa_prompt {
     float sm_scale;            /* logit scale; 0 means 1/sqrt(nope_dim + rope_dim)                           */
     int32_t q_tokens;          /* rows of q, out and lse                                                     */
     int32_t kv_tokens;         /* rows of k_nope, k_rope and v                                               */
-    int32_t max_q_len;         /* HOST upper bound of a request's queries; sizes the launch.  Queries beyond */
+    int32_t max_q_len;         /* HOST upper bound of a request's queries (q_tokens will do: however loose   */
+                               /* it is, the launch is sized by q_tokens and batch as well).  Queries beyond */
                                /* it are left out (out and lse stay as they were)                            */
     /* Rows of a token and head, contiguous, 16-byte aligned, at token*stride_token + head*stride_head
      * elements (multiples of 16 bytes): q [.., nope_dim + rope_dim], the others as they are named. */
@@ -734,7 +735,7 @@ typedef struct dsa_token_map {
  * Entries behind the last token: -1 in all three.  start [B + 1], position and request [max_tokens] int32, slot
  * [max_tokens] int64; position and request may be NULL.
  * start is what dsa_prompt takes as q_start / kv_start, slot what the row calls take.  With base NULL and count the
- * cached lengths the map names the tokens in the cache.
+ * cached lengths the map names the tokens in the cache.  batch: at most 8192.
  */
 DSA_API int32_t dsa_map_tokens(const dsa_token_map *map, int32_t *start, int64_t *slot, int32_t *position,
                                int32_t *request, void *stream);
