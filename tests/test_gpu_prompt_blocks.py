@@ -48,6 +48,8 @@ def blocks_of(call, tmp_path):
     p.export_chrome_trace(str(tmp_path / "trace.json"))
     events = json.load(open(tmp_path / "trace.json"))["traceEvents"]
     grids = [e["args"]["grid"] for e in events if "dsa_prompt" in e.get("name", "") and "grid" in e.get("args", {})]
+    if not any("grid" in e.get("args", {}) for e in events):
+        pytest.skip("no launch is shown by the profiler here")
     assert len(grids) == 1
     return grids[0][0]
 
